@@ -321,6 +321,67 @@ int spec_ttt_attention(const void *q, const void *k_pool, const void *v_pool, co
                        int32_t page_size, const void *k_diag, const void *v_diag, int32_t n_steps, void *out, float *lse,
                        int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void *scratch, void *stream);
 
+/* ---- serving and training beside the step: rotary positions, a paged cache in 8 bits, attention of single tokens --------------
+ * The step above keeps its cache in the model's type and rotates whole heads by unscaled frequencies.  These four calls serve
+ * loops of a program's own around other caches and other rotations; they share no state with a ctx, take caller-provided DEVICE
+ * buffers, launch one kernel each on `stream`, allocate nothing and do not synchronise.  dtype: spec_dtype of queries,
+ * keys, values and outputs.  status: optional int32 [4] device words, zero at the start: a sequence, position, length or page out
+ * of range is left out and recorded there (code 2, site 60: sequence or position, 61 / 63: page, 62: length; two details).  Calls with no
+ * token or row return SPEC_OK and launch nothing. */
+
+/* How pairs of a head's first rot_dim dimensions turn: at position p, pair i becomes mscale (a cos t - b sin t, b cos t + a sin t)
+ * with t = p * inv_freq[i], formed in 64 bits.  layout 0: dimension i pairs with i + rot_dim / 2; 1: 2 i with 2 i + 1. */
+typedef struct {
+  const double *inv_freq;   /* device, [rot_dim / 2]: scaled frequencies for long contexts are the caller's table            */
+  int32_t rot_dim;          /* even, <= head_dim; the other dimensions pass unchanged (and without mscale)                   */
+  int32_t layout;
+  float mscale;
+} spec_rope;
+
+enum spec_kv_format { SPEC_KV_F32 = 0, SPEC_KV_BF16 = 1, SPEC_KV_E4M3 = 2, SPEC_KV_INT8 = 3 };
+
+/* A paged cache: pools [num_pages][n_kv_heads][page_size][head_dim] of `format`, position p of sequence s in page
+ * page_table[s][p / page_size].  The 8-bit formats have a scale for each token and head, [num_pages][n_kv_heads][page_size]:
+ * value = code * scale, scale = max(largest magnitude / top, 2^-120), top 448 (E4M3) or 127 (INT8: codes -127..127), codes rounded to
+ * nearest even.  A row with an infinity or a NaN reads back as NaN.  head_dim % 16 == 0, <= 256; pools 16-byte aligned; any page size.
+ * F32 goes with dtype F32, BF16 with BF16, the 8-bit formats with both. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale; /* NULL for F32 and BF16 */
+  const int32_t *page_table;/* device, [n_seq][pages_per_seq] */
+  int32_t n_seq, pages_per_seq, page_size, num_pages, n_kv_heads, head_dim, format;
+} spec_kv_cache;
+
+/* out[t][h] = x[t][h] turned to position pos[t] (int32, may be negative); transpose != 0: by the transposed matrix, which takes a gradient
+ * with respect to the output to one with respect to the input.  Strides in elements; a head's dimensions are adjacent.  out may be x with
+ * the same strides; otherwise they must not overlap.  head_dim <= 256. */
+int spec_rotary(int32_t dtype, const void *x, int64_t x_token_stride, int64_t x_head_stride, void *out, int64_t out_token_stride,
+                int64_t out_head_stride, const int32_t *pos, int32_t tokens, int32_t heads, int32_t head_dim, const spec_rope *rope,
+                int32_t transpose, void *stream);
+
+/* Token t's keys, turned to row_pos[t] and then quantised, and its values go to cache position row_kvpos[t] (NULL: row_pos[t]) of
+ * sequence row_seq[t] (-1: nowhere); its n_heads query heads, if q is not NULL, turned, to q_out [tokens][n_heads][head_dim] (whatever
+ * row_seq says).  rope NULL: nothing turns.  No two tokens may go to one position. */
+int spec_kv_append(int32_t dtype, const void *q, int64_t q_token_stride, int64_t q_head_stride, void *q_out, int32_t n_heads,
+                   const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride,
+                   int64_t v_head_stride, const int32_t *row_seq, const int32_t *row_pos, const int32_t *row_kvpos, int32_t tokens,
+                   const spec_rope *rope, const spec_kv_cache *cache, int32_t *status, void *stream);
+
+/* k_out / v_out [rows][n_kv_heads][head_dim] of out_dtype: position row_kvpos[r] of sequence row_seq[r], zeros for sequence -1. */
+int spec_kv_read(const spec_kv_cache *cache, const int32_t *row_seq, const int32_t *row_kvpos, int32_t rows, int32_t out_dtype,
+                 void *k_out, void *v_out, int32_t *status, void *stream);
+
+/* One query token per sequence: out[b][h] = softmax over t < lengths[b] of (scale q[b][h].k[t][g]) applied to v[t][g],
+ * g = h / (n_heads / n_kv_heads), over sequence b of the cache; lse (optional) float [batch][n_heads], the natural-log normaliser.
+ * lengths int32 [batch]; a length of 0 gives zeros and -inf.  q: heads adjacent, tokens q_token_stride elements apart, 16-byte
+ * aligned (stride too); out [batch][n_heads][head_dim].  scale 0: head_dim^-1/2.  batch <= 8192, batch <= n_seq.
+ * workspace: spec_decode_attention_workspace_bytes() bytes, 256-byte aligned, zero before the first call; a call leaves it ready for
+ * the next on the same stream, and calls that may overlap need one each. */
+size_t spec_decode_attention_workspace_bytes(void);
+int spec_decode_attention(int32_t dtype, const void *q, int64_t q_token_stride, const spec_kv_cache *cache, const int32_t *lengths,
+                          int32_t batch, int32_t n_heads, float scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                          int32_t *status, void *stream);
+
 /* Test hook for the calling thread's causal attention launches (prefill and training-time test): 0 = off, 1 = the warps that
  * wait for the last contraction of a tile come tens of microseconds late (results do not depend on it), 2 = one CTA never
  * receives its queries and its bounded waits run out: a prefill returns SPEC_ERR_DEVICE_STATUS, training-time test gives NaN

@@ -56,11 +56,21 @@ class _Cfg(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
 
 
+class _Rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("mscale", C.c_float)]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table")] + \
+               [(n, C.c_int32) for n in ("n_seq", "pages_per_seq", "page_size", "num_pages", "n_kv_heads", "head_dim", "format")]
+
+
 EXPORTS = ("spec_workspace_bytes", "spec_init", "spec_prefill", "spec_step", "spec_step_async", "spec_step_sampled", "spec_plain_step",
            "spec_lengths", "spec_profile_step", "spec_tune", "spec_launches_per_step", "spec_step_bytes", "spec_free", "spec_last_error",
            "spec_debug_read", "spec_debug_read_kv", "spec_gemm", "spec_gemm_fused", "spec_gemm_swiglu", "spec_gemm_wide", "spec_gemm_topk_scratch_bytes", "spec_gemm_topk", "spec_ttt_attention_scratch_bytes", "spec_ttt_attention",
            "spec_debug_causal", "spec_debug_wide_gemm", "spec_topk_scratch_bytes", "spec_attn_scratch_bytes",
-           "spec_attention", "spec_attention_static", "spec_attention_static_capacity", "spec_logsoftmax_topk", "spec_argmax")
+           "spec_attention", "spec_attention_static", "spec_attention_static_capacity", "spec_logsoftmax_topk", "spec_argmax",
+           "spec_rotary", "spec_kv_append", "spec_kv_read", "spec_decode_attention_workspace_bytes", "spec_decode_attention")
 
 
 def library_path() -> str:
@@ -117,6 +127,13 @@ def lib():
     L.spec_topk_scratch_bytes.restype = sz
     L.spec_logsoftmax_topk.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp]
     L.spec_argmax.argtypes = [vp, i32, i32, vp, vp]
+    rope, cache = C.POINTER(_Rope), C.POINTER(_KvCache)
+    L.spec_rotary.argtypes = [i32, vp, i64, i64, vp, i64, i64, vp, i32, i32, i32, rope, i32, vp]
+    L.spec_kv_append.argtypes = [i32, vp, i64, i64, vp, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, i32, rope, cache, vp, vp]
+    L.spec_kv_read.argtypes = [cache, vp, vp, i32, i32, vp, vp, vp, vp]
+    L.spec_decode_attention_workspace_bytes.argtypes = []
+    L.spec_decode_attention_workspace_bytes.restype = sz
+    L.spec_decode_attention.argtypes = [i32, vp, i64, cache, vp, i32, i32, C.c_float, vp, vp, vp, sz, vp, vp]
     _lib = L
     return L
 
@@ -467,3 +484,193 @@ def argmax(logits: torch.Tensor) -> torch.Tensor:
     if rc:
         raise SpecError(rc, "spec_argmax")
     return idx
+
+
+# ------------------------------------------------------------------ rotary positions, the paged cache in 8 bits, single-token attention
+_KV_FORMAT = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch.int8: 3}
+_LAYOUT = {"half": 0, "interleaved": 1}
+_workspaces: Dict = {}
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(t: torch.Tensor, n: int, what: str) -> int:
+    _need(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.is_cuda, what)
+    return t.data_ptr()
+
+
+def _status_ptr(status: Optional[torch.Tensor]):
+    return None if status is None else _ints(status, 4, "status: int32 [4] on the GPU")
+
+
+def rope_frequencies(rot_dim: int, theta: float, scaling: Optional[str] = None, factor: float = 1.0, trained: int = 8192, low: float = 1.0,
+                     high: float = 4.0, device="cuda"):
+    """(inv_freq float64 [rot_dim / 2] in radians a position, mscale) of rotary positions, theta^(-2 i / rot_dim) scaled for contexts
+    `factor` times the `trained` one:
+      None          as they are
+      "linear"      all divided by the factor (positions interpolated)
+      "ntk"         theta grown so that the slowest pair is divided by the factor and the fastest kept
+      "wavelength"  pairs that turn more than `high` times in the trained context kept, less than `low` times divided, in between
+                    mixed in proportion to the turns
+      "rotations"   the same with the mixing in proportion to the pair's index (YaRN: low 1, high 32), and mscale 0.1 ln(factor) + 1"""
+    _need(rot_dim > 0 and rot_dim % 2 == 0 and theta > 1 and factor >= 1 and trained > 0 and 0 < low < high,
+          "rope_frequencies: rot_dim even and positive, theta > 1, factor >= 1, 0 < low < high")
+    i = np.arange(0, rot_dim, 2, dtype=np.float64) / rot_dim
+    f, mscale = float(theta) ** -i, 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "ntk":
+        _need(rot_dim > 2, "rope_frequencies: ntk needs two pairs")
+        f = (theta * factor ** (rot_dim / (rot_dim - 2.0))) ** -i
+    elif scaling == "wavelength":
+        keep = np.clip((trained * f / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
+        f = f * keep + f / factor * (1 - keep)
+    elif scaling == "rotations":
+        index = [rot_dim * np.log(trained / (t * 2 * np.pi)) / (2 * np.log(theta)) for t in (high, low)]
+        first, last = max(np.floor(index[0]), 0), min(np.ceil(index[1]), rot_dim - 1)
+        keep = 1.0 - np.clip((np.arange(rot_dim // 2) - first) / max(last - first, 1e-3), 0.0, 1.0)
+        f, mscale = f * keep + f / factor * (1 - keep), 0.1 * float(np.log(factor)) + 1.0
+    else:
+        _need(scaling is None, "rope_frequencies: scaling is None, 'linear', 'ntk', 'wavelength' or 'rotations'")
+    return torch.from_numpy(f).to(device), mscale
+
+
+def _rope(inv_freq: Optional[torch.Tensor], layout: str, mscale: float):
+    if inv_freq is None:
+        return None
+    _need(inv_freq.dtype == torch.float64 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.is_cuda, "inv_freq: float64 [pairs] on the GPU")
+    _need(layout in _LAYOUT, "layout is 'half' or 'interleaved'")
+    return _Rope(inv_freq.data_ptr(), 2 * inv_freq.shape[0], _LAYOUT[layout], mscale)
+
+
+def _heads(t: torch.Tensor, what: str):
+    """(pointer, token stride, head stride) of [tokens][heads][head_dim]"""
+    _need(t.dim() == 3 and t.is_cuda and (t.stride(2) == 1 or t.shape[2] == 1), what)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _turn(x, positions, inv_freq, layout, mscale, out, transpose):
+    T, H, hd = x.shape
+    if out is None:
+        out = torch.empty(T, H, hd, dtype=x.dtype, device=x.device)
+    _need(out.shape == x.shape and out.dtype == x.dtype, "rotary: out has x's shape and dtype")
+    _need(inv_freq is not None, "rotary: inv_freq")
+    rc = lib().spec_rotary(_dt(x.dtype), *_heads(x, "rotary: x [tokens][heads][head_dim] with adjacent dimensions"),
+                           *_heads(out, "rotary: out [tokens][heads][head_dim] with adjacent dimensions"),
+                           _ints(positions, T, "rotary: positions int32 [tokens]"), T, H, hd, C.byref(_rope(inv_freq, layout, mscale)), transpose,
+                           _stream_ptr(None))
+    if rc:
+        raise SpecError(rc, "spec_rotary")
+    return out
+
+
+def rotary(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0,
+           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [tokens][heads][head_dim] (any token and head stride: a view of a fused projection will do) with the first 2 * pairs dimensions of
+    every head turned to positions int32 [tokens].  out may be x."""
+    return _turn(x, positions, inv_freq, layout, mscale, out, 0)
+
+
+def rotary_backward(grad: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient with respect to rotary's x of one with respect to its output."""
+    return _turn(grad, positions, inv_freq, layout, mscale, out, 1)
+
+
+def _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale) -> _KvCache:
+    shape = k_pool.shape
+    fmt = _KV_FORMAT.get(k_pool.dtype)
+    if fmt is None:
+        raise TypeError(f"unsupported cache dtype {k_pool.dtype}")
+    _need(len(shape) == 4 and v_pool.shape == shape and v_pool.dtype == k_pool.dtype and k_pool.is_contiguous() and v_pool.is_contiguous() and
+          k_pool.is_cuda and v_pool.is_cuda, "pools: two contiguous [pages][kv heads][page size][head_dim] of one dtype")
+    _need(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous() and page_table.is_cuda,
+          "page_table: int32 [sequences][pages]")
+    ks = vs = None
+    if fmt >= 2:
+        for s in (k_scale, v_scale):
+            _need(s is not None and s.dtype == torch.float32 and s.shape == shape[:3] and s.is_contiguous() and s.is_cuda,
+                  "scales of an 8-bit cache: contiguous float32 [pages][kv heads][page size]")
+        ks, vs = k_scale.data_ptr(), v_scale.data_ptr()
+    return _KvCache(k_pool.data_ptr(), v_pool.data_ptr(), ks, vs, page_table.data_ptr(), page_table.shape[0], page_table.shape[1], shape[2], shape[0],
+                    shape[1], shape[3], fmt)
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_seq: torch.Tensor,
+              row_pos: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+              q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, layout: str = "half", mscale: float = 1.0,
+              row_kvpos: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Writes k, v [tokens][kv heads][head_dim] to a paged cache: token t to position row_kvpos[t] (default row_pos[t]) of sequence row_seq[t]
+    (-1: nowhere), its keys turned to row_pos[t] where inv_freq is given, both quantised where the pools are float8_e4m3fn or int8.
+    Returns the turned q [tokens][heads][head_dim], if there is one."""
+    T, G, hd = k.shape
+    cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
+    _need(G == cache.n_kv_heads and hd == cache.head_dim and v.shape == k.shape and v.dtype == k.dtype, "kv_append: k and v [tokens][kv heads][head_dim] of the cache")
+    q_out, H, qa = None, 0, (None, 0, 0)
+    if q is not None:
+        H = q.shape[1]
+        _need(q.dim() == 3 and q.shape[0] == T and q.shape[2] == hd and q.dtype == k.dtype, "kv_append: q [tokens][heads][head_dim] of k's dtype")
+        q_out = torch.empty(T, H, hd, dtype=q.dtype, device=q.device)
+        qa = _heads(q, "kv_append: q [tokens][heads][head_dim] with adjacent dimensions")
+    rope = _rope(inv_freq, layout, mscale)
+    rc = lib().spec_kv_append(_dt(k.dtype), *qa, None if q_out is None else q_out.data_ptr(), H,
+                              *_heads(k, "kv_append: k [tokens][kv heads][head_dim] with adjacent dimensions"),
+                              *_heads(v, "kv_append: v [tokens][kv heads][head_dim] with adjacent dimensions"),
+                              _ints(row_seq, T, "kv_append: row_seq int32 [tokens]"), _ints(row_pos, T, "kv_append: row_pos int32 [tokens]"),
+                              None if row_kvpos is None else _ints(row_kvpos, T, "kv_append: row_kvpos int32 [tokens]"), T,
+                              None if rope is None else C.byref(rope), C.byref(cache), _status_ptr(status), _stream_ptr(None))
+    if rc:
+        raise SpecError(rc, "spec_kv_append")
+    return q_out
+
+
+def kv_read(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_seq: torch.Tensor, row_kvpos: torch.Tensor,
+            k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+            status: Optional[torch.Tensor] = None):
+    """(k, v) [rows][kv heads][head_dim] of dtype: position row_kvpos[r] of sequence row_seq[r] of a paged cache, zeros for sequence -1."""
+    cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
+    rows = row_seq.shape[0]
+    out = torch.empty(2, rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=k_pool.device)
+    k, v = out.unbind(0)
+    rc = lib().spec_kv_read(C.byref(cache), _ints(row_seq, rows, "kv_read: row_seq int32 [rows]"), _ints(row_kvpos, rows, "kv_read: row_kvpos int32 [rows]"),
+                            rows, _dt(dtype), k.data_ptr(), v.data_ptr(), _status_ptr(status), _stream_ptr(None))
+    if rc:
+        raise SpecError(rc, "spec_kv_read")
+    return k, v
+
+
+def decode_workspace(device="cuda") -> torch.Tensor:
+    """A workspace for decode_attention: one for each stream whose calls may overlap."""
+    return torch.zeros(lib().spec_decode_attention_workspace_bytes(), dtype=torch.uint8, device=device)
+
+
+def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                     k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                     want_lse: bool = False, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None):
+    """Attention of one new token per sequence: q [batch][heads][head_dim] over the first lengths[b] positions of sequence b of a paged cache.
+    Returns out [batch][heads][head_dim] (and the float32 [batch][heads] log-normaliser when want_lse).  workspace: decode_workspace();
+    without one, a workspace that is kept for the current stream (made by its first call, which must not be under graph capture)."""
+    B, H, hd = q.shape
+    cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
+    _need(hd == cache.head_dim and q.is_cuda and q.stride(2) == 1 and q.stride(1) == hd, "decode_attention: q [batch][heads][head_dim], heads adjacent")
+    if out is None:
+        out = torch.empty(B, H, hd, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "decode_attention: out contiguous, of q's shape and dtype")
+    lse = torch.empty(B, H, dtype=torch.float32, device=q.device) if want_lse else None
+    stream = _stream_ptr(None)
+    if workspace is None:
+        at = (q.device, stream)
+        workspace = _workspaces.get(at)
+        if workspace is None:
+            workspace = _workspaces[at] = decode_workspace(q.device)
+    _need(scale is None or (scale != 0 and scale == scale), "decode_attention: scale")
+    rc = lib().spec_decode_attention(_dt(q.dtype), q.data_ptr(), q.stride(0), C.byref(cache), _ints(lengths, B, "decode_attention: lengths int32 [batch]"), B, H,
+                                     0.0 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _status_ptr(status), stream)
+    if rc:
+        raise SpecError(rc, "spec_decode_attention")
+    return (out, lse) if want_lse else out

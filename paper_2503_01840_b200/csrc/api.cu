@@ -16,6 +16,7 @@
 #include "gemm_wide.cuh"
 #include "attn_fast.cuh"
 #include "attn_causal.cuh"
+#include "attn_decode.cuh"
 #include "state.cuh"
 
 using namespace spec;
@@ -1736,4 +1737,103 @@ extern "C" int spec_argmax(const float *logits, int32_t rows, int32_t n, int32_t
   if (rows < 1 || n < 1) return SPEC_ERR_INVALID_CFG;
   launch_argmax(logits, rows, n, out_idx, (cudaStream_t)stream);
   return cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------- rotary positions, the 8-bit cache, attention of single tokens
+static bool kv_aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+static int rope_of(const spec_rope *r, int head_dim, int transpose, Rope *out) {
+  *out = Rope{nullptr, 0, 0, 1.0f, 1.0f};
+  if (!r) return SPEC_OK;
+  if (r->rot_dim < 0 || r->rot_dim > head_dim || r->rot_dim % 2 || r->layout < 0 || r->layout > 1) return SPEC_ERR_INVALID_CFG;
+  if (r->rot_dim && !r->inv_freq) return SPEC_ERR_NULL;
+  *out = Rope{r->inv_freq, r->rot_dim / 2, r->layout, r->mscale, transpose ? -1.0f : 1.0f};
+  return SPEC_OK;
+}
+
+static int cache_of(const spec_kv_cache *c, KvCache *out) {
+  if (!c || !c->k || !c->v || !c->page_table) return SPEC_ERR_NULL;
+  if (c->format < SPEC_KV_F32 || c->format > SPEC_KV_INT8) return SPEC_ERR_INVALID_CFG;
+  if (kv_is_8bit(c->format) && (!c->k_scale || !c->v_scale)) return SPEC_ERR_NULL;
+  if (c->n_seq < 1 || c->pages_per_seq < 1 || c->page_size < 1 || c->num_pages < 1 || c->n_kv_heads < 1) return SPEC_ERR_INVALID_CFG;
+  if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16) return SPEC_ERR_UNSUPPORTED;
+  if (!kv_aligned(c->k, 16) || !kv_aligned(c->v, 16) || !kv_aligned(c->k_scale, 4) || !kv_aligned(c->v_scale, 4)) return SPEC_ERR_INVALID_CFG;
+  // rows of the pool and positions of a sequence are counted in 32 bits on the device
+  const double rows = (double)c->num_pages * c->n_kv_heads * c->page_size, positions = (double)c->pages_per_seq * c->page_size;
+  if (rows > 2147483647.0 || positions > 2147483647.0) return SPEC_ERR_UNSUPPORTED;
+  *out = KvCache{c->k, c->v, c->k_scale, c->v_scale, c->page_table, c->n_seq, c->pages_per_seq, c->page_size, c->num_pages, c->n_kv_heads, c->head_dim};
+  return SPEC_OK;
+}
+static bool kv_goes_with(int dtype, int format) {
+  return dtype == SPEC_F32 ? format != SPEC_KV_BF16 : dtype == SPEC_BF16 && format != SPEC_KV_F32;
+}
+static int kv_status(cudaError_t e) { return e == cudaSuccess ? SPEC_OK : e == cudaErrorNotSupported ? SPEC_ERR_UNSUPPORTED : SPEC_ERR_CUDA; }
+
+extern "C" int spec_rotary(int32_t dtype, const void *x, int64_t x_ts, int64_t x_hs, void *out, int64_t out_ts, int64_t out_hs, const int32_t *pos,
+                           int32_t tokens, int32_t heads, int32_t head_dim, const spec_rope *rope, int32_t transpose, void *stream) {
+  if (tokens < 0 || heads < 0 || head_dim < 1 || (dtype != SPEC_F32 && dtype != SPEC_BF16)) return SPEC_ERR_INVALID_CFG;
+  if (head_dim > 256) return SPEC_ERR_UNSUPPORTED;
+  if (!rope) return SPEC_ERR_NULL;
+  RopeAppend a{};
+  if (const int rc = rope_of(rope, head_dim, transpose, &a.rope)) return rc;
+  if (tokens == 0 || heads == 0) return SPEC_OK;
+  if (!x || !out || !pos) return SPEC_ERR_NULL;
+  const size_t e = dtype == SPEC_F32 ? 4 : 2;
+  if (!kv_aligned(x, e) || !kv_aligned(out, e)) return SPEC_ERR_INVALID_CFG;
+  if (x == out && (x_ts != out_ts || x_hs != out_hs)) return SPEC_ERR_INVALID_CFG;
+  a.q = HeadView{x, x_ts, x_hs};
+  a.q_out = out; a.qo_ts = out_ts; a.qo_hs = out_hs;
+  a.H = heads; a.hd = head_dim; a.tokens = tokens; a.pos = pos;
+  return kv_status(launch_rope_append(a, dtype, dtype == SPEC_F32 ? KV_F32 : KV_BF16, (cudaStream_t)stream));
+}
+
+extern "C" int spec_kv_append(int32_t dtype, const void *q, int64_t q_ts, int64_t q_hs, void *q_out, int32_t n_heads, const void *k, int64_t k_ts,
+                              int64_t k_hs, const void *v, int64_t v_ts, int64_t v_hs, const int32_t *row_seq, const int32_t *row_pos,
+                              const int32_t *row_kvpos, int32_t tokens, const spec_rope *rope, const spec_kv_cache *cache, int32_t *status,
+                              void *stream) {
+  RopeAppend a{};
+  if (const int rc = cache_of(cache, &a.cache)) return rc;
+  if (const int rc = rope_of(rope, cache->head_dim, 0, &a.rope)) return rc;
+  if (!kv_goes_with(dtype, cache->format) || tokens < 0 || (q && n_heads < 1)) return SPEC_ERR_INVALID_CFG;
+  if (tokens == 0) return SPEC_OK;
+  if (!k || !v || !row_seq || !row_pos || (q && !q_out)) return SPEC_ERR_NULL;
+  const size_t e = dtype == SPEC_F32 ? 4 : 2;
+  if (!kv_aligned(q, e) || !kv_aligned(q_out, e) || !kv_aligned(k, e) || !kv_aligned(v, e)) return SPEC_ERR_INVALID_CFG;
+  a.hd = cache->head_dim; a.tokens = tokens; a.H = q ? n_heads : 0;
+  if (q && q == q_out && (q_hs != a.hd || q_ts != (int64_t)n_heads * a.hd)) return SPEC_ERR_INVALID_CFG;
+  a.q = HeadView{q, q_ts, q_hs}; a.k = HeadView{k, k_ts, k_hs}; a.v = HeadView{v, v_ts, v_hs};
+  a.q_out = q_out; a.qo_hs = a.hd; a.qo_ts = (long long)a.H * a.hd;
+  a.seq = row_seq; a.pos = row_pos; a.kvpos = row_kvpos ? row_kvpos : row_pos; a.status = status;
+  return kv_status(launch_rope_append(a, dtype, cache->format, (cudaStream_t)stream));
+}
+
+extern "C" int spec_kv_read(const spec_kv_cache *cache, const int32_t *row_seq, const int32_t *row_kvpos, int32_t rows, int32_t out_dtype, void *k_out,
+                            void *v_out, int32_t *status, void *stream) {
+  KvRead a{};
+  if (const int rc = cache_of(cache, &a.cache)) return rc;
+  if (rows < 0 || (out_dtype != SPEC_F32 && out_dtype != SPEC_BF16)) return SPEC_ERR_INVALID_CFG;
+  if (rows == 0) return SPEC_OK;
+  if (!row_seq || !row_kvpos || !k_out || !v_out) return SPEC_ERR_NULL;
+  if (!kv_aligned(k_out, 16) || !kv_aligned(v_out, 16)) return SPEC_ERR_INVALID_CFG;
+  a.seq = row_seq; a.kvpos = row_kvpos; a.rows = rows; a.k_out = k_out; a.v_out = v_out; a.status = status;
+  return kv_status(launch_kv_read(a, cache->format, out_dtype, (cudaStream_t)stream));
+}
+
+extern "C" size_t spec_decode_attention_workspace_bytes(void) { return decode_attn_workspace_bytes(); }
+
+extern "C" int spec_decode_attention(int32_t dtype, const void *q, int64_t q_ts, const spec_kv_cache *cache, const int32_t *lengths, int32_t batch,
+                                     int32_t n_heads, float scale, void *out, float *lse, void *workspace, size_t workspace_bytes, int32_t *status,
+                                     void *stream) {
+  DecodeAttn a{};
+  if (const int rc = cache_of(cache, &a.cache)) return rc;
+  if (!kv_goes_with(dtype, cache->format) || batch < 0 || n_heads < 1 || n_heads % cache->n_kv_heads || batch > cache->n_seq || !(fabsf(scale) < INFINITY))
+    return SPEC_ERR_INVALID_CFG;
+  if (batch > DECODE_MAX_BATCH) return SPEC_ERR_UNSUPPORTED;
+  if (batch == 0) return SPEC_OK;
+  if (!q || !lengths || !out || !workspace) return SPEC_ERR_NULL;
+  if (workspace_bytes < decode_attn_workspace_bytes() || !kv_aligned(workspace, 256)) return SPEC_ERR_WORKSPACE;
+  if (!kv_aligned(q, 16) || !kv_aligned(out, 16) || q_ts * (dtype == SPEC_F32 ? 4 : 2) % 16) return SPEC_ERR_INVALID_CFG;
+  a.q = q; a.q_ts = q_ts; a.len = lengths; a.out = out; a.lse = lse; a.batch = batch; a.H = n_heads; a.workspace = workspace; a.status = status;
+  a.scale = scale != 0.0f ? scale : 1.0f / sqrtf((float)cache->head_dim);
+  return kv_status(launch_decode_attn(a, dtype, cache->format, (cudaStream_t)stream));
 }

@@ -1,0 +1,24 @@
+// Attention of one new token per sequence over the paged cache: host-side interface.
+#pragma once
+#include "kv_cache.cuh"
+
+namespace spec {
+
+struct DecodeAttn {
+  const void *q;                // [batch][H][hd], tokens q_ts elements apart
+  long long q_ts;
+  KvCache cache;
+  const int32_t *len;           // [batch]
+  void *out;                    // [batch][H][hd]
+  float *lse;                   // [batch][H] or null
+  int batch, H;
+  float scale;
+  void *workspace;
+  int32_t *status;
+};
+size_t decode_attn_workspace_bytes();
+constexpr int DECODE_MAX_BATCH = 8192;
+// cudaErrorNotSupported: more tiles of positions than an int counts
+cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStream_t s);
+
+}  // namespace spec
