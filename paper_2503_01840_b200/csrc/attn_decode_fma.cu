@@ -1,0 +1,168 @@
+// Single-token attention on plain FMAs: fp32 queries, and head sizes that the tensor-core body is not made for.
+#include "attn_decode_kernel.cuh"
+
+namespace spec {
+
+// A lane takes a position's whole score; then LPT lanes share a position's values, DV vectors of four dimensions each.
+template <int FMT_, int HP_, int DCLASS> struct FmaBody {
+  static constexpr int FMT = FMT_, HP = HP_, TILE = 32, WARPS = 8;
+  static constexpr int LPT = DCLASS == 64 ? 16 : 32, NV = DCLASS == 256 ? 2 : 1, PER = 32 / LPT;
+  typedef typename KvElem<FMT>::type E;
+  static constexpr int VEC = 16 / sizeof(E);
+  static __host__ __device__ int warp_smem_floats(int hd) { return HP * hd + 64; }
+
+  float m[HP], l[HP], acc[HP][NV][4];
+  float *qs;                    // [HP][hd], times scale * log2 e
+
+  __device__ void init(const DaArgs &p, const DaSeg &sg, bool q_f32, float *mem, int lane) {
+    qs = mem;
+    const int hd = p.a.cache.hd, group = p.a.H / p.a.cache.G, h0 = (sg.v / p.chunks) * group + (sg.v % p.chunks) * p.heads;
+    const int have = min(p.heads, group - (sg.v % p.chunks) * p.heads);
+    __syncwarp();
+    for (int i = lane; i < HP * hd; i += 32) {
+      const int h = i / hd;
+      const size_t at = (size_t)sg.b * p.a.q_ts + (size_t)(h0 + h) * hd + (i - h * hd);
+      qs[i] = h < have ? (q_f32 ? ((const float *)p.a.q)[at] : to_f32(((const bf16 *)p.a.q)[at])) * (p.a.scale * 1.44269504088896341f) : 0.0f;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < HP; h++) {
+      m[h] = -INFINITY, l[h] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) acc[h][j][e] = 0.0f;
+    }
+  }
+
+  static __device__ __forceinline__ void unpack(const uint4 &u, float (&x)[VEC]) {
+    const E *e = (const E *)&u;
+#pragma unroll
+    for (int i = 0; i < VEC; i++) x[i] = kv_decode<FMT>(e[i]);
+  }
+
+  __device__ void run(const DaArgs &p, const DaSeg &sg, int len, int lane) {
+    const KvCache &c = p.a.cache;
+    const int hd = c.hd, g = sg.v / p.chunks;
+    const E *K = (const E *)c.k, *V = (const E *)c.v;
+    for (int t = sg.t0; t < sg.t1; t++) {
+      const int pos = t * TILE + lane, n = min(TILE, len - t * TILE);
+      const int row = pos < len ? da_row(p, sg.b, g, pos) : -1;
+      float s[HP];
+#pragma unroll
+      for (int h = 0; h < HP; h++) s[h] = 0.0f;
+      float vsc = 1.0f;
+      if (row >= 0) {
+        const uint4 *kr = (const uint4 *)(K + (size_t)row * hd);
+#pragma unroll 4
+        for (int i = 0; i < hd / VEC; i++) {
+          float x[VEC];
+          unpack(kr[i], x);
+#pragma unroll
+          for (int h = 0; h < HP; h++)
+#pragma unroll
+            for (int e = 0; e < VEC; e += 4) {
+              const float4 w = *(const float4 *)(qs + h * hd + i * VEC + e);
+              s[h] = fmaf(w.x, x[e], fmaf(w.y, x[e + 1], fmaf(w.z, x[e + 2], fmaf(w.w, x[e + 3], s[h]))));
+            }
+        }
+        if constexpr (kv_is_8bit(FMT)) {
+          const float ksc = c.ks[row];
+          vsc = c.vs[row];
+#pragma unroll
+          for (int h = 0; h < HP; h++) s[h] *= ksc;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < HP; h++) {
+        if (row < 0) s[h] = -INFINITY;
+        float mx = s[h];
+#pragma unroll
+        for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        mx = fmaxf(mx, m[h]);
+        const float f = da_exp2(m[h] - da_ref(mx));
+        s[h] = da_exp2(s[h] - da_ref(mx));
+        m[h] = mx;
+        l[h] = l[h] * f + s[h];                                // each lane its own positions' sum
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) acc[h][j][e] *= f;
+        s[h] *= vsc;
+      }
+      const int dim = (lane % LPT) * 4;
+#pragma unroll 4
+      for (int j = 0; j < n; j += PER) {
+        const int from = PER == 1 ? j : j + lane / LPT;
+        const int r = __shfl_sync(0xffffffffu, row, from);
+        float x[NV][4];
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+          const int d = dim + i * 128;
+#pragma unroll
+          for (int e = 0; e < 4; e++) x[i][e] = 0.0f;
+          if (r >= 0 && d < hd) {
+            struct alignas(4 * sizeof(E)) Four { E e[4]; };
+            const Four u = *(const Four *)(V + (size_t)r * hd + d);
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[i][e] = kv_decode<FMT>(u.e[e]);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < HP; h++) {
+          const float w = __shfl_sync(0xffffffffu, s[h], from);
+          if (r < 0) continue;
+#pragma unroll
+          for (int i = 0; i < NV; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) acc[h][i][e] = fmaf(w, x[i][e], acc[h][i][e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < HP; h++) {
+#pragma unroll
+      for (int o = 16; o; o >>= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], o);
+      if constexpr (PER == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) acc[h][0][e] += __shfl_xor_sync(0xffffffffu, acc[h][0][e], 16);
+      }
+    }
+  }
+
+  // f(head, dimension, four values of O, sum) by the lanes that hold them; stat(head, max, sum) by one lane
+  template <typename F, typename G> __device__ void each(int hd, int lane, F f, G stat) {
+#pragma unroll
+    for (int h = 0; h < HP; h++) {
+      if (lane < LPT)
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+          if (lane * 4 + i * 128 < hd) f(h, lane * 4 + i * 128, make_float4(acc[h][i][0], acc[h][i][1], acc[h][i][2], acc[h][i][3]), l[h]);
+      if (lane == 0) stat(h, m[h], l[h]);
+    }
+  }
+};
+
+template <int FMT, int HP> static cudaError_t fma_by_hd(const DaArgs &p, bool q_f32, int ctas, cudaStream_t s) {
+  const int hd = p.a.cache.hd;
+  if (hd <= 64) return launch<FmaBody<FMT, HP, 64>>(p, q_f32, ctas, s);
+  if (hd <= 128) return launch<FmaBody<FMT, HP, 128>>(p, q_f32, ctas, s);
+  return launch<FmaBody<FMT, HP, 256>>(p, q_f32, ctas, s);
+}
+template <int FMT> static cudaError_t fma_by_heads(const DaArgs &p, bool q_f32, int ctas, cudaStream_t s) {
+  if (p.heads <= 1) return fma_by_hd<FMT, 1>(p, q_f32, ctas, s);
+  if (p.heads <= 2) return fma_by_hd<FMT, 2>(p, q_f32, ctas, s);
+  if (p.heads <= 4) return fma_by_hd<FMT, 4>(p, q_f32, ctas, s);
+  return fma_by_hd<FMT, 8>(p, q_f32, ctas, s);
+}
+
+cudaError_t launch_decode_fma(const DaArgs &p, int fmt, bool q_f32, int ctas, cudaStream_t s) {
+  switch (fmt) {
+    case KV_F32: return fma_by_heads<KV_F32>(p, q_f32, ctas, s);
+    case KV_BF16: return fma_by_heads<KV_BF16>(p, q_f32, ctas, s);
+    case KV_E4M3: return fma_by_heads<KV_E4M3>(p, q_f32, ctas, s);
+    default: return fma_by_heads<KV_INT8>(p, q_f32, ctas, s);
+  }
+}
+
+}  // namespace spec

@@ -1,0 +1,360 @@
+// Single-token attention on tensor cores: bf16 queries, head sizes 64, 128 and 256, up to MR = 8 or 16 query heads per KV head.  For a tile of 16 positions
+//   S^T [16 positions][MR heads] = K Q^T,   O^T [hd][MR heads] += V^T P^T     (mma m16n8k16: the cache is the A operand, so no row of it is wasted)
+// Lane (g, t) = (lane / 4, lane % 4) holds keys of positions g and g + 8 and values of positions 2t, 2t + 1, 2t + 8, 2t + 9.  Which
+// dimension stands at which place of a contraction is free as long as Q agrees, so a lane's keys are whole 16-byte pieces of a row,
+// likewise its values (piece g of a row): everything comes straight from global memory into the registers that the MMA reads,
+// one tile ahead.  Eight bits become f16, which holds every e4m3 and int8 number; Q becomes f16 times a power of two that puts its
+// largest element below 2^15, so that no element that counts loses a bit.  Scales of keys go onto the scores.  Scales of values go onto
+// the probabilities, divided by the largest scale so far (f16 holds 2^-24 .. 2^16) and by that much less in the end.
+// The reference that probabilities are relative to follows the maximum only where a score passes it by more than 2^8.
+#include "attn_decode_kernel.cuh"
+
+namespace spec {
+
+__device__ __forceinline__ float da_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool F16> __device__ __forceinline__ void da_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t da_transpose(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint4 da_load16(const void *p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint2 da_load8(const void *p) {
+  uint2 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+// four 8-bit numbers as two pairs of f16
+template <int FMT> __device__ __forceinline__ void da_to_f16(uint32_t x, uint32_t &lo, uint32_t &hi) {
+  if constexpr (FMT == KV_E4M3) {
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffffu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x >> 16), __NV_E4M3);
+    lo = a.x | ((uint32_t)a.y << 16);
+    hi = b.x | ((uint32_t)b.y << 16);
+  } else {                                               // bits 0x6400 | u are 1024 + u, u = x + 128
+    x ^= 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(0x6480));
+    const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+    const __half2 l = __hsub2(*(const __half2 *)&a, off), h = __hsub2(*(const __half2 *)&b, off);
+    lo = *(const uint32_t *)&l;
+    hi = *(const uint32_t *)&h;
+  }
+}
+
+template <int FMT_, int HD, int MR> struct MmaBody {
+  static constexpr int FMT = FMT_, TILE = 16, NB = MR / 8;
+  static constexpr bool Q8 = kv_is_8bit(FMT);
+  typedef typename KvElem<FMT>::type E;
+  static constexpr int EB = sizeof(E), KP = HD * EB / 64, VB = HD * EB / 8 < 16 ? HD * EB / 8 : 16, VP = HD * EB / 8 / VB, EP = VB / EB;
+  static constexpr int STEPS = HD / 16;
+  // values a tile ahead as well, where keys and values of a tile are not half a thread's registers
+  static constexpr bool V_AHEAD = HD * EB < 512;
+  static constexpr int WARPS = HD * EB <= 128 && MR == 8 ? 16 : 8;
+  static __host__ __device__ int warp_smem_floats(int) { return 0; }
+
+  float m[NB][2], l[NB][2], o[NB][STEPS][4];             // of heads 8 n + 2 t and the next
+  uint32_t q[NB][STEPS][2];
+  float qf[NB][2];                                       // scale * log2 e / the power of two on Q
+  float c;                                               // largest scale of a value so far
+
+  __device__ __forceinline__ void init(const DaArgs &p, const DaSeg &sg, bool, float *, int lane) {
+    const int g = lane >> 2, t = lane & 3, group = p.a.H / p.a.cache.G, h0 = (sg.v / p.chunks) * group + (sg.v % p.chunks) * p.heads;
+    const int have = min(p.heads, group - (sg.v % p.chunks) * p.heads);
+#pragma unroll
+    for (int n = 0; n < NB; n++) {
+      const bool in = 8 * n + g < have;
+      const bf16 *x = (const bf16 *)p.a.q + (size_t)sg.b * p.a.q_ts + (size_t)(h0 + (in ? 8 * n + g : 0)) * HD;
+#pragma unroll
+      for (int s = 0; s < STEPS; s++) {                  // the four dimensions of contraction s that this lane's piece of a key holds
+        const int d = EB == 1 ? (s / 4) * 64 + t * 16 + (s % 4) * 4 : (s / 2) * 32 + t * 8 + (s % 2) * 4;
+        const uint2 u = in ? *(const uint2 *)(x + d) : make_uint2(0, 0);
+        q[n][s][0] = u.x, q[n][s][1] = u.y;
+      }
+      float f = p.a.scale * 1.44269504088896341f;
+      if constexpr (Q8) {
+        float top = 0.0f;
+#pragma unroll
+        for (int s = 0; s < STEPS; s++)
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            const float2 v = __bfloat1622float2(*(const __nv_bfloat162 *)&q[n][s][e]);
+            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^(14 - exponent), kept where it and its reciprocal are normal numbers; a head with an infinity is taken as it is
+        int e = (int)(__float_as_uint(top) >> 23) - 127;
+        e = e > 127 ? 14 : max(e, -100);
+        const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+        f *= __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+#pragma unroll
+        for (int s = 0; s < STEPS; s++)
+#pragma unroll
+          for (int i = 0; i < 2; i++) {
+            const float2 v = __bfloat1622float2(*(const __nv_bfloat162 *)&q[n][s][i]);
+            const __half2 h = __floats2half2_rn(v.x * up, v.y * up);
+            q[n][s][i] = *(const uint32_t *)&h;
+          }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        qf[n][e] = __shfl_sync(0xffffffffu, f, (2 * t + e) * 4);
+        m[n][e] = -INFINITY, l[n][e] = 0.0f;
+      }
+#pragma unroll
+      for (int s = 0; s < STEPS; s++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[n][s][e] = 0.0f;
+    }
+    c = 0.0f;
+  }
+
+  struct Keys { uint4 x[2][KP]; };
+  struct Values { uint32_t x[4][VP * VB / 4]; };
+  static __device__ __forceinline__ void load_keys(const char *pool, int row, int g, int t, Keys &k) {
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const char *at = pool + (size_t)(uint32_t)__shfl_sync(0xffffffffu, row, g + 8 * i) * (HD * EB) + t * 16;
+#pragma unroll
+      for (int j = 0; j < KP; j++) k.x[i][j] = da_load16(at + j * 64);
+    }
+  }
+  static __device__ __forceinline__ void load_values(const char *pool, int row, int g, int t, Values &v) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const char *at = pool + (size_t)(uint32_t)__shfl_sync(0xffffffffu, row, 2 * t + (i & 1) + 4 * (i & 2)) * (HD * EB) + g * VB;
+#pragma unroll
+      for (int j = 0; j < VP; j++)
+        if constexpr (VB == 16) {
+          const uint4 u = da_load16(at + j * 128);
+          v.x[i][4 * j] = u.x, v.x[i][4 * j + 1] = u.y, v.x[i][4 * j + 2] = u.z, v.x[i][4 * j + 3] = u.w;
+        } else {
+          const uint2 u = da_load8(at);
+          v.x[i][0] = u.x, v.x[i][1] = u.y;
+        }
+    }
+  }
+
+  __device__ __forceinline__ void run(const DaArgs &p, const DaSeg &sg, int len, int lane) {
+    const KvCache &cc = p.a.cache;
+    const int g = lane >> 2, t = lane & 3, head = sg.v / p.chunks, tok = lane & 15;
+    const char *K = (const char *)cc.k, *V = (const char *)cc.v;
+    const float *SC = lane < 16 ? cc.ks : cc.vs;
+    const int32_t *table = cc.table + (size_t)sg.b * cc.pages_per_seq;
+    // the page of this lane's position of a tile (past the end: of the last position), then its row
+    int off = 0;
+    auto page_of = [&](int tile) {
+      const int pos = min(tile * TILE + tok, len - 1), at = p.page_shift >= 0 ? pos >> p.page_shift : pos / cc.page_size;
+      off = pos - at * cc.page_size;
+      return table[at];
+    };
+    // row of this lane's position; valid: bit i is set where position i counts.  A page that is none of the pool's is read as page 0.
+    auto row_of = [&](int tile, int page, uint32_t &valid) {
+      const bool ok = page >= 0 && page < cc.num_pages;
+      if (!ok) set_status(p.a.status, ST_BOUNDS, 63, sg.b, page);
+      valid = __ballot_sync(0xffffffffu, ok && tile * TILE + tok < len) & 0xffffu;
+      return ((ok ? page : 0) * cc.G + head) * cc.page_size + off;
+    };
+    uint32_t valid, valid_next = 0;
+    int row = 0, row_next = 0, page;
+    row = row_of(sg.t0, page_of(sg.t0), valid);
+    Keys k;
+    Values v;
+    float sc = 1.0f, sc_next = 1.0f;
+    load_keys(K, row, g, t, k);
+    if constexpr (Q8) sc = SC[row];
+    if constexpr (V_AHEAD) load_values(V, row, g, t, v);
+    page = page_of(min(sg.t0 + 1, sg.t1 - 1));
+    for (int tile = sg.t0; tile < sg.t1; tile++) {
+      const int next = min(tile + 1, sg.t1 - 1);         // the last tile is asked for once more
+      row_next = row_of(next, page, valid_next);
+      page = page_of(min(tile + 2, sg.t1 - 1));
+      // ---- scores
+      float s[NB][4];
+#pragma unroll
+      for (int n = 0; n < NB; n++) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < KP; j++) {
+        const uint32_t x[4] = {k.x[0][j].x, k.x[0][j].y, k.x[0][j].z, k.x[0][j].w}, y[4] = {k.x[1][j].x, k.x[1][j].y, k.x[1][j].z, k.x[1][j].w};
+        if constexpr (Q8) {
+#pragma unroll
+          for (int w = 0; w < 4; w++) {
+            uint32_t a0, a1, a2, a3;
+            da_to_f16<FMT>(x[w], a0, a2);
+            da_to_f16<FMT>(y[w], a1, a3);
+#pragma unroll
+            for (int n = 0; n < NB; n++) da_mma<true>(s[n], a0, a1, a2, a3, q[n][4 * j + w][0], q[n][4 * j + w][1]);
+          }
+        } else {
+#pragma unroll
+          for (int w = 0; w < 4; w += 2)
+#pragma unroll
+            for (int n = 0; n < NB; n++) da_mma<false>(s[n], x[w], y[w], x[w + 1], y[w + 1], q[n][2 * j + w / 2][0], q[n][2 * j + w / 2][1]);
+        }
+      }
+      if constexpr (V_AHEAD) {
+        load_keys(K, row_next, g, t, k);
+        if constexpr (Q8) sc_next = SC[row_next];
+      } else {
+        load_values(V, row, g, t, v);
+      }
+      // ---- probabilities: positions g and g + 8 (elements 0, 1 and 2, 3) of two heads
+      float ks[2] = {1.0f, 1.0f}, vs[2] = {1.0f, 1.0f};
+      float grow = 1.0f;
+      if constexpr (Q8) {
+        if (!((valid >> tok) & 1)) sc = 0.0f;            // what stands there may be no number
+        ks[0] = __shfl_sync(0xffffffffu, sc, g), ks[1] = __shfl_sync(0xffffffffu, sc, g + 8);
+        vs[0] = __shfl_sync(0xffffffffu, sc, g + 16), vs[1] = __shfl_sync(0xffffffffu, sc, g + 24);
+        const float top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : __float_as_uint(sc))), 8.0e-31f);
+        if (!(top <= c)) {
+          grow = c / top;
+          c = top;
+        }
+      }
+      bool over = false;
+#pragma unroll
+      for (int n = 0; n < NB; n++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          s[n][e] *= ks[e >> 1] * qf[n][e & 1];
+          if (valid != 0xffffu && !((valid >> (g + 8 * (e >> 1))) & 1)) s[n][e] = -INFINITY;
+          over |= s[n][e] > m[n][e & 1] + 8.0f;
+        }
+      if (__any_sync(0xffffffffu, over) || grow != 1.0f) {
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            float x = fmaxf(fmaxf(s[n][e], s[n][e + 2]), m[n][e]);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+            const float f = da_ex2(m[n][e] - da_ref(x));
+            m[n][e] = x;
+            l[n][e] *= f;
+#pragma unroll
+            for (int i = 0; i < STEPS; i++) o[n][i][e] *= f * grow, o[n][i][e + 2] *= f * grow;
+          }
+      }
+      const float to_f16 = Q8 ? 64.0f / c : 1.0f;
+      uint32_t b[NB][2];
+#pragma unroll
+      for (int n = 0; n < NB; n++) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          s[n][e] = da_ex2(s[n][e] - da_ref(m[n][e & 1]));
+          l[n][e & 1] += s[n][e];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+          uint32_t pair;
+          if constexpr (Q8) {
+            const float w = vs[i] * to_f16;
+            const __half2 h = __floats2half2_rn(s[n][2 * i] * w, s[n][2 * i + 1] * w);
+            pair = *(const uint32_t *)&h;
+          } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(s[n][2 * i], s[n][2 * i + 1]);
+            pair = *(const uint32_t *)&h;
+          }
+          b[n][i] = da_transpose(pair);                  // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
+        }
+      }
+      // ---- output
+      if (valid != 0xffffu) {                            // a page that is none: zero times whatever stands in page 0 is to be zero
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+          if (!((valid >> (2 * t + (i & 1) + 4 * (i & 2))) & 1))
+#pragma unroll
+            for (int j = 0; j < VP * VB / 4; j++) v.x[i][j] = 0;
+      }
+#pragma unroll
+      for (int j = 0; j < VP * VB / 4; j++) {
+        if constexpr (Q8) {                              // four dimensions: two contractions' rows g and g + 8
+          uint32_t lo[2], hi[2], lo8[2], hi8[2];         // [positions 2t, 2t + 1 | 2t + 8, 2t + 9] of dimensions 0, 1 / 2, 3
+#pragma unroll
+          for (int i = 0; i < 2; i++) {
+            const uint32_t x = v.x[2 * i][j], y = v.x[2 * i + 1][j];
+            da_to_f16<FMT>(__byte_perm(x, y, 0x5140), lo[i], hi[i]);
+            da_to_f16<FMT>(__byte_perm(x, y, 0x7362), lo8[i], hi8[i]);
+          }
+#pragma unroll
+          for (int n = 0; n < NB; n++) {
+            da_mma<true>(o[n][2 * j], lo[0], hi[0], lo[1], hi[1], b[n][0], b[n][1]);
+            da_mma<true>(o[n][2 * j + 1], lo8[0], hi8[0], lo8[1], hi8[1], b[n][0], b[n][1]);
+          }
+        } else {
+          const uint32_t a0 = __byte_perm(v.x[0][j], v.x[1][j], 0x5410), a1 = __byte_perm(v.x[0][j], v.x[1][j], 0x7632);
+          const uint32_t a2 = __byte_perm(v.x[2][j], v.x[3][j], 0x5410), a3 = __byte_perm(v.x[2][j], v.x[3][j], 0x7632);
+#pragma unroll
+          for (int n = 0; n < NB; n++) da_mma<false>(o[n][j], a0, a1, a2, a3, b[n][0], b[n][1]);
+        }
+      }
+      if constexpr (V_AHEAD) {
+        load_values(V, row_next, g, t, v);
+      } else {
+        load_keys(K, row_next, g, t, k);
+        if constexpr (Q8) sc_next = SC[row_next];
+      }
+      sc = sc_next;
+      row = row_next;
+      valid = valid_next;
+    }
+#pragma unroll
+    for (int n = 0; n < NB; n++)
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+        if constexpr (Q8)
+#pragma unroll
+          for (int i = 0; i < STEPS; i++) o[n][i][e] *= c * 0.015625f, o[n][i][e + 2] *= c * 0.015625f;
+      }
+  }
+
+  template <typename F, typename G> __device__ __forceinline__ void each(int, int lane, F f, G stat) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NB; n++)
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        const int h = 8 * n + 2 * t + e;
+#pragma unroll
+        for (int j = 0; j < VP; j++)
+#pragma unroll
+          for (int i = 0; i < EP; i += 4) {
+            const int at = (j * EP + i) / 2;
+            f(h, j * 8 * EP + g * EP + i, make_float4(o[n][at][e], o[n][at][e + 2], o[n][at + 1][e], o[n][at + 1][e + 2]), l[n][e]);
+          }
+        if (g == 0) stat(h, m[n][e], l[n][e]);
+      }
+  }
+};
+
+template <int FMT, int HD> static cudaError_t mma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
+  if constexpr (HD < 256)
+    if (p.heads > 8) return launch<MmaBody<FMT, HD, 16>>(p, false, ctas, s);
+  return launch<MmaBody<FMT, HD, 8>>(p, false, ctas, s);
+}
+template <int FMT> static cudaError_t mma_by_hd(const DaArgs &p, int ctas, cudaStream_t s) {
+  return p.a.cache.hd == 64 ? mma_by_heads<FMT, 64>(p, ctas, s) : p.a.cache.hd == 128 ? mma_by_heads<FMT, 128>(p, ctas, s) : mma_by_heads<FMT, 256>(p, ctas, s);
+}
+
+cudaError_t launch_decode_mma(const DaArgs &p, int fmt, int ctas, cudaStream_t s) {
+  return fmt == KV_BF16 ? mma_by_hd<KV_BF16>(p, ctas, s) : fmt == KV_E4M3 ? mma_by_hd<KV_E4M3>(p, ctas, s) : mma_by_hd<KV_INT8>(p, ctas, s);
+}
+
+}  // namespace spec
