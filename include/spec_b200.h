@@ -343,7 +343,7 @@ enum spec_kv_format { SPEC_KV_F32 = 0, SPEC_KV_BF16 = 1, SPEC_KV_E4M3 = 2, SPEC_
 /* A paged cache: pools [num_pages][n_kv_heads][page_size][head_dim] of `format`, position p of sequence s in page
  * page_table[s][p / page_size].  The 8-bit formats have a scale for each token and head, [num_pages][n_kv_heads][page_size]:
  * value = code * scale, scale = max(largest magnitude / top, 2^-120), top 448 (E4M3) or 127 (INT8: codes -127..127), codes rounded to
- * nearest even.  A row with an infinity or a NaN reads back as NaN.  head_dim % 16 == 0, <= 256; pools 16-byte aligned; any page size.
+ * nearest even.  A row with an infinity or a NaN reads back as NaN.  head_dim % 16 == 0, <= 256; n_kv_heads <= 1024; pools 16-byte aligned; any page size.
  * F32 goes with dtype F32, BF16 with BF16, the 8-bit formats with both. */
 typedef struct {
   void *k, *v;

@@ -497,6 +497,13 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _stream_of(t: torch.Tensor) -> int:
+    """The current stream of a tensor's device, which has to be the current device (a launch goes there)."""
+    at = t.get_device()
+    _need(at == torch.cuda.current_device(), "the tensors are on another device than the current one")
+    return torch._C._cuda_getCurrentRawStream(at)
+
+
 def _ints(t: torch.Tensor, n: int, what: str) -> int:
     _need(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.is_cuda, what)
     return t.data_ptr()
@@ -561,7 +568,7 @@ def _turn(x, positions, inv_freq, layout, mscale, out, transpose):
     rc = lib().spec_rotary(_dt(x.dtype), *_heads(x, "rotary: x [tokens][heads][head_dim] with adjacent dimensions"),
                            *_heads(out, "rotary: out [tokens][heads][head_dim] with adjacent dimensions"),
                            _ints(positions, T, "rotary: positions int32 [tokens]"), T, H, hd, C.byref(_rope(inv_freq, layout, mscale)), transpose,
-                           _stream_ptr(None))
+                           _stream_of(x))
     if rc:
         raise SpecError(rc, "spec_rotary")
     return out
@@ -621,7 +628,7 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: to
                               *_heads(v, "kv_append: v [tokens][kv heads][head_dim] with adjacent dimensions"),
                               _ints(row_seq, T, "kv_append: row_seq int32 [tokens]"), _ints(row_pos, T, "kv_append: row_pos int32 [tokens]"),
                               None if row_kvpos is None else _ints(row_kvpos, T, "kv_append: row_kvpos int32 [tokens]"), T,
-                              None if rope is None else C.byref(rope), C.byref(cache), _status_ptr(status), _stream_ptr(None))
+                              None if rope is None else C.byref(rope), C.byref(cache), _status_ptr(status), _stream_of(k))
     if rc:
         raise SpecError(rc, "spec_kv_append")
     return q_out
@@ -636,7 +643,7 @@ def kv_read(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor
     out = torch.empty(2, rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=k_pool.device)
     k, v = out.unbind(0)
     rc = lib().spec_kv_read(C.byref(cache), _ints(row_seq, rows, "kv_read: row_seq int32 [rows]"), _ints(row_kvpos, rows, "kv_read: row_kvpos int32 [rows]"),
-                            rows, _dt(dtype), k.data_ptr(), v.data_ptr(), _status_ptr(status), _stream_ptr(None))
+                            rows, _dt(dtype), k.data_ptr(), v.data_ptr(), _status_ptr(status), _stream_of(k_pool))
     if rc:
         raise SpecError(rc, "spec_kv_read")
     return k, v
@@ -661,9 +668,9 @@ def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor
         out = torch.empty(B, H, hd, dtype=q.dtype, device=q.device)
     _need(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "decode_attention: out contiguous, of q's shape and dtype")
     lse = torch.empty(B, H, dtype=torch.float32, device=q.device) if want_lse else None
-    stream = _stream_ptr(None)
+    stream = _stream_of(q)
     if workspace is None:
-        at = (q.device, stream)
+        at = (q.get_device(), stream)
         workspace = _workspaces.get(at)
         if workspace is None:
             workspace = _workspaces[at] = decode_workspace(q.device)

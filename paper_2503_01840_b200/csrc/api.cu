@@ -1756,7 +1756,7 @@ static int cache_of(const spec_kv_cache *c, KvCache *out) {
   if (c->format < SPEC_KV_F32 || c->format > SPEC_KV_INT8) return SPEC_ERR_INVALID_CFG;
   if (kv_is_8bit(c->format) && (!c->k_scale || !c->v_scale)) return SPEC_ERR_NULL;
   if (c->n_seq < 1 || c->pages_per_seq < 1 || c->page_size < 1 || c->num_pages < 1 || c->n_kv_heads < 1) return SPEC_ERR_INVALID_CFG;
-  if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16) return SPEC_ERR_UNSUPPORTED;
+  if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16 || c->n_kv_heads > 1024) return SPEC_ERR_UNSUPPORTED;
   if (!kv_aligned(c->k, 16) || !kv_aligned(c->v, 16) || !kv_aligned(c->k_scale, 4) || !kv_aligned(c->v_scale, 4)) return SPEC_ERR_INVALID_CFG;
   // rows of the pool and positions of a sequence are counted in 32 bits on the device
   const double rows = (double)c->num_pages * c->n_kv_heads * c->page_size, positions = (double)c->pages_per_seq * c->page_size;

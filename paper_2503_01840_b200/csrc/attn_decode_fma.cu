@@ -36,9 +36,12 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
   }
 
   static __device__ __forceinline__ void unpack(const uint4 &u, float (&x)[VEC]) {
-    const E *e = (const E *)&u;
+    const typename Four<FMT>::raw *r = (const typename Four<FMT>::raw *)&u;
 #pragma unroll
-    for (int i = 0; i < VEC; i++) x[i] = kv_decode<FMT>(e[i]);
+    for (int i = 0; i < VEC / 4; i++) {
+      const float4 f = kv_decode_four<FMT>(r[i]);
+      x[4 * i] = f.x, x[4 * i + 1] = f.y, x[4 * i + 2] = f.z, x[4 * i + 3] = f.w;
+    }
   }
 
   __device__ void run(const DaArgs &p, const DaSeg &sg, int len, int lane) {
@@ -102,10 +105,8 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
 #pragma unroll
           for (int e = 0; e < 4; e++) x[i][e] = 0.0f;
           if (r >= 0 && d < hd) {
-            struct alignas(4 * sizeof(E)) Four { E e[4]; };
-            const Four u = *(const Four *)(V + (size_t)r * hd + d);
-#pragma unroll
-            for (int e = 0; e < 4; e++) x[i][e] = kv_decode<FMT>(u.e[e]);
+            const float4 f = kv_decode_four<FMT>(*(const typename Four<FMT>::raw *)(V + (size_t)r * hd + d));
+            x[i][0] = f.x, x[i][1] = f.y, x[i][2] = f.z, x[i][3] = f.w;
           }
         }
 #pragma unroll

@@ -2,11 +2,16 @@
 //
 // Rotation: the pair (a, b) of a head's dimensions at position p becomes m (a cos t - b sin t, b cos t + a sin t), t = p f; its
 // gradient is the transposed matrix, -t for t.  Quantisation, for each token and head: scale = max(amax / top, 2^-120) over the
-// rotated 32-bit values, code = round(x / scale).  A row with an infinity or a NaN gets a scale that is infinite or NaN and
-// reads back as NaN throughout.
+// rotated 32-bit values, code = round(x / scale).  A row with an infinity or a NaN gets a scale of NaN and reads
+// back as NaN throughout.
 #include "kv_cache.cuh"
 
+#include <algorithm>
+
 namespace spec {
+
+using std::max;
+using std::min;
 
 constexpr int ROPE_THREADS = 256, ROPE_MAX_HD = 256;
 
@@ -59,11 +64,10 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_any_kernel(RopeAppen
     const long long row = row0 + (long long)h * a.cache.page_size;
     E *o = (E *)(kind == 1 ? a.cache.k : a.cache.v) + row * hd;
     if constexpr (kv_is_8bit(FMT)) {
-      const float amax = __uint_as_float(__reduce_max_sync(0xffffffffu, top)) * (1.0f / kv_top<FMT>());
-      const float scale = amax < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : amax, inv = 1.0f / scale;
+      const float scale = kv_scale<FMT>(__reduce_max_sync(0xffffffffu, top)), inv = 1.0f / scale;
 #pragma unroll
       for (int j = 0; j < ROPE_MAX_HD / 32; j++)
-        if (lane + j * 32 < hd) o[lane + j * 32] = kv_encode<FMT>(y[j] * inv);
+        if (lane + j * 32 < hd) o[lane + j * 32] = (E)kv_encode4<FMT>(y[j] * inv, 0.0f, 0.0f, 0.0f);
       if (lane == 0) (kind == 1 ? a.cache.ks : a.cache.vs)[row] = scale;
     } else {
 #pragma unroll
@@ -73,8 +77,178 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_any_kernel(RopeAppen
   }
 }
 
+// ---------------------------------------------------------------- heads of whole 16-byte pieces
+// A head is shared by LH lanes, a power of two, each with two 16-byte pieces: the two whose elements pair up in the half layout,
+// neighbours in the interleaved one and past the rotated dimensions.  So a pair never leaves a lane, and a head's largest magnitude is LH
+// lanes' exchange.  A block takes some heads of some tokens; their cosines and sines are formed once, in shared memory.
+// Bytes bound it: a thread asks for its first U heads before it forms the angles.
+__device__ __forceinline__ void unpack_piece(uint4 u, float (&y)[4]) {
+  y[0] = __uint_as_float(u.x), y[1] = __uint_as_float(u.y), y[2] = __uint_as_float(u.z), y[3] = __uint_as_float(u.w);
+}
+__device__ __forceinline__ void unpack_piece(uint4 u, float (&y)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) y[2 * i] = __uint_as_float(w[i] << 16), y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+}
+__device__ __forceinline__ uint4 pack_piece(const float (&y)[4]) {
+  return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+}
+__device__ __forceinline__ uint4 pack_piece(const float (&y)[8]) {
+  return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+}
+struct RopeGrid {
+  int per_block, heads;         // tokens and heads of a block
+  int lh_shift;                 // log2 of LH
+  uint32_t by_heads;            // ceil(2^32 / heads): quotients of the small numbers here by a product
+};
+constexpr int ROPE_MAX_TOKENS = 16;
+
+template <typename T, int FMT, bool INTER, int U>
+__global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(RopeAppend a, RopeGrid gr) {
+  pdl_wait();
+  pdl_trigger();
+  typedef typename KvElem<FMT>::type E;
+  constexpr int VE = 16 / sizeof(T);
+  extern __shared__ __align__(16) float trig[];          // [tokens][cos half | sin half]
+  __shared__ long long rows[ROPE_MAX_TOKENS];
+  const int tid = threadIdx.x, hd = a.hd, half = a.rope.half, G = a.k.p ? a.cache.G : 0;
+  const int t0 = blockIdx.x * gr.per_block, nt = min(gr.per_block, a.tokens - t0), h0 = blockIdx.y * gr.heads, nh = min(gr.heads, a.H + 2 * G - h0);
+  const int l = tid & ((1 << gr.lh_shift) - 1), slot = tid >> gr.lh_shift, step = ROPE_THREADS >> gr.lh_shift;
+  // this lane's two pieces of a head (in elements), and whether they turn
+  const bool paired = !INTER && l * VE < half;
+  const int d0 = paired ? l * VE : 2 * l * VE, d1 = paired ? half + l * VE : d0 + VE;
+  const bool turn0 = INTER ? d0 < 2 * half : paired, turn1 = INTER ? d1 < 2 * half : paired;
+
+  uint4 x[U][2];
+  auto source = [&](int j, int &t, int &h) -> const T * {                // head j of the block's; null: there is none
+    t = (int)__umulhi((uint32_t)j, gr.by_heads);
+    h = h0 + j - t * gr.heads;
+    if (t >= nt || h - h0 >= nh) return nullptr;
+    const HeadView &v = h < a.H ? a.q : h < a.H + G ? a.k : a.v;
+    return (const T *)v.p + (long long)(t0 + t) * v.ts + (long long)(h < a.H ? h : h < a.H + G ? h - a.H : h - a.H - G) * v.hs;
+  };
+  const int most = gr.per_block * gr.heads;
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      int t, h;
+      const int j = j0 + u * step;
+      const T *p = j < most ? source(j, t, h) : nullptr;
+      if (p) x[u][0] = *(const uint4 *)(p + d0), x[u][1] = *(const uint4 *)(p + d1);
+    }
+  };
+  load(slot);
+  for (int i = tid; i < nt * half; i += ROPE_THREADS) {
+    const int t = i / half, pair = i - t * half;
+    const float2 c = rope_angle(a.rope, a.pos[t0 + t], pair);
+    trig[t * 2 * half + pair] = c.x;
+    trig[t * 2 * half + half + pair] = c.y;
+  }
+  if (G && tid < nt) rows[tid] = kv_row(a.cache, a.seq[t0 + tid], a.kvpos[t0 + tid], a.status, t0 + tid);
+  __syncthreads();
+  for (int j0 = slot; j0 < most; j0 += U * step) {
+    if (j0 != slot) load(j0);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      int t, h;
+      const int j = j0 + u * step;
+      if (j >= most || !source(j, t, h)) continue;
+      float y0[VE], y1[VE];
+      unpack_piece(x[u][0], y0);
+      unpack_piece(x[u][1], y1);
+      if (h < a.H + G) {
+        const float *cs = trig + t * 2 * half, *sn = cs + half;
+        if constexpr (INTER) {
+          if (turn0)
+#pragma unroll
+            for (int i = 0; i < VE; i += 2) {
+              const float c = cs[(d0 + i) / 2], s = sn[(d0 + i) / 2], p = y0[i], q = y0[i + 1];
+              y0[i] = fmaf(p, c, -(q * s)), y0[i + 1] = fmaf(q, c, p * s);
+            }
+          if (turn1)
+#pragma unroll
+            for (int i = 0; i < VE; i += 2) {
+              const float c = cs[(d1 + i) / 2], s = sn[(d1 + i) / 2], p = y1[i], q = y1[i + 1];
+              y1[i] = fmaf(p, c, -(q * s)), y1[i + 1] = fmaf(q, c, p * s);
+            }
+        } else if (paired) {
+#pragma unroll
+          for (int i = 0; i < VE; i += 4) {
+            const float4 c = *(const float4 *)(cs + d0 + i), s = *(const float4 *)(sn + d0 + i);
+            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+              const float p = y0[i + e], q = y1[i + e];
+              y0[i + e] = fmaf(p, cc[e], -(q * ss[e])), y1[i + e] = fmaf(q, cc[e], p * ss[e]);
+            }
+          }
+        }
+      }
+      if (h < a.H) {
+        T *o = (T *)a.q_out + (long long)(t0 + t) * a.qo_ts + (long long)h * a.qo_hs;
+        *(uint4 *)(o + d0) = pack_piece(y0);
+        *(uint4 *)(o + d1) = pack_piece(y1);
+        continue;
+      }
+      if (rows[t] < 0) continue;                         // all lanes of a head alike
+      const bool key = h < a.H + G;
+      const long long row = rows[t] + (long long)(key ? h - a.H : h - a.H - G) * a.cache.page_size;
+      E *o = (E *)(key ? a.cache.k : a.cache.v) + row * hd;
+      if constexpr (kv_is_8bit(FMT)) {
+        uint32_t top = 0;                                // bits of the largest magnitude: NaN counts as the largest of all
+#pragma unroll
+        for (int i = 0; i < VE; i++) top = max(top, max(__float_as_uint(y0[i]) & 0x7fffffffu, __float_as_uint(y1[i]) & 0x7fffffffu));
+        const uint32_t group = (gr.lh_shift == 5 ? 0xffffffffu : ((1u << (1 << gr.lh_shift)) - 1)) << (tid & 31 & ~((1 << gr.lh_shift) - 1));
+        for (int d = 1; d < 1 << gr.lh_shift; d <<= 1) top = max(top, __shfl_xor_sync(group, top, d));
+        const float scale = kv_scale<FMT>(top), inv = 1.0f / scale;
+#pragma unroll
+        for (int i = 0; i < VE; i++) y0[i] *= inv, y1[i] *= inv;
+        if constexpr (VE == 8) {
+          *(uint2 *)(o + d0) = make_uint2(kv_encode4<FMT>(y0[0], y0[1], y0[2], y0[3]), kv_encode4<FMT>(y0[4], y0[5], y0[6], y0[7]));
+          *(uint2 *)(o + d1) = make_uint2(kv_encode4<FMT>(y1[0], y1[1], y1[2], y1[3]), kv_encode4<FMT>(y1[4], y1[5], y1[6], y1[7]));
+        } else {
+          *(uint32_t *)(o + d0) = kv_encode4<FMT>(y0[0], y0[1], y0[2], y0[3]);
+          *(uint32_t *)(o + d1) = kv_encode4<FMT>(y1[0], y1[1], y1[2], y1[3]);
+        }
+        if (l == 0) (key ? a.cache.ks : a.cache.vs)[row] = scale;
+      } else {                                           // of the keys' own type
+        *(uint4 *)(o + d0) = pack_piece(y0);
+        *(uint4 *)(o + d1) = pack_piece(y1);
+      }
+    }
+  }
+}
+
+static bool whole_pieces(const void *p, long long ts, long long hs, size_t e) {
+  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ts * (long long)e) | (uintptr_t)(hs * (long long)e)) & 15) == 0;
+}
+
 template <typename T, int FMT> static cudaError_t rope_append(const RopeAppend &a, cudaStream_t s) {
-  return launch_k(rope_append_any_kernel<T, FMT>, dim3(a.tokens), dim3(ROPE_THREADS), 0, s, a);
+  constexpr int VE = 16 / sizeof(T);
+  const int G = a.k.p ? a.cache.G : 0, all = a.H + 2 * G, lh = a.hd / (2 * VE);
+  const bool pieces = a.hd % (2 * VE) == 0 && (lh & (lh - 1)) == 0 && lh <= 32 && (a.rope.interleaved ? 2 * a.rope.half : a.rope.half) % VE == 0 &&
+                      (!a.H || (whole_pieces(a.q.p, a.q.ts, a.q.hs, sizeof(T)) && whole_pieces(a.q_out, a.qo_ts, a.qo_hs, sizeof(T)))) &&
+                      (!G || (whole_pieces(a.k.p, a.k.ts, a.k.hs, sizeof(T)) && whole_pieces(a.v.p, a.v.ts, a.v.hs, sizeof(T))));
+  if (!pieces || all > 4096) return launch_k(rope_append_any_kernel<T, FMT>, dim3(a.tokens), dim3(ROPE_THREADS), 0, s, a);
+  RopeGrid gr;
+  gr.lh_shift = __builtin_ctz(lh);
+  const int step = ROPE_THREADS / lh;                    // heads of a round of the block
+  constexpr int U = 2;
+  // few tokens: a round's heads a block, so that no thread has a second round to wait for; many: about 4 U rounds a block
+  const long long rounds = ((long long)a.tokens * all + step - 1) / step;
+  if (rounds <= 1184) {
+    gr.per_block = 1;
+    gr.heads = min(all, step);
+  } else {
+    gr.heads = all;
+    gr.per_block = max(1, min(ROPE_MAX_TOKENS, 4 * U * step / all));
+  }
+  gr.by_heads = gr.heads == 1 ? 0xffffffffu : (uint32_t)((0x100000000ull + gr.heads - 1) / gr.heads);
+  if (gr.heads == 1 && gr.per_block > 1) gr.per_block = 1;
+  const dim3 grid((a.tokens + gr.per_block - 1) / gr.per_block, (all + gr.heads - 1) / gr.heads);
+  const size_t smem = (size_t)gr.per_block * 2 * a.rope.half * sizeof(float);
+  if (a.rope.interleaved) return launch_k(rope_append_kernel<T, FMT, true, U>, grid, dim3(ROPE_THREADS), smem, s, a, gr);
+  return launch_k(rope_append_kernel<T, FMT, false, U>, grid, dim3(ROPE_THREADS), smem, s, a, gr);
 }
 
 cudaError_t launch_rope_append(const RopeAppend &a, int dtype, int fmt, cudaStream_t s) {
@@ -83,31 +257,71 @@ cudaError_t launch_rope_append(const RopeAppend &a, int dtype, int fmt, cudaStre
 }
 
 // ---------------------------------------------------------------- reading back
-// A block per row: row r of the output is position kvpos[r] of sequence seq[r], zeros where there is none.
+// Row r of the output is position kvpos[r] of sequence seq[r], zeros where there is none.  A thread takes eight elements, so that a
+// warp's stores of bf16 are whole lines; a block some rows, whose places in the pool are looked up once.
+constexpr int READ_MAX_ROWS = 64;
+struct ReadGrid { int rows, items; uint32_t by_items; };                 // rows of a block, eights of a row (keys, then values)
+
 template <int FMT, typename T>
-__global__ void __launch_bounds__(256) kv_read_any_kernel(KvRead a) {
+__global__ void __launch_bounds__(256) kv_read_kernel(KvRead a, ReadGrid gr) {
   pdl_wait();
   pdl_trigger();
   typedef typename KvElem<FMT>::type E;
-  const int r = blockIdx.x, hd = a.cache.hd, n = a.cache.G * hd;
-  __shared__ long long row0;
-  if (threadIdx.x == 0) row0 = kv_row(a.cache, a.seq[r], a.kvpos[r], a.status, r);
+  const int hd8 = a.cache.hd / 8, r0 = blockIdx.x * gr.rows, nr = min(gr.rows, a.rows - r0);
+  __shared__ long long at[READ_MAX_ROWS];
+  if (threadIdx.x < nr) at[threadIdx.x] = kv_row(a.cache, a.seq[r0 + threadIdx.x], a.kvpos[r0 + threadIdx.x], a.status, r0 + threadIdx.x);
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * n; i += 256) {
-    const int kv = i >= n, e = i - kv * n, h = e / hd;
-    float x = 0.0f;
-    if (row0 >= 0) {
-      const long long row = row0 + (long long)h * a.cache.page_size;
-      x = kv_decode<FMT>(((const E *)(kv ? a.cache.v : a.cache.k))[row * hd + (e - h * hd)]);
-      if constexpr (kv_is_8bit(FMT)) x *= (kv ? a.cache.vs : a.cache.ks)[row];
+  const int half = gr.items / 2, n = nr * gr.items;
+  typedef typename Four<FMT>::raw Raw;
+  struct alignas(sizeof(E) == 4 ? 16 : 8 * sizeof(E)) Eight { Raw e[2]; };
+  constexpr int U = 4;                                   // in flight
+  for (int i0 = threadIdx.x; i0 < n; i0 += U * 256) {
+    Eight x[U];
+    float sc[U];
+    T *to[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int i = i0 + u * 256;
+      const int r = (int)__umulhi((uint32_t)i, gr.by_items), e = i - r * gr.items, kv = e >= half, w = e - kv * half, h = w / hd8, d = (w - h * hd8) * 8;
+      to[u] = nullptr;
+      if (i >= n) continue;
+      to[u] = (T *)(kv ? a.v_out : a.k_out) + ((size_t)(r0 + r) * half + w) * 8;
+      const long long row = at[r] + (long long)h * a.cache.page_size;
+      x[u] = Eight{};
+      sc[u] = 0.0f;
+      if (at[r] < 0) continue;
+      x[u] = *(const Eight *)((const E *)(kv ? a.cache.v : a.cache.k) + row * a.cache.hd + d);
+      if constexpr (kv_is_8bit(FMT)) sc[u] = (kv ? a.cache.vs : a.cache.ks)[row];
     }
-    ((T *)(kv ? a.v_out : a.k_out))[(size_t)r * n + e] = from_f32<T>(x);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      if (!to[u]) continue;
+      float4 lo = kv_decode_four<FMT>(x[u].e[0]), hi = kv_decode_four<FMT>(x[u].e[1]);
+      if constexpr (kv_is_8bit(FMT)) {
+        lo.x *= sc[u], lo.y *= sc[u], lo.z *= sc[u], lo.w *= sc[u];
+        hi.x *= sc[u], hi.y *= sc[u], hi.z *= sc[u], hi.w *= sc[u];
+      }
+      if constexpr (sizeof(T) == 4) {
+        ((float4 *)to[u])[0] = lo;
+        ((float4 *)to[u])[1] = hi;
+      } else {
+        *(uint4 *)to[u] = make_uint4(pack_bf16(lo.x, lo.y), pack_bf16(lo.z, lo.w), pack_bf16(hi.x, hi.y), pack_bf16(hi.z, hi.w));
+      }
+    }
   }
 }
 
 template <int FMT> static cudaError_t kv_read(const KvRead &a, int out_dtype, cudaStream_t s) {
-  if (out_dtype == KV_F32) return launch_k(kv_read_any_kernel<FMT, float>, dim3(a.rows), dim3(256), 0, s, a);
-  return launch_k(kv_read_any_kernel<FMT, bf16>, dim3(a.rows), dim3(256), 0, s, a);
+  ReadGrid gr;
+  gr.items = 2 * a.cache.G * (a.cache.hd / 8);
+  // about four items a thread, fewer where that leaves SMs without a block
+  const long long total = (long long)a.rows * gr.items;
+  const int want = total >= 4ll * 256 * 592 ? 1024 : 256;
+  gr.rows = max(1, min(READ_MAX_ROWS, want / gr.items));
+  gr.by_items = (uint32_t)((0x100000000ull + gr.items - 1) / gr.items);
+  const dim3 grid((a.rows + gr.rows - 1) / gr.rows);
+  if (out_dtype == KV_F32) return launch_k(kv_read_kernel<FMT, float>, grid, dim3(256), 0, s, a, gr);
+  return launch_k(kv_read_kernel<FMT, bf16>, grid, dim3(256), 0, s, a, gr);
 }
 
 cudaError_t launch_kv_read(const KvRead &a, int fmt, int out_dtype, cudaStream_t s) {

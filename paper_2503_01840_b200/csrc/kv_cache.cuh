@@ -17,7 +17,6 @@ constexpr bool kv_is_8bit(int fmt) { return fmt == KV_E4M3 || fmt == KV_INT8; }
 
 // A scale is max(amax / top, 2^-120): its reciprocal is then finite for every row of finite numbers, one of zeros too.
 constexpr float KV_SCALE_FLOOR = 7.52316384526264e-37f;
-template <int FMT> constexpr float kv_top() { return FMT == KV_E4M3 ? 448.0f : 127.0f; }
 
 // pools [num_pages][G][page_size][hd], scales [num_pages][G][page_size] (8-bit formats), table [n_seq][pages_per_seq]
 struct KvCache {
@@ -86,14 +85,55 @@ __device__ __forceinline__ float2 rope_angle(const Rope &r, int pos, int pair) {
   return make_float2(c * r.mscale, s * (r.mscale * r.sign));
 }
 
-template <int FMT> __device__ __forceinline__ float kv_decode(typename KvElem<FMT>::type x) {
-  if constexpr (FMT == KV_E4M3) return __half2float(__half(__nv_cvt_fp8_to_halfraw(x, __NV_E4M3)));
-  else return (float)x;
+// Conversions by pairs and quadruples: one to a type or from it at a time runs at a quarter of the rate or less, and is then what
+// bounds a kernel that should be bound by its bytes.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *(const uint32_t *)&v;
 }
-// x / scale rounded to nearest even; numbers past the format's largest (the product's own rounding) become the largest
-template <int FMT> __device__ __forceinline__ typename KvElem<FMT>::type kv_encode(float y) {
-  if constexpr (FMT == KV_E4M3) return __nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3);
-  else return (int8_t)max(-127, min(127, __float2int_rn(y)));
+// four elements; int8 by bits: 0x4b000000 | u is 2^23 + u
+template <int FMT> struct Four;
+template <> struct Four<KV_F32> { typedef uint4 raw; };
+template <> struct Four<KV_BF16> { typedef uint2 raw; };
+template <> struct Four<KV_E4M3> { typedef uint32_t raw; };
+template <> struct Four<KV_INT8> { typedef uint32_t raw; };
+__device__ __forceinline__ float4 kv_decode4(uint4 u) { return make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)); }
+__device__ __forceinline__ float4 kv_decode4(uint2 u) {
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+}
+template <int FMT> __device__ __forceinline__ float4 kv_decode4(uint32_t u) {
+  if constexpr (FMT == KV_E4M3) {
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u & 0xffffu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u >> 16), __NV_E4M3);
+    const float2 x = __half22float2(__half2(a)), y = __half22float2(__half2(b));
+    return make_float4(x.x, x.y, y.x, y.y);
+  } else {
+    u ^= 0x80808080u;
+    const float off = 8388736.0f;
+    return make_float4(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)) - off, __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441)) - off,
+                       __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)) - off, __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - off);
+  }
+}
+template <int FMT> __device__ __forceinline__ float4 kv_decode_four(typename Four<FMT>::raw u) {
+  if constexpr (kv_is_8bit(FMT)) return kv_decode4<FMT>(u);
+  else return kv_decode4(u);
+}
+// four numbers over their scale as codes, rounded to nearest even; what the product's own rounding puts past the largest becomes the
+// largest.  int8: after y + 1.5 2^23 the integer stands in the low bits.
+template <int FMT> __device__ __forceinline__ uint32_t kv_encode4(float a, float b, float c, float d) {
+  if constexpr (FMT == KV_E4M3) {
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
+           (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
+  } else {
+    auto bits = [](float y) { return __float_as_uint(fminf(fmaxf(y, -127.0f), 127.0f) + 12582912.0f); };
+    return __byte_perm(__byte_perm(bits(a), bits(b), 0x0040), __byte_perm(bits(c), bits(d), 0x0040), 0x5410);
+  }
+}
+// The scale of a head whose largest magnitude has these bits.  An infinity or a NaN among its numbers makes it a NaN: whatever the codes are,
+// the row then reads back as NaN.
+template <int FMT> __device__ __forceinline__ float kv_scale(uint32_t top_bits) {
+  const float amax = __uint_as_float(top_bits) * (1.0f / (FMT == KV_E4M3 ? 448.0f : 127.0f));
+  return fmaf(amax, 0.0f, amax < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : amax);
 }
 
 }  // namespace spec
