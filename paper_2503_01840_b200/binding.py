@@ -500,12 +500,14 @@ def _need(ok: bool, what: str):
 def _stream_of(t: torch.Tensor) -> int:
     """The current stream of a tensor's device, which has to be the current device (a launch goes there)."""
     at = t.get_device()
-    _need(at == torch.cuda.current_device(), "the tensors are on another device than the current one")
+    if at != torch._C._cuda_getDevice():
+        raise ValueError("the tensors are on another device than the current one")
     return torch._C._cuda_getCurrentRawStream(at)
 
 
 def _ints(t: torch.Tensor, n: int, what: str) -> int:
-    _need(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.is_cuda, what)
+    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(what)
     return t.data_ptr()
 
 
@@ -545,30 +547,28 @@ def rope_frequencies(rot_dim: int, theta: float, scaling: Optional[str] = None, 
     return torch.from_numpy(f).to(device), mscale
 
 
-def _rope(inv_freq: Optional[torch.Tensor], layout: str, mscale: float):
-    if inv_freq is None:
-        return None
-    _need(inv_freq.dtype == torch.float64 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.is_cuda, "inv_freq: float64 [pairs] on the GPU")
-    _need(layout in _LAYOUT, "layout is 'half' or 'interleaved'")
-    return _Rope(inv_freq.data_ptr(), 2 * inv_freq.shape[0], _LAYOUT[layout], mscale)
+def _rope(inv_freq: torch.Tensor, layout: str, mscale: float):
+    if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_cuda or not inv_freq.is_contiguous() or layout not in _LAYOUT:
+        raise ValueError("inv_freq: float64 [pairs] on the GPU; layout: 'half' or 'interleaved'")
+    return C.byref(_Rope(inv_freq.data_ptr(), 2 * inv_freq.shape[0], _LAYOUT[layout], mscale))
 
 
-def _heads(t: torch.Tensor, what: str):
-    """(pointer, token stride, head stride) of [tokens][heads][head_dim]"""
-    _need(t.dim() == 3 and t.is_cuda and (t.stride(2) == 1 or t.shape[2] == 1), what)
-    return t.data_ptr(), t.stride(0), t.stride(1)
+_HEADS = "{} is [tokens][heads][head_dim] on the GPU with adjacent dimensions"
 
 
 def _turn(x, positions, inv_freq, layout, mscale, out, transpose):
     T, H, hd = x.shape
+    xt, xh, xd = x.stride()
     if out is None:
-        out = torch.empty(T, H, hd, dtype=x.dtype, device=x.device)
-    _need(out.shape == x.shape and out.dtype == x.dtype, "rotary: out has x's shape and dtype")
-    _need(inv_freq is not None, "rotary: inv_freq")
-    rc = lib().spec_rotary(_dt(x.dtype), *_heads(x, "rotary: x [tokens][heads][head_dim] with adjacent dimensions"),
-                           *_heads(out, "rotary: out [tokens][heads][head_dim] with adjacent dimensions"),
-                           _ints(positions, T, "rotary: positions int32 [tokens]"), T, H, hd, C.byref(_rope(inv_freq, layout, mscale)), transpose,
-                           _stream_of(x))
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        ot, oh = H * hd, hd
+    else:
+        _need(out.shape == x.shape and out.dtype is x.dtype and out.is_cuda and (out.stride(2) == 1 or hd == 1), "rotary: out has x's shape and dtype, and adjacent dimensions")
+        ot, oh = out.stride(0), out.stride(1)
+    if inv_freq is None or not x.is_cuda or (xd != 1 and hd != 1):
+        raise ValueError("rotary: inv_freq; " + _HEADS.format("x"))
+    rc = (_lib or lib()).spec_rotary(_dt(x.dtype), x.data_ptr(), xt, xh, out.data_ptr(), ot, oh, _ints(positions, T, "rotary: positions int32 [tokens] on the GPU"),
+                                     T, H, hd, _rope(inv_freq, layout, mscale), transpose, _stream_of(x))
     if rc:
         raise SpecError(rc, "spec_rotary")
     return out
@@ -588,22 +588,24 @@ def rotary_backward(grad: torch.Tensor, positions: torch.Tensor, inv_freq: torch
 
 
 def _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale) -> _KvCache:
-    shape = k_pool.shape
-    fmt = _KV_FORMAT.get(k_pool.dtype)
+    shape, dtype = k_pool.shape, k_pool.dtype
+    fmt = _KV_FORMAT.get(dtype)
     if fmt is None:
-        raise TypeError(f"unsupported cache dtype {k_pool.dtype}")
-    _need(len(shape) == 4 and v_pool.shape == shape and v_pool.dtype == k_pool.dtype and k_pool.is_contiguous() and v_pool.is_contiguous() and
-          k_pool.is_cuda and v_pool.is_cuda, "pools: two contiguous [pages][kv heads][page size][head_dim] of one dtype")
-    _need(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous() and page_table.is_cuda,
-          "page_table: int32 [sequences][pages]")
+        raise TypeError(f"unsupported cache dtype {dtype}")
+    if len(shape) != 4 or v_pool.shape != shape or v_pool.dtype is not dtype or not (k_pool.is_contiguous() and v_pool.is_contiguous() and k_pool.is_cuda and v_pool.is_cuda):
+        raise ValueError("pools: two contiguous [pages][kv heads][page size][head_dim] of one dtype on the GPU")
+    if page_table.dtype is not torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous() or not page_table.is_cuda:
+        raise ValueError("page_table: contiguous int32 [sequences][pages] on the GPU")
+    pages, G, ps, hd = shape
     ks = vs = None
     if fmt >= 2:
+        want = (pages, G, ps)
         for s in (k_scale, v_scale):
-            _need(s is not None and s.dtype == torch.float32 and s.shape == shape[:3] and s.is_contiguous() and s.is_cuda,
-                  "scales of an 8-bit cache: contiguous float32 [pages][kv heads][page size]")
+            if s is None or s.dtype is not torch.float32 or s.shape != want or not s.is_contiguous() or not s.is_cuda:
+                raise ValueError("scales of an 8-bit cache: contiguous float32 [pages][kv heads][page size] on the GPU")
         ks, vs = k_scale.data_ptr(), v_scale.data_ptr()
-    return _KvCache(k_pool.data_ptr(), v_pool.data_ptr(), ks, vs, page_table.data_ptr(), page_table.shape[0], page_table.shape[1], shape[2], shape[0],
-                    shape[1], shape[3], fmt)
+    n_seq, per_seq = page_table.shape
+    return _KvCache(k_pool.data_ptr(), v_pool.data_ptr(), ks, vs, page_table.data_ptr(), n_seq, per_seq, ps, pages, G, hd, fmt)
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_seq: torch.Tensor,
@@ -613,22 +615,25 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: to
     """Writes k, v [tokens][kv heads][head_dim] to a paged cache: token t to position row_kvpos[t] (default row_pos[t]) of sequence row_seq[t]
     (-1: nowhere), its keys turned to row_pos[t] where inv_freq is given, both quantised where the pools are float8_e4m3fn or int8.
     Returns the turned q [tokens][heads][head_dim], if there is one."""
-    T, G, hd = k.shape
+    T, G, hd = shape = k.shape
+    dtype = k.dtype
     cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
-    _need(G == cache.n_kv_heads and hd == cache.head_dim and v.shape == k.shape and v.dtype == k.dtype, "kv_append: k and v [tokens][kv heads][head_dim] of the cache")
-    q_out, H, qa = None, 0, (None, 0, 0)
+    kt, kh, kd = k.stride()
+    vt, vh, vd = v.stride() if v.dim() == 3 else (0, 0, 0)
+    if G != cache.n_kv_heads or hd != cache.head_dim or v.shape != shape or v.dtype is not dtype or kd != 1 or vd != 1 or not (k.is_cuda and v.is_cuda):
+        raise ValueError("kv_append: k and v [tokens][kv heads][head_dim] of the cache's heads, on the GPU, with adjacent dimensions")
+    q_out, qp, qo, H, qt, qh = None, None, None, 0, 0, 0
     if q is not None:
-        H = q.shape[1]
-        _need(q.dim() == 3 and q.shape[0] == T and q.shape[2] == hd and q.dtype == k.dtype, "kv_append: q [tokens][heads][head_dim] of k's dtype")
-        q_out = torch.empty(T, H, hd, dtype=q.dtype, device=q.device)
-        qa = _heads(q, "kv_append: q [tokens][heads][head_dim] with adjacent dimensions")
-    rope = _rope(inv_freq, layout, mscale)
-    rc = lib().spec_kv_append(_dt(k.dtype), *qa, None if q_out is None else q_out.data_ptr(), H,
-                              *_heads(k, "kv_append: k [tokens][kv heads][head_dim] with adjacent dimensions"),
-                              *_heads(v, "kv_append: v [tokens][kv heads][head_dim] with adjacent dimensions"),
-                              _ints(row_seq, T, "kv_append: row_seq int32 [tokens]"), _ints(row_pos, T, "kv_append: row_pos int32 [tokens]"),
-                              None if row_kvpos is None else _ints(row_kvpos, T, "kv_append: row_kvpos int32 [tokens]"), T,
-                              None if rope is None else C.byref(rope), C.byref(cache), _status_ptr(status), _stream_of(k))
+        QT, H, qd = q.shape
+        qt, qh, q1 = q.stride()
+        if QT != T or qd != hd or q.dtype is not dtype or q1 != 1 or not q.is_cuda:
+            raise ValueError("kv_append: q [tokens][heads][head_dim] like k")
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        qp, qo = q.data_ptr(), q_out.data_ptr()
+    rc = (_lib or lib()).spec_kv_append(_dt(dtype), qp, qt, qh, qo, H, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
+                                        _ints(row_seq, T, "kv_append: row_seq int32 [tokens] on the GPU"), _ints(row_pos, T, "kv_append: row_pos int32 [tokens] on the GPU"),
+                                        None if row_kvpos is None else _ints(row_kvpos, T, "kv_append: row_kvpos int32 [tokens] on the GPU"), T,
+                                        None if inv_freq is None else _rope(inv_freq, layout, mscale), C.byref(cache), _status_ptr(status), _stream_of(k))
     if rc:
         raise SpecError(rc, "spec_kv_append")
     return q_out
@@ -640,10 +645,12 @@ def kv_read(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor
     """(k, v) [rows][kv heads][head_dim] of dtype: position row_kvpos[r] of sequence row_seq[r] of a paged cache, zeros for sequence -1."""
     cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
     rows = row_seq.shape[0]
-    out = torch.empty(2, rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=k_pool.device)
-    k, v = out.unbind(0)
-    rc = lib().spec_kv_read(C.byref(cache), _ints(row_seq, rows, "kv_read: row_seq int32 [rows]"), _ints(row_kvpos, rows, "kv_read: row_kvpos int32 [rows]"),
-                            rows, _dt(dtype), k.data_ptr(), v.data_ptr(), _status_ptr(status), _stream_of(k_pool))
+    shape = (rows, cache.n_kv_heads, cache.head_dim)
+    code = _dt(dtype)
+    k, v = torch.empty(shape, dtype=dtype, device=k_pool.device), torch.empty(shape, dtype=dtype, device=k_pool.device)
+    rc = (_lib or lib()).spec_kv_read(C.byref(cache), _ints(row_seq, rows, "kv_read: row_seq int32 [rows] on the GPU"),
+                                      _ints(row_kvpos, rows, "kv_read: row_kvpos int32 [rows] on the GPU"), rows, code, k.data_ptr(), v.data_ptr(),
+                                      _status_ptr(status), _stream_of(k_pool))
     if rc:
         raise SpecError(rc, "spec_kv_read")
     return k, v
@@ -661,23 +668,29 @@ def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor
     """Attention of one new token per sequence: q [batch][heads][head_dim] over the first lengths[b] positions of sequence b of a paged cache.
     Returns out [batch][heads][head_dim] (and the float32 [batch][heads] log-normaliser when want_lse).  workspace: decode_workspace();
     without one, a workspace that is kept for the current stream (made by its first call, which must not be under graph capture)."""
-    B, H, hd = q.shape
+    B, H, hd = shape = q.shape
+    qt, qh, qd = q.stride()
     cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
-    _need(hd == cache.head_dim and q.is_cuda and q.stride(2) == 1 and q.stride(1) == hd, "decode_attention: q [batch][heads][head_dim], heads adjacent")
+    if hd != cache.head_dim or not q.is_cuda or qd != 1 or (qh != hd and H != 1):
+        raise ValueError("decode_attention: q [batch][heads][head_dim] on the GPU, heads adjacent")
     if out is None:
-        out = torch.empty(B, H, hd, dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "decode_attention: out contiguous, of q's shape and dtype")
-    lse = torch.empty(B, H, dtype=torch.float32, device=q.device) if want_lse else None
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != shape or out.dtype is not q.dtype or not out.is_contiguous() or not out.is_cuda:
+        raise ValueError("decode_attention: out contiguous, of q's shape and dtype")
+    if scale is not None and not (scale < 0 or scale > 0):
+        raise ValueError("decode_attention: scale is a number and not 0")
+    lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if want_lse else None
     stream = _stream_of(q)
     if workspace is None:
         at = (q.get_device(), stream)
         workspace = _workspaces.get(at)
         if workspace is None:
             workspace = _workspaces[at] = decode_workspace(q.device)
-    _need(scale is None or (scale != 0 and scale == scale), "decode_attention: scale")
-    rc = lib().spec_decode_attention(_dt(q.dtype), q.data_ptr(), q.stride(0), C.byref(cache), _ints(lengths, B, "decode_attention: lengths int32 [batch]"), B, H,
-                                     0.0 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), _status_ptr(status), stream)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("decode_attention: workspace of decode_workspace()")
+    rc = (_lib or lib()).spec_decode_attention(_dt(q.dtype), q.data_ptr(), qt, C.byref(cache), _ints(lengths, B, "decode_attention: lengths int32 [batch] on the GPU"), B, H,
+                                               0.0 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                               workspace.nbytes, _status_ptr(status), stream)
     if rc:
         raise SpecError(rc, "spec_decode_attention")
     return (out, lse) if want_lse else out

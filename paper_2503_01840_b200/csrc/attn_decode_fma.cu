@@ -14,7 +14,12 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
   float m[HP], l[HP], acc[HP][NV][4];
   float *qs;                    // [HP][hd], times scale * log2 e
 
-  __device__ void init(const DaArgs &p, const DaSeg &sg, bool q_f32, float *mem, int lane) {
+  __device__ __forceinline__ void run(const DaArgs &p, const DaSeg &sg, int len, float *mem, int lane) {
+    init(p, sg, mem, lane);
+    walk(p, sg, len, lane);
+  }
+
+  __device__ __forceinline__ void init(const DaArgs &p, const DaSeg &sg, float *mem, int lane) {
     qs = mem;
     const int hd = p.a.cache.hd, group = p.a.H / p.a.cache.G, h0 = (sg.v / p.chunks) * group + (sg.v % p.chunks) * p.heads;
     const int have = min(p.heads, group - (sg.v % p.chunks) * p.heads);
@@ -22,7 +27,7 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
     for (int i = lane; i < HP * hd; i += 32) {
       const int h = i / hd;
       const size_t at = (size_t)sg.b * p.a.q_ts + (size_t)(h0 + h) * hd + (i - h * hd);
-      qs[i] = h < have ? (q_f32 ? ((const float *)p.a.q)[at] : to_f32(((const bf16 *)p.a.q)[at])) * (p.a.scale * 1.44269504088896341f) : 0.0f;
+      qs[i] = h < have ? (p.q_f32 ? ((const float *)p.a.q)[at] : to_f32(((const bf16 *)p.a.q)[at])) * (p.a.scale * 1.44269504088896341f) : 0.0f;
     }
     __syncwarp();
 #pragma unroll
@@ -44,7 +49,7 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
     }
   }
 
-  __device__ void run(const DaArgs &p, const DaSeg &sg, int len, int lane) {
+  __device__ __forceinline__ void walk(const DaArgs &p, const DaSeg &sg, int len, int lane) {
     const KvCache &c = p.a.cache;
     const int hd = c.hd, g = sg.v / p.chunks;
     const E *K = (const E *)c.k, *V = (const E *)c.v;
@@ -131,38 +136,38 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
     }
   }
 
-  // f(head, dimension, four values of O, sum) by the lanes that hold them; stat(head, max, sum) by one lane
+  // f(head, dimension, four values of O) by the lanes that hold them; stat(head, max, sum) by one lane
   template <typename F, typename G> __device__ void each(int hd, int lane, F f, G stat) {
 #pragma unroll
     for (int h = 0; h < HP; h++) {
       if (lane < LPT)
 #pragma unroll
         for (int i = 0; i < NV; i++)
-          if (lane * 4 + i * 128 < hd) f(h, lane * 4 + i * 128, make_float4(acc[h][i][0], acc[h][i][1], acc[h][i][2], acc[h][i][3]), l[h]);
+          if (lane * 4 + i * 128 < hd) f(h, lane * 4 + i * 128, make_float4(acc[h][i][0], acc[h][i][1], acc[h][i][2], acc[h][i][3]));
       if (lane == 0) stat(h, m[h], l[h]);
     }
   }
 };
 
-template <int FMT, int HP> static cudaError_t fma_by_hd(const DaArgs &p, bool q_f32, int ctas, cudaStream_t s) {
+template <int FMT, int HP> static cudaError_t fma_by_hd(const DaArgs &p, int ctas, cudaStream_t s) {
   const int hd = p.a.cache.hd;
-  if (hd <= 64) return launch<FmaBody<FMT, HP, 64>>(p, q_f32, ctas, s);
-  if (hd <= 128) return launch<FmaBody<FMT, HP, 128>>(p, q_f32, ctas, s);
-  return launch<FmaBody<FMT, HP, 256>>(p, q_f32, ctas, s);
+  if (hd <= 64) return launch<FmaBody<FMT, HP, 64>>(p, ctas, s);
+  if (hd <= 128) return launch<FmaBody<FMT, HP, 128>>(p, ctas, s);
+  return launch<FmaBody<FMT, HP, 256>>(p, ctas, s);
 }
-template <int FMT> static cudaError_t fma_by_heads(const DaArgs &p, bool q_f32, int ctas, cudaStream_t s) {
-  if (p.heads <= 1) return fma_by_hd<FMT, 1>(p, q_f32, ctas, s);
-  if (p.heads <= 2) return fma_by_hd<FMT, 2>(p, q_f32, ctas, s);
-  if (p.heads <= 4) return fma_by_hd<FMT, 4>(p, q_f32, ctas, s);
-  return fma_by_hd<FMT, 8>(p, q_f32, ctas, s);
+template <int FMT> static cudaError_t fma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
+  if (p.heads <= 1) return fma_by_hd<FMT, 1>(p, ctas, s);
+  if (p.heads <= 2) return fma_by_hd<FMT, 2>(p, ctas, s);
+  if (p.heads <= 4) return fma_by_hd<FMT, 4>(p, ctas, s);
+  return fma_by_hd<FMT, 8>(p, ctas, s);
 }
 
-cudaError_t launch_decode_fma(const DaArgs &p, int fmt, bool q_f32, int ctas, cudaStream_t s) {
+cudaError_t launch_decode_fma(const DaArgs &p, int fmt, int ctas, cudaStream_t s) {
   switch (fmt) {
-    case KV_F32: return fma_by_heads<KV_F32>(p, q_f32, ctas, s);
-    case KV_BF16: return fma_by_heads<KV_BF16>(p, q_f32, ctas, s);
-    case KV_E4M3: return fma_by_heads<KV_E4M3>(p, q_f32, ctas, s);
-    default: return fma_by_heads<KV_INT8>(p, q_f32, ctas, s);
+    case KV_F32: return fma_by_heads<KV_F32>(p, ctas, s);
+    case KV_BF16: return fma_by_heads<KV_BF16>(p, ctas, s);
+    case KV_E4M3: return fma_by_heads<KV_E4M3>(p, ctas, s);
+    default: return fma_by_heads<KV_INT8>(p, ctas, s);
   }
 }
 

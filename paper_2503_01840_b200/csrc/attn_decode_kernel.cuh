@@ -11,16 +11,18 @@
 
 namespace spec {
 
-constexpr int DA_MAX_CTAS = 304;           // CTAs of a launch, at most
+constexpr int DA_MAX_CTAS = 160;           // CTAs of a launch, at most
 constexpr int DA_PART_FLOATS = 8 * 256 + 16 * 2;      // a partial state: O of heads x hd <= 2048 elements, then (max, sum) of up to 16 heads
 
 // workspace: partial states of each CTA's first and last segment, and a counter per CTA for the segment that starts in it
 struct DaArgs {
   DecodeAttn a;
   int page_shift;               // log2 of the page size, or -1
+  int q_f32;                    // queries and output in fp32
+  int min_tiles;                // of a CTA that takes part
   int heads, chunks;            // query heads a warp takes together, and how many such chunks share a KV head
-  float *part;                  // [CTAs][2][DA_PART_FLOATS]
   unsigned *count;              // [CTAs], zero between calls
+  float *part;                  // [CTAs][2][part_floats], close together: another page of memory costs a walk of the page tables
 };
 
 __host__ __device__ constexpr int da_part_floats(int heads, int hd) { return heads * hd + (2 * heads + 3) / 4 * 4; }
@@ -31,10 +33,30 @@ struct DaSeg {
   int t0, t1, tiles;            // tiles t0 .. t1 - 1 of `tiles`
 };
 
+// States of one segment that are joined: `mask` of those that stand `stride` floats apart from `from`, the first `skew` further on; into `to`, or
+// where that is null into rows `row` .. of the output
+struct DaRun {
+  const float *from;
+  float *to;
+  int row, heads, stride, skew;
+  uint32_t mask;
+};
+
 __device__ __forceinline__ float da_exp2(float x) { return exp2f(x); }
 __device__ __forceinline__ float da_ref(float m) { return m == -INFINITY ? 0.0f : m; }      // keeps inf - inf out of a row whose scores are all -inf
 
 __device__ __forceinline__ float da_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }      // a row whose scores are all -inf gives 0
+
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
 
 // first row (of hd elements) of a position of KV head g; -1 where the page is none of the pool's
 __device__ __forceinline__ int da_row(const DaArgs &p, int b, int g, int pos) {
@@ -60,17 +82,58 @@ __device__ __forceinline__ int da_length(const DaArgs &p, int b) {
   return len;
 }
 
-__device__ __forceinline__ void da_store(const DaArgs &p, bool f32, size_t at, float4 o) {
-  if (f32) *(float4 *)((float *)p.a.out + at) = o;
-  else {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x, o.y), hi = __floats2bfloat162_rn(o.z, o.w);
-    *(uint2 *)((bf16 *)p.a.out + at) = make_uint2(*(const uint32_t *)&lo, *(const uint32_t *)&hi);
-  }
+__device__ __forceinline__ void da_store(void *out, bool f32, size_t at, float4 o) {
+  if (f32) *(float4 *)((float *)out + at) = o;
+  else *(uint2 *)((bf16 *)out + at) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
 }
 
-// smem: int before[batch + 1] (tiles before each sequence), then per warp the body's floats and two partial states
+// A warp joins one head of the states (O [heads][hd], then (max, sum) [heads]) whose bits are set in `run`, `stride` floats apart, the first `skew`
+// further on, (max, sum) `stats` into a state: into its rows of the output and of lse, or as a state into `to`.  One piece of code for all joins, kept short: a call runs it once or twice, and
+// fetching cold instructions takes longer than what they do.
+// (Its arguments are values: fields of the kernel's parameters behind a pointer would be loads, from the L2 after the fence.)
+static __device__ __noinline__ void da_join_head(const float *states, int stride, int skew, uint32_t run, int stats, int h, int hd, float *to, void *out, bool f32, float *lse) {
+  const int lane = threadIdx.x & 31;
+  const int first = __ffs(run) - 1;
+  constexpr int U = 8;                                   // states in flight; the first ones are asked for together with the sums
+  float4 y[U];
+  auto ask = [&](uint32_t left, int d) {
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (!left) continue;
+      const int k = __ffs(left) - 1;
+      left &= left - 1;
+      if (d < hd) y[u] = *(const float4 *)(states + (size_t)k * stride + (k == first ? skew : 0) + h * hd + d);
+    }
+  };
+  const bool in = (run >> lane) & 1;
+  const float2 x = in ? *(const float2 *)(states + (size_t)lane * stride + (lane == first ? skew : 0) + stats + 2 * h) : make_float2(-INFINITY, 0.0f);
+  ask(run, lane * 4);
+  const float m = warp_max(x.x), f = in ? da_exp2(x.x - da_ref(m)) : 0.0f, l = warp_sum(x.y * f), inv = da_inverse(l);
+  for (int d = lane * 4; d - lane * 4 < hd; d += 128) {
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t left = run; left;) {
+      if (left != run || d >= 128) ask(left, d);
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        if (!left) continue;
+        const float w = __shfl_sync(0xffffffffu, f, __ffs(left) - 1);
+        left &= left - 1;
+        o.x = fmaf(y[u].x, w, o.x), o.y = fmaf(y[u].y, w, o.y), o.z = fmaf(y[u].z, w, o.z), o.w = fmaf(y[u].w, w, o.w);
+      }
+    }
+    if (d >= hd) continue;
+    if (to) *(float4 *)(to + h * hd + d) = o;
+    else da_store(out, f32, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  }
+  if (lane != 0) return;
+  if (to) *(float2 *)(to + stats + 2 * h) = make_float2(m, l);
+  else if (lse) *lse = (da_ref(m) + log2f(l)) * 0.693147180559945309f;
+}
+
+// smem: int before[batch + 1] (tiles before each sequence), per warp the body's floats and two partial states
 template <typename Body>
-__global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(DaArgs p, int q_f32) {
+__global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const __grid_constant__ DaArgs p) {
   pdl_wait();
   pdl_trigger();
   constexpr int W = Body::WARPS, THREADS = W * 32, TILE = Body::TILE;
@@ -83,7 +146,8 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(DaArgs
   float *states = mem + W * Body::warp_smem_floats(hd);                  // [2 W][part_floats]
   __shared__ int scan[W];
   __shared__ DaSeg seg[2 * W];                                           // of the partial states; b = -1: none
-  __shared__ unsigned last;
+  __shared__ DaRun runs[2 * W];
+  __shared__ int to_do[3];
 
   // ---- tiles before each sequence: a run of sequences per thread, then a scan over the threads
   {
@@ -109,19 +173,20 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(DaArgs
     __syncthreads();
   }
   const int VH = p.a.cache.G * p.chunks;
-  const long long total = (long long)before[B] * VH;
-  const int cta = blockIdx.x, N = (int)min((long long)gridDim.x, max(total, 1ll));      // CTAs that take part: a tile each at least
-  const int c0 = cta < N ? (int)(total * cta / N) : 0, c1 = cta < N ? (int)(total * (cta + 1) / N) : 0;
-  const int w0 = c0 + (int)((long long)(c1 - c0) * warp / W), w1 = c0 + (int)((long long)(c1 - c0) * (warp + 1) / W);
-  auto out_at = [&](const DaSeg &s, int h) {                             // element of the output of a segment's head h
-    return ((size_t)s.b * p.a.H + (s.v / p.chunks) * group + (s.v % p.chunks) * heads + h) * hd;
-  };
-  auto have = [&](const DaSeg &s) { return min(heads, group - (s.v % p.chunks) * heads); };
+  const int total = before[B] * VH;
+  // CTAs that take part: with at least min_tiles tiles each, as states that CTAs share cost more to join than those of a CTA's warps.
+  // Each has total / N tiles, the first total % N one more.  (32-bit quotients: 64-bit ones take microseconds here.)
+  const int cta = blockIdx.x, N = max(1, min((int)gridDim.x, (total + p.min_tiles - 1) / p.min_tiles));
+  const int each = total / N, more = total - each * N;
+  auto begin_of = [&](int i) { return i * each + min(i, more); };
+  auto cta_of = [&](int u) { return u < more * (each + 1) ? u / (each + 1) : more + (u - more * (each + 1)) / each; };
+  const int c0 = cta < N ? begin_of(cta) : 0, c1 = cta < N ? begin_of(cta + 1) : 0;
+  const int w0 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)warp / W), w1 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)(warp + 1) / W);
 
   // ---- sequences without a position
   for (int b = cta; b < B; b += gridDim.x)
     if (before[b + 1] == before[b]) {
-      for (int i = tid * 4; i < p.a.H * hd; i += THREADS * 4) da_store(p, q_f32, (size_t)b * p.a.H * hd + i, make_float4(0.f, 0.f, 0.f, 0.f));
+      for (int i = tid * 4; i < p.a.H * hd; i += THREADS * 4) da_store(p.a.out, p.q_f32, (size_t)b * p.a.H * hd + i, make_float4(0.f, 0.f, 0.f, 0.f));
       if (p.a.lse)
         for (int h = tid; h < p.a.H; h += THREADS) p.a.lse[(size_t)b * p.a.H + h] = -INFINITY;
     }
@@ -133,7 +198,7 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(DaArgs
     int lo = 0, hi = B;                                                  // the last sequence with before * VH <= u: it has tiles
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if ((long long)before[mid] * VH <= u) lo = mid;
+      if (before[mid] * VH <= u) lo = mid;
       else hi = mid;
     }
     s.b = lo;
@@ -144,92 +209,117 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(DaArgs
     s.t1 = min(s.tiles, s.t0 + (w1 - u));
     u += s.t1 - s.t0;
     Body body;
-    body.init(p, s, q_f32, warp_mem, lane);
-    body.run(p, s, da_length(p, s.b), lane);
-    const int nh = have(s);
-    if (s.t0 == 0 && s.t1 == s.tiles) {
-      body.each(hd, lane, [&](int h, int d, float4 o, float l) {
-        if (h >= nh) return;
-        const float f = da_inverse(l);
-        da_store(p, q_f32, out_at(s, h) + d, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
-      }, [&](int h, float m, float l) {
-        if (h < nh && p.a.lse) p.a.lse[out_at(s, h) / hd] = (da_ref(m) + log2f(l)) * 0.693147180559945309f;
-      });
+    body.run(p, s, da_length(p, s.b), warp_mem, lane);
+    const bool whole = s.t0 == 0 && s.t1 == s.tiles;
+    float *st = states + (size_t)(2 * warp + (whole ? 1 : slot)) * part_floats;
+    __syncwarp();
+    body.each(hd, lane, [&](int h, int d, float4 o) {
+      if (h < heads) *(float4 *)(st + h * hd + d) = o;
+    }, [&](int h, float m, float l) {
+      if (h < heads) *(float2 *)(st + heads * hd + 2 * h) = make_float2(m, l);
+    });
+    if (whole) {                                                         // the slot is free again until the run's last segment
+      __syncwarp();
+      const int chunk = p.chunks == 1 ? 0 : s.v % p.chunks, kv = p.chunks == 1 ? s.v : s.v / p.chunks;
+      const size_t row = (size_t)s.b * p.a.H + kv * group + chunk * heads;
+      for (int h = 0; h < min(heads, group - chunk * heads); h++)
+        da_join_head(st, part_floats, 0, 1u, heads * hd, h, hd, nullptr, (char *)p.a.out + (row + h) * hd * (p.q_f32 ? 4 : 2), p.q_f32, p.a.lse ? p.a.lse + row + h : nullptr);
     } else {
-      float *st = states + (size_t)(2 * warp + slot) * part_floats;
-      body.each(hd, lane, [&](int h, int d, float4 o, float) {
-        if (h < heads) *(float4 *)(st + h * hd + d) = o;
-      }, [&](int h, float m, float l) {
-        if (h < heads) *(float2 *)(st + heads * hd + 2 * h) = make_float2(m, l);
-      });
       if (lane == 0) seg[2 * warp + slot] = s;
       slot++;                                                            // only a run's first and last segment can be parts
     }
   }
   __syncthreads();
 
-  // ---- what this CTA's warps share: partial states i .. j of one segment, in the order of the positions
-  const int hv = hd / 4;
-  // joins n states; st(k): the k-th.  Writes the output, or to `to` a joined state.
-  auto join = [&](const DaSeg &s, int n, auto st, float *to) {
-    const int nh = have(s);
-    for (int i = tid; i < nh * hv; i += THREADS) {
-      const int h = i / hv, d = (i - h * hv) * 4;
-      float m = -INFINITY, l = 0.0f;
-      for (int k = 0; k < n; k++) m = fmaxf(m, st(k)[heads * hd + 2 * h]);
-      const float ref = da_ref(m);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = 0; k < n; k++) {
-        const float *x = st(k);
-        const float2 ml = *(const float2 *)(x + heads * hd + 2 * h);
-        const float4 y = *(const float4 *)(x + h * hd + d);
-        const float f = da_exp2(ml.x - ref);
-        l = fmaf(ml.y, f, l);
-        o.x = fmaf(y.x, f, o.x), o.y = fmaf(y.y, f, o.y), o.z = fmaf(y.z, f, o.z), o.w = fmaf(y.w, f, o.w);
-      }
-      if (to) {
-        *(float4 *)(to + h * hd + d) = o;
-        if (d == 0) *(float2 *)(to + heads * hd + 2 * h) = make_float2(m, l);
-      } else {
-        const float f = da_inverse(l);
-        da_store(p, q_f32, out_at(s, h) + d, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
-        if (d == 0 && p.a.lse) p.a.lse[out_at(s, h) / hd] = (ref + log2f(l)) * 0.693147180559945309f;
-      }
-    }
+  // ---- joins: of the states that this CTA's warps share (level 0); of those that CTAs share, eight or sixteen at a time, by the CTA that
+  // comes last (1); of what that leaves (2).  All levels run the same code, a warp a run and head by turns: code that only the last
+  // CTA ran took it microseconds to fetch.
+  static_assert(2 * W <= 32, "a lane per partial state");
+  constexpr int SHIFT = W == 16 ? 3 : 4;                                 // parts of both segments of a CTA fit its 2 W states
+  static_assert(DA_MAX_CTAS / (1 << SHIFT) + 2 <= 2 * W, "room for the parts of level 1");
+  auto make_run = [&](int at, const DaSeg &s, const float *from, int stride, int skew, uint32_t mask, float *to) {
+    const int chunk = p.chunks == 1 ? 0 : s.v % p.chunks, kv = p.chunks == 1 ? s.v : s.v / p.chunks;
+    runs[at] = DaRun{from, to, (int)(s.b * p.a.H + kv * group + chunk * heads), min(heads, group - chunk * heads), stride, skew, mask};
   };
-  for (int i = 0; i < 2 * W;) {
-    if (seg[i].b < 0) { i++; continue; }
-    DaSeg s = seg[i];
-    int j = i, n = 0;
-    short at[2 * W];
-    while (j < 2 * W && (seg[j].b < 0 || (seg[j].b == s.b && seg[j].v == s.v))) {
-      if (seg[j].b >= 0) {
-        s.t1 = seg[j].t1;
-        at[n++] = (short)j;
+  int n_runs = 0, n_open = 0;
+  DaSeg open_seg{};                                                      // lanes 0 and 1 of warp 0: what other CTAs have the rest of
+  if (warp == 0) {
+    // lane i looks at partial state i; a run of one segment's states begins where the one before it is another's
+    const DaSeg mine = lane < 2 * W ? seg[lane] : DaSeg{-1, 0, 0, 0, 0};
+    const uint32_t some = __ballot_sync(0xffffffffu, mine.b >= 0), below = (1u << lane) - 1;
+    const int prev = (some & below) ? 31 - __clz(some & below) : lane;
+    const int pb = __shfl_sync(0xffffffffu, mine.b, prev), pv = __shfl_sync(0xffffffffu, mine.v, prev);
+    const bool begins = mine.b >= 0 && (prev == lane || pb != mine.b || pv != mine.v);
+    const uint32_t all = __ballot_sync(0xffffffffu, begins), after = all & ~below & ~(1u << lane);
+    const uint32_t run = some & ~below & (after ? (1u << (__ffs(after) - 1)) - 1 : 0xffffffffu);
+    const int t1 = __shfl_sync(0xffffffffu, mine.t1, begins ? 31 - __clz(run) : lane);
+    const bool open = begins && (mine.t0 != 0 || t1 != mine.tiles);
+    if (begins)
+      make_run(__popc(all & below), mine, states, part_floats, 0, run, open ? p.part + (size_t)(2 * cta + (mine.t0 == 0)) * part_floats : nullptr);
+    // at most two are open: the first run, which began in an earlier CTA, and the last
+    const uint32_t opens = __ballot_sync(0xffffffffu, open);
+    n_open = __popc(opens);
+    const int from = lane == 0 ? __ffs(opens) - 1 : 31 - __clz(opens);
+    open_seg.b = __shfl_sync(0xffffffffu, mine.b, from & 31), open_seg.v = __shfl_sync(0xffffffffu, mine.v, from & 31);
+    open_seg.tiles = __shfl_sync(0xffffffffu, mine.tiles, from & 31);
+    if (lane == 0) to_do[0] = __popc(all), to_do[1] = n_open;
+  }
+  __syncthreads();
+  n_runs = to_do[0];
+  n_open = to_do[1];
+  bool mine_last = false;                                                // lanes 0 and 1 of warp 0 again
+  int shared_from = 0, shared_by = 0;
+#pragma unroll 1
+  for (int level = 0;; level++) {
+    const int per = heads <= 1 ? 0 : 32 - __clz(heads - 1);              // heads of a run: a power of two, so that no quotient is taken
+#pragma unroll 1
+    for (int j = warp; j < n_runs << per; j += W) {
+      const DaRun r = runs[j >> per];
+      const int h = j & ((1 << per) - 1);
+      if (h >= r.heads) continue;
+      da_join_head(r.from, r.stride, r.skew, r.mask, heads * hd, h, hd, r.to, (char *)p.a.out + (size_t)(r.row + h) * hd * (p.q_f32 ? 4 : 2), p.q_f32,
+                   p.a.lse ? p.a.lse + r.row + h : nullptr);
+    }
+    if (n_open == 0 || level == 2) return;
+    __syncthreads();                                                     // the block's states are written
+    if (warp == 0) {
+      int parts = 0;
+      if (level == 0) {                                                  // the CTA that starts a segment keeps its count
+        if (lane < n_open) {
+          const int u0 = before[open_seg.b] * VH + open_seg.v * open_seg.tiles;
+          shared_from = cta_of(u0);
+          shared_by = cta_of(u0 + open_seg.tiles - 1) - shared_from + 1;
+          __threadfence();
+          mine_last = atomicAdd(p.count + shared_from, 1u) == (unsigned)(shared_by - 1);
+          if (mine_last) p.count[shared_from] = 0;                       // as the next call wants it
+          __threadfence();
+        }
+        parts = mine_last ? (shared_by + (1 << SHIFT) - 1) >> SHIFT : 0;
+      } else {
+        parts = mine_last && shared_by > 1 << SHIFT ? 1 : 0;
       }
-      j++;
-    }
-    i = j;
-    auto mine = [&](int k) { return states + (size_t)at[k] * part_floats; };
-    if (s.t0 == 0 && s.t1 == s.tiles) {
-      join(s, n, mine, nullptr);
-      continue;
-    }
-    // other CTAs have the rest of it: the one that starts it keeps its count
-    float *const part = p.part;
-    join(s, n, mine, part + (size_t)(2 * cta + (s.t0 == 0)) * DA_PART_FLOATS);
-    const long long u0 = (long long)before[s.b] * VH + (long long)s.v * s.tiles;
-    const int first = (int)(((u0 + 1) * N - 1) / total), final_ = (int)(((u0 + s.tiles) * N - 1) / total);
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) last = atomicAdd(p.count + first, 1u) == (unsigned)(final_ - first);
-    __syncthreads();
-    if (last) {
-      __threadfence();
-      if (tid == 0) p.count[first] = 0;                                  // as the next call wants it
-      join(s, final_ - first + 1, [&](int k) { return part + (size_t)(2 * (first + k) + (k == 0)) * DA_PART_FLOATS; }, nullptr);
+      const int other = __shfl_sync(0xffffffffu, parts, 0), first_slot = lane == 0 ? 0 : other;
+      if (level == 0) {
+        // a CTA's state stands where its number says, but for the first CTA, whose last segment it is
+        for (int i = 0; i < parts; i++) {
+          const int k0 = i << SHIFT, k = min(1 << SHIFT, shared_by - k0);
+          make_run(first_slot + i, open_seg, p.part + (size_t)2 * (shared_from + k0) * part_floats, 2 * part_floats, i == 0 ? part_floats : 0, (1u << k) - 1,
+                   parts == 1 ? nullptr : states + (size_t)(first_slot + i) * part_floats);
+        }
+      } else if (parts) {
+        const int k = (shared_by + (1 << SHIFT) - 1) >> SHIFT;
+        const int slots = lane == 0 ? 0 : to_do[2];
+        make_run(first_slot, open_seg, states + (size_t)slots * part_floats, part_floats, 0, k == 32 ? 0xffffffffu : (1u << k) - 1, nullptr);
+      }
+      const int sum = __shfl_sync(0xffffffffu, parts, 0) + __shfl_sync(0xffffffffu, parts, 1);
+      if (lane == 0) {
+        to_do[0] = sum;
+        if (level == 0) to_do[2] = parts;                                // where the second segment's states begin
+      }
     }
     __syncthreads();
+    n_runs = to_do[0];
+    if (n_runs == 0) return;
   }
 }
 
@@ -237,16 +327,16 @@ constexpr size_t DA_SMEM = 224 * 1024;
 inline size_t da_smem_bytes(int batch, int warps, int own_floats, int heads, int hd) {
   return ((size_t)(batch + 1) * 4 + 15) / 16 * 16 + sizeof(float) * warps * (own_floats + 2 * da_part_floats(heads, hd));
 }
-template <typename Body> static cudaError_t launch(const DaArgs &p, bool q_f32, int ctas, cudaStream_t s) {
+template <typename Body> static cudaError_t launch(const DaArgs &p, int ctas, cudaStream_t s) {
   static SmemLimit limit;
   const long long tiles = ((long long)p.a.cache.pages_per_seq * p.a.cache.page_size + Body::TILE - 1) / Body::TILE;
-  if (tiles * p.a.batch * p.a.cache.G * p.chunks > INT32_MAX) return cudaErrorNotSupported;
+  if (tiles * p.a.batch * p.a.cache.G * p.chunks > (1 << 30)) return cudaErrorNotSupported;
   const size_t smem = da_smem_bytes(p.a.batch, Body::WARPS, Body::warp_smem_floats(p.a.cache.hd), p.heads, p.a.cache.hd);
   if (smem > DA_SMEM || !limit.ensure(decode_attn_kernel<Body>, (int)smem)) return cudaErrorInvalidValue;
-  return launch_k(decode_attn_kernel<Body>, dim3(ctas), dim3(Body::WARPS * 32), smem, s, p, (int)q_f32);
+  return launch_k(decode_attn_kernel<Body>, dim3(ctas), dim3(Body::WARPS * 32), smem, s, p);
 }
 
-cudaError_t launch_decode_fma(const DaArgs &p, int fmt, bool q_f32, int ctas, cudaStream_t s);
+cudaError_t launch_decode_fma(const DaArgs &p, int fmt, int ctas, cudaStream_t s);
 cudaError_t launch_decode_mma(const DaArgs &p, int fmt, int ctas, cudaStream_t s);
 
 }  // namespace spec

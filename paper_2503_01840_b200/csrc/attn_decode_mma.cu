@@ -72,19 +72,25 @@ template <int FMT_, int HD, int MR> struct MmaBody {
   float qf[NB][2];                                       // scale * log2 e / the power of two on Q
   float c;                                               // largest scale of a value so far
 
-  __device__ __forceinline__ void init(const DaArgs &p, const DaSeg &sg, bool, float *, int lane) {
-    const int g = lane >> 2, t = lane & 3, group = p.a.H / p.a.cache.G, h0 = (sg.v / p.chunks) * group + (sg.v % p.chunks) * p.heads;
+  // the dimensions of Q that this lane's piece of a key meets in contraction s, four at a time; heads past the last are zero
+  __device__ __forceinline__ void load_queries(const DaArgs &p, const DaSeg &sg, int g, int t) {
+    const int group = p.a.H / p.a.cache.G, h0 = (sg.v / p.chunks) * group + (sg.v % p.chunks) * p.heads;
     const int have = min(p.heads, group - (sg.v % p.chunks) * p.heads);
 #pragma unroll
     for (int n = 0; n < NB; n++) {
       const bool in = 8 * n + g < have;
       const bf16 *x = (const bf16 *)p.a.q + (size_t)sg.b * p.a.q_ts + (size_t)(h0 + (in ? 8 * n + g : 0)) * HD;
 #pragma unroll
-      for (int s = 0; s < STEPS; s++) {                  // the four dimensions of contraction s that this lane's piece of a key holds
+      for (int s = 0; s < STEPS; s++) {
         const int d = EB == 1 ? (s / 4) * 64 + t * 16 + (s % 4) * 4 : (s / 2) * 32 + t * 8 + (s % 2) * 4;
         const uint2 u = in ? *(const uint2 *)(x + d) : make_uint2(0, 0);
         q[n][s][0] = u.x, q[n][s][1] = u.y;
       }
+    }
+  }
+  __device__ __forceinline__ void begin(const DaArgs &p, int t) {
+#pragma unroll
+    for (int n = 0; n < NB; n++) {
       float f = p.a.scale * 1.44269504088896341f;
       if constexpr (Q8) {
         float top = 0.0f;
@@ -150,7 +156,7 @@ template <int FMT_, int HD, int MR> struct MmaBody {
     }
   }
 
-  __device__ __forceinline__ void run(const DaArgs &p, const DaSeg &sg, int len, int lane) {
+  __device__ __forceinline__ void run(const DaArgs &p, const DaSeg &sg, int len, float *, int lane) {
     const KvCache &cc = p.a.cache;
     const int g = lane >> 2, t = lane & 3, head = sg.v / p.chunks, tok = lane & 15;
     const char *K = (const char *)cc.k, *V = (const char *)cc.v;
@@ -172,7 +178,9 @@ template <int FMT_, int HD, int MR> struct MmaBody {
     };
     uint32_t valid, valid_next = 0;
     int row = 0, row_next = 0, page;
-    row = row_of(sg.t0, page_of(sg.t0), valid);
+    page = page_of(sg.t0);
+    load_queries(p, sg, g, t);
+    row = row_of(sg.t0, page, valid);
     Keys k;
     Values v;
     float sc = 1.0f, sc_next = 1.0f;
@@ -180,6 +188,7 @@ template <int FMT_, int HD, int MR> struct MmaBody {
     if constexpr (Q8) sc = SC[row];
     if constexpr (V_AHEAD) load_values(V, row, g, t, v);
     page = page_of(min(sg.t0 + 1, sg.t1 - 1));
+    begin(p, t);
     for (int tile = sg.t0; tile < sg.t1; tile++) {
       const int next = min(tile + 1, sg.t1 - 1);         // the last tile is asked for once more
       row_next = row_of(next, page, valid_next);
@@ -337,7 +346,7 @@ template <int FMT_, int HD, int MR> struct MmaBody {
 #pragma unroll
           for (int i = 0; i < EP; i += 4) {
             const int at = (j * EP + i) / 2;
-            f(h, j * 8 * EP + g * EP + i, make_float4(o[n][at][e], o[n][at][e + 2], o[n][at + 1][e], o[n][at + 1][e + 2]), l[n][e]);
+            f(h, j * 8 * EP + g * EP + i, make_float4(o[n][at][e], o[n][at][e + 2], o[n][at + 1][e], o[n][at + 1][e + 2]));
           }
         if (g == 0) stat(h, m[n][e], l[n][e]);
       }
@@ -346,8 +355,8 @@ template <int FMT_, int HD, int MR> struct MmaBody {
 
 template <int FMT, int HD> static cudaError_t mma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
   if constexpr (HD < 256)
-    if (p.heads > 8) return launch<MmaBody<FMT, HD, 16>>(p, false, ctas, s);
-  return launch<MmaBody<FMT, HD, 8>>(p, false, ctas, s);
+    if (p.heads > 8) return launch<MmaBody<FMT, HD, 16>>(p, ctas, s);
+  return launch<MmaBody<FMT, HD, 8>>(p, ctas, s);
 }
 template <int FMT> static cudaError_t mma_by_hd(const DaArgs &p, int ctas, cudaStream_t s) {
   return p.a.cache.hd == 64 ? mma_by_heads<FMT, 64>(p, ctas, s) : p.a.cache.hd == 128 ? mma_by_heads<FMT, 128>(p, ctas, s) : mma_by_heads<FMT, 256>(p, ctas, s);
