@@ -1767,6 +1767,11 @@ static int cache_of(const spec_kv_cache *c, KvCache *out) {
 static bool kv_goes_with(int dtype, int format) {
   return dtype == SPEC_F32 ? format != SPEC_KV_BF16 : dtype == SPEC_BF16 && format != SPEC_KV_F32;
 }
+// These kernels wait for their predecessor before they touch memory, so they may be resident by the time it ends.
+struct EarlyLaunch {
+  EarlyLaunch() { tl_pdl = true; }
+  ~EarlyLaunch() { tl_pdl = false; }
+};
 static int kv_status(cudaError_t e) { return e == cudaSuccess ? SPEC_OK : e == cudaErrorNotSupported ? SPEC_ERR_UNSUPPORTED : SPEC_ERR_CUDA; }
 
 extern "C" int spec_rotary(int32_t dtype, const void *x, int64_t x_ts, int64_t x_hs, void *out, int64_t out_ts, int64_t out_hs, const int32_t *pos,
@@ -1784,6 +1789,7 @@ extern "C" int spec_rotary(int32_t dtype, const void *x, int64_t x_ts, int64_t x
   a.q = HeadView{x, x_ts, x_hs};
   a.q_out = out; a.qo_ts = out_ts; a.qo_hs = out_hs;
   a.H = heads; a.hd = head_dim; a.tokens = tokens; a.pos = pos;
+  EarlyLaunch early;
   return kv_status(launch_rope_append(a, dtype, dtype == SPEC_F32 ? KV_F32 : KV_BF16, (cudaStream_t)stream));
 }
 
@@ -1804,6 +1810,7 @@ extern "C" int spec_kv_append(int32_t dtype, const void *q, int64_t q_ts, int64_
   a.q = HeadView{q, q_ts, q_hs}; a.k = HeadView{k, k_ts, k_hs}; a.v = HeadView{v, v_ts, v_hs};
   a.q_out = q_out; a.qo_hs = a.hd; a.qo_ts = (long long)a.H * a.hd;
   a.seq = row_seq; a.pos = row_pos; a.kvpos = row_kvpos ? row_kvpos : row_pos; a.status = status;
+  EarlyLaunch early;
   return kv_status(launch_rope_append(a, dtype, cache->format, (cudaStream_t)stream));
 }
 
@@ -1816,6 +1823,7 @@ extern "C" int spec_kv_read(const spec_kv_cache *cache, const int32_t *row_seq, 
   if (!row_seq || !row_kvpos || !k_out || !v_out) return SPEC_ERR_NULL;
   if (!kv_aligned(k_out, 16) || !kv_aligned(v_out, 16)) return SPEC_ERR_INVALID_CFG;
   a.seq = row_seq; a.kvpos = row_kvpos; a.rows = rows; a.k_out = k_out; a.v_out = v_out; a.status = status;
+  EarlyLaunch early;
   return kv_status(launch_kv_read(a, cache->format, out_dtype, (cudaStream_t)stream));
 }
 
@@ -1835,5 +1843,6 @@ extern "C" int spec_decode_attention(int32_t dtype, const void *q, int64_t q_ts,
   if (!kv_aligned(q, 16) || !kv_aligned(out, 16) || q_ts * (dtype == SPEC_F32 ? 4 : 2) % 16) return SPEC_ERR_INVALID_CFG;
   a.q = q; a.q_ts = q_ts; a.len = lengths; a.out = out; a.lse = lse; a.batch = batch; a.H = n_heads; a.workspace = workspace; a.status = status;
   a.scale = scale != 0.0f ? scale : 1.0f / sqrtf((float)cache->head_dim);
+  EarlyLaunch early;
   return kv_status(launch_decode_attn(a, dtype, cache->format, (cudaStream_t)stream));
 }

@@ -104,7 +104,7 @@ struct RopeGrid {
 constexpr int ROPE_MAX_TOKENS = 16;
 
 template <typename T, int FMT, bool INTER, int U>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(RopeAppend a, RopeGrid gr) {
+__global__ void __launch_bounds__(ROPE_THREADS, 5) rope_append_kernel(RopeAppend a, RopeGrid gr) {
   pdl_wait();
   pdl_trigger();
   typedef typename KvElem<FMT>::type E;
@@ -234,14 +234,14 @@ template <typename T, int FMT> static cudaError_t rope_append(const RopeAppend &
   gr.lh_shift = __builtin_ctz(lh);
   const int step = ROPE_THREADS / lh;                    // heads of a round of the block
   constexpr int U = 2;
-  // few tokens: a round's heads a block, so that no thread has a second round to wait for; many: about 4 U rounds a block
+  // few tokens: a round's heads a block, so that no thread has a second round to wait for; many: about six rounds a block
   const long long rounds = ((long long)a.tokens * all + step - 1) / step;
   if (rounds <= 1184) {
     gr.per_block = 1;
     gr.heads = min(all, step);
   } else {
     gr.heads = all;
-    gr.per_block = max(1, min(ROPE_MAX_TOKENS, 4 * U * step / all));
+    gr.per_block = max(1, min(ROPE_MAX_TOKENS, 6 * step / all));
   }
   gr.by_heads = gr.heads == 1 ? 0xffffffffu : (uint32_t)((0x100000000ull + gr.heads - 1) / gr.heads);
   if (gr.heads == 1 && gr.per_block > 1) gr.per_block = 1;
@@ -259,7 +259,7 @@ cudaError_t launch_rope_append(const RopeAppend &a, int dtype, int fmt, cudaStre
 // ---------------------------------------------------------------- reading back
 // Row r of the output is position kvpos[r] of sequence seq[r], zeros where there is none.  A thread takes eight elements, so that a
 // warp's stores of bf16 are whole lines; a block some rows, whose places in the pool are looked up once.
-constexpr int READ_MAX_ROWS = 64;
+constexpr int READ_MAX_ROWS = 64;      // 256 / the least items a row (4)
 struct ReadGrid { int rows, items; uint32_t by_items; };                 // rows of a block, eights of a row (keys, then values)
 
 template <int FMT, typename T>
@@ -314,10 +314,8 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRead a, ReadGrid gr) {
 template <int FMT> static cudaError_t kv_read(const KvRead &a, int out_dtype, cudaStream_t s) {
   ReadGrid gr;
   gr.items = 2 * a.cache.G * (a.cache.hd / 8);
-  // about four items a thread, fewer where that leaves SMs without a block
-  const long long total = (long long)a.rows * gr.items;
-  const int want = total >= 4ll * 256 * 592 ? 1024 : 256;
-  gr.rows = max(1, min(READ_MAX_ROWS, want / gr.items));
+  // one wave of blocks (five an SM) where there is enough to do: a block's look-ups come before everything else it does
+  gr.rows = max(max(1, 256 / gr.items), min(READ_MAX_ROWS, (a.rows + 739) / 740));
   gr.by_items = (uint32_t)((0x100000000ull + gr.items - 1) / gr.items);
   const dim3 grid((a.rows + gr.rows - 1) / gr.rows);
   if (out_dtype == KV_F32) return launch_k(kv_read_kernel<FMT, float>, grid, dim3(256), 0, s, a, gr);
