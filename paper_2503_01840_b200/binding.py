@@ -8,6 +8,7 @@ cannot be built, importing the symbols raises.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -487,32 +488,26 @@ def argmax(logits: torch.Tensor) -> torch.Tensor:
 
 
 # ------------------------------------------------------------------ rotary positions, the paged cache in 8 bits, single-token attention
-_KV_FORMAT = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch.int8: 3}
-_LAYOUT = {"half": 0, "interleaved": 1}
-_workspaces: Dict = {}
+# marshalled in C++ (csrc/marshal.cpp): these are called once a layer, and Python's share of such a call was longer than most of the kernels
+_marshal_module = None
+
+
+def _marshal():
+    """Loads the C++ part of the binding, and the library behind it."""
+    global _marshal_module
+    if _marshal_module is None:
+        L = lib()
+        spec = importlib.util.spec_from_file_location("_marshal", _build.MARSHAL)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        m.use(*[C.cast(f, C.c_void_p).value for f in (L.spec_rotary, L.spec_kv_append, L.spec_kv_read, L.spec_decode_attention, L.spec_decode_attention_workspace_bytes)])
+        _marshal_module = m
+    return _marshal_module
 
 
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
-
-
-def _stream_of(t: torch.Tensor) -> int:
-    """The current stream of a tensor's device, which has to be the current device (a launch goes there)."""
-    at = t.get_device()
-    if at != torch._C._cuda_getDevice():
-        raise ValueError("the tensors are on another device than the current one")
-    return torch._C._cuda_getCurrentRawStream(at)
-
-
-def _ints(t: torch.Tensor, n: int, what: str) -> int:
-    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(what)
-    return t.data_ptr()
-
-
-def _status_ptr(status: Optional[torch.Tensor]):
-    return None if status is None else _ints(status, 4, "status: int32 [4] on the GPU")
 
 
 def rope_frequencies(rot_dim: int, theta: float, scaling: Optional[str] = None, factor: float = 1.0, trained: int = 8192, low: float = 1.0,
@@ -547,65 +542,23 @@ def rope_frequencies(rot_dim: int, theta: float, scaling: Optional[str] = None, 
     return torch.from_numpy(f).to(device), mscale
 
 
-def _rope(inv_freq: torch.Tensor, layout: str, mscale: float):
-    if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_cuda or not inv_freq.is_contiguous() or layout not in _LAYOUT:
-        raise ValueError("inv_freq: float64 [pairs] on the GPU; layout: 'half' or 'interleaved'")
-    return C.byref(_Rope(inv_freq.data_ptr(), 2 * inv_freq.shape[0], _LAYOUT[layout], mscale))
-
-
-_HEADS = "{} is [tokens][heads][head_dim] on the GPU with adjacent dimensions"
-
-
-def _turn(x, positions, inv_freq, layout, mscale, out, transpose):
-    T, H, hd = x.shape
-    xt, xh, xd = x.stride()
-    if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
-        ot, oh = H * hd, hd
-    else:
-        _need(out.shape == x.shape and out.dtype is x.dtype and out.is_cuda and (out.stride(2) == 1 or hd == 1), "rotary: out has x's shape and dtype, and adjacent dimensions")
-        ot, oh = out.stride(0), out.stride(1)
-    if inv_freq is None or not x.is_cuda or (xd != 1 and hd != 1):
-        raise ValueError("rotary: inv_freq; " + _HEADS.format("x"))
-    rc = (_lib or lib()).spec_rotary(_dt(x.dtype), x.data_ptr(), xt, xh, out.data_ptr(), ot, oh, _ints(positions, T, "rotary: positions int32 [tokens] on the GPU"),
-                                     T, H, hd, _rope(inv_freq, layout, mscale), transpose, _stream_of(x))
-    if rc:
-        raise SpecError(rc, "spec_rotary")
-    return out
-
-
 def rotary(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0,
            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [tokens][heads][head_dim] (any token and head stride: a view of a fused projection will do) with the first 2 * pairs dimensions of
     every head turned to positions int32 [tokens].  out may be x."""
-    return _turn(x, positions, inv_freq, layout, mscale, out, 0)
+    r = (_marshal_module or _marshal()).rotary(x, positions, inv_freq, layout, mscale, out, False)
+    if type(r) is int:
+        raise SpecError(r, "spec_rotary")
+    return r
 
 
 def rotary_backward(grad: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0,
                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The gradient with respect to rotary's x of one with respect to its output."""
-    return _turn(grad, positions, inv_freq, layout, mscale, out, 1)
-
-
-def _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale) -> _KvCache:
-    shape, dtype = k_pool.shape, k_pool.dtype
-    fmt = _KV_FORMAT.get(dtype)
-    if fmt is None:
-        raise TypeError(f"unsupported cache dtype {dtype}")
-    if len(shape) != 4 or v_pool.shape != shape or v_pool.dtype is not dtype or not (k_pool.is_contiguous() and v_pool.is_contiguous() and k_pool.is_cuda and v_pool.is_cuda):
-        raise ValueError("pools: two contiguous [pages][kv heads][page size][head_dim] of one dtype on the GPU")
-    if page_table.dtype is not torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous() or not page_table.is_cuda:
-        raise ValueError("page_table: contiguous int32 [sequences][pages] on the GPU")
-    pages, G, ps, hd = shape
-    ks = vs = None
-    if fmt >= 2:
-        want = (pages, G, ps)
-        for s in (k_scale, v_scale):
-            if s is None or s.dtype is not torch.float32 or s.shape != want or not s.is_contiguous() or not s.is_cuda:
-                raise ValueError("scales of an 8-bit cache: contiguous float32 [pages][kv heads][page size] on the GPU")
-        ks, vs = k_scale.data_ptr(), v_scale.data_ptr()
-    n_seq, per_seq = page_table.shape
-    return _KvCache(k_pool.data_ptr(), v_pool.data_ptr(), ks, vs, page_table.data_ptr(), n_seq, per_seq, ps, pages, G, hd, fmt)
+    r = (_marshal_module or _marshal()).rotary(grad, positions, inv_freq, layout, mscale, out, True)
+    if type(r) is int:
+        raise SpecError(r, "spec_rotary")
+    return r
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_seq: torch.Tensor,
@@ -615,46 +568,20 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: to
     """Writes k, v [tokens][kv heads][head_dim] to a paged cache: token t to position row_kvpos[t] (default row_pos[t]) of sequence row_seq[t]
     (-1: nowhere), its keys turned to row_pos[t] where inv_freq is given, both quantised where the pools are float8_e4m3fn or int8.
     Returns the turned q [tokens][heads][head_dim], if there is one."""
-    T, G, hd = shape = k.shape
-    dtype = k.dtype
-    cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
-    kt, kh, kd = k.stride()
-    vt, vh, vd = v.stride() if v.dim() == 3 else (0, 0, 0)
-    if G != cache.n_kv_heads or hd != cache.head_dim or v.shape != shape or v.dtype is not dtype or kd != 1 or vd != 1 or not (k.is_cuda and v.is_cuda):
-        raise ValueError("kv_append: k and v [tokens][kv heads][head_dim] of the cache's heads, on the GPU, with adjacent dimensions")
-    q_out, qp, qo, H, qt, qh = None, None, None, 0, 0, 0
-    if q is not None:
-        QT, H, qd = q.shape
-        qt, qh, q1 = q.stride()
-        if QT != T or qd != hd or q.dtype is not dtype or q1 != 1 or not q.is_cuda:
-            raise ValueError("kv_append: q [tokens][heads][head_dim] like k")
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        qp, qo = q.data_ptr(), q_out.data_ptr()
-    rc = (_lib or lib()).spec_kv_append(_dt(dtype), qp, qt, qh, qo, H, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
-                                        _ints(row_seq, T, "kv_append: row_seq int32 [tokens] on the GPU"), _ints(row_pos, T, "kv_append: row_pos int32 [tokens] on the GPU"),
-                                        None if row_kvpos is None else _ints(row_kvpos, T, "kv_append: row_kvpos int32 [tokens] on the GPU"), T,
-                                        None if inv_freq is None else _rope(inv_freq, layout, mscale), C.byref(cache), _status_ptr(status), _stream_of(k))
-    if rc:
-        raise SpecError(rc, "spec_kv_append")
-    return q_out
+    r = (_marshal_module or _marshal()).kv_append(k, v, k_pool, v_pool, page_table, k_scale, v_scale, row_seq, row_pos, row_kvpos, q, inv_freq, layout, mscale, status)
+    if type(r) is int:
+        raise SpecError(r, "spec_kv_append")
+    return r
 
 
 def kv_read(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_seq: torch.Tensor, row_kvpos: torch.Tensor,
             k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
             status: Optional[torch.Tensor] = None):
     """(k, v) [rows][kv heads][head_dim] of dtype: position row_kvpos[r] of sequence row_seq[r] of a paged cache, zeros for sequence -1."""
-    cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
-    rows = row_seq.shape[0]
-    G, hd = cache.n_kv_heads, cache.head_dim
-    shape, strides, code, device = (rows, G, hd), (G * hd, hd, 1), _dt(dtype), k_pool.device
-    k = torch.empty_strided(shape, strides, dtype=dtype, device=device)
-    v = torch.empty_strided(shape, strides, dtype=dtype, device=device)
-    rc = (_lib or lib()).spec_kv_read(C.byref(cache), _ints(row_seq, rows, "kv_read: row_seq int32 [rows] on the GPU"),
-                                      _ints(row_kvpos, rows, "kv_read: row_kvpos int32 [rows] on the GPU"), rows, code, k.data_ptr(), v.data_ptr(),
-                                      _status_ptr(status), _stream_of(k_pool))
-    if rc:
-        raise SpecError(rc, "spec_kv_read")
-    return k, v
+    r = (_marshal_module or _marshal()).kv_read(k_pool, v_pool, page_table, k_scale, v_scale, row_seq, row_kvpos, _dt(dtype), status)
+    if type(r) is int:
+        raise SpecError(r, "spec_kv_read")
+    return r
 
 
 def decode_workspace(device="cuda") -> torch.Tensor:
@@ -669,29 +596,7 @@ def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor
     """Attention of one new token per sequence: q [batch][heads][head_dim] over the first lengths[b] positions of sequence b of a paged cache.
     Returns out [batch][heads][head_dim] (and the float32 [batch][heads] log-normaliser when want_lse).  workspace: decode_workspace();
     without one, a workspace that is kept for the current stream (made by its first call, which must not be under graph capture)."""
-    B, H, hd = shape = q.shape
-    qt, qh, qd = q.stride()
-    cache = _kv_cache(k_pool, v_pool, page_table, k_scale, v_scale)
-    if hd != cache.head_dim or not q.is_cuda or qd != 1 or (qh != hd and H != 1):
-        raise ValueError("decode_attention: q [batch][heads][head_dim] on the GPU, heads adjacent")
-    if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    elif out.shape != shape or out.dtype is not q.dtype or not out.is_contiguous() or not out.is_cuda:
-        raise ValueError("decode_attention: out contiguous, of q's shape and dtype")
-    if scale is not None and not (scale < 0 or scale > 0):
-        raise ValueError("decode_attention: scale is a number and not 0")
-    lse = torch.empty_strided((B, H), (H, 1), dtype=torch.float32, device=q.device) if want_lse else None      # half the time of torch.empty
-    stream = _stream_of(q)
-    if workspace is None:
-        at = (q.get_device(), stream)
-        workspace = _workspaces.get(at)
-        if workspace is None:
-            workspace = _workspaces[at] = decode_workspace(q.device)
-    elif not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("decode_attention: workspace of decode_workspace()")
-    rc = (_lib or lib()).spec_decode_attention(_dt(q.dtype), q.data_ptr(), qt, C.byref(cache), _ints(lengths, B, "decode_attention: lengths int32 [batch] on the GPU"), B, H,
-                                               0.0 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                               workspace.nbytes, _status_ptr(status), stream)
-    if rc:
-        raise SpecError(rc, "spec_decode_attention")
-    return (out, lse) if want_lse else out
+    r = (_marshal_module or _marshal()).decode_attention(q, k_pool, v_pool, page_table, k_scale, v_scale, lengths, scale, want_lse, out, workspace, status)
+    if type(r) is int:
+        raise SpecError(r, "spec_decode_attention")
+    return r

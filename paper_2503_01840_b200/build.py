@@ -2,7 +2,8 @@
 
     python -m paper_2503_01840_b200.build [--force] [--verbose]
 
-nvcc cross-compiles without a GPU; the resulting .so is loaded by `binding` through ctypes.
+nvcc cross-compiles without a GPU; the resulting .so is loaded by `binding` through ctypes.  g++ compiles _marshal.so, the part of the
+binding that takes torch tensors apart in C++.
 """
 import concurrent.futures
 import os
@@ -13,6 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libspec_b200.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["api.cu", "elementwise.cu", "gemm_ref.cu", "tma_maps.cu", "gemm_fused.cu", "gemm_wide.cu", "attn_ref.cu", "attn_fast.cu",
            "attn_causal.cu", "tree.cu", "kv_cache.cu", "attn_decode.cu", "attn_decode_fma.cu", "attn_decode_mma.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
@@ -24,13 +26,14 @@ def _deps_mtime():
     m = 0.0
     for root in (CSRC, os.path.join(os.path.dirname(HERE), "include")):
         for f in os.listdir(root):
-            if f.endswith((".cu", ".cuh", ".h")):
+            if f.endswith((".cu", ".cuh", ".h", ".cpp")):
                 m = max(m, os.path.getmtime(os.path.join(root, f)))
     return m
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _deps_mtime():
+    newest = _deps_mtime()
+    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= newest for f in (LIB, MARSHAL)):
         return LIB
     os.makedirs(OBJ, exist_ok=True)
     extra = ["-Xptxas", "-v"] if verbose else []
@@ -40,16 +43,35 @@ def build(force: bool = False, verbose: bool = False) -> str:
         r = subprocess.run([NVCC, *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj], capture_output=True, text=True)
         return src, obj, r
 
+    def marshal():
+        import sysconfig
+
+        import torch
+        at = os.path.dirname(torch.__file__)
+        tmp = MARSHAL + ".%d.tmp" % os.getpid()
+        cuda = os.path.dirname(os.path.dirname(NVCC))
+        r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                            *["-I" + d for d in (at + "/include", at + "/include/torch/csrc/api/include", cuda + "/include", sysconfig.get_paths()["include"])],
+                            os.path.join(CSRC, "marshal.cpp"), "-o", tmp, "-L" + at + "/lib", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda",
+                            "-Wl,-rpath," + at + "/lib"], capture_output=True, text=True)
+        return tmp, r
+
     objs = []
     with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
+        tail = ex.submit(marshal)
         for src, obj, r in ex.map(cc, SOURCES):
             if verbose or r.returncode:
                 sys.stderr.write(f"--- {src}\n{r.stdout}{r.stderr}\n")
             if r.returncode:
                 raise RuntimeError(f"nvcc failed on {src}")
             objs.append(obj)
+        made, r = tail.result()
+        if r.returncode:
+            sys.stderr.write(f"--- marshal.cpp\n{r.stdout}{r.stderr}\n")
+            raise RuntimeError("g++ failed on marshal.cpp")
     tmp = LIB + ".%d.tmp" % os.getpid()
     subprocess.run([NVCC, "-shared", "-o", tmp, *objs, "-gencode", "arch=compute_100a,code=sm_100a"], check=True)
+    os.replace(made, MARSHAL)
     os.replace(tmp, LIB)
     return LIB
 
