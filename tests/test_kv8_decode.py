@@ -1,0 +1,31 @@
+"""The decoding loop over an 8-bit cache against SpecDecoder's plain steps on the same weights."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_01840_b200 import binding as sb
+from paper_2503_01840_b200 import synth
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3", "int8"])
+def test_tokens_and_hidden_states_as_the_decoder_without_a_draft(cache):
+    from paper_2503_01840_b200.kv8_decode import CachedDecoder
+    cfg = synth.ModelCfg("K", "bf16", 2, 512, 4, 2, 128, 1408, 2048, 1024, (0, 0, 1), 5e5, batch=3, tree_depth=2, tree_topk=2, tree_nodes=4, seed=11)
+    w, dw, _, _ = synth.make_structured(cfg, 1.0, device="cuda", residual_scale=1.0)
+    d2t = dw["d2t"].cpu()
+    prompts = [synth.structured_prompt(cfg, d2t, n, seed=n).numpy() for n in (1, 40, 301)]
+    dec = sb.SpecDecoder(cfg, w, dw, batch=3, max_ctx=400)
+    mine = CachedDecoder(cfg, w, 3, 400, cache)
+    assert np.array_equal(mine.prefill(prompts).cpu().numpy(), dec.prefill(prompts, 64))
+    for _ in range(6):
+        tokens, hidden = mine.step()
+        assert np.array_equal(tokens.cpu().numpy(), dec.plain_step())
+        for b in range(3):
+            h = torch.from_numpy(dec.debug(sb.DBG_NODE_HIDDEN, b).reshape(-1, cfg.hidden)[0].copy()).cuda()
+            want = h * torch.rsqrt(h.square().mean() + cfg.rms_eps) * w["final_norm"].float()
+            # bf16 activations of two layers round a few times by 2^-9 in the mean; the cache's rounding (e4m3: 2.6e-2 of a value in the mean)
+            # reaches the hidden state through attention outputs that are a part of it
+            assert (hidden[b].float() - want).norm() / want.norm() < (0.03 if cache == "e4m3" else 0.01), (cache, b)
+    dec.close()
