@@ -1,6 +1,5 @@
 // Single-token attention: which body takes a call, and how many query heads a warp takes together.
 #include <algorithm>
-#include <stdlib.h>
 
 #include "attn_decode_kernel.cuh"
 
@@ -33,7 +32,6 @@ cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStre
   while (most > 1 && !fits(std::min(most, group))) most /= 2;
   p.chunks = (group + most - 1) / most;
   p.heads = (group + p.chunks - 1) / p.chunks;
-  p.min_tiles = getenv("DA_MIN") ? atoi(getenv("DA_MIN")) : 8;
   p.count = (unsigned *)a.workspace;
   p.part = (float *)((char *)a.workspace + DA_COUNT_BYTES);
   return mma ? launch_decode_mma(p, fmt, ctas, s) : launch_decode_fma(p, fmt, ctas, s);

@@ -9,6 +9,8 @@
 #pragma once
 #include "attn_decode.cuh"
 
+#include <stdlib.h>
+
 namespace spec {
 
 constexpr int DA_MAX_CTAS = 160;           // CTAs of a launch, at most
@@ -19,7 +21,7 @@ struct DaArgs {
   DecodeAttn a;
   int page_shift;               // log2 of the page size, or -1
   int q_f32;                    // queries and output in fp32
-  int min_tiles;                // of a CTA that takes part
+  int spare;                    // tiles that a CTA reads while states of several CTAs are joined
   int heads, chunks;            // query heads a warp takes together, and how many such chunks share a KV head
   unsigned *count;              // [CTAs], zero between calls
   float *part;                  // [CTAs][2][part_floats], close together: another page of memory costs a walk of the page tables
@@ -144,7 +146,8 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   float *mem = (float *)(smem + ((size_t)(B + 1) * 4 + 15) / 16 * 16);
   float *warp_mem = mem + warp * Body::warp_smem_floats(hd);
   float *states = mem + W * Body::warp_smem_floats(hd);                  // [2 W][part_floats]
-  __shared__ int scan[W];
+  __shared__ int2 scan[W];
+  int longest = 0;
   __shared__ DaSeg seg[2 * W];                                           // of the partial states; b = -1: none
   __shared__ DaRun runs[2 * W];
   __shared__ int to_do[3];
@@ -152,18 +155,26 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   // ---- tiles before each sequence: a run of sequences per thread, then a scan over the threads
   {
     const int per = (B + THREADS - 1) / THREADS, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-    int sum = 0;
-    for (int b = b0; b < b1; b++) sum += (da_length(p, b) + TILE - 1) / TILE;
+    int sum = 0, most = 0;
+    for (int b = b0; b < b1; b++) {
+      const int t = (da_length(p, b) + TILE - 1) / TILE;
+      sum += t;
+      most = max(most, t);
+    }
     int inc = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += x;
     }
-    if (lane == 31) scan[warp] = inc;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 31) scan[warp] = make_int2(inc, most);
     __syncthreads();
     int at = inc - sum;
-    for (int w = 0; w < warp; w++) at += scan[w];
+    for (int w = 0; w < W; w++) {
+      if (w < warp) at += scan[w].x;
+      longest = max(longest, scan[w].y);
+    }
     for (int b = b0; b < b1; b++) {
       before[b] = at;
       at += (da_length(p, b) + TILE - 1) / TILE;
@@ -172,15 +183,26 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     if (lane < 2) seg[2 * warp + lane].b = -1;
     __syncthreads();
   }
-  const int VH = p.a.cache.G * p.chunks;
+  const int VH = p.a.cache.G * p.chunks, cta = blockIdx.x;
   const int total = before[B] * VH;
-  // CTAs that take part: with at least min_tiles tiles each, as states that CTAs share cost more to join than those of a CTA's warps.
-  // Each has total / N tiles, the first total % N one more.  (32-bit quotients: 64-bit ones take microseconds here.)
-  const int cta = blockIdx.x, N = max(1, min((int)gridDim.x, (total + p.min_tiles - 1) / p.min_tiles));
+  // The tiles are dealt out evenly: each of N CTAs has total / N, the first total % N one more.  (32-bit quotients: 64-bit ones take
+  // microseconds here.)  At least eight tiles a CTA: states that CTAs share cost more to join than those of a CTA's warps.
+  const int N = max(1, min((int)gridDim.x, (total + 7) / 8));
   const int each = total / N, more = total - each * N;
   auto begin_of = [&](int i) { return i * each + min(i, more); };
   auto cta_of = [&](int u) { return u < more * (each + 1) ? u / (each + 1) : more + (u - more * (each + 1)) / each; };
-  const int c0 = cta < N ? begin_of(cta) : 0, c1 = cta < N ? begin_of(cta + 1) : 0;
+  int c0 = cta < N ? begin_of(cta) : 0, c1 = cta < N ? begin_of(cta + 1) : 0;
+  // Joining states of several CTAs takes six microseconds, in which a CTA reads `spare` tiles more than its share.  Where no CTA gets more
+  // than that when (sequence, KV head)s stay whole, they do.
+  const int segs = B * VH, whole = (segs + (int)gridDim.x - 1) / (int)gridDim.x;
+  if ((long long)whole * longest - total / (int)gridDim.x <= p.spare) {
+    auto start_of = [&](int j) {
+      const int b = j / VH;
+      return b == B ? total : before[b] * VH + (j - b * VH) * (before[b + 1] - before[b]);
+    };
+    c0 = start_of((int)((unsigned)segs * (unsigned)cta / gridDim.x));
+    c1 = start_of((int)((unsigned)segs * (unsigned)(cta + 1) / gridDim.x));
+  }
   const int w0 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)warp / W), w1 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)(warp + 1) / W);
 
   // ---- sequences without a position
@@ -324,13 +346,16 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
 }
 
 constexpr size_t DA_SMEM = 224 * 1024;
+inline int da_spare_bytes() { static const char *e = getenv("DA_SPARE"); return e ? atoi(e) * 1024 : 256 * 1024; }
+#define DA_SPARE_BYTES da_spare_bytes()
 inline size_t da_smem_bytes(int batch, int warps, int own_floats, int heads, int hd) {
   return ((size_t)(batch + 1) * 4 + 15) / 16 * 16 + sizeof(float) * warps * (own_floats + 2 * da_part_floats(heads, hd));
 }
-template <typename Body> static cudaError_t launch(const DaArgs &p, int ctas, cudaStream_t s) {
+template <typename Body> static cudaError_t launch(DaArgs p, int ctas, cudaStream_t s) {
   static SmemLimit limit;
   const long long tiles = ((long long)p.a.cache.pages_per_seq * p.a.cache.page_size + Body::TILE - 1) / Body::TILE;
   if (tiles * p.a.batch * p.a.cache.G * p.chunks > (1 << 30)) return cudaErrorNotSupported;
+  p.spare = DA_SPARE_BYTES / (Body::TILE * p.a.cache.hd * 2 * (int)sizeof(typename Body::E));
   const size_t smem = da_smem_bytes(p.a.batch, Body::WARPS, Body::warp_smem_floats(p.a.cache.hd), p.heads, p.a.cache.hd);
   if (smem > DA_SMEM || !limit.ensure(decode_attn_kernel<Body>, (int)smem)) return cudaErrorInvalidValue;
   return launch_k(decode_attn_kernel<Body>, dim3(ctas), dim3(Body::WARPS * 32), smem, s, p);

@@ -42,10 +42,7 @@ __device__ __forceinline__ uint2 da_load8(const void *p) {
 // four 8-bit numbers as two pairs of f16
 template <int FMT> __device__ __forceinline__ void da_to_f16(uint32_t x, uint32_t &lo, uint32_t &hi) {
   if constexpr (FMT == KV_E4M3) {
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffffu), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x >> 16), __NV_E4M3);
-    lo = a.x | ((uint32_t)a.y << 16);
-    hi = b.x | ((uint32_t)b.y << 16);
+    e4m3_to_f16(x, lo, hi);
   } else {                                               // bits 0x6400 | u are 1024 + u, u = x + 128
     x ^= 0x80808080u;
     const __half2 off = __half2half2(__ushort_as_half(0x6480));
@@ -57,7 +54,7 @@ template <int FMT> __device__ __forceinline__ void da_to_f16(uint32_t x, uint32_
 }
 
 template <int FMT_, int HD, int MR> struct MmaBody {
-  static constexpr int FMT = FMT_, TILE = 16, NB = MR / 8;
+  static constexpr int FMT = FMT_, TILE = 32, SUB = 16, NB = MR / 8;
   static constexpr bool Q8 = kv_is_8bit(FMT);
   typedef typename KvElem<FMT>::type E;
   static constexpr int EB = sizeof(E), KP = HD * EB / 64, VB = HD * EB / 8 < 16 ? HD * EB / 8 : 16, VP = HD * EB / 8 / VB, EP = VB / EB;
@@ -67,10 +64,11 @@ template <int FMT_, int HD, int MR> struct MmaBody {
   static constexpr int WARPS = HD * EB <= 128 && MR == 8 ? 16 : 8;
   static __host__ __device__ int warp_smem_floats(int) { return 0; }
 
-  float m[NB][2], l[NB][2], o[NB][STEPS][4];             // of heads 8 n + 2 t and the next
+  static constexpr float NONE = -1e30f;                  // the reference before any score: far below every one, and yet a number
+  float r[NB][2], l[NB][2], o[NB][STEPS][4];             // reference, sum and O of heads 8 n + 2 t and the next
   uint32_t q[NB][STEPS][2];
   float qf[NB][2];                                       // scale * log2 e / the power of two on Q
-  float c;                                               // largest scale of a value so far
+  float c, rc;                                           // what scales of values are divided by, at least the largest so far; 64 / c
 
   // the dimensions of Q that this lane's piece of a key meets in contraction s, four at a time; heads past the last are zero
   __device__ __forceinline__ void load_queries(const DaArgs &p, const DaSeg &sg, int g, int t) {
@@ -120,37 +118,40 @@ template <int FMT_, int HD, int MR> struct MmaBody {
 #pragma unroll
       for (int e = 0; e < 2; e++) {
         qf[n][e] = __shfl_sync(0xffffffffu, f, (2 * t + e) * 4);
-        m[n][e] = -INFINITY, l[n][e] = 0.0f;
+        r[n][e] = NONE, l[n][e] = 0.0f;
       }
 #pragma unroll
       for (int s = 0; s < STEPS; s++)
 #pragma unroll
         for (int e = 0; e < 4; e++) o[n][s][e] = 0.0f;
     }
-    c = 0.0f;
+    c = rc = 0.0f;
   }
 
-  struct Keys { uint4 x[2][KP]; };
+  struct Keys { uint4 x[2][KP]; float ks[2], vs[2]; };   // keys and both scales of positions g and g + 8
   struct Values { uint32_t x[4][VP * VB / 4]; };
-  static __device__ __forceinline__ void load_keys(const char *pool, int row, int g, int t, Keys &k) {
+  // `row`: of this lane's position of a tile; `at`: 0 or 16, the tile's half
+  static __device__ __forceinline__ void load_keys(const KvCache &cc, int row, int at, int g, int t, Keys &k) {
 #pragma unroll
     for (int i = 0; i < 2; i++) {
-      const char *at = pool + (size_t)(uint32_t)__shfl_sync(0xffffffffu, row, g + 8 * i) * (HD * EB) + t * 16;
+      const uint32_t r = __shfl_sync(0xffffffffu, row, at + g + 8 * i);
+      const char *from = (const char *)cc.k + (size_t)r * (HD * EB) + t * 16;
 #pragma unroll
-      for (int j = 0; j < KP; j++) k.x[i][j] = da_load16(at + j * 64);
+      for (int j = 0; j < KP; j++) k.x[i][j] = da_load16(from + j * 64);
+      if constexpr (Q8) k.ks[i] = __ldg(cc.ks + r), k.vs[i] = __ldg(cc.vs + r);
     }
   }
-  static __device__ __forceinline__ void load_values(const char *pool, int row, int g, int t, Values &v) {
+  static __device__ __forceinline__ void load_values(const KvCache &cc, int row, int at, int g, int t, Values &v) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const char *at = pool + (size_t)(uint32_t)__shfl_sync(0xffffffffu, row, 2 * t + (i & 1) + 4 * (i & 2)) * (HD * EB) + g * VB;
+      const char *from = (const char *)cc.v + (size_t)(uint32_t)__shfl_sync(0xffffffffu, row, at + 2 * t + (i & 1) + 4 * (i & 2)) * (HD * EB) + g * VB;
 #pragma unroll
       for (int j = 0; j < VP; j++)
         if constexpr (VB == 16) {
-          const uint4 u = da_load16(at + j * 128);
+          const uint4 u = da_load16(from + j * 128);
           v.x[i][4 * j] = u.x, v.x[i][4 * j + 1] = u.y, v.x[i][4 * j + 2] = u.z, v.x[i][4 * j + 3] = u.w;
         } else {
-          const uint2 u = da_load8(at);
+          const uint2 u = da_load8(from);
           v.x[i][0] = u.x, v.x[i][1] = u.y;
         }
     }
@@ -158,41 +159,43 @@ template <int FMT_, int HD, int MR> struct MmaBody {
 
   __device__ __forceinline__ void run(const DaArgs &p, const DaSeg &sg, int len, float *, int lane) {
     const KvCache &cc = p.a.cache;
-    const int g = lane >> 2, t = lane & 3, head = sg.v / p.chunks, tok = lane & 15;
-    const char *K = (const char *)cc.k, *V = (const char *)cc.v;
-    const float *SC = lane < 16 ? cc.ks : cc.vs;
+    const int g = lane >> 2, t = lane & 3, head = p.chunks == 1 ? sg.v : sg.v / p.chunks;
     const int32_t *table = cc.table + (size_t)sg.b * cc.pages_per_seq;
     // the page of this lane's position of a tile (past the end: of the last position), then its row
     int off = 0;
     auto page_of = [&](int tile) {
-      const int pos = min(tile * TILE + tok, len - 1), at = p.page_shift >= 0 ? pos >> p.page_shift : pos / cc.page_size;
+      const int pos = min(tile * TILE + lane, len - 1), at = p.page_shift >= 0 ? pos >> p.page_shift : pos / cc.page_size;
       off = pos - at * cc.page_size;
       return table[at];
     };
     // row of this lane's position; valid: bit i is set where position i counts.  A page that is none of the pool's is read as page 0.
     auto row_of = [&](int tile, int page, uint32_t &valid) {
-      const bool ok = page >= 0 && page < cc.num_pages;
+      const bool ok = (unsigned)page < (unsigned)cc.num_pages;
       if (!ok) set_status(p.a.status, ST_BOUNDS, 63, sg.b, page);
-      valid = __ballot_sync(0xffffffffu, ok && tile * TILE + tok < len) & 0xffffu;
+      valid = __ballot_sync(0xffffffffu, ok && tile * TILE + lane < len);
       return ((ok ? page : 0) * cc.G + head) * cc.page_size + off;
     };
-    uint32_t valid, valid_next = 0;
-    int row = 0, row_next = 0, page;
-    page = page_of(sg.t0);
+    uint32_t valid;
+    int tile = sg.t0, page = page_of(tile);
     load_queries(p, sg, g, t);
-    row = row_of(sg.t0, page, valid);
+    int row = row_of(tile, page, valid);
     Keys k;
     Values v;
-    float sc = 1.0f, sc_next = 1.0f;
-    load_keys(K, row, g, t, k);
-    if constexpr (Q8) sc = SC[row];
-    if constexpr (V_AHEAD) load_values(V, row, g, t, v);
-    page = page_of(min(sg.t0 + 1, sg.t1 - 1));
+    load_keys(cc, row, 0, g, t, k);
+    if constexpr (V_AHEAD) load_values(cc, row, 0, g, t, v);
+    page = page_of(min(tile + 1, sg.t1 - 1));
     begin(p, t);
-    for (int tile = sg.t0; tile < sg.t1; tile++) {
-      const int next = min(tile + 1, sg.t1 - 1);         // the last tile is asked for once more
-      row_next = row_of(next, page, valid_next);
-      page = page_of(min(tile + 2, sg.t1 - 1));
+    // halves of tiles; the last may have none in its second one
+    const int halves = (min(len, sg.t1 * TILE) - sg.t0 * TILE + SUB - 1) / SUB;
+    for (int half = 0; half < halves; half++) {
+      const int at = (half & 1) * SUB;
+      const uint32_t live = (valid >> at) & 0xffffu;
+      const int row_here = row;
+      if (at) {                                          // the next half is of the next tile (the last tile is asked for once more)
+        tile = min(tile + 1, sg.t1 - 1);
+        row = row_of(tile, page, valid);
+        page = page_of(min(tile + 1, sg.t1 - 1));
+      }
       // ---- scores
       float s[NB][4];
 #pragma unroll
@@ -216,77 +219,88 @@ template <int FMT_, int HD, int MR> struct MmaBody {
             for (int n = 0; n < NB; n++) da_mma<false>(s[n], x[w], y[w], x[w + 1], y[w + 1], q[n][2 * j + w / 2][0], q[n][2 * j + w / 2][1]);
         }
       }
-      if constexpr (V_AHEAD) {
-        load_keys(K, row_next, g, t, k);
-        if constexpr (Q8) sc_next = SC[row_next];
-      } else {
-        load_values(V, row, g, t, v);
-      }
+      float vs[2] = {1.0f, 1.0f}, ks[2] = {1.0f, 1.0f};
+      if constexpr (Q8) vs[0] = k.vs[0], vs[1] = k.vs[1], ks[0] = k.ks[0], ks[1] = k.ks[1];
+      if constexpr (V_AHEAD) load_keys(cc, row, SUB - at, g, t, k);
+      else load_values(cc, row_here, at, g, t, v);
       // ---- probabilities: positions g and g + 8 (elements 0, 1 and 2, 3) of two heads
-      float ks[2] = {1.0f, 1.0f}, vs[2] = {1.0f, 1.0f};
-      float grow = 1.0f;
-      if constexpr (Q8) {
-        if (!((valid >> tok) & 1)) sc = 0.0f;            // what stands there may be no number
-        ks[0] = __shfl_sync(0xffffffffu, sc, g), ks[1] = __shfl_sync(0xffffffffu, sc, g + 8);
-        vs[0] = __shfl_sync(0xffffffffu, sc, g + 16), vs[1] = __shfl_sync(0xffffffffu, sc, g + 24);
-        const float top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, lane < 16 ? 0u : __float_as_uint(sc))), 8.0e-31f);
-        if (!(top <= c)) {
-          grow = c / top;
-          c = top;
-        }
-      }
       bool over = false;
+      float x[NB][4];                                    // scores relative to the reference
 #pragma unroll
       for (int n = 0; n < NB; n++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          s[n][e] *= ks[e >> 1] * qf[n][e & 1];
-          if (valid != 0xffffu && !((valid >> (g + 8 * (e >> 1))) & 1)) s[n][e] = -INFINITY;
-          over |= s[n][e] > m[n][e & 1] + 8.0f;
+          s[n][e] *= Q8 ? ks[e >> 1] * qf[n][e & 1] : qf[n][e & 1];
         }
-      if (__any_sync(0xffffffffu, over) || grow != 1.0f) {
+      if (live != 0xffffu) {
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+          if (!((live >> (g + 8 * i)) & 1)) {
+            vs[i] = 0.0f;                                // what stands there may be no number
+#pragma unroll
+            for (int n = 0; n < NB; n++) s[n][2 * i] = s[n][2 * i + 1] = -INFINITY;
+          }
+      }
+#pragma unroll
+      for (int n = 0; n < NB; n++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          x[n][e] = s[n][e] - r[n][e & 1];
+          over |= x[n][e] > 8.0f;
+        }
+      if constexpr (Q8) over |= vs[0] > c || vs[1] > c;
+      if (__any_sync(0xffffffffu, over)) {               // rare past the first tiles
+        float grow = 1.0f;
+        if constexpr (Q8) {
+          const float top = warp_max(fmaxf(vs[0], vs[1]));
+          if (top > c) {                                 // with room above, so that this stays rare
+            const float up = fmaxf(4.0f * top, 8e-31f);
+            grow = c / up;
+            c = up;
+            rc = 64.0f / up;
+          }
+        }
 #pragma unroll
         for (int n = 0; n < NB; n++)
 #pragma unroll
           for (int e = 0; e < 2; e++) {
-            float x = fmaxf(fmaxf(s[n][e], s[n][e + 2]), m[n][e]);
+            float m = fmaxf(fmaxf(s[n][e], s[n][e + 2]), r[n][e]);
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-            const float f = da_ex2(m[n][e] - da_ref(x));
-            m[n][e] = x;
+            for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            const float f = da_ex2(r[n][e] - m);
+            r[n][e] = m;
             l[n][e] *= f;
+            x[n][e] = s[n][e] - m, x[n][e + 2] = s[n][e + 2] - m;
 #pragma unroll
             for (int i = 0; i < STEPS; i++) o[n][i][e] *= f * grow, o[n][i][e + 2] *= f * grow;
           }
       }
-      const float to_f16 = Q8 ? 64.0f / c : 1.0f;
       uint32_t b[NB][2];
 #pragma unroll
       for (int n = 0; n < NB; n++) {
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          s[n][e] = da_ex2(s[n][e] - da_ref(m[n][e & 1]));
-          l[n][e & 1] += s[n][e];
+          x[n][e] = da_ex2(x[n][e]);
+          l[n][e & 1] += x[n][e];
         }
 #pragma unroll
         for (int i = 0; i < 2; i++) {
           uint32_t pair;
           if constexpr (Q8) {
-            const float w = vs[i] * to_f16;
-            const __half2 h = __floats2half2_rn(s[n][2 * i] * w, s[n][2 * i + 1] * w);
+            const float w = vs[i] * rc;
+            const __half2 h = __floats2half2_rn(x[n][2 * i] * w, x[n][2 * i + 1] * w);
             pair = *(const uint32_t *)&h;
           } else {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(s[n][2 * i], s[n][2 * i + 1]);
-            pair = *(const uint32_t *)&h;
+            pair = pack_bf16(x[n][2 * i], x[n][2 * i + 1]);
           }
           b[n][i] = da_transpose(pair);                  // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
         }
       }
       // ---- output
-      if (valid != 0xffffu) {                            // a page that is none: zero times whatever stands in page 0 is to be zero
+      if (live != 0xffffu) {                             // a page that is none: zero times whatever stands in page 0 is to be zero
 #pragma unroll
         for (int i = 0; i < 4; i++)
-          if (!((valid >> (2 * t + (i & 1) + 4 * (i & 2))) & 1))
+          if (!((live >> (2 * t + (i & 1) + 4 * (i & 2))) & 1))
 #pragma unroll
             for (int j = 0; j < VP * VB / 4; j++) v.x[i][j] = 0;
       }
@@ -296,9 +310,9 @@ template <int FMT_, int HD, int MR> struct MmaBody {
           uint32_t lo[2], hi[2], lo8[2], hi8[2];         // [positions 2t, 2t + 1 | 2t + 8, 2t + 9] of dimensions 0, 1 / 2, 3
 #pragma unroll
           for (int i = 0; i < 2; i++) {
-            const uint32_t x = v.x[2 * i][j], y = v.x[2 * i + 1][j];
-            da_to_f16<FMT>(__byte_perm(x, y, 0x5140), lo[i], hi[i]);
-            da_to_f16<FMT>(__byte_perm(x, y, 0x7362), lo8[i], hi8[i]);
+            const uint32_t a = v.x[2 * i][j], d = v.x[2 * i + 1][j];
+            da_to_f16<FMT>(__byte_perm(a, d, 0x5140), lo[i], hi[i]);
+            da_to_f16<FMT>(__byte_perm(a, d, 0x7362), lo8[i], hi8[i]);
           }
 #pragma unroll
           for (int n = 0; n < NB; n++) {
@@ -312,15 +326,8 @@ template <int FMT_, int HD, int MR> struct MmaBody {
           for (int n = 0; n < NB; n++) da_mma<false>(o[n][j], a0, a1, a2, a3, b[n][0], b[n][1]);
         }
       }
-      if constexpr (V_AHEAD) {
-        load_values(V, row_next, g, t, v);
-      } else {
-        load_keys(K, row_next, g, t, k);
-        if constexpr (Q8) sc_next = SC[row_next];
-      }
-      sc = sc_next;
-      row = row_next;
-      valid = valid_next;
+      if constexpr (V_AHEAD) load_values(cc, row, SUB - at, g, t, v);
+      else load_keys(cc, row, SUB - at, g, t, k);
     }
 #pragma unroll
     for (int n = 0; n < NB; n++)
@@ -348,7 +355,7 @@ template <int FMT_, int HD, int MR> struct MmaBody {
             const int at = (j * EP + i) / 2;
             f(h, j * 8 * EP + g * EP + i, make_float4(o[n][at][e], o[n][at][e + 2], o[n][at + 1][e], o[n][at + 1][e + 2]));
           }
-        if (g == 0) stat(h, m[n][e], l[n][e]);
+        if (g == 0) stat(h, r[n][e], l[n][e]);
       }
   }
 };

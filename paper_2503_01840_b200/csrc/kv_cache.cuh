@@ -101,11 +101,15 @@ __device__ __forceinline__ float4 kv_decode4(uint4 u) { return make_float4(__uin
 __device__ __forceinline__ float4 kv_decode4(uint2 u) {
   return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
 }
+// e4m3 by pairs to f16, which holds them all; straight from the halves of a word (through the type's struct the compiler takes pairs apart)
+__device__ __forceinline__ void e4m3_to_f16(uint32_t u, uint32_t &lo, uint32_t &hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(u));
+}
 template <int FMT> __device__ __forceinline__ float4 kv_decode4(uint32_t u) {
   if constexpr (FMT == KV_E4M3) {
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u & 0xffffu), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u >> 16), __NV_E4M3);
-    const float2 x = __half22float2(__half2(a)), y = __half22float2(__half2(b));
+    uint32_t a, b;
+    e4m3_to_f16(u, a, b);
+    const float2 x = __half22float2(*(const __half2 *)&a), y = __half22float2(*(const __half2 *)&b);
     return make_float4(x.x, x.y, y.x, y.y);
   } else {
     u ^= 0x80808080u;
