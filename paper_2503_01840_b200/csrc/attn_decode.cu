@@ -15,7 +15,7 @@ cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStre
   p.page_shift = (a.cache.page_size & (a.cache.page_size - 1)) == 0 ? __builtin_ctz(a.cache.page_size) : -1;
   const int group = a.H / a.cache.G, hd = a.cache.hd;
   p.q_f32 = dtype == KV_F32;
-  const bool mma = !p.q_f32 && (hd == 64 || hd == 128 || hd == 256);
+  const bool mma = fmt != KV_F32 && (hd == 64 || hd == 128 || hd == 256);
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -25,10 +25,10 @@ cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStre
   auto fits = [&](int heads) {      // the larger of what the bodies take
     int hp = 1;
     while (hp < heads) hp *= 2;
-    const int warps = mma && heads <= 8 && hd <= 128 ? 16 : 8, own = mma ? 0 : hp * hd + 64;
+    const int warps = heads <= (mma && !p.q_f32 ? 8 : 4) && hd <= 128 ? 16 : 8, own = mma ? 0 : hp * hd + 64;
     return da_smem_bytes(a.batch, warps, own, heads, hd) <= DA_SMEM;
   };
-  int most = mma && hd < 256 ? 16 : 8;
+  int most = mma ? (p.q_f32 ? 8 : 16) / (hd < 256 ? 1 : 2) : 8;
   while (most > 1 && !fits(std::min(most, group))) most /= 2;
   p.chunks = (group + most - 1) / most;
   p.heads = (group + p.chunks - 1) / p.chunks;

@@ -3,12 +3,12 @@
 
 namespace spec {
 
-// A lane takes a position's whole score; then LPT lanes share a position's values, DV vectors of four dimensions each.
+// Eight lanes share a position's keys; then LPT lanes share a position's values, NV vectors of four dimensions each.
 template <int FMT_, int HP_, int DCLASS> struct FmaBody {
-  static constexpr int FMT = FMT_, HP = HP_, TILE = 32, WARPS = 8;
+  static constexpr int FMT = FMT_, HP = HP_, TILE = 32, WARPS = HP <= 4 && DCLASS <= 128 ? 16 : 8;      // as many as the registers hold
   static constexpr int LPT = DCLASS == 64 ? 16 : 32, NV = DCLASS == 256 ? 2 : 1, PER = 32 / LPT;
   typedef typename KvElem<FMT>::type E;
-  static constexpr int VEC = 16 / sizeof(E);
+  static constexpr int VEC = 16 / sizeof(E), STEPS = DCLASS / VEC / 8 > 0 ? DCLASS / VEC / 8 : 1;      // rounds of eight 16-byte pieces over a row
   static __host__ __device__ int warp_smem_floats(int hd) { return HP * hd + 64; }
 
   float m[HP], l[HP], acc[HP][NV][4];
@@ -53,34 +53,54 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
     const KvCache &c = p.a.cache;
     const int hd = c.hd, g = sg.v / p.chunks;
     const E *K = (const E *)c.k, *V = (const E *)c.v;
+    const int sub = lane & 7, mine = 4 * sub + (lane >> 3);              // this lane's position of a tile
+    const int pieces = hd / VEC;
     for (int t = sg.t0; t < sg.t1; t++) {
-      const int pos = t * TILE + lane, n = min(TILE, len - t * TILE);
+      const int pos = t * TILE + mine;
       const int row = pos < len ? da_row(p, sg.b, g, pos) : -1;
       float s[HP];
-#pragma unroll
-      for (int h = 0; h < HP; h++) s[h] = 0.0f;
-      float vsc = 1.0f;
-      if (row >= 0) {
-        const uint4 *kr = (const uint4 *)(K + (size_t)row * hd);
+      // four positions at a time, 128 bytes of each by eight lanes: whole lines, where a lane a position asked for 32 at once
 #pragma unroll 4
-        for (int i = 0; i < hd / VEC; i++) {
+      for (int i = 0; i < 8; i++) {
+        const int r = __shfl_sync(0xffffffffu, row, (lane & 24) | i);
+        float d[HP];
+#pragma unroll
+        for (int h = 0; h < HP; h++) d[h] = 0.0f;
+        // loads without a condition, so that they are all under way at once: what a position that does not count brings is not used
+        const uint4 *const kr = (const uint4 *)(K + (size_t)max(r, 0) * hd);
+        uint4 raw[STEPS];
+#pragma unroll
+        for (int j = 0; j < STEPS; j++) raw[j] = __ldg(kr + min(sub + 8 * j, pieces - 1));
+#pragma unroll
+        for (int j = 0; j < STEPS; j++) {
+          const int at = sub + 8 * j;
+          if (at >= pieces) continue;
           float x[VEC];
-          unpack(kr[i], x);
+          unpack(raw[j], x);
 #pragma unroll
           for (int h = 0; h < HP; h++)
 #pragma unroll
             for (int e = 0; e < VEC; e += 4) {
-              const float4 w = *(const float4 *)(qs + h * hd + i * VEC + e);
-              s[h] = fmaf(w.x, x[e], fmaf(w.y, x[e + 1], fmaf(w.z, x[e + 2], fmaf(w.w, x[e + 3], s[h]))));
+              const float4 w = *(const float4 *)(qs + h * hd + at * VEC + e);
+              d[h] = fmaf(w.x, x[e], fmaf(w.y, x[e + 1], fmaf(w.z, x[e + 2], fmaf(w.w, x[e + 3], d[h]))));
             }
         }
-        if constexpr (kv_is_8bit(FMT)) {
+#pragma unroll
+        for (int h = 0; h < HP; h++) {
+          d[h] += __shfl_xor_sync(0xffffffffu, d[h], 1);
+          d[h] += __shfl_xor_sync(0xffffffffu, d[h], 2);
+          d[h] += __shfl_xor_sync(0xffffffffu, d[h], 4);
+          if (sub == i) s[h] = d[h];
+        }
+      }
+      float vsc = 1.0f;
+      if constexpr (kv_is_8bit(FMT))
+        if (row >= 0) {
           const float ksc = c.ks[row];
           vsc = c.vs[row];
 #pragma unroll
           for (int h = 0; h < HP; h++) s[h] *= ksc;
         }
-      }
 #pragma unroll
       for (int h = 0; h < HP; h++) {
         if (row < 0) s[h] = -INFINITY;
@@ -99,30 +119,30 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
         s[h] *= vsc;
       }
       const int dim = (lane % LPT) * 4;
-#pragma unroll 4
-      for (int j = 0; j < n; j += PER) {
-        const int from = PER == 1 ? j : j + lane / LPT;
-        const int r = __shfl_sync(0xffffffffu, row, from);
-        float x[NV][4];
+#pragma unroll 1
+      for (int j0 = 0; j0 < 32; j0 += 8 * PER) {         // eight of a lane's vectors under way
+        typename Four<FMT>::raw raw[8][NV];
+        int r[8];
 #pragma unroll
-        for (int i = 0; i < NV; i++) {
-          const int d = dim + i * 128;
+        for (int u = 0; u < 8; u++) {
+          r[u] = __shfl_sync(0xffffffffu, row, j0 + (PER == 1 ? u : 2 * u + lane / LPT));
+          const E *vr = V + (size_t)max(r[u], 0) * hd;
 #pragma unroll
-          for (int e = 0; e < 4; e++) x[i][e] = 0.0f;
-          if (r >= 0 && d < hd) {
-            const float4 f = kv_decode_four<FMT>(*(const typename Four<FMT>::raw *)(V + (size_t)r * hd + d));
-            x[i][0] = f.x, x[i][1] = f.y, x[i][2] = f.z, x[i][3] = f.w;
+          for (int i = 0; i < NV; i++) raw[u][i] = __ldg((const typename Four<FMT>::raw *)(vr + min(dim + i * 128, hd - 4)));
+        }
+#pragma unroll
+        for (int u = 0; u < 8; u++)
+#pragma unroll
+          for (int h = 0; h < HP; h++) {
+            const float w = __shfl_sync(0xffffffffu, s[h], j0 + (PER == 1 ? u : 2 * u + lane / LPT));
+            if (r[u] < 0) continue;
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+              const float4 x = kv_decode_four<FMT>(raw[u][i]);
+              acc[h][i][0] = fmaf(w, x.x, acc[h][i][0]), acc[h][i][1] = fmaf(w, x.y, acc[h][i][1]);
+              acc[h][i][2] = fmaf(w, x.z, acc[h][i][2]), acc[h][i][3] = fmaf(w, x.w, acc[h][i][3]);
+            }
           }
-        }
-#pragma unroll
-        for (int h = 0; h < HP; h++) {
-          const float w = __shfl_sync(0xffffffffu, s[h], from);
-          if (r < 0) continue;
-#pragma unroll
-          for (int i = 0; i < NV; i++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) acc[h][i][e] = fmaf(w, x[i][e], acc[h][i][e]);
-        }
       }
     }
 #pragma unroll

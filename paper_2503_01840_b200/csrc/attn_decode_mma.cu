@@ -53,9 +53,13 @@ template <int FMT> __device__ __forceinline__ void da_to_f16(uint32_t x, uint32_
   }
 }
 
-template <int FMT_, int HD, int MR> struct MmaBody {
+template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
   static constexpr int FMT = FMT_, TILE = 32, SUB = 16, NB = MR / 8;
   static constexpr bool Q8 = kv_is_8bit(FMT);
+  // fp32 queries (8-bit caches): a block of eight columns is four heads' upper eleven bits and the same heads' next eleven, 2^11 times as
+  // large, of the queries as of the probabilities; the products are exact, and the two sums are put together in fp32
+  static_assert(!SPLIT || Q8, "a bf16 cache has bf16 queries");
+  static constexpr int PER_BLOCK = SPLIT ? 4 : 8;       // heads of a block of columns
   typedef typename KvElem<FMT>::type E;
   static constexpr int EB = sizeof(E), KP = HD * EB / 64, VB = HD * EB / 8 < 16 ? HD * EB / 8 : 16, VP = HD * EB / 8 / VB, EP = VB / EB;
   static constexpr int STEPS = HD / 16;
@@ -67,6 +71,7 @@ template <int FMT_, int HD, int MR> struct MmaBody {
   static constexpr float NONE = -1e30f;                  // the reference before any score: far below every one, and yet a number
   float r[NB][2], l[NB][2], o[NB][STEPS][4];             // reference, sum and O of heads 8 n + 2 t and the next
   uint32_t q[NB][STEPS][2];
+  float wide[SPLIT ? NB : 1][SPLIT ? STEPS : 1][4];      // queries as they are, until begin()
   float qf[NB][2];                                       // scale * log2 e / the power of two on Q
   float c, rc;                                           // what scales of values are divided by, at least the largest so far; 64 / c
 
@@ -76,27 +81,45 @@ template <int FMT_, int HD, int MR> struct MmaBody {
     const int have = min(p.heads, group - (sg.v % p.chunks) * p.heads);
 #pragma unroll
     for (int n = 0; n < NB; n++) {
-      const bool in = 8 * n + g < have;
-      const bf16 *x = (const bf16 *)p.a.q + (size_t)sg.b * p.a.q_ts + (size_t)(h0 + (in ? 8 * n + g : 0)) * HD;
+      const int h = PER_BLOCK * n + g % PER_BLOCK;
+      const bool in = h < have;
+      const size_t x = (size_t)sg.b * p.a.q_ts + (size_t)(h0 + (in ? h : 0)) * HD;
 #pragma unroll
       for (int s = 0; s < STEPS; s++) {
         const int d = EB == 1 ? (s / 4) * 64 + t * 16 + (s % 4) * 4 : (s / 2) * 32 + t * 8 + (s % 2) * 4;
-        const uint2 u = in ? *(const uint2 *)(x + d) : make_uint2(0, 0);
-        q[n][s][0] = u.x, q[n][s][1] = u.y;
+        if constexpr (SPLIT) {
+          const float4 u = in ? *(const float4 *)((const float *)p.a.q + x + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+          wide[n][s][0] = u.x, wide[n][s][1] = u.y, wide[n][s][2] = u.z, wide[n][s][3] = u.w;
+        } else {
+          const uint2 u = in ? *(const uint2 *)((const bf16 *)p.a.q + x + d) : make_uint2(0, 0);
+          q[n][s][0] = u.x, q[n][s][1] = u.y;
+        }
       }
     }
   }
-  __device__ __forceinline__ void begin(const DaArgs &p, int t) {
+  // two numbers as f16 (part 0), or what that leaves of them, times 2^11 (part 1); an infinity leaves nothing
+  static __device__ __forceinline__ uint32_t part_of(float a, float b, int part) {
+    const __half2 hi = __floats2half2_rn(a, b);
+    if (!SPLIT || part == 0) return *(const uint32_t *)&hi;
+    const float2 u = __half22float2(hi);
+    const __half2 lo = __floats2half2_rn(fabsf(u.x) < INFINITY ? (a - u.x) * 2048.0f : 0.0f, fabsf(u.y) < INFINITY ? (b - u.y) * 2048.0f : 0.0f);
+    return *(const uint32_t *)&lo;
+  }
+  __device__ __forceinline__ void begin(const DaArgs &p, int g, int t) {
 #pragma unroll
     for (int n = 0; n < NB; n++) {
       float f = p.a.scale * 1.44269504088896341f;
       if constexpr (Q8) {
         float top = 0.0f;
+        auto pair = [&](int s, int i) {
+          if constexpr (SPLIT) return make_float2(wide[n][s][2 * i], wide[n][s][2 * i + 1]);
+          else return __bfloat1622float2(*(const __nv_bfloat162 *)&q[n][s][i]);
+        };
 #pragma unroll
         for (int s = 0; s < STEPS; s++)
 #pragma unroll
-          for (int e = 0; e < 2; e++) {
-            const float2 v = __bfloat1622float2(*(const __nv_bfloat162 *)&q[n][s][e]);
+          for (int i = 0; i < 2; i++) {
+            const float2 v = pair(s, i);
             top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
           }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -110,14 +133,13 @@ template <int FMT_, int HD, int MR> struct MmaBody {
         for (int s = 0; s < STEPS; s++)
 #pragma unroll
           for (int i = 0; i < 2; i++) {
-            const float2 v = __bfloat1622float2(*(const __nv_bfloat162 *)&q[n][s][i]);
-            const __half2 h = __floats2half2_rn(v.x * up, v.y * up);
-            q[n][s][i] = *(const uint32_t *)&h;
+            const float2 v = pair(s, i);
+            q[n][s][i] = SPLIT ? part_of(v.x * up, v.y * up, g >> 2) : part_of(v.x * up, v.y * up, 0);
           }
       }
 #pragma unroll
       for (int e = 0; e < 2; e++) {
-        qf[n][e] = __shfl_sync(0xffffffffu, f, (2 * t + e) * 4);
+        qf[n][e] = __shfl_sync(0xffffffffu, f, ((2 * t + e) % PER_BLOCK) * 4);
         r[n][e] = NONE, l[n][e] = 0.0f;
       }
 #pragma unroll
@@ -184,7 +206,7 @@ template <int FMT_, int HD, int MR> struct MmaBody {
     load_keys(cc, row, 0, g, t, k);
     if constexpr (V_AHEAD) load_values(cc, row, 0, g, t, v);
     page = page_of(min(tile + 1, sg.t1 - 1));
-    begin(p, t);
+    begin(p, g, t);
     // halves of tiles; the last may have none in its second one
     const int halves = (min(len, sg.t1 * TILE) - sg.t0 * TILE + SUB - 1) / SUB;
     for (int half = 0; half < halves; half++) {
@@ -219,6 +241,14 @@ template <int FMT_, int HD, int MR> struct MmaBody {
             for (int n = 0; n < NB; n++) da_mma<false>(s[n], x[w], y[w], x[w + 1], y[w + 1], q[n][2 * j + w / 2][0], q[n][2 * j + w / 2][1]);
         }
       }
+      if constexpr (SPLIT)                               // the other part of the same head and position is two lanes away
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const float o = __shfl_xor_sync(0xffffffffu, s[n][e], 2);
+            s[n][e] = t < 2 ? fmaf(o, 4.8828125e-4f, s[n][e]) : fmaf(s[n][e], 4.8828125e-4f, o);
+          }
       float vs[2] = {1.0f, 1.0f}, ks[2] = {1.0f, 1.0f};
       if constexpr (Q8) vs[0] = k.vs[0], vs[1] = k.vs[1], ks[0] = k.ks[0], ks[1] = k.ks[1];
       if constexpr (V_AHEAD) load_keys(cc, row, SUB - at, g, t, k);
@@ -288,8 +318,7 @@ template <int FMT_, int HD, int MR> struct MmaBody {
           uint32_t pair;
           if constexpr (Q8) {
             const float w = vs[i] * rc;
-            const __half2 h = __floats2half2_rn(x[n][2 * i] * w, x[n][2 * i + 1] * w);
-            pair = *(const uint32_t *)&h;
+            pair = SPLIT ? part_of(x[n][2 * i] * w, x[n][2 * i + 1] * w, t >> 1) : part_of(x[n][2 * i] * w, x[n][2 * i + 1] * w, 0);
           } else {
             pair = pack_bf16(x[n][2 * i], x[n][2 * i + 1]);
           }
@@ -337,7 +366,13 @@ template <int FMT_, int HD, int MR> struct MmaBody {
         for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
         if constexpr (Q8)
 #pragma unroll
-          for (int i = 0; i < STEPS; i++) o[n][i][e] *= c * 0.015625f, o[n][i][e + 2] *= c * 0.015625f;
+          for (int i = 0; i < STEPS; i++) {
+            if constexpr (SPLIT) {
+              o[n][i][e] = fmaf(__shfl_xor_sync(0xffffffffu, o[n][i][e], 2), 4.8828125e-4f, o[n][i][e]);      // what t < 2 hold is used
+              o[n][i][e + 2] = fmaf(__shfl_xor_sync(0xffffffffu, o[n][i][e + 2], 2), 4.8828125e-4f, o[n][i][e + 2]);
+            }
+            o[n][i][e] *= c * 0.015625f, o[n][i][e + 2] *= c * 0.015625f;
+          }
       }
   }
 
@@ -347,7 +382,8 @@ template <int FMT_, int HD, int MR> struct MmaBody {
     for (int n = 0; n < NB; n++)
 #pragma unroll
       for (int e = 0; e < 2; e++) {
-        const int h = 8 * n + 2 * t + e;
+        const int h = PER_BLOCK * n + 2 * t + e;
+        if (SPLIT && t >= 2) continue;
 #pragma unroll
         for (int j = 0; j < VP; j++)
 #pragma unroll
@@ -361,6 +397,12 @@ template <int FMT_, int HD, int MR> struct MmaBody {
 };
 
 template <int FMT, int HD> static cudaError_t mma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
+  if constexpr (kv_is_8bit(FMT))
+    if (p.q_f32) {
+      if constexpr (HD < 256)
+        if (p.heads > 4) return launch<MmaBody<FMT, HD, 16, true>>(p, ctas, s);
+      return launch<MmaBody<FMT, HD, 8, true>>(p, ctas, s);
+    }
   if constexpr (HD < 256)
     if (p.heads > 8) return launch<MmaBody<FMT, HD, 16>>(p, ctas, s);
   return launch<MmaBody<FMT, HD, 8>>(p, ctas, s);
