@@ -32,6 +32,9 @@ cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStre
   while (most > 1 && !fits(std::min(most, group))) most /= 2;
   p.chunks = (group + most - 1) / most;
   p.heads = (group + p.chunks - 1) / p.chunks;
+  p.group = group;
+  p.vheads = a.cache.G * p.chunks;
+  p.segs = a.batch * p.vheads;
   p.count = (unsigned *)a.workspace;
   p.part = (float *)((char *)a.workspace + DA_COUNT_BYTES);
   return mma ? launch_decode_mma(p, fmt, ctas, s) : launch_decode_fma(p, fmt, ctas, s);

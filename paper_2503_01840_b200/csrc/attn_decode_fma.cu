@@ -21,8 +21,7 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
 
   __device__ __forceinline__ void init(const DaArgs &p, const DaSeg &sg, float *mem, int lane) {
     qs = mem;
-    const int hd = p.a.cache.hd, group = p.a.H / p.a.cache.G, h0 = (sg.v / p.chunks) * group + (sg.v % p.chunks) * p.heads;
-    const int have = min(p.heads, group - (sg.v % p.chunks) * p.heads);
+    const int hd = p.a.cache.hd, h0 = sg.kv * p.group + sg.chunk * p.heads, have = min(p.heads, p.group - sg.chunk * p.heads);
     __syncwarp();
     for (int i = lane; i < HP * hd; i += 32) {
       const int h = i / hd;
@@ -51,7 +50,7 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
 
   __device__ __forceinline__ void walk(const DaArgs &p, const DaSeg &sg, int len, int lane) {
     const KvCache &c = p.a.cache;
-    const int hd = c.hd, g = sg.v / p.chunks;
+    const int hd = c.hd, g = sg.kv;
     const E *K = (const E *)c.k, *V = (const E *)c.v;
     const int sub = lane & 7, mine = 4 * sub + (lane >> 3);              // this lane's position of a tile
     const int pieces = hd / VEC;

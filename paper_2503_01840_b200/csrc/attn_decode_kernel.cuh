@@ -9,8 +9,6 @@
 #pragma once
 #include "attn_decode.cuh"
 
-#include <stdlib.h>
-
 namespace spec {
 
 constexpr int DA_MAX_CTAS = 160;           // CTAs of a launch, at most
@@ -21,7 +19,8 @@ struct DaArgs {
   DecodeAttn a;
   int page_shift;               // log2 of the page size, or -1
   int q_f32;                    // queries and output in fp32
-  int spare;                    // tiles that a CTA reads while states of several CTAs are joined
+  int group, vheads, segs;      // query heads per KV head; KV heads x chunks; segments of the call
+  int whole, spare;             // segments that a CTA gets at most where they stay whole (0: they do not); tiles that one may have beyond its share then
   int heads, chunks;            // query heads a warp takes together, and how many such chunks share a KV head
   unsigned *count;              // [CTAs], zero between calls
   float *part;                  // [CTAs][2][part_floats], close together: another page of memory costs a walk of the page tables
@@ -31,8 +30,9 @@ __host__ __device__ constexpr int da_part_floats(int heads, int hd) { return hea
 
 // A run of tiles of one (sequence, chunk of heads)
 struct DaSeg {
-  int b, v;                     // sequence; KV head * chunks + chunk
+  int b, kv, chunk;             // sequence, KV head, chunk of its query heads
   int t0, t1, tiles;            // tiles t0 .. t1 - 1 of `tiles`
+  int u0;                       // the first of them, counted over all segments
 };
 
 // States of one segment that are joined: `mask` of those that stand `stride` floats apart from `from`, the first `skew` further on; into `to`, or
@@ -48,6 +48,12 @@ __device__ __forceinline__ float da_exp2(float x) { return exp2f(x); }
 __device__ __forceinline__ float da_ref(float m) { return m == -INFINITY ? 0.0f : m; }      // keeps inf - inf out of a row whose scores are all -inf
 
 __device__ __forceinline__ float da_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }      // a row whose scores are all -inf gives 0
+
+// x / d for small quotients (below 2^20) of non-negative numbers, in a third of the instructions of the exact division
+__device__ __forceinline__ int da_quotient(int x, int d) {
+  const int q = (int)__fdividef((float)x, (float)d), r = x - q * d;
+  return q + (r >= d) - (r < 0);
+}
 
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -140,20 +146,33 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   pdl_trigger();
   constexpr int W = Body::WARPS, THREADS = W * 32, TILE = Body::TILE;
   extern __shared__ __align__(16) char smem[];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.a.batch, hd = p.a.cache.hd, group = p.a.H / p.a.cache.G;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.a.batch, hd = p.a.cache.hd, cta = blockIdx.x, VH = p.vheads;
   const int heads = p.heads, part_floats = da_part_floats(heads, hd);     // O [heads][hd], then (max, sum) [heads]
   int *before = (int *)smem;
   float *mem = (float *)(smem + ((size_t)(B + 1) * 4 + 15) / 16 * 16);
   float *warp_mem = mem + warp * Body::warp_smem_floats(hd);
   float *states = mem + W * Body::warp_smem_floats(hd);                  // [2 W][part_floats]
   __shared__ int2 scan[W];
-  int longest = 0;
   __shared__ DaSeg seg[2 * W];                                           // of the partial states; b = -1: none
   __shared__ DaRun runs[2 * W];
   __shared__ int to_do[3];
 
-  // ---- tiles before each sequence: a run of sequences per thread, then a scan over the threads
-  {
+  // ---- tiles before each sequence, their sum, and the longest sequence's.  Up to 32 sequences: a lane each in every warp, and no barrier
+  // on the way to the first load; more: a run of them per thread, a scan over the threads, and a table.
+  const bool few = B <= 32;
+  int total, longest = 0, my_before = 0, my_tiles = 0;
+  if (few) {
+    my_tiles = lane < B ? (da_length(p, lane) + TILE - 1) / TILE : 0;
+    int inc = my_tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += x;
+    }
+    my_before = inc - my_tiles;
+    total = __shfl_sync(0xffffffffu, inc, 31);
+    longest = __reduce_max_sync(0xffffffffu, my_tiles);
+  } else {
     const int per = (B + THREADS - 1) / THREADS, b0 = min(B, tid * per), b1 = min(B, b0 + per);
     int sum = 0, most = 0;
     for (int b = b0; b < b1; b++) {
@@ -180,34 +199,41 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
       at += (da_length(p, b) + TILE - 1) / TILE;
     }
     if (tid == THREADS - 1) before[B] = at;
-    if (lane < 2) seg[2 * warp + lane].b = -1;
     __syncthreads();
+    total = before[B];
   }
-  const int VH = p.a.cache.G * p.chunks, cta = blockIdx.x;
-  const int total = before[B] * VH;
+  total *= VH;
+  if (lane < 2) seg[2 * warp + lane].b = -1;
+  // (tiles before sequence b, its own); all lanes ask for the same one
+  auto tiles_of = [&](int b) {
+    if (few) return make_int2(__shfl_sync(0xffffffffu, my_before, b), __shfl_sync(0xffffffffu, my_tiles, b));
+    return make_int2(before[b], before[b + 1] - before[b]);
+  };
+
   // The tiles are dealt out evenly: each of N CTAs has total / N, the first total % N one more.  (32-bit quotients: 64-bit ones take
   // microseconds here.)  At least eight tiles a CTA: states that CTAs share cost more to join than those of a CTA's warps.
-  const int N = max(1, min((int)gridDim.x, (total + 7) / 8));
+  const int N = max(1, min((int)gridDim.x, (total + 7) >> 3));
   const int each = total / N, more = total - each * N;
   auto begin_of = [&](int i) { return i * each + min(i, more); };
   auto cta_of = [&](int u) { return u < more * (each + 1) ? u / (each + 1) : more + (u - more * (each + 1)) / each; };
   int c0 = cta < N ? begin_of(cta) : 0, c1 = cta < N ? begin_of(cta + 1) : 0;
-  // Joining states of several CTAs takes six microseconds, in which a CTA reads `spare` tiles more than its share.  Where no CTA gets more
-  // than that when (sequence, KV head)s stay whole, they do.
-  const int segs = B * VH, whole = (segs + (int)gridDim.x - 1) / (int)gridDim.x;
-  if ((long long)whole * longest - total / (int)gridDim.x <= p.spare) {
+  // Joining states of several CTAs takes six microseconds, in which a CTA reads `spare` tiles.  Where no CTA gets that many more than its
+  // share when segments stay whole, they do.
+  if (p.whole && ((long long)p.whole * longest - p.spare) * (int)gridDim.x <= total) {
     auto start_of = [&](int j) {
-      const int b = j / VH;
-      return b == B ? total : before[b] * VH + (j - b * VH) * (before[b + 1] - before[b]);
+      const int b = da_quotient(j, VH);
+      if (b >= B) return total;
+      const int2 t = tiles_of(b);
+      return t.x * VH + (j - b * VH) * t.y;
     };
-    c0 = start_of((int)((unsigned)segs * (unsigned)cta / gridDim.x));
-    c1 = start_of((int)((unsigned)segs * (unsigned)(cta + 1) / gridDim.x));
+    c0 = start_of((int)((unsigned)p.segs * (unsigned)cta / gridDim.x));
+    c1 = start_of((int)((unsigned)p.segs * (unsigned)(cta + 1) / gridDim.x));
   }
   const int w0 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)warp / W), w1 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)(warp + 1) / W);
 
   // ---- sequences without a position
   for (int b = cta; b < B; b += gridDim.x)
-    if (before[b + 1] == before[b]) {
+    if (tiles_of(b).y == 0) {
       for (int i = tid * 4; i < p.a.H * hd; i += THREADS * 4) da_store(p.a.out, p.q_f32, (size_t)b * p.a.H * hd + i, make_float4(0.f, 0.f, 0.f, 0.f));
       if (p.a.lse)
         for (int h = tid; h < p.a.H; h += THREADS) p.a.lse[(size_t)b * p.a.H + h] = -INFINITY;
@@ -217,18 +243,25 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   int slot = 0;
   for (int u = w0; u < w1;) {
     DaSeg s;
-    int lo = 0, hi = B;                                                  // the last sequence with before * VH <= u: it has tiles
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (before[mid] * VH <= u) lo = mid;
-      else hi = mid;
+    if (few) {                                                           // the last sequence with before * VH <= u: it has tiles
+      s.b = __popc(__ballot_sync(0xffffffffu, lane < B && my_before * VH <= u)) - 1;
+    } else {
+      int lo = 0, hi = B;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before[mid] * VH <= u) lo = mid;
+        else hi = mid;
+      }
+      s.b = lo;
     }
-    s.b = lo;
-    s.tiles = before[lo + 1] - before[lo];
-    const int r = u - before[lo] * VH;
-    s.v = r / s.tiles;
-    s.t0 = r - s.v * s.tiles;
-    s.t1 = min(s.tiles, s.t0 + (w1 - u));
+    const int2 t = tiles_of(s.b);
+    s.tiles = t.y;
+    const int r = u - t.x * VH, v = da_quotient(r, t.y);
+    s.kv = p.chunks == 1 ? v : da_quotient(v, p.chunks);
+    s.chunk = v - s.kv * p.chunks;
+    s.t0 = r - v * t.y;
+    s.t1 = min(t.y, s.t0 + (w1 - u));
+    s.u0 = u - s.t0;
     u += s.t1 - s.t0;
     Body body;
     body.run(p, s, da_length(p, s.b), warp_mem, lane);
@@ -242,9 +275,8 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     });
     if (whole) {                                                         // the slot is free again until the run's last segment
       __syncwarp();
-      const int chunk = p.chunks == 1 ? 0 : s.v % p.chunks, kv = p.chunks == 1 ? s.v : s.v / p.chunks;
-      const size_t row = (size_t)s.b * p.a.H + kv * group + chunk * heads;
-      for (int h = 0; h < min(heads, group - chunk * heads); h++)
+      const size_t row = (size_t)s.b * p.a.H + s.kv * p.group + s.chunk * heads;
+      for (int h = 0; h < min(heads, p.group - s.chunk * heads); h++)
         da_join_head(st, part_floats, 0, 1u, heads * hd, h, hd, nullptr, (char *)p.a.out + (row + h) * hd * (p.q_f32 ? 4 : 2), p.q_f32, p.a.lse ? p.a.lse + row + h : nullptr);
     } else {
       if (lane == 0) seg[2 * warp + slot] = s;
@@ -260,18 +292,17 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   constexpr int SHIFT = W == 16 ? 3 : 4;                                 // parts of both segments of a CTA fit its 2 W states
   static_assert(DA_MAX_CTAS / (1 << SHIFT) + 2 <= 2 * W, "room for the parts of level 1");
   auto make_run = [&](int at, const DaSeg &s, const float *from, int stride, int skew, uint32_t mask, float *to) {
-    const int chunk = p.chunks == 1 ? 0 : s.v % p.chunks, kv = p.chunks == 1 ? s.v : s.v / p.chunks;
-    runs[at] = DaRun{from, to, (int)(s.b * p.a.H + kv * group + chunk * heads), min(heads, group - chunk * heads), stride, skew, mask};
+    runs[at] = DaRun{from, to, s.b * p.a.H + s.kv * p.group + s.chunk * heads, min(heads, p.group - s.chunk * heads), stride, skew, mask};
   };
   int n_runs = 0, n_open = 0;
   DaSeg open_seg{};                                                      // lanes 0 and 1 of warp 0: what other CTAs have the rest of
   if (warp == 0) {
     // lane i looks at partial state i; a run of one segment's states begins where the one before it is another's
-    const DaSeg mine = lane < 2 * W ? seg[lane] : DaSeg{-1, 0, 0, 0, 0};
+    const DaSeg mine = lane < 2 * W ? seg[lane] : DaSeg{-1, 0, 0, 0, 0, 0, 0};
     const uint32_t some = __ballot_sync(0xffffffffu, mine.b >= 0), below = (1u << lane) - 1;
     const int prev = (some & below) ? 31 - __clz(some & below) : lane;
-    const int pb = __shfl_sync(0xffffffffu, mine.b, prev), pv = __shfl_sync(0xffffffffu, mine.v, prev);
-    const bool begins = mine.b >= 0 && (prev == lane || pb != mine.b || pv != mine.v);
+    const int pu = __shfl_sync(0xffffffffu, mine.u0, prev);
+    const bool begins = mine.b >= 0 && (prev == lane || pu != mine.u0);
     const uint32_t all = __ballot_sync(0xffffffffu, begins), after = all & ~below & ~(1u << lane);
     const uint32_t run = some & ~below & (after ? (1u << (__ffs(after) - 1)) - 1 : 0xffffffffu);
     const int t1 = __shfl_sync(0xffffffffu, mine.t1, begins ? 31 - __clz(run) : lane);
@@ -282,8 +313,9 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     const uint32_t opens = __ballot_sync(0xffffffffu, open);
     n_open = __popc(opens);
     const int from = lane == 0 ? __ffs(opens) - 1 : 31 - __clz(opens);
-    open_seg.b = __shfl_sync(0xffffffffu, mine.b, from & 31), open_seg.v = __shfl_sync(0xffffffffu, mine.v, from & 31);
-    open_seg.tiles = __shfl_sync(0xffffffffu, mine.tiles, from & 31);
+    open_seg.b = __shfl_sync(0xffffffffu, mine.b, from & 31), open_seg.kv = __shfl_sync(0xffffffffu, mine.kv, from & 31);
+    open_seg.chunk = __shfl_sync(0xffffffffu, mine.chunk, from & 31), open_seg.tiles = __shfl_sync(0xffffffffu, mine.tiles, from & 31);
+    open_seg.u0 = __shfl_sync(0xffffffffu, mine.u0, from & 31);
     if (lane == 0) to_do[0] = __popc(all), to_do[1] = n_open;
   }
   __syncthreads();
@@ -308,9 +340,8 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
       int parts = 0;
       if (level == 0) {                                                  // the CTA that starts a segment keeps its count
         if (lane < n_open) {
-          const int u0 = before[open_seg.b] * VH + open_seg.v * open_seg.tiles;
-          shared_from = cta_of(u0);
-          shared_by = cta_of(u0 + open_seg.tiles - 1) - shared_from + 1;
+          shared_from = cta_of(open_seg.u0);
+          shared_by = cta_of(open_seg.u0 + open_seg.tiles - 1) - shared_from + 1;
           __threadfence();
           mine_last = atomicAdd(p.count + shared_from, 1u) == (unsigned)(shared_by - 1);
           if (mine_last) p.count[shared_from] = 0;                       // as the next call wants it
@@ -346,8 +377,9 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
 }
 
 constexpr size_t DA_SMEM = 224 * 1024;
-inline int da_spare_bytes() { static const char *e = getenv("DA_SPARE"); return e ? atoi(e) * 1024 : 256 * 1024; }
-#define DA_SPARE_BYTES da_spare_bytes()
+// What a CTA reads in the time that a join over CTAs takes.  us with none / 128 / 256 / 512 KB: 64 sequences of 10 to 100 tokens, 40 heads 32.2 / 32.3 /
+// 24.8 / 24.7; 32 of 100 to 400, 8 heads 16.7 / 14.1 / 14.2 / 14.2; 8 of 700 to 1500 16.7 / 16.7 / 16.6 / 17.2.
+constexpr int DA_SPARE_BYTES = 256 * 1024;
 inline size_t da_smem_bytes(int batch, int warps, int own_floats, int heads, int hd) {
   return ((size_t)(batch + 1) * 4 + 15) / 16 * 16 + sizeof(float) * warps * (own_floats + 2 * da_part_floats(heads, hd));
 }
@@ -355,6 +387,8 @@ template <typename Body> static cudaError_t launch(DaArgs p, int ctas, cudaStrea
   static SmemLimit limit;
   const long long tiles = ((long long)p.a.cache.pages_per_seq * p.a.cache.page_size + Body::TILE - 1) / Body::TILE;
   if (tiles * p.a.batch * p.a.cache.G * p.chunks > (1 << 30)) return cudaErrorNotSupported;
+  // (with fewer segments than half the CTAs the others stay without work: one user at 613 tokens 12.3 us dealt out evenly, 13.0 whole)
+  p.whole = p.segs * 2 >= ctas ? (p.segs + ctas - 1) / ctas : 0;
   p.spare = DA_SPARE_BYTES / (Body::TILE * p.a.cache.hd * 2 * (int)sizeof(typename Body::E));
   const size_t smem = da_smem_bytes(p.a.batch, Body::WARPS, Body::warp_smem_floats(p.a.cache.hd), p.heads, p.a.cache.hd);
   if (smem > DA_SMEM || !limit.ensure(decode_attn_kernel<Body>, (int)smem)) return cudaErrorInvalidValue;

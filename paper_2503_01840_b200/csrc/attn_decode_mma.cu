@@ -77,8 +77,7 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
 
   // the dimensions of Q that this lane's piece of a key meets in contraction s, four at a time; heads past the last are zero
   __device__ __forceinline__ void load_queries(const DaArgs &p, const DaSeg &sg, int g, int t) {
-    const int group = p.a.H / p.a.cache.G, h0 = (sg.v / p.chunks) * group + (sg.v % p.chunks) * p.heads;
-    const int have = min(p.heads, group - (sg.v % p.chunks) * p.heads);
+    const int h0 = sg.kv * p.group + sg.chunk * p.heads, have = min(p.heads, p.group - sg.chunk * p.heads);
 #pragma unroll
     for (int n = 0; n < NB; n++) {
       const int h = PER_BLOCK * n + g % PER_BLOCK;
@@ -181,7 +180,7 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
 
   __device__ __forceinline__ void run(const DaArgs &p, const DaSeg &sg, int len, float *, int lane) {
     const KvCache &cc = p.a.cache;
-    const int g = lane >> 2, t = lane & 3, head = p.chunks == 1 ? sg.v : sg.v / p.chunks;
+    const int g = lane >> 2, t = lane & 3, head = sg.kv;
     const int32_t *table = cc.table + (size_t)sg.b * cc.pages_per_seq;
     // the page of this lane's position of a tile (past the end: of the last position), then its row
     int off = 0;
