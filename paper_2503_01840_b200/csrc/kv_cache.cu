@@ -234,11 +234,12 @@ template <typename T, int FMT> static cudaError_t rope_append(const RopeAppend &
   gr.lh_shift = __builtin_ctz(lh);
   const int step = ROPE_THREADS / lh;                    // heads of a round of the block
   constexpr int U = 2;
-  // few tokens: a round's heads a block, so that no thread has a second round to wait for; many: about six rounds a block
+  // few tokens: a round's heads a block (of several tokens where one has fewer heads than that), so that no thread has a second round to wait
+  // for; many: about six rounds a block
   const long long rounds = ((long long)a.tokens * all + step - 1) / step;
   if (rounds <= 1184) {
-    gr.per_block = 1;
     gr.heads = min(all, step);
+    gr.per_block = min(ROPE_MAX_TOKENS, step / gr.heads);
   } else {
     gr.heads = all;
     gr.per_block = max(1, min(ROPE_MAX_TOKENS, 6 * step / all));
