@@ -25,7 +25,7 @@ cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStre
   auto fits = [&](int heads) {      // the larger of what the bodies take
     int hp = 1;
     while (hp < heads) hp *= 2;
-    const int warps = heads <= (mma && !p.q_f32 ? 8 : 4) && hd <= 128 ? 16 : 8, own = mma ? 0 : hp * hd + 64;
+    const int warps = hd <= 128 ? 16 : 8, own = mma ? 0 : hp * hd + 64;
     return da_smem_bytes(a.batch, warps, own, heads, hd) <= DA_SMEM;
   };
   int most = mma ? (p.q_f32 ? 8 : 16) / (hd < 256 ? 1 : 2) : 8;

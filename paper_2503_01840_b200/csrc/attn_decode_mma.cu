@@ -53,8 +53,8 @@ template <int FMT> __device__ __forceinline__ void da_to_f16(uint32_t x, uint32_
   }
 }
 
-template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
-  static constexpr int FMT = FMT_, TILE = 32, SUB = 16, NB = MR / 8;
+template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
+  static constexpr int FMT = FMT_, NB = MR / 8, TILE = 16 * NG;
   static constexpr bool Q8 = kv_is_8bit(FMT);
   // fp32 queries (8-bit caches): a block of eight columns is four heads' upper eleven bits and the same heads' next eleven, 2^11 times as
   // large, of the queries as of the probabilities; the products are exact, and the two sums are put together in fp32
@@ -64,8 +64,9 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
   static constexpr int EB = sizeof(E), KP = HD * EB / 64, VB = HD * EB / 8 < 16 ? HD * EB / 8 : 16, VP = HD * EB / 8 / VB, EP = VB / EB;
   static constexpr int STEPS = HD / 16;
   // values a tile ahead as well, where keys and values of a tile are not half a thread's registers
+  static constexpr uint32_t FULL = NG == 2 ? 0xffffffffu : 0xffffu;
   static constexpr bool V_AHEAD = HD * EB < 512;
-  static constexpr int WARPS = HD * EB <= 128 && MR == 8 ? 16 : 8;
+  static constexpr int WARPS = HD * EB * NG <= 128 && MR == 8 ? 16 : 8;
   static __host__ __device__ int warp_smem_floats(int) { return 0; }
 
   static constexpr float NONE = -1e30f;                  // the reference before any score: far below every one, and yet a number
@@ -151,7 +152,7 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
 
   struct Keys { uint4 x[2][KP]; float ks[2], vs[2]; };   // keys and both scales of positions g and g + 8
   struct Values { uint32_t x[4][VP * VB / 4]; };
-  // `row`: of this lane's position of a tile; `at`: 0 or 16, the tile's half
+  // `row`: of this lane's position of a tile; `at`: 0 or 16, where the group begins
   static __device__ __forceinline__ void load_keys(const KvCache &cc, int row, int at, int g, int t, Keys &k) {
 #pragma unroll
     for (int i = 0; i < 2; i++) {
@@ -185,7 +186,7 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
     // the page of this lane's position of a tile (past the end: of the last position), then its row
     int off = 0;
     auto page_of = [&](int tile) {
-      const int pos = min(tile * TILE + lane, len - 1), at = p.page_shift >= 0 ? pos >> p.page_shift : pos / cc.page_size;
+      const int pos = min(tile * TILE + lane % TILE, len - 1), at = p.page_shift >= 0 ? pos >> p.page_shift : pos / cc.page_size;
       off = pos - at * cc.page_size;
       return table[at];
     };
@@ -193,95 +194,111 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
     auto row_of = [&](int tile, int page, uint32_t &valid) {
       const bool ok = (unsigned)page < (unsigned)cc.num_pages;
       if (!ok) set_status(p.a.status, ST_BOUNDS, 63, sg.b, page);
-      valid = __ballot_sync(0xffffffffu, ok && tile * TILE + lane < len);
+      valid = __ballot_sync(0xffffffffu, ok && tile * TILE + lane % TILE < len) & FULL;
       return ((ok ? page : 0) * cc.G + head) * cc.page_size + off;
     };
     uint32_t valid;
     int tile = sg.t0, page = page_of(tile);
     load_queries(p, sg, g, t);
     int row = row_of(tile, page, valid);
-    Keys k;
-    Values v;
-    load_keys(cc, row, 0, g, t, k);
-    if constexpr (V_AHEAD) load_values(cc, row, 0, g, t, v);
+    Keys k[NG];
+    Values v[NG];
+#pragma unroll
+    for (int u = 0; u < NG; u++) load_keys(cc, row, 16 * u, g, t, k[u]);
+    if constexpr (V_AHEAD) {
+#pragma unroll
+      for (int u = 0; u < NG; u++) load_values(cc, row, 16 * u, g, t, v[u]);
+    }
     page = page_of(min(tile + 1, sg.t1 - 1));
     begin(p, g, t);
-    // halves of tiles; the last may have none in its second one
-    const int halves = (min(len, sg.t1 * TILE) - sg.t0 * TILE + SUB - 1) / SUB;
-    for (int half = 0; half < halves; half++) {
-      const int at = (half & 1) * SUB;
-      const uint32_t live = (valid >> at) & 0xffffu;
+    for (; tile < sg.t1; tile++) {
+      const uint32_t live = valid;
       const int row_here = row;
-      if (at) {                                          // the next half is of the next tile (the last tile is asked for once more)
-        tile = min(tile + 1, sg.t1 - 1);
-        row = row_of(tile, page, valid);
-        page = page_of(min(tile + 1, sg.t1 - 1));
-      }
+      row = row_of(min(tile + 1, sg.t1 - 1), page, valid);      // the last tile is asked for once more
+      page = page_of(min(tile + 2, sg.t1 - 1));
       // ---- scores
-      float s[NB][4];
+      float s[NG][NB][4], vs[NG][2], ks[NG][2];
 #pragma unroll
-      for (int n = 0; n < NB; n++) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+      for (int u = 0; u < NG; u++) {
 #pragma unroll
-      for (int j = 0; j < KP; j++) {
-        const uint32_t x[4] = {k.x[0][j].x, k.x[0][j].y, k.x[0][j].z, k.x[0][j].w}, y[4] = {k.x[1][j].x, k.x[1][j].y, k.x[1][j].z, k.x[1][j].w};
-        if constexpr (Q8) {
+        for (int n = 0; n < NB; n++) s[u][n][0] = s[u][n][1] = s[u][n][2] = s[u][n][3] = 0.0f;
 #pragma unroll
-          for (int w = 0; w < 4; w++) {
-            uint32_t a0, a1, a2, a3;
-            da_to_f16<FMT>(x[w], a0, a2);
-            da_to_f16<FMT>(y[w], a1, a3);
+        for (int j = 0; j < KP; j++) {
+          const uint4 k0 = k[u].x[0][j], k1 = k[u].x[1][j];
+          const uint32_t x[4] = {k0.x, k0.y, k0.z, k0.w}, y[4] = {k1.x, k1.y, k1.z, k1.w};
+          if constexpr (Q8) {
 #pragma unroll
-            for (int n = 0; n < NB; n++) da_mma<true>(s[n], a0, a1, a2, a3, q[n][4 * j + w][0], q[n][4 * j + w][1]);
+            for (int w = 0; w < 4; w++) {
+              uint32_t a0, a1, a2, a3;
+              da_to_f16<FMT>(x[w], a0, a2);
+              da_to_f16<FMT>(y[w], a1, a3);
+#pragma unroll
+              for (int n = 0; n < NB; n++) da_mma<true>(s[u][n], a0, a1, a2, a3, q[n][4 * j + w][0], q[n][4 * j + w][1]);
+            }
+          } else {
+#pragma unroll
+            for (int w = 0; w < 4; w += 2)
+#pragma unroll
+              for (int n = 0; n < NB; n++) da_mma<false>(s[u][n], x[w], y[w], x[w + 1], y[w + 1], q[n][2 * j + w / 2][0], q[n][2 * j + w / 2][1]);
           }
-        } else {
-#pragma unroll
-          for (int w = 0; w < 4; w += 2)
-#pragma unroll
-            for (int n = 0; n < NB; n++) da_mma<false>(s[n], x[w], y[w], x[w + 1], y[w + 1], q[n][2 * j + w / 2][0], q[n][2 * j + w / 2][1]);
         }
+#pragma unroll
+        for (int i = 0; i < 2; i++) vs[u][i] = Q8 ? k[u].vs[i] : 1.0f, ks[u][i] = Q8 ? k[u].ks[i] : 1.0f;
       }
-      if constexpr (SPLIT)                               // the other part of the same head and position is two lanes away
+#pragma unroll
+      for (int u = 0; u < NG; u++) {
+        if constexpr (V_AHEAD) load_keys(cc, row, 16 * u, g, t, k[u]);
+        else load_values(cc, row_here, 16 * u, g, t, v[u]);
+      }
+      // ---- probabilities: positions g and g + 8 of a group (elements 0, 1 and 2, 3) of two heads
+      if constexpr (SPLIT) {                             // the other part of the same head and position is two lanes away
+#pragma unroll
+        for (int u = 0; u < NG; u++)
+#pragma unroll
+          for (int n = 0; n < NB; n++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+              const float o = __shfl_xor_sync(0xffffffffu, s[u][n][e], 2);
+              s[u][n][e] = t < 2 ? fmaf(o, 4.8828125e-4f, s[u][n][e]) : fmaf(s[u][n][e], 4.8828125e-4f, o);
+            }
+      }
+#pragma unroll
+      for (int u = 0; u < NG; u++)
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) s[u][n][e] *= Q8 ? ks[u][e >> 1] * qf[n][e & 1] : qf[n][e & 1];
+      if (live != FULL) {
+#pragma unroll
+        for (int u = 0; u < NG; u++)
+#pragma unroll
+          for (int i = 0; i < 2; i++)
+            if (!((live >> (16 * u + g + 8 * i)) & 1)) {
+              vs[u][i] = 0.0f;                           // what stands there may be no number
+#pragma unroll
+              for (int n = 0; n < NB; n++) s[u][n][2 * i] = s[u][n][2 * i + 1] = -INFINITY;
+            }
+      }
+      bool over = false;
+      float x[NG][NB][4];                                // scores relative to the reference
+#pragma unroll
+      for (int u = 0; u < NG; u++) {
 #pragma unroll
         for (int n = 0; n < NB; n++)
 #pragma unroll
           for (int e = 0; e < 4; e++) {
-            const float o = __shfl_xor_sync(0xffffffffu, s[n][e], 2);
-            s[n][e] = t < 2 ? fmaf(o, 4.8828125e-4f, s[n][e]) : fmaf(s[n][e], 4.8828125e-4f, o);
+            x[u][n][e] = s[u][n][e] - r[n][e & 1];
+            over |= x[u][n][e] > 8.0f;
           }
-      float vs[2] = {1.0f, 1.0f}, ks[2] = {1.0f, 1.0f};
-      if constexpr (Q8) vs[0] = k.vs[0], vs[1] = k.vs[1], ks[0] = k.ks[0], ks[1] = k.ks[1];
-      if constexpr (V_AHEAD) load_keys(cc, row, SUB - at, g, t, k);
-      else load_values(cc, row_here, at, g, t, v);
-      // ---- probabilities: positions g and g + 8 (elements 0, 1 and 2, 3) of two heads
-      bool over = false;
-      float x[NB][4];                                    // scores relative to the reference
-#pragma unroll
-      for (int n = 0; n < NB; n++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          s[n][e] *= Q8 ? ks[e >> 1] * qf[n][e & 1] : qf[n][e & 1];
-        }
-      if (live != 0xffffu) {
-#pragma unroll
-        for (int i = 0; i < 2; i++)
-          if (!((live >> (g + 8 * i)) & 1)) {
-            vs[i] = 0.0f;                                // what stands there may be no number
-#pragma unroll
-            for (int n = 0; n < NB; n++) s[n][2 * i] = s[n][2 * i + 1] = -INFINITY;
-          }
+        if constexpr (Q8) over |= vs[u][0] > c || vs[u][1] > c;
       }
-#pragma unroll
-      for (int n = 0; n < NB; n++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          x[n][e] = s[n][e] - r[n][e & 1];
-          over |= x[n][e] > 8.0f;
-        }
-      if constexpr (Q8) over |= vs[0] > c || vs[1] > c;
       if (__any_sync(0xffffffffu, over)) {               // rare past the first tiles
         float grow = 1.0f;
         if constexpr (Q8) {
-          const float top = warp_max(fmaxf(vs[0], vs[1]));
+          float top = fmaxf(vs[0][0], vs[0][1]);
+#pragma unroll
+          for (int u = 1; u < NG; u++) top = fmaxf(top, fmaxf(vs[u][0], vs[u][1]));
+          top = warp_max(top);
           if (top > c) {                                 // with room above, so that this stays rare
             const float up = fmaxf(4.0f * top, 8e-31f);
             grow = c / up;
@@ -293,69 +310,80 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
         for (int n = 0; n < NB; n++)
 #pragma unroll
           for (int e = 0; e < 2; e++) {
-            float m = fmaxf(fmaxf(s[n][e], s[n][e + 2]), r[n][e]);
+            float m = r[n][e];
+#pragma unroll
+            for (int u = 0; u < NG; u++) m = fmaxf(m, fmaxf(s[u][n][e], s[u][n][e + 2]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
             const float f = da_ex2(r[n][e] - m);
             r[n][e] = m;
             l[n][e] *= f;
-            x[n][e] = s[n][e] - m, x[n][e + 2] = s[n][e + 2] - m;
+#pragma unroll
+            for (int u = 0; u < NG; u++) x[u][n][e] = s[u][n][e] - m, x[u][n][e + 2] = s[u][n][e + 2] - m;
 #pragma unroll
             for (int i = 0; i < STEPS; i++) o[n][i][e] *= f * grow, o[n][i][e + 2] *= f * grow;
           }
       }
-      uint32_t b[NB][2];
+      uint32_t b[NG][NB][2];
 #pragma unroll
-      for (int n = 0; n < NB; n++) {
+      for (int u = 0; u < NG; u++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-          x[n][e] = da_ex2(x[n][e]);
-          l[n][e & 1] += x[n][e];
-        }
+        for (int n = 0; n < NB; n++) {
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-          uint32_t pair;
-          if constexpr (Q8) {
-            const float w = vs[i] * rc;
-            pair = SPLIT ? part_of(x[n][2 * i] * w, x[n][2 * i + 1] * w, t >> 1) : part_of(x[n][2 * i] * w, x[n][2 * i + 1] * w, 0);
-          } else {
-            pair = pack_bf16(x[n][2 * i], x[n][2 * i + 1]);
+          for (int e = 0; e < 4; e++) {
+            x[u][n][e] = da_ex2(x[u][n][e]);
+            l[n][e & 1] += x[u][n][e];
           }
-          b[n][i] = da_transpose(pair);                  // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
-        }
-      }
-      // ---- output
-      if (live != 0xffffu) {                             // a page that is none: zero times whatever stands in page 0 is to be zero
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-          if (!((live >> (2 * t + (i & 1) + 4 * (i & 2))) & 1))
-#pragma unroll
-            for (int j = 0; j < VP * VB / 4; j++) v.x[i][j] = 0;
-      }
-#pragma unroll
-      for (int j = 0; j < VP * VB / 4; j++) {
-        if constexpr (Q8) {                              // four dimensions: two contractions' rows g and g + 8
-          uint32_t lo[2], hi[2], lo8[2], hi8[2];         // [positions 2t, 2t + 1 | 2t + 8, 2t + 9] of dimensions 0, 1 / 2, 3
 #pragma unroll
           for (int i = 0; i < 2; i++) {
-            const uint32_t a = v.x[2 * i][j], d = v.x[2 * i + 1][j];
-            da_to_f16<FMT>(__byte_perm(a, d, 0x5140), lo[i], hi[i]);
-            da_to_f16<FMT>(__byte_perm(a, d, 0x7362), lo8[i], hi8[i]);
+            uint32_t pair;
+            if constexpr (Q8) {
+              const float w = vs[u][i] * rc;
+              pair = SPLIT ? part_of(x[u][n][2 * i] * w, x[u][n][2 * i + 1] * w, t >> 1) : part_of(x[u][n][2 * i] * w, x[u][n][2 * i + 1] * w, 0);
+            } else {
+              pair = pack_bf16(x[u][n][2 * i], x[u][n][2 * i + 1]);
+            }
+            b[u][n][i] = da_transpose(pair);             // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
           }
+        }
+      // ---- output
+      if (live != FULL) {                                // a page that is none: zero times whatever stands in page 0 is to be zero
 #pragma unroll
-          for (int n = 0; n < NB; n++) {
-            da_mma<true>(o[n][2 * j], lo[0], hi[0], lo[1], hi[1], b[n][0], b[n][1]);
-            da_mma<true>(o[n][2 * j + 1], lo8[0], hi8[0], lo8[1], hi8[1], b[n][0], b[n][1]);
+        for (int u = 0; u < NG; u++)
+#pragma unroll
+          for (int i = 0; i < 4; i++)
+            if (!((live >> (16 * u + 2 * t + (i & 1) + 4 * (i & 2))) & 1))
+#pragma unroll
+              for (int j = 0; j < VP * VB / 4; j++) v[u].x[i][j] = 0;
+      }
+#pragma unroll
+      for (int u = 0; u < NG; u++) {
+#pragma unroll
+        for (int j = 0; j < VP * VB / 4; j++) {
+          const uint32_t v0 = v[u].x[0][j], v1 = v[u].x[1][j], v2 = v[u].x[2][j], v3 = v[u].x[3][j];
+          if constexpr (Q8) {                            // four dimensions: two contractions' rows g and g + 8
+            uint32_t lo[2], hi[2], lo8[2], hi8[2];       // [positions 2t, 2t + 1 | 2t + 8, 2t + 9] of dimensions 0, 1 / 2, 3
+            da_to_f16<FMT>(__byte_perm(v0, v1, 0x5140), lo[0], hi[0]);
+            da_to_f16<FMT>(__byte_perm(v0, v1, 0x7362), lo8[0], hi8[0]);
+            da_to_f16<FMT>(__byte_perm(v2, v3, 0x5140), lo[1], hi[1]);
+            da_to_f16<FMT>(__byte_perm(v2, v3, 0x7362), lo8[1], hi8[1]);
+#pragma unroll
+            for (int n = 0; n < NB; n++) {
+              da_mma<true>(o[n][2 * j], lo[0], hi[0], lo[1], hi[1], b[u][n][0], b[u][n][1]);
+              da_mma<true>(o[n][2 * j + 1], lo8[0], hi8[0], lo8[1], hi8[1], b[u][n][0], b[u][n][1]);
+            }
+          } else {
+            const uint32_t a0 = __byte_perm(v0, v1, 0x5410), a1 = __byte_perm(v0, v1, 0x7632), a2 = __byte_perm(v2, v3, 0x5410), a3 = __byte_perm(v2, v3, 0x7632);
+#pragma unroll
+            for (int n = 0; n < NB; n++) da_mma<false>(o[n][j], a0, a1, a2, a3, b[u][n][0], b[u][n][1]);
           }
-        } else {
-          const uint32_t a0 = __byte_perm(v.x[0][j], v.x[1][j], 0x5410), a1 = __byte_perm(v.x[0][j], v.x[1][j], 0x7632);
-          const uint32_t a2 = __byte_perm(v.x[2][j], v.x[3][j], 0x5410), a3 = __byte_perm(v.x[2][j], v.x[3][j], 0x7632);
-#pragma unroll
-          for (int n = 0; n < NB; n++) da_mma<false>(o[n][j], a0, a1, a2, a3, b[n][0], b[n][1]);
         }
       }
-      if constexpr (V_AHEAD) load_values(cc, row, SUB - at, g, t, v);
-      else load_keys(cc, row, SUB - at, g, t, k);
+#pragma unroll
+      for (int u = 0; u < NG; u++) {
+        if constexpr (V_AHEAD) load_values(cc, row, 16 * u, g, t, v[u]);
+        else load_keys(cc, row, 16 * u, g, t, k[u]);
+      }
     }
 #pragma unroll
     for (int n = 0; n < NB; n++)
@@ -363,7 +391,7 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
       for (int e = 0; e < 2; e++) {
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
-        if constexpr (Q8)
+        if constexpr (Q8) {
 #pragma unroll
           for (int i = 0; i < STEPS; i++) {
             if constexpr (SPLIT) {
@@ -372,6 +400,7 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
             }
             o[n][i][e] *= c * 0.015625f, o[n][i][e + 2] *= c * 0.015625f;
           }
+        }
       }
   }
 
@@ -395,23 +424,27 @@ template <int FMT_, int HD, int MR, bool SPLIT = false> struct MmaBody {
   }
 };
 
-template <int FMT, int HD> static cudaError_t mma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
-  if constexpr (kv_is_8bit(FMT))
-    if (p.q_f32) {
-      if constexpr (HD < 256)
-        if (p.heads > 4) return launch<MmaBody<FMT, HD, 16, true>>(p, ctas, s);
-      return launch<MmaBody<FMT, HD, 8, true>>(p, ctas, s);
-    }
+// NG groups of 16 positions a tile.  A warp waits for a tile's keys and for its values once each, so with long runs a tile of 4 KB of 8-bit keys
+// or values is better read by 8 warps; 16 warps with half of it lose less where runs are short and every (sequence, KV head) begins with a wait
+// of its own.  us with 16 / 8 warps, 8 KV heads of 128 in e4m3 or int8: one sequence of 613 positions 12.0 / 10.7, 4 of 1000 to 8000 19.3 / 17.2, 32 of
+// 100 to 400 13.1 / 11.7, 16 of 8192 56.2 / 55.9, 64 of 256 to 2048 42.5 / 48.3; 40 KV heads, 64 of 10 to 100 26.6 / 30.1: up to two of them a CTA 8 warps.
+template <int FMT, int HD, bool SPLIT> static cudaError_t mma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
+  constexpr int EB = kv_is_8bit(FMT) ? 1 : 2, NG = HD * EB <= 128 ? 2 : 1, ONE = SPLIT ? 4 : 8;
   if constexpr (HD < 256)
-    if (p.heads > 8) return launch<MmaBody<FMT, HD, 16>>(p, ctas, s);
-  return launch<MmaBody<FMT, HD, 8>>(p, ctas, s);
+    if (p.heads > ONE) return launch<MmaBody<FMT, HD, 16, SPLIT, NG>>(p, ctas, s);
+  if constexpr (HD * EB == 128 && EB == 1)
+    if (p.segs > 2 * ctas) return launch<MmaBody<FMT, HD, 8, SPLIT, 1>>(p, ctas, s);
+  return launch<MmaBody<FMT, HD, 8, SPLIT, NG>>(p, ctas, s);
 }
-template <int FMT> static cudaError_t mma_by_hd(const DaArgs &p, int ctas, cudaStream_t s) {
-  return p.a.cache.hd == 64 ? mma_by_heads<FMT, 64>(p, ctas, s) : p.a.cache.hd == 128 ? mma_by_heads<FMT, 128>(p, ctas, s) : mma_by_heads<FMT, 256>(p, ctas, s);
+template <int FMT, bool SPLIT> static cudaError_t mma_by_hd(const DaArgs &p, int ctas, cudaStream_t s) {
+  return p.a.cache.hd == 64 ? mma_by_heads<FMT, 64, SPLIT>(p, ctas, s) : p.a.cache.hd == 128 ? mma_by_heads<FMT, 128, SPLIT>(p, ctas, s)
+                                                                                            : mma_by_heads<FMT, 256, SPLIT>(p, ctas, s);
 }
 
 cudaError_t launch_decode_mma(const DaArgs &p, int fmt, int ctas, cudaStream_t s) {
-  return fmt == KV_BF16 ? mma_by_hd<KV_BF16>(p, ctas, s) : fmt == KV_E4M3 ? mma_by_hd<KV_E4M3>(p, ctas, s) : mma_by_hd<KV_INT8>(p, ctas, s);
+  if (fmt == KV_BF16) return mma_by_hd<KV_BF16, false>(p, ctas, s);
+  if (fmt == KV_E4M3) return p.q_f32 ? mma_by_hd<KV_E4M3, true>(p, ctas, s) : mma_by_hd<KV_E4M3, false>(p, ctas, s);
+  return p.q_f32 ? mma_by_hd<KV_INT8, true>(p, ctas, s) : mma_by_hd<KV_INT8, false>(p, ctas, s);
 }
 
 }  // namespace spec
