@@ -140,6 +140,22 @@ def test_many_sequences(dtype, fmt):
 
 
 @pytest.mark.parametrize("dtype,fmt", KINDS)
+@pytest.mark.parametrize("B,H,G,hd,ps,least,most", [(60, 32, 8, 128, 16, 0, 300),        # several (sequence, KV head)s a CTA, dealt out evenly
+                                                    (20, 24, 8, 128, 16, 90, 100),       # whole ones, one or two a CTA
+                                                    (33, 40, 40, 128, 16, 1, 40),        # many short ones, whole
+                                                    (33, 64, 2, 128, 64, 200, 900),      # chunks of heads
+                                                    (2, 16, 1, 64, 32, 3000, 5000),      # one of them shared by all CTAs, in two levels of joins
+                                                    (3, 4, 1, 256, 16, 2000, 2500)])
+def test_ways_of_dealing_out_the_work(dtype, fmt, B, H, G, hd, ps, least, most):
+    g = torch.Generator(device="cuda").manual_seed(B * hd)
+    lens = torch.randint(least, most + 1, (B,), generator=g, device="cuda").tolist()
+    table, pages = table_for(g, lens, ps)
+    cache = pools(g, fmt, pages, G, ps, hd)
+    spoil(cache, table, lens, ps)
+    check(torch.randn(B, H, hd, generator=g, device="cuda").to(DT[dtype]), cache, table, lens, ps)
+
+
+@pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("hd", [128, 80])
 def test_scales_queries_and_scores_of_very_different_sizes(dtype, fmt, hd):
     """Values whose scales differ by 2^16 from token to token, queries of 2^-60 and 2^40, a scale of its own, scores that rise with the

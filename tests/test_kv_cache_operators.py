@@ -195,6 +195,60 @@ def test_append_and_read(dtype, fmt, T, H, G, hd, rot, layout, ps, seqs):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "e4m3"), ("bf16", "int8"), ("fp32", "fp32")])
+def test_long_prompt(dtype, fmt):
+    """Blocks of several tokens and several rounds of heads, and reading back by blocks of several rows: as the definition, token by token."""
+    T, H, G, hd, ps = 3001, 8, 4, 128, 16
+    g = torch.Generator().manual_seed(8)
+    cache = make_cache(g, fmt, 200, G, ps, hd, 1, 190)
+    qkv = torch.randn(T, H + 2 * G, hd, generator=g).to(DT[dtype])
+    freq, _ = sb.rope_frequencies(hd, 5e5, device="cpu")
+    seq, pos = torch.zeros(T, dtype=torch.int32).cuda(), torch.arange(T, dtype=torch.int32).cuda()
+    dev = qkv.cuda()
+    sc = {"k_scale": cache["k_scale"], "v_scale": cache["v_scale"]}
+    args = cache["k_pool"], cache["v_pool"], cache["page_table"], seq, pos
+    q = sb.kv_append(dev[:, H: H + G], dev[:, H + G:], *args, **sc, q=dev[:, :H], inv_freq=freq.cuda())
+    k, v = sb.kv_read(*args, **sc, dtype=torch.float32)
+    x = qkv.double()
+    want = turned(x[:, : H + G], pos.cpu(), freq, "half", 1.0)
+    err = turn_error(x[:, : H + G], freq, "half", 1.0)
+    assert ((q.cpu().double() - want[:, :H]).abs() <= err[:, :H] + (want[:, :H].abs() * 2.0 ** -8 if dtype == "bf16" else 0)).all()
+    for got, rows, e in ((k, want[:, H:], err[:, H:]), (v, x[:, H + G:], 0.0)):
+        if fmt in TOP:
+            scale = (rows.abs().amax(-1, keepdim=True) / TOP[fmt])
+            e = e + code_error(rows / scale, fmt) * scale * (1 + 2.0 ** -20)
+        assert ((got.cpu().double() - rows).abs() <= e + rows.abs() * 2.0 ** -20).all()
+
+
+@gpu
+def test_many_tokens_of_few_heads():
+    """Blocks of sixteen tokens with a few heads each, both types, and blocks that a token's heads do not fill."""
+    for T, H, hd, dtype, layout in ((20003, 5, 64, "fp32", "half"), (30001, 3, 64, "bf16", "interleaved"), (901, 1, 128, "bf16", "half"), (9000, 1, 16, "fp32", "half")):
+        g = torch.Generator().manual_seed(T)
+        x = torch.randn(T, H, hd, generator=g).to(DT[dtype])
+        pos = torch.randint(0, 200000, (T,), generator=g, dtype=torch.int32)
+        freq, _ = sb.rope_frequencies(hd, 1e4, device="cpu")
+        want = turned(x.double(), pos, freq, layout, 1.0)
+        got = sb.rotary(x.cuda(), pos.cuda(), freq.cuda(), layout=layout)
+        assert ((got.cpu().double() - want).abs() <= turn_error(x.double(), freq, layout, 1.0) + (want.abs() * 2.0 ** -8 if dtype == "bf16" else 0)).all()
+
+
+def test_tensors_that_are_not_on_the_gpu_are_refused():
+    """The C++ part of the binding loads and checks without a device."""
+    x, pos = torch.zeros(2, 4, 64), torch.zeros(2, dtype=torch.int32)
+    freq, _ = sb.rope_frequencies(64, 1e4, device="cpu")
+    pool, table = torch.zeros(4, 2, 16, 64), torch.zeros(1, 4, dtype=torch.int32)
+    for call in (lambda: sb.rotary(x, pos, freq), lambda: sb.rotary_backward(x, pos, freq), lambda: sb.kv_append(x[:, :2], x[:, :2], pool, pool, table, pos, pos),
+                 lambda: sb.kv_read(pool, pool, table, pos, pos), lambda: sb.decode_attention(x, pool, pool, table, pos)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        sb.rotary(None, pos, freq)
+    with pytest.raises(TypeError):
+        sb.decode_attention(x, pool.half(), pool.half(), table, pos)
+
+
+@gpu
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("hd", [64, 80, 128])
 def test_rows_with_infinities_and_nan_read_back_as_nan(fmt, hd):
