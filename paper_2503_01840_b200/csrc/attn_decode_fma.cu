@@ -1,4 +1,6 @@
-// Single-token attention on plain FMAs: fp32 queries, and head sizes that the tensor-core body is not made for.
+// Single-token attention on plain FMAs: fp32 caches, and head sizes that the tensor-core body is not made for.  16 sequences of 4096 positions,
+// 8 KV heads of 128 for 32 query heads in fp32: 114 us, 4.7 TB/s (231 with a lane a position's keys, whose loads touch 32 lines each, and loads
+// that stand behind conditions).
 #include "attn_decode_kernel.cuh"
 
 namespace spec {

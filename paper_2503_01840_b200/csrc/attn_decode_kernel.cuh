@@ -95,9 +95,9 @@ __device__ __forceinline__ void da_store(void *out, bool f32, size_t at, float4 
   else *(uint2 *)((bf16 *)out + at) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
 }
 
-// A warp joins one head of the states (O [heads][hd], then (max, sum) [heads]) whose bits are set in `run`, `stride` floats apart, the first `skew`
-// further on, (max, sum) `stats` into a state: into its rows of the output and of lse, or as a state into `to`.  One piece of code for all joins, kept short: a call runs it once or twice, and
-// fetching cold instructions takes longer than what they do.
+// A warp joins one head of the states (O [heads][hd], then, `stats` floats on, (max, sum) [heads]) whose bits are set in `run`, `stride` floats apart,
+// the first `skew` further on: into its rows of the output and of lse, or as a state into `to`.  One piece of code for all joins, kept short: a
+// call runs it once or twice, and fetching cold instructions takes longer than what they do.
 // (Its arguments are values: fields of the kernel's parameters behind a pointer would be loads, from the L2 after the fence.)
 static __device__ __noinline__ void da_join_head(const float *states, int stride, int skew, uint32_t run, int stats, int h, int hd, float *to, void *out, bool f32, float *lse) {
   const int lane = threadIdx.x & 31;

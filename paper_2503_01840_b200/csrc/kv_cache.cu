@@ -259,7 +259,8 @@ cudaError_t launch_rope_append(const RopeAppend &a, int dtype, int fmt, cudaStre
 
 // ---------------------------------------------------------------- reading back
 // Row r of the output is position kvpos[r] of sequence seq[r], zeros where there is none.  A thread takes eight elements, so that a
-// warp's stores of bf16 are whole lines; a block some rows, whose places in the pool are looked up once.
+// warp's stores of bf16 are whole lines; a block some rows, whose places in the pool are looked up once.  Bytes bound it: 16384 tokens
+// of 8 heads of 128 from e4m3 22 us (4.6 TB/s), 8000 of 40 heads from int8 50 us (4.9 TB/s).
 constexpr int READ_MAX_ROWS = 64;      // 256 / the least items a row (4)
 struct ReadGrid { int rows, items; uint32_t by_items; };                 // rows of a block, eights of a row (keys, then values)
 
