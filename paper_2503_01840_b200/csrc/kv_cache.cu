@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_any_kernel(RopeAppen
     const int pos = a.pos[t];
     for (int i = threadIdx.x; i < half; i += ROPE_THREADS) cs[i] = rope_angle(a.rope, pos, i);
   }
-  __shared__ long long row0;
+  __shared__ int row0;
   if (threadIdx.x == 0) row0 = a.k.p ? kv_row(a.cache, a.seq[t], a.kvpos[t], a.status, t) : -1;
   __syncthreads();
   const int G = a.k.p ? a.cache.G : 0;
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_any_kernel(RopeAppen
         if (lane + j * 32 < hd) o[lane + j * 32] = from_f32<T>(y[j]);
       continue;
     }
-    const long long row = row0 + (long long)h * a.cache.page_size;
+    const size_t row = (uint32_t)(row0 + h * a.cache.page_size);
     E *o = (E *)(kind == 1 ? a.cache.k : a.cache.v) + row * hd;
     if constexpr (kv_is_8bit(FMT)) {
       const float scale = kv_scale<FMT>(__reduce_max_sync(0xffffffffu, top)), inv = 1.0f / scale;
@@ -81,7 +81,11 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_any_kernel(RopeAppen
 // A head is shared by LH lanes, a power of two, each with two 16-byte pieces: the two whose elements pair up in the half layout,
 // neighbours in the interleaved one and past the rotated dimensions.  So a pair never leaves a lane, and a head's largest magnitude is LH
 // lanes' exchange.  A block takes some heads of some tokens; their cosines and sines are formed once, in shared memory.
-// Bytes bound it: a thread asks for its first U heads before it forms the angles.
+// Bytes bound it: a thread asks for its first U heads before it forms the angles.  Measured: 16384 tokens of 40 heads of 128 in bf16 57 us
+// (5.9 TB/s, 92 % of a copy's rate), 4096 of 80 heads in fp32 53 us (6.3 TB/s); with keys and values to e4m3 as well, 16384 of 32 + 8 + 8 heads,
+// 68 us (5.4 TB/s): the look-ups of the cache rows stand before a block's first store.  One head under way a thread and six blocks an SM; with two and five
+// 61 / 53 / 72 us, one and eight 57 / 54 / 82; with two rounds a block instead of six 64 / 53 / 94, eight 62 / 53 / 74; one wave of blocks that walk tokens with
+// copies to shared memory four heads ahead 59 / 81 / 79; with 64-bit offsets 59 / 54 / 74.
 __device__ __forceinline__ void unpack_piece(uint4 u, float (&y)[4]) {
   y[0] = __uint_as_float(u.x), y[1] = __uint_as_float(u.y), y[2] = __uint_as_float(u.z), y[3] = __uint_as_float(u.w);
 }
@@ -99,18 +103,27 @@ __device__ __forceinline__ uint4 pack_piece(const float (&y)[8]) {
 struct RopeGrid {
   int per_block, heads;         // tokens and heads of a block
   int lh_shift;                 // log2 of LH
-  uint32_t by_heads;            // ceil(2^32 / heads): quotients of the small numbers here by a product
+  uint32_t by_heads, by_half;   // ceil(2^32 / heads), / pairs: quotients of the small numbers here by a product
+  int q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;      // strides: within a block offsets are 32-bit, which halves their instructions
 };
 constexpr int ROPE_MAX_TOKENS = 16;
 
+template <int N> __device__ __forceinline__ void turn_neighbours(float (&y)[N], const float (&c)[N / 2], const float (&s)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const float p = y[i], q = y[i + 1];
+    y[i] = fmaf(p, c[i / 2], -(q * s[i / 2])), y[i + 1] = fmaf(q, c[i / 2], p * s[i / 2]);
+  }
+}
+
 template <typename T, int FMT, bool INTER, int U>
-__global__ void __launch_bounds__(ROPE_THREADS, 5) rope_append_kernel(RopeAppend a, RopeGrid gr) {
+__global__ void __launch_bounds__(ROPE_THREADS, 6) rope_append_kernel(const __grid_constant__ RopeAppend a, const __grid_constant__ RopeGrid gr) {
   pdl_wait();
   pdl_trigger();
   typedef typename KvElem<FMT>::type E;
   constexpr int VE = 16 / sizeof(T);
   extern __shared__ __align__(16) float trig[];          // [tokens][cos half | sin half]
-  __shared__ long long rows[ROPE_MAX_TOKENS];
+  __shared__ int rows[ROPE_MAX_TOKENS];
   const int tid = threadIdx.x, hd = a.hd, half = a.rope.half, G = a.k.p ? a.cache.G : 0;
   const int t0 = blockIdx.x * gr.per_block, nt = min(gr.per_block, a.tokens - t0), h0 = blockIdx.y * gr.heads, nh = min(gr.heads, a.H + 2 * G - h0);
   const int l = tid & ((1 << gr.lh_shift) - 1), slot = tid >> gr.lh_shift, step = ROPE_THREADS >> gr.lh_shift;
@@ -119,58 +132,46 @@ __global__ void __launch_bounds__(ROPE_THREADS, 5) rope_append_kernel(RopeAppend
   const int d0 = paired ? l * VE : 2 * l * VE, d1 = paired ? half + l * VE : d0 + VE;
   const bool turn0 = INTER ? d0 < 2 * half : paired, turn1 = INTER ? d1 < 2 * half : paired;
 
+  const T *const q = (const T *)a.q.p + (long long)t0 * a.q.ts, *const k = (const T *)a.k.p + (long long)t0 * a.k.ts, *const v = (const T *)a.v.p + (long long)t0 * a.v.ts;
+  T *const q_out = (T *)a.q_out + (long long)t0 * a.qo_ts;
   uint4 x[U][2];
-  auto source = [&](int j, int &t, int &h) -> const T * {                // head j of the block's; null: there is none
-    t = (int)__umulhi((uint32_t)j, gr.by_heads);
-    h = h0 + j - t * gr.heads;
-    if (t >= nt || h - h0 >= nh) return nullptr;
-    const HeadView &v = h < a.H ? a.q : h < a.H + G ? a.k : a.v;
-    return (const T *)v.p + (long long)(t0 + t) * v.ts + (long long)(h < a.H ? h : h < a.H + G ? h - a.H : h - a.H - G) * v.hs;
-  };
-  const int most = gr.per_block * gr.heads;
+  int of_t[U], of_h[U];                                  // token and head; token -1: there is none
   auto load = [&](int j0) {
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      int t, h;
-      const int j = j0 + u * step;
-      const T *p = j < most ? source(j, t, h) : nullptr;
-      if (p) x[u][0] = *(const uint4 *)(p + d0), x[u][1] = *(const uint4 *)(p + d1);
+      const int j = j0 + u * step, t = (int)__umulhi((uint32_t)j, gr.by_heads), i = j - t * gr.heads, h = h0 + i;
+      of_t[u] = -1, of_h[u] = h;
+      if (t >= nt || i >= nh) continue;
+      of_t[u] = t;
+      const T *p = h < a.H ? q + (t * gr.q_ts + h * gr.q_hs) : h < a.H + G ? k + (t * gr.k_ts + (h - a.H) * gr.k_hs) : v + (t * gr.v_ts + (h - a.H - G) * gr.v_hs);
+      x[u][0] = *(const uint4 *)(p + d0), x[u][1] = *(const uint4 *)(p + d1);
     }
   };
   load(slot);
   for (int i = tid; i < nt * half; i += ROPE_THREADS) {
-    const int t = i / half, pair = i - t * half;
+    const int t = (int)__umulhi((uint32_t)i, gr.by_half), pair = i - t * half;
     const float2 c = rope_angle(a.rope, a.pos[t0 + t], pair);
     trig[t * 2 * half + pair] = c.x;
     trig[t * 2 * half + half + pair] = c.y;
   }
   if (G && tid < nt) rows[tid] = kv_row(a.cache, a.seq[t0 + tid], a.kvpos[t0 + tid], a.status, t0 + tid);
   __syncthreads();
+  const int most = nt * gr.heads;
   for (int j0 = slot; j0 < most; j0 += U * step) {
     if (j0 != slot) load(j0);
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      int t, h;
-      const int j = j0 + u * step;
-      if (j >= most || !source(j, t, h)) continue;
+      const int t = of_t[u], h = of_h[u];
+      if (t < 0) continue;
       float y0[VE], y1[VE];
       unpack_piece(x[u][0], y0);
       unpack_piece(x[u][1], y1);
       if (h < a.H + G) {
         const float *cs = trig + t * 2 * half, *sn = cs + half;
         if constexpr (INTER) {
-          if (turn0)
-#pragma unroll
-            for (int i = 0; i < VE; i += 2) {
-              const float c = cs[(d0 + i) / 2], s = sn[(d0 + i) / 2], p = y0[i], q = y0[i + 1];
-              y0[i] = fmaf(p, c, -(q * s)), y0[i + 1] = fmaf(q, c, p * s);
-            }
-          if (turn1)
-#pragma unroll
-            for (int i = 0; i < VE; i += 2) {
-              const float c = cs[(d1 + i) / 2], s = sn[(d1 + i) / 2], p = y1[i], q = y1[i + 1];
-              y1[i] = fmaf(p, c, -(q * s)), y1[i + 1] = fmaf(q, c, p * s);
-            }
+          struct alignas(2 * VE) Some { float f[VE / 2]; };
+          if (turn0) turn_neighbours(y0, (*(const Some *)(cs + d0 / 2)).f, (*(const Some *)(sn + d0 / 2)).f);
+          if (turn1) turn_neighbours(y1, (*(const Some *)(cs + d1 / 2)).f, (*(const Some *)(sn + d1 / 2)).f);
         } else if (paired) {
 #pragma unroll
           for (int i = 0; i < VE; i += 4) {
@@ -185,14 +186,14 @@ __global__ void __launch_bounds__(ROPE_THREADS, 5) rope_append_kernel(RopeAppend
         }
       }
       if (h < a.H) {
-        T *o = (T *)a.q_out + (long long)(t0 + t) * a.qo_ts + (long long)h * a.qo_hs;
+        T *o = q_out + (t * gr.o_ts + h * gr.o_hs);
         *(uint4 *)(o + d0) = pack_piece(y0);
         *(uint4 *)(o + d1) = pack_piece(y1);
         continue;
       }
       if (rows[t] < 0) continue;                         // all lanes of a head alike
       const bool key = h < a.H + G;
-      const long long row = rows[t] + (long long)(key ? h - a.H : h - a.H - G) * a.cache.page_size;
+      const size_t row = (uint32_t)(rows[t] + (key ? h - a.H : h - a.H - G) * a.cache.page_size);
       E *o = (E *)(key ? a.cache.k : a.cache.v) + row * hd;
       if constexpr (kv_is_8bit(FMT)) {
         uint32_t top = 0;                                // bits of the largest magnitude: NaN counts as the largest of all
@@ -219,7 +220,9 @@ __global__ void __launch_bounds__(ROPE_THREADS, 5) rope_append_kernel(RopeAppend
   }
 }
 
-static bool whole_pieces(const void *p, long long ts, long long hs, size_t e) {
+static bool whole_pieces(const void *p, long long ts, long long hs, size_t e) {      // and strides whose offsets in a block stay below 2^31
+  const long long most = 1 << 26, heads = 1 << 18;
+  if (ts > most || ts < -most || hs > heads || hs < -heads) return false;
   return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ts * (long long)e) | (uintptr_t)(hs * (long long)e)) & 15) == 0;
 }
 
@@ -233,7 +236,7 @@ template <typename T, int FMT> static cudaError_t rope_append(const RopeAppend &
   RopeGrid gr;
   gr.lh_shift = __builtin_ctz(lh);
   const int step = ROPE_THREADS / lh;                    // heads of a round of the block
-  constexpr int U = 2;
+  constexpr int U = 1;
   // few tokens: a round's heads a block (of several tokens where one has fewer heads than that), so that no thread has a second round to wait
   // for; many: about six rounds a block
   const long long rounds = ((long long)a.tokens * all + step - 1) / step;
@@ -244,6 +247,9 @@ template <typename T, int FMT> static cudaError_t rope_append(const RopeAppend &
     gr.heads = all;
     gr.per_block = max(1, min(ROPE_MAX_TOKENS, 6 * step / all));
   }
+  gr.by_half = a.rope.half > 1 ? (uint32_t)((0x100000000ull + a.rope.half - 1) / a.rope.half) : 0;
+  gr.q_ts = (int)a.q.ts, gr.q_hs = (int)a.q.hs, gr.k_ts = (int)a.k.ts, gr.k_hs = (int)a.k.hs, gr.v_ts = (int)a.v.ts, gr.v_hs = (int)a.v.hs;
+  gr.o_ts = (int)a.qo_ts, gr.o_hs = (int)a.qo_hs;
   gr.by_heads = gr.heads == 1 ? 0xffffffffu : (uint32_t)((0x100000000ull + gr.heads - 1) / gr.heads);
   if (gr.heads == 1 && gr.per_block > 1) gr.per_block = 1;
   const dim3 grid((a.tokens + gr.per_block - 1) / gr.per_block, (all + gr.heads - 1) / gr.heads);
@@ -260,23 +266,25 @@ cudaError_t launch_rope_append(const RopeAppend &a, int dtype, int fmt, cudaStre
 // ---------------------------------------------------------------- reading back
 // Row r of the output is position kvpos[r] of sequence seq[r], zeros where there is none.  A thread takes eight elements, so that a
 // warp's stores of bf16 are whole lines; a block some rows, whose places in the pool are looked up once.  Bytes bound it: 16384 tokens
-// of 8 heads of 128 from e4m3 22 us (4.6 TB/s), 8000 of 40 heads from int8 50 us (4.9 TB/s).
+// of 8 heads of 128 from e4m3 21 us (4.8 TB/s), 8000 of 40 heads from int8 49 us (5.1 TB/s).  Two, four and eight items a thread under way, with as many
+// blocks an SM as that leaves room for: 21 / 23 / 24 us.
 constexpr int READ_MAX_ROWS = 64;      // 256 / the least items a row (4)
-struct ReadGrid { int rows, items; uint32_t by_items; };                 // rows of a block, eights of a row (keys, then values)
+struct ReadGrid { int rows, items; uint32_t by_items, by_hd8; };         // rows of a block, eights of a row (keys, then values); ceil(2^32 / items), / a head's eights
 
 template <int FMT, typename T>
-__global__ void __launch_bounds__(256) kv_read_kernel(KvRead a, ReadGrid gr) {
+__global__ void __launch_bounds__(256, 8) kv_read_kernel(KvRead a, ReadGrid gr) {
   pdl_wait();
   pdl_trigger();
   typedef typename KvElem<FMT>::type E;
   const int hd8 = a.cache.hd / 8, r0 = blockIdx.x * gr.rows, nr = min(gr.rows, a.rows - r0);
-  __shared__ long long at[READ_MAX_ROWS];
+  __shared__ int at[READ_MAX_ROWS];
   if (threadIdx.x < nr) at[threadIdx.x] = kv_row(a.cache, a.seq[r0 + threadIdx.x], a.kvpos[r0 + threadIdx.x], a.status, r0 + threadIdx.x);
   __syncthreads();
   const int half = gr.items / 2, n = nr * gr.items;
+  T *const k_out = (T *)a.k_out + (size_t)r0 * half * 8, *const v_out = (T *)a.v_out + (size_t)r0 * half * 8;
   typedef typename Four<FMT>::raw Raw;
   struct alignas(sizeof(E) == 4 ? 16 : 8 * sizeof(E)) Eight { Raw e[2]; };
-  constexpr int U = 4;                                   // in flight
+  constexpr int U = 2;                                   // in flight
   for (int i0 = threadIdx.x; i0 < n; i0 += U * 256) {
     Eight x[U];
     float sc[U];
@@ -284,11 +292,12 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRead a, ReadGrid gr) {
 #pragma unroll
     for (int u = 0; u < U; u++) {
       const int i = i0 + u * 256;
-      const int r = (int)__umulhi((uint32_t)i, gr.by_items), e = i - r * gr.items, kv = e >= half, w = e - kv * half, h = w / hd8, d = (w - h * hd8) * 8;
+      const int r = (int)__umulhi((uint32_t)i, gr.by_items), e = i - r * gr.items, kv = e >= half, w = e - kv * half;
+      const int h = (int)__umulhi((uint32_t)w, gr.by_hd8), d = (w - h * hd8) * 8;
       to[u] = nullptr;
       if (i >= n) continue;
-      to[u] = (T *)(kv ? a.v_out : a.k_out) + ((size_t)(r0 + r) * half + w) * 8;
-      const long long row = at[r] + (long long)h * a.cache.page_size;
+      to[u] = (kv ? v_out : k_out) + (uint32_t)(r * half + w) * 8;
+      const size_t row = (uint32_t)(at[r] + h * a.cache.page_size);
       x[u] = Eight{};
       sc[u] = 0.0f;
       if (at[r] < 0) continue;
@@ -316,9 +325,11 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRead a, ReadGrid gr) {
 template <int FMT> static cudaError_t kv_read(const KvRead &a, int out_dtype, cudaStream_t s) {
   ReadGrid gr;
   gr.items = 2 * a.cache.G * (a.cache.hd / 8);
-  // one wave of blocks (five an SM) where there is enough to do: a block's look-ups come before everything else it does
-  gr.rows = max(max(1, 256 / gr.items), min(READ_MAX_ROWS, (a.rows + 739) / 740));
+  // one wave of blocks (eight an SM) where there is enough to do, and about 4096 items each where there is more: a block's look-ups come before
+  // everything else it does
+  gr.rows = max(max(1, 256 / gr.items), min(min(READ_MAX_ROWS, (a.rows + 1183) / 1184), max(1, 4096 / gr.items)));
   gr.by_items = (uint32_t)((0x100000000ull + gr.items - 1) / gr.items);
+  gr.by_hd8 = (uint32_t)((0x100000000ull + a.cache.hd / 8 - 1) / (a.cache.hd / 8));
   const dim3 grid((a.rows + gr.rows - 1) / gr.rows);
   if (out_dtype == KV_F32) return launch_k(kv_read_kernel<FMT, float>, grid, dim3(256), 0, s, a, gr);
   return launch_k(kv_read_kernel<FMT, bf16>, grid, dim3(256), 0, s, a, gr);

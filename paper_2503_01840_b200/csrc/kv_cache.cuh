@@ -60,8 +60,9 @@ struct KvRead {
 };
 cudaError_t launch_kv_read(const KvRead &a, int fmt, int out_dtype, cudaStream_t s);
 
-// Row (of hd elements) of a cache position's first head, -1 where there is none; the heads follow page_size rows apart.
-__device__ __forceinline__ long long kv_row(const KvCache &c, int seq, int pos, int32_t *status, int row) {
+// Row (of hd elements; a pool has fewer than 2^31) of a cache position's first head, -1 where there is none; the heads follow page_size
+// rows apart.
+__device__ __forceinline__ int kv_row(const KvCache &c, int seq, int pos, int32_t *status, int row) {
   if (seq < 0) return -1;
   const int at = pos / c.page_size;
   if (seq >= c.n_seq || pos < 0 || at >= c.pages_per_seq) {
@@ -73,7 +74,7 @@ __device__ __forceinline__ long long kv_row(const KvCache &c, int seq, int pos, 
     set_status(status, ST_BOUNDS, 61, row, page);
     return -1;
   }
-  return (long long)page * c.G * c.page_size + (pos - at * c.page_size);
+  return page * c.G * c.page_size + (pos - at * c.page_size);
 }
 
 // Cosine and sine of position * frequency.  The angle is formed in 64 bits and brought to less than half a turn there: at position

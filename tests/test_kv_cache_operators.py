@@ -233,6 +233,23 @@ def test_many_tokens_of_few_heads():
         assert ((got.cpu().double() - want).abs() <= turn_error(x.double(), freq, layout, 1.0) + (want.abs() * 2.0 ** -8 if dtype == "bf16" else 0)).all()
 
 
+@gpu
+@pytest.mark.parametrize("ts,hs", [(1 << 26, 64), ((1 << 26) + 8, 64), (128, 1 << 18), (64, (1 << 18) + 8)])
+def test_long_strides(ts, hs):
+    """Token and head strides at both sides of what 32-bit offsets in a block allow."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    T, H, hd = (17, 2, 64) if ts > 1 << 20 else (2, 40, 64)
+    buf = torch.zeros((T - 1) * ts + (H - 1) * hs + hd, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((T, H, hd), (ts, hs, 1))
+    x.copy_(torch.randn(T, H, hd, generator=g, device="cuda"))
+    pos = torch.arange(1000, 1000 + T, dtype=torch.int32, device="cuda")
+    freq, _ = sb.rope_frequencies(hd, 1e4)
+    want = sb.rotary(x.contiguous(), pos, freq)
+    assert torch.equal(sb.rotary(x, pos, freq), want)
+    out = torch.zeros_like(buf).as_strided((T, H, hd), (ts, hs, 1))
+    assert torch.equal(sb.rotary(x, pos, freq, out=out), want)
+
+
 def test_tensors_that_are_not_on_the_gpu_are_refused():
     """The C++ part of the binding loads and checks without a device."""
     x, pos = torch.zeros(2, 4, 64), torch.zeros(2, dtype=torch.int32)
