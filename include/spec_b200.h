@@ -374,7 +374,8 @@ int spec_kv_read(const spec_kv_cache *cache, const int32_t *row_seq, const int32
 /* One query token per sequence: out[b][h] = softmax over t < lengths[b] of (scale q[b][h].k[t][g]) applied to v[t][g],
  * g = h / (n_heads / n_kv_heads), over sequence b of the cache; lse (optional) float [batch][n_heads], the natural-log normaliser.
  * lengths int32 [batch]; a length of 0 gives zeros and -inf.  q: heads adjacent, tokens q_token_stride elements apart, 16-byte
- * aligned (stride too); out [batch][n_heads][head_dim].  scale 0: head_dim^-1/2.  batch <= 8192, batch <= n_seq.
+ * aligned (stride too); out [batch][n_heads][head_dim].  scale 0: head_dim^-1/2.  batch <= 8192, batch <= n_seq,
+ * n_heads <= 65536.
  * workspace: spec_decode_attention_workspace_bytes() bytes, 256-byte aligned, zero before the first call; a call leaves it ready for
  * the next on the same stream, and calls that may overlap need one each. */
 size_t spec_decode_attention_workspace_bytes(void);

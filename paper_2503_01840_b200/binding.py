@@ -595,7 +595,7 @@ def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor
                      status: Optional[torch.Tensor] = None):
     """Attention of one new token per sequence: q [batch][heads][head_dim] over the first lengths[b] positions of sequence b of a paged cache.
     Returns out [batch][heads][head_dim] (and the float32 [batch][heads] log-normaliser when want_lse).  workspace: decode_workspace();
-    without one, a workspace that is kept for the current stream (made by its first call, which must not be under graph capture)."""
+    without one, a workspace that is kept for the current stream (made by its first call, which is refused under graph capture)."""
     r = (_marshal_module or _marshal()).decode_attention(q, k_pool, v_pool, page_table, k_scale, v_scale, lengths, scale, want_lse, out, workspace, status)
     if type(r) is int:
         raise SpecError(r, "spec_decode_attention")

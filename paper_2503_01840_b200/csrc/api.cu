@@ -1836,7 +1836,7 @@ extern "C" int spec_decode_attention(int32_t dtype, const void *q, int64_t q_ts,
   if (const int rc = cache_of(cache, &a.cache)) return rc;
   if (!kv_goes_with(dtype, cache->format) || batch < 0 || n_heads < 1 || n_heads % cache->n_kv_heads || batch > cache->n_seq || !(fabsf(scale) < INFINITY))
     return SPEC_ERR_INVALID_CFG;
-  if (batch > DECODE_MAX_BATCH) return SPEC_ERR_UNSUPPORTED;
+  if (batch > DECODE_MAX_BATCH || n_heads > 65536) return SPEC_ERR_UNSUPPORTED;
   if (batch == 0) return SPEC_OK;
   if (!q || !lengths || !out || !workspace) return SPEC_ERR_NULL;
   if (workspace_bytes < decode_attn_workspace_bytes() || !kv_aligned(workspace, 256)) return SPEC_ERR_WORKSPACE;

@@ -285,11 +285,11 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   }
   __syncthreads();
 
-  // ---- joins: of the states that this CTA's warps share (level 0); of those that CTAs share, eight or sixteen at a time, by the CTA that
-  // comes last (1); of what that leaves (2).  All levels run the same code, a warp a run and head by turns: code that only the last
-  // CTA ran took it microseconds to fetch.
+  // ---- joins: of the states that this CTA's warps share (level 0); of those that CTAs share, 32 at a time, by the CTA that comes last (1);
+  // of what that leaves where a segment has more (2).  All levels run the same code, a warp a run and head by turns: code that only the
+  // last CTA ran took it microseconds to fetch.  (Eight or sixteen at a time, and level 2 for the rest: 21.4 us against 18.4 for one sequence of 16384.)
   static_assert(2 * W <= 32, "a lane per partial state");
-  constexpr int SHIFT = W == 16 ? 3 : 4;                                 // parts of both segments of a CTA fit its 2 W states
+  constexpr int SHIFT = 5;                                               // states of a part
   static_assert(DA_MAX_CTAS / (1 << SHIFT) + 2 <= 2 * W, "room for the parts of level 1");
   auto make_run = [&](int at, const DaSeg &s, const float *from, int stride, int skew, uint32_t mask, float *to) {
     runs[at] = DaRun{from, to, s.b * p.a.H + s.kv * p.group + s.chunk * heads, min(heads, p.group - s.chunk * heads), stride, skew, mask};
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
         // a CTA's state stands where its number says, but for the first CTA, whose last segment it is
         for (int i = 0; i < parts; i++) {
           const int k0 = i << SHIFT, k = min(1 << SHIFT, shared_by - k0);
-          make_run(first_slot + i, open_seg, p.part + (size_t)2 * (shared_from + k0) * part_floats, 2 * part_floats, i == 0 ? part_floats : 0, (1u << k) - 1,
+          make_run(first_slot + i, open_seg, p.part + (size_t)2 * (shared_from + k0) * part_floats, 2 * part_floats, i == 0 ? part_floats : 0, k == 32 ? 0xffffffffu : (1u << k) - 1,
                    parts == 1 ? nullptr : states + (size_t)(first_slot + i) * part_floats);
         }
       } else if (parts) {
@@ -388,7 +388,7 @@ template <typename Body> static cudaError_t launch(DaArgs p, int ctas, cudaStrea
   const long long tiles = ((long long)p.a.cache.pages_per_seq * p.a.cache.page_size + Body::TILE - 1) / Body::TILE;
   if (tiles * p.a.batch * p.a.cache.G * p.chunks > (1 << 30)) return cudaErrorNotSupported;
   // (with fewer segments than half the CTAs the others stay without work: one user at 613 tokens 12.3 us dealt out evenly, 13.0 whole)
-  p.whole = p.segs * 2 >= ctas ? (p.segs + ctas - 1) / ctas : 0;
+  p.whole = p.segs * 2 >= ctas && p.segs < (1 << 24) ? (p.segs + ctas - 1) / ctas : 0;
   p.spare = DA_SPARE_BYTES / (Body::TILE * p.a.cache.hd * 2 * (int)sizeof(typename Body::E));
   const size_t smem = da_smem_bytes(p.a.batch, Body::WARPS, Body::warp_smem_floats(p.a.cache.hd), p.heads, p.a.cache.hd);
   if (smem > DA_SMEM || !limit.ensure(decode_attn_kernel<Body>, (int)smem)) return cudaErrorInvalidValue;

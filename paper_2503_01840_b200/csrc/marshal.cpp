@@ -8,6 +8,7 @@
 
 #include <ATen/Functions.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <map>
@@ -222,7 +223,10 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
 at::Tensor workspace_of(const at::Tensor &q, void *stream) {
   static auto *kept = new std::map<std::pair<int, void *>, at::Tensor>;
   at::Tensor &w = (*kept)[{(int)q.get_device(), stream}];
-  if (!w.defined()) w = at::zeros({(int64_t)workspace_bytes_()}, q.options().dtype(at::kByte));
+  if (!w.defined()) {
+    need(c10::cuda::currentStreamCaptureStatusMayInitCtx() == c10::cuda::CaptureStatus::None, "decode_attention: under graph capture a workspace of decode_workspace()");
+    w = at::zeros({(int64_t)workspace_bytes_()}, q.options().dtype(at::kByte));
+  }
   return w;
 }
 

@@ -260,6 +260,11 @@ def test_streams_graphs_and_workspaces():
         static.copy_(q * s)
         graph.replay()
         assert torch.equal(held, sb.decode_attention(static, cache["k_pool"], cache["v_pool"], table, length, **sc))
+    other = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(other, stream=torch.cuda.Stream()):            # a capture of a stream without a workspace has to bring one
+        static.add_(0)
+        with pytest.raises(ValueError):
+            sb.decode_attention(static, cache["k_pool"], cache["v_pool"], table, length, **sc, out=held)
     with pytest.raises(sb.SpecError) as e:
         sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, length, **sc, workspace=ws[:1024])
     assert e.value.code == -3
