@@ -2,7 +2,7 @@
 //   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q.k_t - max),  lse = max + log sum_t p_t,   t < length of the sequence.
 //
 // Every key and value is read once and used for the few query heads that share it, so the cache's bytes bound it.  They are dealt out
-// evenly: all tiles of TILE positions, of every sequence and KV head one after the other, are cut into equal runs for the CTAs
+// evenly: all tiles of TILE positions, of every sequence and KV head (a segment) one after the other, are cut into equal runs for the CTAs
 // (one wave of them), a CTA's run into equal runs for its warps.  A warp walks its run with a softmax state of its own; what is left
 // of a (sequence, head) that several warps share is joined in shared memory, and of one that several CTAs share by the CTA that
 // finishes last, out of the workspace, in the order of the positions whoever that is: the result does not depend on timing.
@@ -11,6 +11,10 @@
 
 namespace spec {
 
+// Work is counted in tiles, and the beginning of a segment (queries, page, first keys: nothing is under way meanwhile) as so many more.  us with 0 / 1 / 2 / 3:
+// one sequence of 16384 18.6 / 17.5 / 17.4 / 17.7, 8 of 700 to 1500 14.0 / 12.6 / 12.7 / 13.3, 4 of 1000 to 8000 17.6 / 16.3 / 16.2 / 16.1, 64 of 256 to 2048
+// 42.1 / 41.8 / 41.4 / 40.9.
+constexpr int DA_START = 2;
 constexpr int DA_MAX_CTAS = 160;           // CTAs of a launch, at most
 constexpr int DA_PART_FLOATS = 8 * 256 + 16 * 2;      // a partial state: O of heads x hd <= 2048 elements, then (max, sum) of up to 16 heads
 
@@ -32,7 +36,7 @@ __host__ __device__ constexpr int da_part_floats(int heads, int hd) { return hea
 struct DaSeg {
   int b, kv, chunk;             // sequence, KV head, chunk of its query heads
   int t0, t1, tiles;            // tiles t0 .. t1 - 1 of `tiles`
-  int u0;                       // the first of them, counted over all segments
+  int u0;                       // the first of them, in units over all segments
 };
 
 // States of one segment that are joined: `mask` of those that stand `stride` floats apart from `from`, the first `skew` further on; into `to`, or
@@ -79,7 +83,7 @@ __device__ __forceinline__ int da_row(const DaArgs &p, int b, int g, int pos) {
 }
 
 // ---------------------------------------------------------------- the kernel
-// tiles before sequence b, for every b; -1 and lengths past the cache are reported and clamped
+// a sequence's length; one below zero or past the cache is reported and clamped
 __device__ __forceinline__ int da_length(const DaArgs &p, int b) {
   const int len = p.a.len[b];
   const long long cap = (long long)p.a.cache.pages_per_seq * p.a.cache.page_size;
@@ -139,7 +143,7 @@ static __device__ __noinline__ void da_join_head(const float *states, int stride
   else if (lse) *lse = (da_ref(m) + log2f(l)) * 0.693147180559945309f;
 }
 
-// smem: int before[batch + 1] (tiles before each sequence), per warp the body's floats and two partial states
+// smem: int before[batch + 1] (units before each sequence), per warp the body's floats and two partial states
 template <typename Body>
 __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const __grid_constant__ DaArgs p) {
   pdl_wait();
@@ -157,12 +161,13 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   __shared__ DaRun runs[2 * W];
   __shared__ int to_do[3];
 
-  // ---- tiles before each sequence, their sum, and the longest sequence's.  Up to 32 sequences: a lane each in every warp, and no barrier
+  // ---- units (tiles and beginnings) before each sequence, their sum, and the longest sequence's.  Up to 32 sequences: a lane each in every warp, and no barrier
   // on the way to the first load; more: a run of them per thread, a scan over the threads, and a table.
   const bool few = B <= 32;
+  auto units_of = [&](int len) { return len ? (len + TILE - 1) / TILE + DA_START : 0; };
   int total, longest = 0, my_before = 0, my_tiles = 0;
   if (few) {
-    my_tiles = lane < B ? (da_length(p, lane) + TILE - 1) / TILE : 0;
+    my_tiles = lane < B ? units_of(da_length(p, lane)) : 0;
     int inc = my_tiles;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -176,7 +181,7 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     const int per = (B + THREADS - 1) / THREADS, b0 = min(B, tid * per), b1 = min(B, b0 + per);
     int sum = 0, most = 0;
     for (int b = b0; b < b1; b++) {
-      const int t = (da_length(p, b) + TILE - 1) / TILE;
+      const int t = units_of(da_length(p, b));
       sum += t;
       most = max(most, t);
     }
@@ -196,7 +201,7 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     }
     for (int b = b0; b < b1; b++) {
       before[b] = at;
-      at += (da_length(p, b) + TILE - 1) / TILE;
+      at += units_of(da_length(p, b));
     }
     if (tid == THREADS - 1) before[B] = at;
     __syncthreads();
@@ -204,13 +209,13 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   }
   total *= VH;
   if (lane < 2) seg[2 * warp + lane].b = -1;
-  // (tiles before sequence b, its own); all lanes ask for the same one
+  // (units before sequence b, those of each of its segments); all lanes ask for the same one
   auto tiles_of = [&](int b) {
     if (few) return make_int2(__shfl_sync(0xffffffffu, my_before, b), __shfl_sync(0xffffffffu, my_tiles, b));
     return make_int2(before[b], before[b + 1] - before[b]);
   };
 
-  // The tiles are dealt out evenly: each of N CTAs has total / N, the first total % N one more.  (32-bit quotients: 64-bit ones take
+  // The units are dealt out evenly: each of N CTAs has total / N, the first total % N one more.  (32-bit quotients: 64-bit ones take
   // microseconds here.)  At least eight tiles a CTA: states that CTAs share cost more to join than those of a CTA's warps.
   const int N = max(1, min((int)gridDim.x, (total + 7) >> 3));
   const int each = total / N, more = total - each * N;
@@ -255,14 +260,15 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
       s.b = lo;
     }
     const int2 t = tiles_of(s.b);
-    s.tiles = t.y;
-    const int r = u - t.x * VH, v = da_quotient(r, t.y);
+    const int r = u - t.x * VH, v = da_quotient(r, t.y), x = r - v * t.y, end = min(t.y, x + (w1 - u));      // units x .. end - 1 of the segment's
     s.kv = p.chunks == 1 ? v : da_quotient(v, p.chunks);
     s.chunk = v - s.kv * p.chunks;
-    s.t0 = r - v * t.y;
-    s.t1 = min(t.y, s.t0 + (w1 - u));
-    s.u0 = u - s.t0;
-    u += s.t1 - s.t0;
+    s.tiles = t.y - DA_START;
+    s.t0 = max(x - DA_START, 0);
+    s.t1 = end - DA_START;
+    s.u0 = u - x + DA_START;
+    u += end - x;
+    if (s.t1 <= s.t0) continue;                                          // nothing but its beginning
     Body body;
     body.run(p, s, da_length(p, s.b), warp_mem, lane);
     const bool whole = s.t0 == 0 && s.t1 == s.tiles;
@@ -386,7 +392,7 @@ inline size_t da_smem_bytes(int batch, int warps, int own_floats, int heads, int
 template <typename Body> static cudaError_t launch(DaArgs p, int ctas, cudaStream_t s) {
   static SmemLimit limit;
   const long long tiles = ((long long)p.a.cache.pages_per_seq * p.a.cache.page_size + Body::TILE - 1) / Body::TILE;
-  if (tiles * p.a.batch * p.a.cache.G * p.chunks > (1 << 30)) return cudaErrorNotSupported;
+  if ((tiles + DA_START) * p.a.batch * p.a.cache.G * p.chunks > (1 << 30)) return cudaErrorNotSupported;
   // (with fewer segments than half the CTAs the others stay without work: one user at 613 tokens 12.3 us dealt out evenly, 13.0 whole)
   p.whole = p.segs * 2 >= ctas && p.segs < (1 << 24) ? (p.segs + ctas - 1) / ctas : 0;
   p.spare = DA_SPARE_BYTES / (Body::TILE * p.a.cache.hd * 2 * (int)sizeof(typename Body::E));
