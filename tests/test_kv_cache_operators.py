@@ -250,6 +250,36 @@ def test_long_strides(ts, hs):
     assert torch.equal(sb.rotary(x, pos, freq, out=out), want)
 
 
+@gpu
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "e4m3"), ("bf16", "bf16"), ("fp32", "int8"), ("fp32", "fp32")])
+@pytest.mark.parametrize("shift", [1, 4])
+def test_heads_off_their_alignment(dtype, fmt, shift):
+    """Tensors that start `shift` elements into their allocation give what aligned ones give: the same bits for values, the codes of rotated keys
+    within what the two kernels' roundings may differ by."""
+    T, H, G, hd, ps = 19, 4, 2, 128, 16
+    g = torch.Generator().manual_seed(shift)
+    qkv = torch.randn(T, H + 2 * G, hd, generator=g).to(DT[dtype])
+    freq, _ = sb.rope_frequencies(hd, 1e4)
+    pos, seq = torch.arange(T, dtype=torch.int32).cuda(), torch.zeros(T, dtype=torch.int32).cuda()
+    buf = torch.zeros(qkv.numel() + shift, dtype=DT[dtype], device="cuda")
+    off = buf[shift:].view(qkv.shape)
+    off.copy_(qkv)
+    outs = []
+    for x in (qkv.cuda(), off):
+        cache = make_cache(torch.Generator().manual_seed(1), fmt, 6, G, ps, hd, 1, 4)
+        sc = {"k_scale": cache["k_scale"], "v_scale": cache["v_scale"]}
+        args = cache["k_pool"], cache["v_pool"], cache["page_table"], seq, pos
+        q = sb.kv_append(x[:, H: H + G], x[:, H + G:], *args, **sc, q=x[:, :H], inv_freq=freq)
+        outs.append((q, sb.rotary(x[:, :H], pos, freq), *sb.kv_read(*args, **sc, dtype=torch.float32)))
+    (q0, r0, k0, v0), (q1, r1, k1, v1) = outs
+    assert torch.equal(v0, v1) and torch.equal(q0, r0) and torch.equal(q1, r1)
+    err = turn_error(qkv[:, :H].double(), freq.cpu(), "half", 1.0).cuda()
+    assert ((q0.double() - q1.double()).abs() <= 2 * err + (q0.double().abs() * 2.0 ** -7 if dtype == "bf16" else 0)).all()
+    top = k0.abs().amax(-1, keepdim=True).double()
+    step = (k0.double().abs() * 2.0 ** -3 + top / 448 * 2.0 ** -8) if fmt == "e4m3" else top / 127 if fmt == "int8" else k0.double().abs() * (2.0 ** -7 if fmt == "bf16" else 0)
+    assert ((k0.double() - k1.double()).abs() <= step * 1.001 + 2 * turn_error(qkv[:, H: H + G].double(), freq.cpu(), "half", 1.0).cuda()).all()
+
+
 def test_tensors_that_are_not_on_the_gpu_are_refused():
     """The C++ part of the binding loads and checks without a device."""
     x, pos = torch.zeros(2, 4, 64), torch.zeros(2, dtype=torch.int32)
