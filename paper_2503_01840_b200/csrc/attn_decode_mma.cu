@@ -9,8 +9,8 @@
 // the probabilities, divided by a number above the largest scale so far (f16 holds 2^-24 .. 2^16), which comes back in the end.
 // The reference that probabilities are relative to follows the maximum only where a score passes it by more than 2^8.
 //
-// Measured: 16 sequences of 4097 to 32768 positions, 64 / 8 heads of 128, in bf16 192 us (6.3 TB/s, 97 % of a copy's rate); 16 of 8192, 32 / 8 heads, in
-// bf16 90 us, in e4m3 56 (4.9 TB/s), in int8 58.  What is left there is the ten microseconds around the loop (launch, first loads, joins).
+// Measured: 16 sequences of 4097 to 32768 positions, 64 / 8 heads of 128, in bf16 192 us (6.3 TB/s, 98 % of a copy's rate); 16 of 8192, 32 / 8 heads, in
+// bf16 91 us, in e4m3 55 (5.0 TB/s), in int8 57.  What is left there is the ten microseconds around the loop (launch, first loads, joins).
 // Tried without a gain: lines of the tile after the next asked for to the L2 (e4m3 56 -> 61 us; heads of 64 28 -> 24), one load of scales a tile and
 // shuffles of them (310 -> 495 instructions a group with the division and the maximum of scales that went along with it).
 #include "attn_decode_kernel.cuh"

@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_any_kernel(RopeAppen
 // lanes' exchange.  A block takes some heads of some tokens; their cosines and sines are formed once, in shared memory.
 // Bytes bound it: a thread asks for its first U heads before it forms the angles.  Measured: 16384 tokens of 40 heads of 128 in bf16 57 us
 // (5.9 TB/s, 92 % of a copy's rate), 4096 of 80 heads in fp32 53 us (6.3 TB/s); with keys and values to e4m3 as well, 16384 of 32 + 8 + 8 heads,
-// 68 us (5.4 TB/s): the look-ups of the cache rows stand before a block's first store.  One head under way a thread and six blocks an SM; with two and five
+// 69 us (5.4 TB/s): the look-ups of the cache rows stand before a block's first store.  One head under way a thread and six blocks an SM; with two and five
 // 61 / 53 / 72 us, one and eight 57 / 54 / 82; with two rounds a block instead of six 64 / 53 / 94, eight 62 / 53 / 74; one wave of blocks that walk tokens with
 // copies to shared memory four heads ahead 59 / 81 / 79; with 64-bit offsets 59 / 54 / 74.
 __device__ __forceinline__ void unpack_piece(uint4 u, float (&y)[4]) {
@@ -266,7 +266,7 @@ cudaError_t launch_rope_append(const RopeAppend &a, int dtype, int fmt, cudaStre
 // ---------------------------------------------------------------- reading back
 // Row r of the output is position kvpos[r] of sequence seq[r], zeros where there is none.  A thread takes eight elements, so that a
 // warp's stores of bf16 are whole lines; a block some rows, whose places in the pool are looked up once.  Bytes bound it: 16384 tokens
-// of 8 heads of 128 from e4m3 21 us (4.8 TB/s), 8000 of 40 heads from int8 49 us (5.1 TB/s).  Two, four and eight items a thread under way, with as many
+// of 8 heads of 128 from e4m3 21 us (4.8 TB/s), 8000 of 40 heads from int8 52 us (4.8 TB/s).  Two, four and eight items a thread under way, with as many
 // blocks an SM as that leaves room for: 21 / 23 / 24 us.
 constexpr int READ_MAX_ROWS = 64;      // 256 / the least items a row (4)
 struct ReadGrid { int rows, items; uint32_t by_items, by_hd8; };         // rows of a block, eights of a row (keys, then values); ceil(2^32 / items), / a head's eights
