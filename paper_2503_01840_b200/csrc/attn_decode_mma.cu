@@ -11,7 +11,8 @@
 //
 // Measured: 16 sequences of 4097 to 32768 positions, 64 / 8 heads of 128, in bf16 192 us (6.3 TB/s, 98 % of a copy's rate); 16 of 8192, 32 / 8 heads, in
 // bf16 91 us, in e4m3 55 (5.0 TB/s), in int8 57.  What is left there is the ten microseconds around the loop (launch, first loads, joins).
-// Tried without a gain: lines of the tile after the next asked for to the L2 (e4m3 56 -> 61 us; heads of 64 28 -> 24), one load of scales a tile and
+// Tried without a gain: lines of the tile after the next asked for to the L2 (e4m3 56 -> 61 us; heads of 64 28 -> 24 where larger tiles brought 23), one load of
+// scales a tile and
 // shuffles of them (310 -> 495 instructions a group with the division and the maximum of scales that went along with it).
 #include "attn_decode_kernel.cuh"
 

@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_any_kernel(RopeAppen
 // Bytes bound it: a thread asks for its first U heads before it forms the angles.  Measured: 16384 tokens of 40 heads of 128 in bf16 57 us
 // (5.9 TB/s, 92 % of a copy's rate), 4096 of 80 heads in fp32 53 us (6.3 TB/s); with keys and values to e4m3 as well, 16384 of 32 + 8 + 8 heads,
 // 69 us (5.4 TB/s): the look-ups of the cache rows stand before a block's first store.  One head under way a thread and six blocks an SM; with two and five
-// 61 / 53 / 72 us, one and eight 57 / 54 / 82; with two rounds a block instead of six 64 / 53 / 94, eight 62 / 53 / 74; one wave of blocks that walk tokens with
+// 61 / 53 / 72 us, one and eight 57 / 54 / 82; with two rounds a block instead of six 64 / 53 / 94, two heads and eight rounds 62 / 53 / 74; one wave of blocks that walk tokens with
 // copies to shared memory four heads ahead 59 / 81 / 79; with 64-bit offsets 59 / 54 / 74.
 __device__ __forceinline__ void unpack_piece(uint4 u, float (&y)[4]) {
   y[0] = __uint_as_float(u.x), y[1] = __uint_as_float(u.y), y[2] = __uint_as_float(u.z), y[3] = __uint_as_float(u.w);
