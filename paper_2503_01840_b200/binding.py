@@ -585,7 +585,7 @@ def kv_read(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor
 
 
 def decode_workspace(device="cuda") -> torch.Tensor:
-    """A workspace for decode_attention: one for each stream whose calls may overlap."""
+    """A workspace for decode_attention: one for each stream, and each captured graph, whose calls may overlap with others."""
     return torch.zeros(lib().spec_decode_attention_workspace_bytes(), dtype=torch.uint8, device=device)
 
 
@@ -595,7 +595,8 @@ def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor
                      status: Optional[torch.Tensor] = None):
     """Attention of one new token per sequence: q [batch][heads][head_dim] over the first lengths[b] positions of sequence b of a paged cache.
     Returns out [batch][heads][head_dim] (and the float32 [batch][heads] log-normaliser when want_lse).  workspace: decode_workspace();
-    without one, a workspace that is kept for the current stream (made by its first call, which is refused under graph capture)."""
+    without one, a workspace that is kept for the current stream.  Under graph capture a call without one is refused: replays may run beside
+    the stream's own calls, or another graph's, and would share it with them."""
     r = (_marshal_module or _marshal()).decode_attention(q, k_pool, v_pool, page_table, k_scale, v_scale, lengths, scale, want_lse, out, workspace, status)
     if type(r) is int:
         raise SpecError(r, "spec_decode_attention")

@@ -218,15 +218,13 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// A workspace for each stream that a call without one of its own was made on, kept for the next.  (Never taken down: the process's end may
-// have taken the driver down first.)
+// A workspace for each stream that a call without one of its own was made on, kept for the next.  A graph never gets it: its replays may run on
+// any stream, beside the stream's own calls or another graph's.  (Never taken down: the process's end may have taken the driver down first.)
 at::Tensor workspace_of(const at::Tensor &q, void *stream) {
+  need(c10::cuda::currentStreamCaptureStatusMayInitCtx() == c10::cuda::CaptureStatus::None, "decode_attention: under graph capture a workspace of decode_workspace()");
   static auto *kept = new std::map<std::pair<int, void *>, at::Tensor>;
   at::Tensor &w = (*kept)[{(int)q.get_device(), stream}];
-  if (!w.defined()) {
-    need(c10::cuda::currentStreamCaptureStatusMayInitCtx() == c10::cuda::CaptureStatus::None, "decode_attention: under graph capture a workspace of decode_workspace()");
-    w = at::zeros({(int64_t)workspace_bytes_()}, q.options().dtype(at::kByte));
-  }
+  if (!w.defined()) w = at::zeros({(int64_t)workspace_bytes_()}, q.options().dtype(at::kByte));
   return w;
 }
 

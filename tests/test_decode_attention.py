@@ -270,6 +270,49 @@ def test_streams_graphs_and_workspaces():
     assert e.value.code == -3
 
 
+def test_captures_do_not_get_a_streams_kept_workspace():
+    """Nor on a stream that has one from the calls before: two graphs, or a graph and a call on that stream, would share it.  Two graphs with a
+    workspace each replay side by side, beside calls on the stream of their captures."""
+    g = torch.Generator(device="cuda").manual_seed(15)
+    lens, ps, H, G, hd = [3000, 17, 900], 16, 32, 8, 128
+    table, pages = table_for(g, lens, ps)
+    cache = pools(g, "e4m3", pages, G, ps, hd)
+    qs = [torch.randn(3, H, hd, generator=g, device="cuda").to(torch.bfloat16) for _ in range(3)]
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    run = lambda q, **kw: sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, length, k_scale=cache["k_scale"], v_scale=cache["v_scale"], **kw)
+    want = [run(q) for q in qs]
+    warm, beside = torch.cuda.Stream(), torch.cuda.Stream()
+    warm.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(warm):
+        run(qs[0])
+    warm.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=warm):
+        qs[0].add_(0)
+        with pytest.raises(ValueError):
+            run(qs[0])
+    graphs, outs = [], []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        outs.append(torch.empty_like(qs[i]))
+        ws = sb.decode_workspace()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graphs[i], stream=warm):
+            for _ in range(8):
+                run(qs[i], out=outs[i], workspace=ws)
+    for _ in range(5):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(beside):
+            graphs[0].replay()
+        graphs[1].replay()
+        with torch.cuda.stream(warm):
+            mine = [run(qs[2]) for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1]) and all(torch.equal(m, want[2]) for m in mine)
+
+
 def test_lengths_and_pages_out_of_range_are_recorded():
     g = torch.Generator(device="cuda").manual_seed(6)
     lens, ps, H, G, hd = [40, 20], 16, 4, 2, 64
