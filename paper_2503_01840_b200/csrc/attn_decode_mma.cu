@@ -6,8 +6,10 @@
 // likewise its values (piece g of a row): everything comes straight from global memory into the registers that the MMA reads,
 // one tile ahead.  Eight bits become f16, which holds every e4m3 and int8 number; Q becomes f16 times a power of two that puts its
 // largest element below 2^15, so that no element that counts loses a bit.  Scales of keys go onto the scores.  Scales of values go onto
-// the probabilities, divided by a number above the largest scale so far (f16 holds 2^-24 .. 2^16), which comes back in the end.
-// The reference that probabilities are relative to follows the maximum only where a score passes it by more than 2^8.
+// the probabilities: each head's products are multiplied by a power of two that puts its largest so far near 2^6 (f16 holds 2^-24 .. 2^16), and O is divided by it
+// in the end.  It follows the products, not the scales: a value's scale far above the others' costs those nothing where its probability is small.
+// The reference that probabilities are relative to follows the maximum only where a score passes it by more than 8 (in powers of two), and that power only where a product
+// passes 2^15; both change by whole powers of two, exactly.
 //
 // Measured: 16 sequences of 4097 to 32768 positions, 64 / 8 heads of 128, in bf16 192 us (6.3 TB/s, 98 % of a copy's rate); 16 of 8192, 32 / 8 heads, in
 // bf16 91 us, in e4m3 55 (5.0 TB/s), in int8 57.  What is left there is the ten microseconds around the loop (launch, first loads, joins).
@@ -81,7 +83,7 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
   uint32_t q[NB][STEPS][2];
   float wide[SPLIT ? NB : 1][SPLIT ? STEPS : 1][4];      // queries as they are, until begin()
   float qf[NB][2];                                       // scale * log2 e / the power of two on Q
-  float c, rc;                                           // what scales of values are divided by, at least the largest so far; 64 / c
+  float up[Q8 ? NB : 1][2];                              // the power of two on probability times scale, and so on O
 
   // the dimensions of Q that this lane's piece of a key meets in contraction s, four at a time; heads past the last are zero
   __device__ __forceinline__ void load_queries(const DaArgs &p, const DaSeg &sg, int g, int t) {
@@ -104,6 +106,8 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
       }
     }
   }
+  static __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+  static __device__ __forceinline__ float inverse_power(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }      // 1 / p, of a power of two from 2^-126 to 2^126
   // two numbers as f16 (part 0), or what that leaves of them, times 2^11 (part 1); an infinity leaves nothing
   static __device__ __forceinline__ uint32_t part_of(float a, float b, int part) {
     const __half2 hi = __floats2half2_rn(a, b);
@@ -148,13 +152,13 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
       for (int e = 0; e < 2; e++) {
         qf[n][e] = __shfl_sync(0xffffffffu, f, ((2 * t + e) % PER_BLOCK) * 4);
         r[n][e] = NONE, l[n][e] = 0.0f;
+        if constexpr (Q8) up[n][e] = 8.507059173023462e37f;       // 2^126
       }
 #pragma unroll
       for (int s = 0; s < STEPS; s++)
 #pragma unroll
         for (int e = 0; e < 4; e++) o[n][s][e] = 0.0f;
     }
-    c = rc = 0.0f;
   }
 
   struct Keys { uint4 x[2][KP]; float ks[2], vs[2]; };   // keys and both scales of positions g and g + 8
@@ -286,33 +290,35 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
               for (int n = 0; n < NB; n++) s[u][n][2 * i] = s[u][n][2 * i + 1] = -INFINITY;
             }
       }
-      bool over = false;
-      float x[NG][NB][4];                                // scores relative to the reference
+      uint32_t b[NG][NB][2];                             // as the MMA takes them
+      float sum[NB][2];
+      // A second pass, after a reference or a power has changed, is rare past the first tiles.  (One copy of this code: with two, heads of 256 took 65 us
+      // instead of 56, 16 sequences of 4096, 8 KV heads in e4m3.)
+#pragma unroll 1
+      for (int pass = 0;; pass++) {
+        bool over = false;
 #pragma unroll
-      for (int u = 0; u < NG; u++) {
+        for (int n = 0; n < NB; n++) {
+          sum[n][0] = sum[n][1] = 0.0f;
 #pragma unroll
-        for (int n = 0; n < NB; n++)
+          for (int u = 0; u < NG; u++)
 #pragma unroll
-          for (int e = 0; e < 4; e++) {
-            x[u][n][e] = s[u][n][e] - r[n][e & 1];
-            over |= x[u][n][e] > 8.0f;
-          }
-        if constexpr (Q8) over |= vs[u][0] > c || vs[u][1] > c;
-      }
-      if (__any_sync(0xffffffffu, over)) {               // rare past the first tiles
-        float grow = 1.0f;
-        if constexpr (Q8) {
-          float top = fmaxf(vs[0][0], vs[0][1]);
+            for (int i = 0; i < 2; i++) {
+              float w[2];
 #pragma unroll
-          for (int u = 1; u < NG; u++) top = fmaxf(top, fmaxf(vs[u][0], vs[u][1]));
-          top = warp_max(top);
-          if (top > c) {                                 // with room above, so that this stays rare
-            const float up = fmaxf(4.0f * top, 8e-31f);
-            grow = c / up;
-            c = up;
-            rc = 64.0f / up;
-          }
+              for (int e = 0; e < 2; e++) {
+                w[e] = da_ex2(s[u][n][2 * i + e] - r[n][e]);
+                over |= w[e] > 256.0f;
+                sum[n][e] += w[e];
+                if constexpr (Q8) {
+                  w[e] *= vs[u][i] * up[n][e];
+                  over |= w[e] > 32768.0f;
+                }
+              }
+              b[u][n][i] = Q8 ? part_of(w[0], w[1], SPLIT ? t >> 1 : 0) : pack_bf16(w[0], w[1]);
+            }
         }
+        if (!__any_sync(0xffffffffu, over && pass == 0)) break;
 #pragma unroll
         for (int n = 0; n < NB; n++)
 #pragma unroll
@@ -322,37 +328,33 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
             for (int u = 0; u < NG; u++) m = fmaxf(m, fmaxf(s[u][n][e], s[u][n][e + 2]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            const float f = da_ex2(r[n][e] - m);
+            m = ceilf(m);
+            float f = power_of_two(-(int)fminf(m - r[n][e], 127.0f));      // 2^-127: 0
             r[n][e] = m;
             l[n][e] *= f;
+            if constexpr (Q8) {
+              float top = 7.52316384526264e-37f;         // 2^-120, the least scale
 #pragma unroll
-            for (int u = 0; u < NG; u++) x[u][n][e] = s[u][n][e] - m, x[u][n][e + 2] = s[u][n][e + 2] - m;
+              for (int u = 0; u < NG; u++) top = fmaxf(top, fmaxf(da_ex2(s[u][n][e] - m) * vs[u][0], da_ex2(s[u][n][e + 2] - m) * vs[u][1]));
 #pragma unroll
-            for (int i = 0; i < STEPS; i++) o[n][i][e] *= f * grow, o[n][i][e + 2] *= f * grow;
+              for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              f *= inverse_power(up[n][e]);
+              top = fminf(fmaxf(top, 64.0f * f), 1.329227995784916e36f);      // 2^120
+              up[n][e] = power_of_two(6 + 127 - (int)(__float_as_uint(top) >> 23));
+              f *= up[n][e];
+            }
+#pragma unroll
+            for (int i = 0; i < STEPS; i++) o[n][i][e] *= f, o[n][i][e + 2] *= f;
           }
       }
-      uint32_t b[NG][NB][2];
 #pragma unroll
-      for (int u = 0; u < NG; u++)
+      for (int n = 0; n < NB; n++) {
+        l[n][0] += sum[n][0], l[n][1] += sum[n][1];
 #pragma unroll
-        for (int n = 0; n < NB; n++) {
+        for (int u = 0; u < NG; u++)
 #pragma unroll
-          for (int e = 0; e < 4; e++) {
-            x[u][n][e] = da_ex2(x[u][n][e]);
-            l[n][e & 1] += x[u][n][e];
-          }
-#pragma unroll
-          for (int i = 0; i < 2; i++) {
-            uint32_t pair;
-            if constexpr (Q8) {
-              const float w = vs[u][i] * rc;
-              pair = SPLIT ? part_of(x[u][n][2 * i] * w, x[u][n][2 * i + 1] * w, t >> 1) : part_of(x[u][n][2 * i] * w, x[u][n][2 * i + 1] * w, 0);
-            } else {
-              pair = pack_bf16(x[u][n][2 * i], x[u][n][2 * i + 1]);
-            }
-            b[u][n][i] = da_transpose(pair);             // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
-          }
-        }
+          for (int i = 0; i < 2; i++) b[u][n][i] = da_transpose(b[u][n][i]);      // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
+      }
       // ---- output
       if (live != FULL) {                                // a page that is none: zero times whatever stands in page 0 is to be zero
 #pragma unroll
@@ -405,7 +407,7 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
               o[n][i][e] = fmaf(__shfl_xor_sync(0xffffffffu, o[n][i][e], 2), 4.8828125e-4f, o[n][i][e]);      // what t < 2 hold is used
               o[n][i][e + 2] = fmaf(__shfl_xor_sync(0xffffffffu, o[n][i][e + 2], 2), 4.8828125e-4f, o[n][i][e + 2]);
             }
-            o[n][i][e] *= c * 0.015625f, o[n][i][e + 2] *= c * 0.015625f;
+            o[n][i][e] *= inverse_power(up[n][e]), o[n][i][e + 2] *= inverse_power(up[n][e]);
           }
         }
       }

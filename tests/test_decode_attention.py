@@ -181,6 +181,48 @@ def test_scales_queries_and_scores_of_very_different_sizes(dtype, fmt, hd):
         check(up, flat, table, lens, ps, scale=-800.0 / hd)              # all but the first tokens underflow
 
 
+@pytest.mark.parametrize("dtype,fmt", KINDS[1:3] + KINDS[4:])
+@pytest.mark.parametrize("H,G,hd", [(8, 2, 128), (16, 1, 64), (4, 1, 256), (8, 2, 80)])
+@pytest.mark.parametrize("at", [0, 17, 350, 699])
+def test_a_value_far_above_the_others_that_hardly_counts(dtype, fmt, H, G, hd, at):
+    """One position's values are 2^16 .. 2^40 times the others'.  Half of the heads see its key far below their maximum, so that it is next to nothing of
+    their output; for the other half of them it outweighs everything.  Neither may cost the other its bits."""
+    g = torch.Generator(device="cuda").manual_seed(at + hd)
+    lens, ps = [700, 64], 16
+    table, pages = table_for(g, lens, ps)
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    for power in (16, 24, 40):
+        cache = pools(g, fmt, pages, G, ps, hd)
+        where = (int(table[0, at // ps]), slice(None), at % ps)
+        cache["v_scale"][where] *= 2.0 ** power
+        code = torch.full((G, hd), TOP[fmt], device="cuda")
+        cache["k_pool"][where] = code.to(DT[fmt])
+        cache["k_scale"][where] = 1.0 / TOP[fmt]                         # a key of ones
+        q = torch.randn(2, H, hd, generator=g, device="cuda") * 0.5
+        # q . ones = -+ 2 power sqrt(hd): a score of that over sqrt(hd), 2^-2.9 power of the others' weight or 2^2.9 power
+        q -= q.mean(-1, keepdim=True)
+        q[:, 0::2] -= 2.0 * power / hd ** 0.5
+        q[:, 1::2] += 2.0 * power / hd ** 0.5
+        q = q.to(DT[dtype])
+        sc = {"k_scale": cache["k_scale"], "v_scale": cache["v_scale"]}
+        out, lse = sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, length, **sc, want_lse=True)
+        want, want_lse, mag = definition(q, cache, table, lens, ps, hd ** -0.5)
+        # the largest p times scale of each head: as an output over values whose every element is their scale
+        largest = torch.zeros(2, H, 1, dtype=torch.float64, device="cuda")
+        for b, n in enumerate(lens):
+            t = torch.arange(n, device="cuda")
+            page, off = table[b].long()[t // ps], t % ps
+            k = (u8(cache["k_pool"])[page, :, off].view(DT[fmt]).double() * cache["k_scale"][page, :, off].double()[..., None]).repeat_interleave(H // G, 1)
+            p = (torch.einsum("hd,nhd->hn", q[b].double(), k) * hd ** -0.5 - want_lse[b][:, None]).exp()
+            largest[b, :, 0] = (p * cache["v_scale"][page, :, off].double().repeat_interleave(H // G, 1).T).amax(1)
+        # As in check(); and products of a probability and a scale are f16, the largest of a run at 2^6 or more of its 2^-25: no position is off by more than 2^-31 of the
+        # largest product times the largest code.  (Where that one's code is 0 the other positions' sum may be below it.)
+        high = want_lse.abs().max().item() * 2.0 ** -21
+        tol = mag * ((2.0 ** -7 if dtype == "bf16" else 0.0) + 5e-5 + high) + max(lens) * 2.0 ** -31 * largest * TOP[fmt]
+        assert ((out.double() - want).abs() <= tol).all(), ((out.double() - want).abs() / tol).max()
+        assert ((lse - want_lse).abs() <= 5e-5 + 1e-6 * want_lse.abs()).all()
+
+
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "bf16"), ("fp32", "fp32"), ("bf16", "e4m3")])
 def test_infinities_and_nan(dtype, fmt):
     """Rows whose scores are all -inf give 0 and -inf; a NaN among the visible positions reaches the heads that see it and no others."""
