@@ -19,6 +19,10 @@ struct DecodeAttn {
 size_t decode_attn_workspace_bytes();
 constexpr int DECODE_MAX_BATCH = 8192;
 // cudaErrorNotSupported: more tiles of positions than an int counts
+// How a call is taken apart: `heads` query heads a warp takes together, `chunks` of them a KV head; the body's columns (tensor cores, else room for as many heads),
+// groups of 16 positions a tile (0: plain FMAs) and warps
+struct DecodePlan { int chunks, heads, columns, groups, warps; };
+DecodePlan decode_attn_plan(int q_f32, int fmt, int batch, int H, int G, int hd, int ctas);
 cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStream_t s);
 
 }  // namespace spec

@@ -7,7 +7,7 @@ namespace spec {
 
 // Eight lanes share a position's keys; then LPT lanes share a position's values, NV vectors of four dimensions each.
 template <int FMT_, int HP_, int DCLASS> struct FmaBody {
-  static constexpr int FMT = FMT_, HP = HP_, TILE = 32, WARPS = HP <= 4 && DCLASS <= 128 ? 16 : 8;      // as many as the registers hold
+  static constexpr int FMT = FMT_, HP = HP_, TILE = 32, WARPS = da_fma_warps(DCLASS, HP);
   static constexpr int LPT = DCLASS == 64 ? 16 : 32, NV = DCLASS == 256 ? 2 : 1, PER = 32 / LPT;
   typedef typename KvElem<FMT>::type E;
   static constexpr int VEC = 16 / sizeof(E), STEPS = DCLASS / VEC / 8 > 0 ? DCLASS / VEC / 8 : 1;      // rounds of eight 16-byte pieces over a row

@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over the paged cache:
 //   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q.k_t - max),  lse = max + log sum_t p_t,   t < length of the sequence.
 //
-// Every key and value is read once and used for the few query heads that share it, so the cache's bytes bound it.  They are dealt out
+// Every key and value is read once for up to 16 of the query heads that share it (a chunk; eight with few sequences, large heads or plain FMAs), so the cache's bytes bound it.  They are dealt out
 // evenly: all tiles of TILE positions, of every sequence and KV head (a segment) one after the other, are cut into equal runs for the CTAs
 // (one wave of them), a CTA's run into equal runs for its warps.  A warp walks its run with a softmax state of its own; what is left
 // of a (sequence, head) that several warps share is joined in shared memory, and of one that several CTAs share by the CTA that
@@ -386,6 +386,9 @@ constexpr size_t DA_SMEM = 224 * 1024;
 // What a CTA reads in the time that a join over CTAs takes.  us with none / 128 / 256 / 512 KB: 64 sequences of 10 to 100 tokens, 40 heads 32.2 / 32.3 /
 // 24.8 / 24.7; 32 of 100 to 400, 8 heads 16.7 / 14.1 / 14.2 / 14.2; 8 of 700 to 1500 16.7 / 16.7 / 16.6 / 17.2.
 constexpr int DA_SPARE_BYTES = 256 * 1024;
+// warps of the bodies: as many as their registers leave room for
+constexpr int da_mma_warps(int hd, int bytes, int columns, int groups) { return hd * bytes * groups <= 128 && columns == 8 ? 16 : 8; }
+constexpr int da_fma_warps(int hd, int heads) { return heads <= 4 && hd <= 128 ? 16 : 8; }
 inline size_t da_smem_bytes(int batch, int warps, int own_floats, int heads, int hd) {
   return ((size_t)(batch + 1) * 4 + 15) / 16 * 16 + sizeof(float) * warps * (own_floats + 2 * da_part_floats(heads, hd));
 }
@@ -402,6 +405,6 @@ template <typename Body> static cudaError_t launch(DaArgs p, int ctas, cudaStrea
 }
 
 cudaError_t launch_decode_fma(const DaArgs &p, int fmt, int ctas, cudaStream_t s);
-cudaError_t launch_decode_mma(const DaArgs &p, int fmt, int ctas, cudaStream_t s);
+cudaError_t launch_decode_mma(const DaArgs &p, int fmt, const DecodePlan &plan, int ctas, cudaStream_t s);
 
 }  // namespace spec

@@ -75,7 +75,7 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
   static constexpr uint32_t FULL = NG == 2 ? 0xffffffffu : 0xffffu;      // all positions of a tile count
   // values a tile ahead as well, where keys and values of a tile are not half a thread's registers
   static constexpr bool V_AHEAD = HD * EB < 512;
-  static constexpr int WARPS = HD * EB * NG <= 128 && MR == 8 ? 16 : 8;
+  static constexpr int WARPS = da_mma_warps(HD, EB, MR, NG);
   static __host__ __device__ int warp_smem_floats(int) { return 0; }
 
   static constexpr float NONE = -1e30f;                  // the reference before any score: far below every one, and yet a number
@@ -433,27 +433,23 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
   }
 };
 
-// NG groups of 16 positions a tile.  A warp waits for a tile's keys and for its values once each, so with long runs a tile of 4 KB of 8-bit keys
-// or values is better read by 8 warps; 16 warps with half of it lose less where runs are short and every (sequence, KV head) begins with a wait
-// of its own.  us with 16 / 8 warps, 8 KV heads of 128 in e4m3 or int8: one sequence of 613 positions 12.0 / 10.7, 4 of 1000 to 8000 19.3 / 17.2, 32 of
-// 100 to 400 13.1 / 11.7, 16 of 8192 56.2 / 55.9, 64 of 256 to 2048 42.5 / 48.3; 40 KV heads, 64 of 10 to 100 26.6 / 30.1: up to two of them a CTA 8 warps.
-template <int FMT, int HD, bool SPLIT> static cudaError_t mma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
-  constexpr int EB = kv_is_8bit(FMT) ? 1 : 2, NG = HD * EB <= 128 ? 2 : 1, ONE = SPLIT ? 4 : 8;
+template <int FMT, int HD, bool SPLIT> static cudaError_t mma_by_heads(const DaArgs &p, const DecodePlan &plan, int ctas, cudaStream_t s) {
+  constexpr int EB = kv_is_8bit(FMT) ? 1 : 2, NG = HD * EB <= 128 ? 2 : 1;
   if constexpr (HD < 256)
-    if (p.heads > ONE) return launch<MmaBody<FMT, HD, 16, SPLIT, NG>>(p, ctas, s);
+    if (plan.columns == 16) return launch<MmaBody<FMT, HD, 16, SPLIT, NG>>(p, ctas, s);
   if constexpr (HD * EB == 128 && EB == 1)
-    if (p.segs > 2 * ctas) return launch<MmaBody<FMT, HD, 8, SPLIT, 1>>(p, ctas, s);
+    if (plan.groups == 1) return launch<MmaBody<FMT, HD, 8, SPLIT, 1>>(p, ctas, s);
   return launch<MmaBody<FMT, HD, 8, SPLIT, NG>>(p, ctas, s);
 }
-template <int FMT, bool SPLIT> static cudaError_t mma_by_hd(const DaArgs &p, int ctas, cudaStream_t s) {
-  return p.a.cache.hd == 64 ? mma_by_heads<FMT, 64, SPLIT>(p, ctas, s) : p.a.cache.hd == 128 ? mma_by_heads<FMT, 128, SPLIT>(p, ctas, s)
-                                                                                            : mma_by_heads<FMT, 256, SPLIT>(p, ctas, s);
+template <int FMT, bool SPLIT> static cudaError_t mma_by_hd(const DaArgs &p, const DecodePlan &plan, int ctas, cudaStream_t s) {
+  return p.a.cache.hd == 64 ? mma_by_heads<FMT, 64, SPLIT>(p, plan, ctas, s) : p.a.cache.hd == 128 ? mma_by_heads<FMT, 128, SPLIT>(p, plan, ctas, s)
+                                                                                                  : mma_by_heads<FMT, 256, SPLIT>(p, plan, ctas, s);
 }
 
-cudaError_t launch_decode_mma(const DaArgs &p, int fmt, int ctas, cudaStream_t s) {
-  if (fmt == KV_BF16) return mma_by_hd<KV_BF16, false>(p, ctas, s);
-  if (fmt == KV_E4M3) return p.q_f32 ? mma_by_hd<KV_E4M3, true>(p, ctas, s) : mma_by_hd<KV_E4M3, false>(p, ctas, s);
-  return p.q_f32 ? mma_by_hd<KV_INT8, true>(p, ctas, s) : mma_by_hd<KV_INT8, false>(p, ctas, s);
+cudaError_t launch_decode_mma(const DaArgs &p, int fmt, const DecodePlan &plan, int ctas, cudaStream_t s) {
+  if (fmt == KV_BF16) return mma_by_hd<KV_BF16, false>(p, plan, ctas, s);
+  if (fmt == KV_E4M3) return p.q_f32 ? mma_by_hd<KV_E4M3, true>(p, plan, ctas, s) : mma_by_hd<KV_E4M3, false>(p, plan, ctas, s);
+  return p.q_f32 ? mma_by_hd<KV_INT8, true>(p, plan, ctas, s) : mma_by_hd<KV_INT8, false>(p, plan, ctas, s);
 }
 
 }  // namespace spec

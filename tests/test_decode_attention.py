@@ -156,6 +156,18 @@ def test_ways_of_dealing_out_the_work(dtype, fmt, B, H, G, hd, ps, least, most):
 
 
 @pytest.mark.parametrize("dtype,fmt", KINDS)
+@pytest.mark.parametrize("B,H,G,hd", [(24, 16, 1, 128), (12, 28, 2, 128), (3, 128, 8, 128), (23, 15, 1, 64), (11, 66, 2, 128), (5, 80, 5, 256)])
+def test_fourteen_and_more_heads_of_a_kv_head(dtype, fmt, B, H, G, hd):
+    """All of them walk the cache together, or by chunks; with 22 (sequence, KV head)s and more."""
+    g = torch.Generator(device="cuda").manual_seed(B * H)
+    lens = torch.randint(0, 500, (B,), generator=g, device="cuda").tolist()
+    table, pages = table_for(g, lens, 16)
+    cache = pools(g, fmt, pages, G, 16, hd)
+    spoil(cache, table, lens, 16)
+    check(torch.randn(B, H, hd, generator=g, device="cuda").to(DT[dtype]), cache, table, lens, 16)
+
+
+@pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("hd", [128, 80])
 def test_scales_queries_and_scores_of_very_different_sizes(dtype, fmt, hd):
     """Values whose scales differ by 2^16 from token to token, queries of 2^-60 and 2^40, a scale of its own, scores that rise with the
