@@ -21,11 +21,11 @@ FORMATS = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.in
 
 
 class CachedDecoder:
-    """A bf16 target (weights as of synth.make_target_weights) with its own paged cache.  scaling: arguments of rope_frequencies for contexts
-    longer than the trained one, e.g. dict(scaling="wavelength", factor=8.0)."""
+    """A bf16 target (weights as of synth.make_target_weights) with its own paged cache for `batch` sequences of up to max_ctx positions; a prompt or step beyond
+    them is refused.  scaling: arguments of rope_frequencies for contexts longer than the trained one, e.g. dict(scaling="wavelength", factor=8.0)."""
 
     def __init__(self, cfg, weights, batch: int, max_ctx: int, cache: str = "e4m3", scaling=None):
-        self.m, self.w, self.batch = cfg, weights, batch
+        self.m, self.w, self.batch, self.max_ctx = cfg, weights, batch, max_ctx
         per_seq = -(-max_ctx // cfg.page_size)
         g = torch.Generator().manual_seed(1)
         self.table = torch.randperm(batch * per_seq, generator=g).view(batch, per_seq).to(torch.int32).cuda()
@@ -69,6 +69,8 @@ class CachedDecoder:
     # -- the loop
     def prefill(self, prompts):
         """Prompts (id sequences) one after the other; the first token of each."""
+        if len(prompts) != self.batch or not all(1 <= len(p) <= self.max_ctx for p in prompts):
+            raise ValueError(f"prefill: {self.batch} prompts of 1 to {self.max_ctx} tokens")
         first, m, ps = [], self.m, 16
         for b, prompt in enumerate(prompts):
             T = len(prompt)
@@ -89,11 +91,15 @@ class CachedDecoder:
             first.append(self._tokens(x[-1:].contiguous())[0])
         self.tokens = torch.cat(first)
         self.lengths = torch.tensor([len(p) for p in prompts], dtype=torch.int32, device="cuda")
+        self.longest = max(len(p) for p in prompts)                      # known here without asking the GPU
         self.seqs = torch.arange(self.batch, dtype=torch.int32, device="cuda")
         return self.tokens
 
     def step(self):
         """(the next token of every sequence int32 [batch] on the GPU, hidden states); nothing waits for the GPU."""
+        if self.longest >= self.max_ctx:
+            raise ValueError(f"step: a sequence has the cache's {self.max_ctx} positions")
+        self.longest += 1
         pos, seen = self.lengths, self.lengths + 1
         x = self.w["embed"][self.tokens.long()].float()
         for i in range(self.m.n_layers):

@@ -29,3 +29,28 @@ def test_tokens_and_hidden_states_as_the_decoder_without_a_draft(cache):
             # reaches the hidden state through attention outputs that are a part of it
             assert (hidden[b].float() - want).norm() / want.norm() < (0.03 if cache == "e4m3" else 0.01), (cache, b)
     dec.close()
+
+
+def test_what_the_cache_has_no_room_for_is_refused():
+    """Prompts longer than max_ctx or none at all, another number of them than sequences, and the step that would pass max_ctx; what fits is computed as in a larger cache."""
+    from paper_2503_01840_b200.kv8_decode import CachedDecoder
+    cfg = synth.ModelCfg("K", "bf16", 1, 512, 4, 2, 128, 1408, 2048, 1024, (0, 0, 0), 1e4, batch=2, tree_depth=2, tree_topk=2, tree_nodes=4, seed=3)
+    w = synth.make_target_weights(cfg, "cuda")
+    small, large = CachedDecoder(cfg, w, 2, 24, "e4m3"), CachedDecoder(cfg, w, 2, 64, "e4m3")
+    g = torch.Generator().manual_seed(2)
+    ids = lambda n: torch.randint(0, 2048, (n,), generator=g).numpy()
+    for bad in ([ids(25), ids(3)], [ids(0), ids(3)], [ids(3)], [ids(3)] * 3):
+        with pytest.raises(ValueError):
+            small.prefill(bad)
+    prompts = [ids(22), ids(7)]
+    assert torch.equal(small.prefill(prompts), large.prefill(prompts))
+    for _ in range(2):
+        assert torch.equal(small.step()[0], large.step()[0])
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            small.step()
+    assert small.lengths.tolist() == [24, 9]
+    large.step()
+    small.prefill([ids(24), ids(24)])
+    with pytest.raises(ValueError):
+        small.step()
