@@ -42,19 +42,22 @@ int dtype_of(at::ScalarType t) {
   if (t == at::kBFloat16) return SPEC_BF16;
   throw Refusal{PyExc_TypeError, std::string("unsupported dtype ") + c10::toString(t)};
 }
+// The current device, asked for once a call (each of the binding's functions sets it to -1): a launch goes there, so every tensor has to be there.
+thread_local int device_of_call = -1;
+void *address(const at::Tensor &t) {
+  if (device_of_call < 0) device_of_call = c10::cuda::current_device();
+  need(t.is_cuda() && t.get_device() == device_of_call, "a tensor is on another device than the current one");
+  return t.data_ptr();
+}
 // int32 of n elements, one behind the other, on the GPU
 void *ints(PyObject *o, int64_t n, const char *what) {
   const at::Tensor &t = tensor(o, what);
   need(t.scalar_type() == at::kInt && t.dim() == 1 && t.size(0) == n && t.is_cuda() && t.is_contiguous(), what);
-  return t.data_ptr();
+  return address(t);
 }
 int32_t *status_of(PyObject *o) { return o == Py_None ? nullptr : (int32_t *)ints(o, 4, "status: int32 [4] on the GPU"); }
 
-// the current stream of a tensor's device, which has to be the current device: a launch goes there
-void *stream_of(const at::Tensor &t) {
-  need(t.is_cuda() && t.get_device() == c10::cuda::current_device(), "the tensors are on another device than the current one");
-  return c10::cuda::getCurrentCUDAStream(t.get_device()).stream();
-}
+void *stream_of_call() { return c10::cuda::getCurrentCUDAStream(device_of_call).stream(); }      // after the first address()
 
 struct Heads {
   void *p;
@@ -63,7 +66,7 @@ struct Heads {
 // [tokens][heads][head_dim] on the GPU with adjacent dimensions
 Heads heads(const at::Tensor &t, const char *what) {
   need(t.dim() == 3 && t.is_cuda() && (t.stride(2) == 1 || t.size(2) == 1), what);
-  return {t.data_ptr(), t.stride(0), t.stride(1)};
+  return {address(t), t.stride(0), t.stride(1)};
 }
 
 bool rope_of(PyObject *freq, PyObject *layout, PyObject *mscale, spec_rope *r) {
@@ -74,7 +77,7 @@ bool rope_of(PyObject *freq, PyObject *layout, PyObject *mscale, spec_rope *r) {
   need(half || (PyUnicode_Check(layout) && PyUnicode_CompareWithASCIIString(layout, "interleaved") == 0), "layout is 'half' or 'interleaved'");
   const double m = PyFloat_AsDouble(mscale);
   if (m == -1.0 && PyErr_Occurred()) throw python_error();
-  *r = spec_rope{(const double *)f.data_ptr(), (int32_t)(2 * f.size(0)), half ? 0 : 1, (float)m};
+  *r = spec_rope{(const double *)address(f), (int32_t)(2 * f.size(0)), half ? 0 : 1, (float)m};
   return true;
 }
 
@@ -97,13 +100,13 @@ spec_kv_cache cache_of(PyObject *const *a) {             // k_pool, v_pool, page
       need(a[i] != Py_None, what);
       const at::Tensor &s = tensor(a[i], what);
       need(s.scalar_type() == at::kFloat && s.sizes() == k.sizes().slice(0, 3) && s.is_contiguous() && s.is_cuda(), what);
-      (i == 3 ? c.k_scale : c.v_scale) = (float *)s.data_ptr();
+      (i == 3 ? c.k_scale : c.v_scale) = (float *)address(s);
     }
   }
   for (int64_t n : {k.size(0), k.size(1), k.size(2), k.size(3), table.size(0), table.size(1)}) need(n <= INT32_MAX, "a cache with more than 2^31 - 1 of something");
-  c.k = k.data_ptr();
-  c.v = v.data_ptr();
-  c.page_table = (const int32_t *)table.data_ptr();
+  c.k = address(k);
+  c.v = address(v);
+  c.page_table = (const int32_t *)address(table);
   c.n_seq = (int32_t)table.size(0);
   c.pages_per_seq = (int32_t)table.size(1);
   c.num_pages = (int32_t)k.size(0);
@@ -116,6 +119,7 @@ spec_kv_cache cache_of(PyObject *const *a) {             // k_pool, v_pool, page
 template <typename F> PyObject *guarded(Py_ssize_t have, Py_ssize_t want, F f) {
   HANDLE_TH_ERRORS
   try {
+    device_of_call = -1;
     if (have != want) throw Refusal{PyExc_TypeError, "wrong number of arguments"};
     return f();
   } catch (const Refusal &r) {
@@ -144,7 +148,7 @@ PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const Heads to = heads(out, "rotary: out [tokens][heads][head_dim] on the GPU with adjacent dimensions");
     need(rope_of(a[2], a[3], a[4], &r), "rotary: inv_freq");
     const int32_t *pos = (const int32_t *)ints(a[1], x.size(0), "rotary: positions int32 [tokens] on the GPU");
-    void *const s = stream_of(x);
+    void *const s = stream_of_call();
     const bool transpose = PyObject_IsTrue(a[6]) == 1;
     const int32_t T = (int32_t)x.size(0), H = (int32_t)x.size(1), hd = (int32_t)x.size(2);
     const int rc = call([&] { return rotary_(dtype, from.p, from.ts, from.hs, to.p, to.ts, to.hs, pos, T, H, hd, &r, transpose, s); });
@@ -179,7 +183,7 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int32_t *pos = (const int32_t *)ints(a[8], T, "kv_append: row_pos int32 [tokens] on the GPU");
     const int32_t *kvpos = a[9] == Py_None ? nullptr : (const int32_t *)ints(a[9], T, "kv_append: row_kvpos int32 [tokens] on the GPU");
     int32_t *const status = status_of(a[14]);
-    void *const s = stream_of(k);
+    void *const s = stream_of_call();
     // a call without tokens has queries without an address
     const int rc = T == 0 ? SPEC_OK : call([&] {
       return append_(dtype, hq.p, hq.ts, hq.hs, q_out.defined() ? q_out.data_ptr() : nullptr, (int32_t)H, hk.p, hk.ts, hk.hs, hv.p, hv.ts, hv.hs, seq, pos, kvpos, (int32_t)T,
@@ -212,7 +216,7 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int32_t *const status = status_of(a[8]);
     const auto options = pool.options().dtype(dtype == SPEC_F32 ? at::kFloat : at::kBFloat16);
     const at::Tensor k = at::empty({rows, c.n_kv_heads, c.head_dim}, options), v = at::empty({rows, c.n_kv_heads, c.head_dim}, options);
-    void *const s = stream_of(pool);
+    void *const s = stream_of_call();
     const int rc = call([&] { return read_(&c, seq, pos, (int32_t)rows, (int32_t)dtype, k.data_ptr(), v.data_ptr(), status, s); });
     return rc ? PyLong_FromLong(rc) : pair(k, v);
   });
@@ -245,16 +249,18 @@ PyObject *decode_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
     const at::Tensor out = a[9] == Py_None ? at::empty(q.sizes(), q.options(), at::MemoryFormat::Contiguous) : tensor(a[9], "out");
     need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type() && out.is_contiguous() && out.is_cuda(), "decode_attention: out contiguous, of q's shape and dtype");
+    void *const to = address(out);
     const bool want_lse = PyObject_IsTrue(a[8]) == 1;
     at::Tensor lse;
     if (want_lse) lse = at::empty({B, H}, q.options().dtype(at::kFloat));
     const int32_t *length = (const int32_t *)ints(a[6], B, "decode_attention: lengths int32 [batch] on the GPU");
     int32_t *const status = status_of(a[11]);
-    void *const s = stream_of(q);
+    void *const s = stream_of_call();
     const at::Tensor w = a[10] == Py_None ? workspace_of(q, s) : tensor(a[10], "workspace");
     need(w.is_cuda() && w.is_contiguous(), "decode_attention: workspace of decode_workspace()");
+    void *const work = address(w);
     const int rc = call([&] {
-      return attend_(dtype, hq.p, hq.ts, &c, length, (int32_t)B, (int32_t)H, (float)scale, out.data_ptr(), want_lse ? (float *)lse.data_ptr() : nullptr, w.data_ptr(), w.nbytes(),
+      return attend_(dtype, hq.p, hq.ts, &c, length, (int32_t)B, (int32_t)H, (float)scale, to, want_lse ? (float *)lse.data_ptr() : nullptr, work, w.nbytes(),
                      status, s);
     });
     if (rc) return PyLong_FromLong(rc);

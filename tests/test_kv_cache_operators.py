@@ -416,3 +416,33 @@ def test_c_refusals_without_a_device():
     assert attend(cache(), scale=math.nan) == -1 and attend(cache(), q=None) == -2 and attend(cache(), q=258) == -1 and attend(cache(), ts=257) == -1
     assert attend(cache(), ws=None) == -2 and attend(cache(), ws=264) == -3 and attend(cache(), nb=n - 1) == -3 and attend(cache(n_seq=9000), batch=9000) == -8
     assert attend(cache(), dtype=0) == -1
+
+
+@gpu
+def test_tensors_of_another_gpu_are_refused(monkeypatch):
+    """Each tensor of a call by turns; torch's fake tensors stand for those of a second GPU (they have its device and no memory, and it need not be there)."""
+    from torch._subclasses import fake_tensor
+    monkeypatch.setattr(fake_tensor, "init_gpu_context", lambda device: None)
+    fake = fake_tensor.FakeTensorMode()
+
+    def away(t):
+        with fake:
+            return torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device="cuda:1")
+
+    cache = make_cache(torch.Generator().manual_seed(1), "int8", 4, 2, 16, 64, 2, 2)
+    x, k, pos = torch.zeros(2, 4, 64, device="cuda"), torch.zeros(2, 2, 64, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    freq, _ = sb.rope_frequencies(64, 1e4)
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    seq = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    calls = ((sb.rotary, dict(x=x, positions=pos, inv_freq=freq, out=torch.empty_like(x))),
+             (sb.rotary_backward, dict(grad=x, positions=pos, inv_freq=freq, out=torch.empty_like(x))),
+             (sb.kv_append, dict(cache, k=k, v=k.clone(), row_seq=seq, row_pos=pos, row_kvpos=pos.clone(), q=x, inv_freq=freq, status=status)),
+             (sb.kv_read, dict(cache, row_seq=seq, row_kvpos=pos, status=status)),
+             (sb.decode_attention, dict(cache, q=x, lengths=pos, out=torch.empty_like(x), workspace=sb.decode_workspace(), status=status)))
+    for f, good in calls:
+        f(**good)
+        for name, t in good.items():
+            with pytest.raises(ValueError):
+                f(**{**good, name: away(t)})
+        f(**good)
+    assert not status.any()
