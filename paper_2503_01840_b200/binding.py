@@ -542,23 +542,45 @@ def rope_frequencies(rot_dim: int, theta: float, scaling: Optional[str] = None, 
     return torch.from_numpy(f).to(device), mscale
 
 
+class _Rotary(torch.autograd.Function):
+    """The map is linear and its transpose is the same kernel's other direction, so a gradient can be differentiated again."""
+
+    @staticmethod
+    def forward(ctx, x, positions, inv_freq, layout, mscale, transpose):
+        ctx.save_for_backward(positions, inv_freq)
+        ctx.how = layout, mscale, transpose
+        return _rotary(x, positions, inv_freq, layout, mscale, None, transpose)
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, inv_freq = ctx.saved_tensors
+        layout, mscale, transpose = ctx.how
+        if grad.stride(2) != 1:                          # of a sum, for one: expanded
+            grad = grad.contiguous()
+        return _rotary(grad, positions, inv_freq, layout, mscale, None, not transpose), None, None, None, None, None
+
+
+def _rotary(x, positions, inv_freq, layout, mscale, out, transpose):
+    r = (_marshal_module or _marshal()).rotary(x, positions, inv_freq, layout, mscale, out, transpose)
+    if type(r) is int:
+        raise SpecError(r, "spec_rotary")
+    if r is NotImplemented:
+        _need(out is None, "rotary: out goes with tensors that need no gradient")
+        return _Rotary.apply(x, positions, inv_freq, layout, mscale, transpose)
+    return r
+
+
 def rotary(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0,
            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [tokens][heads][head_dim] (any token and head stride: a view of a fused projection will do) with the first 2 * pairs dimensions of
-    every head turned to positions int32 [tokens].  out may be x."""
-    r = (_marshal_module or _marshal()).rotary(x, positions, inv_freq, layout, mscale, out, False)
-    if type(r) is int:
-        raise SpecError(r, "spec_rotary")
-    return r
+    every head turned to positions int32 [tokens].  out may be x.  Autograd takes x's gradient through it (with out it refuses an x that needs one)."""
+    return _rotary(x, positions, inv_freq, layout, mscale, out, False)
 
 
 def rotary_backward(grad: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0,
                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """The gradient with respect to rotary's x of one with respect to its output."""
-    r = (_marshal_module or _marshal()).rotary(grad, positions, inv_freq, layout, mscale, out, True)
-    if type(r) is int:
-        raise SpecError(r, "spec_rotary")
-    return r
+    """The gradient with respect to rotary's x of one with respect to its output, for loops that take it by hand."""
+    return _rotary(grad, positions, inv_freq, layout, mscale, out, True)
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_seq: torch.Tensor,
@@ -567,7 +589,7 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: to
               row_kvpos: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """Writes k, v [tokens][kv heads][head_dim] to a paged cache: token t to position row_kvpos[t] (default row_pos[t]) of sequence row_seq[t]
     (-1: nowhere), its keys turned to row_pos[t] where inv_freq is given, both quantised where the pools are float8_e4m3fn or int8.
-    Returns the turned q [tokens][heads][head_dim], if there is one."""
+    Returns the turned q [tokens][heads][head_dim], if there is one.  For serving: autograd does not see it, nor what is read back or attended to."""
     r = (_marshal_module or _marshal()).kv_append(k, v, k_pool, v_pool, page_table, k_scale, v_scale, row_seq, row_pos, row_kvpos, q, inv_freq, layout, mscale, status)
     if type(r) is int:
         raise SpecError(r, "spec_kv_append")

@@ -7,6 +7,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/Functions.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
@@ -136,7 +137,7 @@ template <typename F> int call(F f) {
   return rc;
 }
 
-// x, positions, inv_freq, layout, mscale, out, transpose
+// x, positions, inv_freq, layout, mscale, out, transpose.  NotImplemented where autograd has to record it: binding.py wraps it then.
 PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> PyObject * {
     const at::Tensor &x = tensor(a[0], "x");
@@ -145,6 +146,7 @@ PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int dtype = dtype_of(x.scalar_type());
     const at::Tensor out = a[5] == Py_None ? at::empty(x.sizes(), x.options(), at::MemoryFormat::Contiguous) : tensor(a[5], "out");
     need(out.sizes() == x.sizes() && out.scalar_type() == x.scalar_type(), "rotary: out has x's shape and dtype");
+    if (at::GradMode::is_enabled() && (x.requires_grad() || out.requires_grad())) Py_RETURN_NOTIMPLEMENTED;
     const Heads to = heads(out, "rotary: out [tokens][heads][head_dim] on the GPU with adjacent dimensions");
     need(rope_of(a[2], a[3], a[4], &r), "rotary: inv_freq");
     const int32_t *pos = (const int32_t *)ints(a[1], x.size(0), "rotary: positions int32 [tokens] on the GPU");

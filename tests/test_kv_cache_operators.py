@@ -75,6 +75,43 @@ def test_rotary_and_gradient(dtype, T, H, hd, rot, layout):
     assert torch.equal(dev.cpu()[rest], wide[rest])
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_autograd_takes_the_gradient(dtype, layout):
+    """Of a view of a projection, through a sum (whose gradient is expanded), with a second pass over the same x, and of the gradient itself; the same bits as
+    rotary_backward's.  No graph where none is wanted."""
+    T, H, hd = 33, 3, 64
+    g = torch.Generator().manual_seed(7)
+    wide = torch.randn(T, H + 1, hd, generator=g).to(DT[dtype]).cuda().requires_grad_()
+    pos = torch.randint(0, 100000, (T,), generator=g, dtype=torch.int32).cuda()
+    freq = sb.rope_frequencies(hd // 2, 1e4)[0]
+    w = torch.randn(T, H, hd, generator=g).to(DT[dtype]).cuda()
+    kw = dict(layout=layout, mscale=1.25)
+    y = sb.rotary(wide[:, :H], pos, freq, **kw)
+    with torch.no_grad():
+        plain = sb.rotary(wide[:, :H], pos, freq, **kw)
+    assert y.requires_grad and not plain.requires_grad and torch.equal(y, plain) and not sb.rotary(wide.detach(), pos, freq, **kw).requires_grad
+    (y * w).sum().backward()
+    want = sb.rotary_backward(w, pos, freq, **kw)
+    assert torch.equal(wide.grad[:, :H], want) and not wide.grad[:, H:].any()
+    wide.grad = None
+    sb.rotary(wide[:, :H], pos, freq, **kw).sum().backward()
+    assert torch.equal(wide.grad[:, :H], sb.rotary_backward(torch.ones_like(w), pos, freq, **kw))
+    x, v = wide.detach()[:, :H].clone().requires_grad_(), w.clone().requires_grad_()
+    (gx,) = torch.autograd.grad(sb.rotary(x, pos, freq, **kw), x, v, create_graph=True)
+    (gv,) = torch.autograd.grad((gx * x.detach()).sum(), v)
+    assert torch.equal(gx, sb.rotary_backward(v.detach(), pos, freq, **kw)) and torch.equal(gv, sb.rotary(x.detach(), pos, freq, **kw))
+    (gb,) = torch.autograd.grad(sb.rotary_backward(x, pos, freq, **kw), x, w)
+    assert torch.equal(gb, sb.rotary(w, pos, freq, **kw))
+    with pytest.raises(ValueError):
+        sb.rotary(x, pos, freq, out=torch.empty_like(w), **kw)
+    with pytest.raises(ValueError):
+        sb.rotary(w, pos, freq, out=x, **kw)
+    with torch.no_grad():
+        assert torch.equal(sb.rotary(x, pos, freq, out=torch.empty_like(w), **kw), sb.rotary(x, pos, freq, **kw))
+
+
 def test_frequencies():
     """The kinds of scaling at their ends: fast pairs kept, the slowest divided by the factor, everything between the two."""
     base, one = sb.rope_frequencies(128, 5e5, device="cpu")
