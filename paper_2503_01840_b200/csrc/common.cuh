@@ -5,6 +5,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+#include <mutex>
+
 namespace spec {
 
 typedef __nv_bfloat16 bf16;
@@ -96,15 +99,23 @@ inline cudaError_t launch_k(void (*kern)(KArgs...), dim3 grid, dim3 block, size_
 
 // Kernel function attributes belong to one device: remembers, per device ordinal, the largest dynamic
 // shared-memory size a kernel has been configured with, and raises the limit on the current device when needed.
+// Threads may come with different sizes at once: under the lock a limit only ever grows.
 struct SmemLimit {
-  int have[64] = {};
+  std::atomic<int> have[64] = {};
+  std::mutex lock;
+  template <typename Set> bool raise(int dev, int smem, Set set) {      // set(size): false where the device refuses it
+    const bool kept = dev >= 0 && dev < 64;
+    if (kept && smem <= have[dev].load(std::memory_order_acquire)) return true;
+    std::lock_guard<std::mutex> held(lock);
+    if (kept && smem <= have[dev].load(std::memory_order_relaxed)) return true;
+    if (!set(smem)) return false;
+    if (kept) have[dev].store(smem, std::memory_order_release);
+    return true;
+  }
   template <typename F> bool ensure(F kern, int smem) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
-    if (dev >= 0 && dev < 64 && smem <= have[dev]) return true;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return false;
-    if (dev >= 0 && dev < 64) have[dev] = smem;
-    return true;
+    return raise(dev, smem, [&](int size) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, size) == cudaSuccess; });
   }
 };
 
