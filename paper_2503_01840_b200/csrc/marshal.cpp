@@ -247,7 +247,7 @@ PyObject *decode_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (a[7] != Py_None) {
       scale = PyFloat_AsDouble(a[7]);
       if (scale == -1.0 && PyErr_Occurred()) throw python_error();
-      need(scale < 0 || scale > 0, "decode_attention: scale is a number and not 0");
+      need((float)scale < 0 || (float)scale > 0, "decode_attention: scale is a number, and not 0 in 32 bits");      // 0: the entry point's default
     }
     const at::Tensor out = a[9] == Py_None ? at::empty(q.sizes(), q.options(), at::MemoryFormat::Contiguous) : tensor(a[9], "out");
     need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type() && out.is_contiguous() && out.is_cuda(), "decode_attention: out contiguous, of q's shape and dtype");

@@ -408,3 +408,22 @@ def test_refusals():
         assert e.value.code == code
     with pytest.raises(TypeError):
         sb.decode_attention(**{**good, "q": q.half()})
+
+
+def test_a_scale_that_is_zero_in_32_bits_is_refused():
+    """The C entry point takes 0 for its default.  The smallest scales that are not 0 count: all scores then are as good as 0."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    cache = pools(g, "int8", 4, 2, 16, 64)
+    table, n = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2), torch.tensor([20, 32], dtype=torch.int32, device="cuda")
+    q = torch.randn(2, 4, 64, generator=g, device="cuda")
+    run = lambda scale: sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, n, k_scale=cache["k_scale"], v_scale=cache["v_scale"], scale=scale)
+    for scale in (1e-60, -1e-60, 2.0 ** -151):
+        with pytest.raises(ValueError):
+            run(scale)
+    v = cache["v_pool"].float() * cache["v_scale"][..., None]
+    for scale in (2.0 ** -149, -1e-40):
+        out = run(scale)
+        for b in range(2):
+            mean = v[table[b].long()].transpose(1, 2).reshape(32, 2, 64)[: int(n[b])].mean(0).repeat_interleave(2, 0)
+            # sums of at most 32 values of up to 4 or so, rounded to 22 bits of the products at worst
+            assert ((out[b] - mean).abs() <= 1e-5).all()
