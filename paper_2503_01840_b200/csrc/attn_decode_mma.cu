@@ -78,7 +78,7 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
   static constexpr int WARPS = da_mma_warps(HD, EB, MR, NG);
   static __host__ __device__ int warp_smem_floats(int) { return 0; }
 
-  static constexpr float NONE = -1e30f;                  // the reference before any score: far below every one, and yet a number
+  static constexpr float NONE = -3.40282346638528860e38f;      // the reference before any score: the lowest number, so that none is below it
   float r[NB][2], l[NB][2], o[NB][STEPS][4];             // reference, sum and O of heads 8 n + 2 t and the next
   uint32_t q[NB][STEPS][2];
   float wide[SPLIT ? NB : 1][SPLIT ? STEPS : 1][4];      // queries as they are, until begin()

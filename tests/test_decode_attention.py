@@ -427,3 +427,39 @@ def test_a_scale_that_is_zero_in_32_bits_is_refused():
             mean = v[table[b].long()].transpose(1, 2).reshape(32, 2, 64)[: int(n[b])].mean(0).repeat_interleave(2, 0)
             # sums of at most 32 values of up to 4 or so, rounded to 22 bits of the products at worst
             assert ((out[b] - mean).abs() <= 1e-5).all()
+
+
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+@pytest.mark.parametrize("hd", [64, 80, 128, 256])
+def test_scores_far_below_zero(dtype, fmt, hd):
+    """All scores of a head at -1e29 .. -2e38: where they are equal the output is the mean of the values, where one is higher than the others by a 64th it is that one's value."""
+    g = torch.Generator(device="cuda").manual_seed(hd)
+    lens, ps, H, G = [77, 16, 1], 16, 4, 2
+    table, pages = table_for(g, lens, ps)
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q = -torch.ones(3, H, hd, device="cuda").to(DT[dtype])
+    for size in (1e29, 1e31, 1e35, 2e38):
+        for best in (None, 0, 13):
+            cache = pools(g, fmt, pages, G, ps, hd)
+            k = torch.full((pages, G, ps), size / hd, device="cuda")
+            if best is not None:
+                for b, n in enumerate(lens):
+                    k[int(table[b, min(best, n - 1) // ps]), :, min(best, n - 1) % ps] *= 63 / 64
+            if fmt in TOP:
+                cache["k_pool"], cache["k_scale"] = torch.ones_like(cache["k_pool"], dtype=torch.float32).to(DT[fmt]), k
+            else:
+                cache["k_pool"] = k[..., None].expand(-1, -1, -1, hd).contiguous().to(DT[fmt])
+            out, lse = sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, length, k_scale=cache["k_scale"], v_scale=cache["v_scale"], scale=1.0, want_lse=True)
+            for b, n in enumerate(lens):
+                t = torch.arange(n, device="cuda") if best is None else torch.tensor([min(best, n - 1)], device="cuda")
+                page, off = table[b].long()[t // ps], t % ps
+                v = u8(cache["v_pool"])[page, :, off].view(cache["v_pool"].dtype).double()
+                if fmt in TOP:
+                    v = v * cache["v_scale"][page, :, off].double()[..., None]
+                v = v.repeat_interleave(H // G, 1)
+                # weights of 1 / n are exact in every type but for the sum's rounding; bf16 outputs round by 2^-8 at most, products in f16 by 2^-11
+                tol = v.abs().mean(0) * ((2.0 ** -8 + 2.0 ** -11 if dtype == "bf16" else 0.0) + 5e-5)
+                assert ((out[b].double() - v.mean(0)).abs() <= tol).all(), (size, best, b)
+                # the score in its keys' rounding (bf16: 2^-8), sums of equal terms and the turn to powers of two and back
+                want = -size * (1.0 if best is None else 63 / 64)
+                assert ((lse[b].double() - want).abs() <= size * (2.0 ** -8 if fmt == "bf16" else 1e-5)).all(), (size, best, b)
