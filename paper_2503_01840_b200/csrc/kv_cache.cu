@@ -226,6 +226,17 @@ static bool whole_pieces(const void *p, long long ts, long long hs, size_t e) { 
   return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ts * (long long)e) | (uintptr_t)(hs * (long long)e)) & 15) == 0;
 }
 
+// Few tokens: a round's heads a block (of several tokens where one has fewer heads than that and every SM has a block), so that no thread has a second round to wait
+// for; many: about six rounds a block.  One head goes as two of which the second is not there: ceil(2^32 / 1) is no 32-bit number.  us of 16384 tokens of one head of
+// 64 / 128 in bf16: a token a block 22.2 / 20.8, sixteen 4.3 / 6.1; of 64 tokens of two heads: sixteen a block 2.5, one 1.8.
+RopePlan rope_plan(int tokens, int heads, int step) {
+  const long long rounds = ((long long)tokens * heads + step - 1) / step;
+  const int slots = max(2, heads);
+  if (rounds > 1184) return {max(1, min(ROPE_MAX_TOKENS, 6 * step / slots)), slots};
+  const int h = min(slots, step);
+  return {min(min(ROPE_MAX_TOKENS, step / h), (tokens + 147) / 148), h};
+}
+
 template <typename T, int FMT> static cudaError_t rope_append(const RopeAppend &a, cudaStream_t s) {
   constexpr int VE = 16 / sizeof(T);
   const int G = a.k.p ? a.cache.G : 0, all = a.H + 2 * G, lh = a.hd / (2 * VE);
@@ -237,21 +248,13 @@ template <typename T, int FMT> static cudaError_t rope_append(const RopeAppend &
   gr.lh_shift = __builtin_ctz(lh);
   const int step = ROPE_THREADS / lh;                    // heads of a round of the block
   constexpr int U = 1;
-  // few tokens: a round's heads a block (of several tokens where one has fewer heads than that), so that no thread has a second round to wait
-  // for; many: about six rounds a block
-  const long long rounds = ((long long)a.tokens * all + step - 1) / step;
-  if (rounds <= 1184) {
-    gr.heads = min(all, step);
-    gr.per_block = min(ROPE_MAX_TOKENS, step / gr.heads);
-  } else {
-    gr.heads = all;
-    gr.per_block = max(1, min(ROPE_MAX_TOKENS, 6 * step / all));
-  }
+  const RopePlan plan = rope_plan(a.tokens, all, step);
+  gr.heads = plan.heads;
+  gr.per_block = plan.per_block;
   gr.by_half = a.rope.half > 1 ? (uint32_t)((0x100000000ull + a.rope.half - 1) / a.rope.half) : 0;
   gr.q_ts = (int)a.q.ts, gr.q_hs = (int)a.q.hs, gr.k_ts = (int)a.k.ts, gr.k_hs = (int)a.k.hs, gr.v_ts = (int)a.v.ts, gr.v_hs = (int)a.v.hs;
   gr.o_ts = (int)a.qo_ts, gr.o_hs = (int)a.qo_hs;
-  gr.by_heads = gr.heads == 1 ? 0xffffffffu : (uint32_t)((0x100000000ull + gr.heads - 1) / gr.heads);
-  if (gr.heads == 1 && gr.per_block > 1) gr.per_block = 1;
+  gr.by_heads = (uint32_t)((0x100000000ull + gr.heads - 1) / gr.heads);
   const dim3 grid((a.tokens + gr.per_block - 1) / gr.per_block, (all + gr.heads - 1) / gr.heads);
   const size_t smem = (size_t)gr.per_block * 2 * a.rope.half * sizeof(float);
   if (a.rope.interleaved) return launch_k(rope_append_kernel<T, FMT, true, U>, grid, dim3(ROPE_THREADS), smem, s, a, gr);

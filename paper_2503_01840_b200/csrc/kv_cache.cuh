@@ -49,6 +49,9 @@ struct RopeAppend {
   KvCache cache;
   int32_t *status;
 };
+// Tokens and heads of a block, of `heads` heads a token, `step` of which it rotates at a time
+struct RopePlan { int per_block, heads; };
+RopePlan rope_plan(int tokens, int heads, int step);
 cudaError_t launch_rope_append(const RopeAppend &a, int dtype, int fmt, cudaStream_t s);
 
 struct KvRead {
