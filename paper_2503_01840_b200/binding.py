@@ -83,7 +83,7 @@ def lib():
     global _lib
     if _lib is not None:
         return _lib
-    path = _build.build()
+    path = _build.build_library()
     L = C.CDLL(path)
     vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
     L.spec_workspace_bytes.restype = sz
@@ -497,7 +497,7 @@ def _marshal():
     global _marshal_module
     if _marshal_module is None:
         L = lib()
-        spec = importlib.util.spec_from_file_location("_marshal", _build.MARSHAL)
+        spec = importlib.util.spec_from_file_location("_marshal", _build.build_marshal())
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)
         m.use(*[C.cast(f, C.c_void_p).value for f in (L.spec_rotary, L.spec_kv_append, L.spec_kv_read, L.spec_decode_attention, L.spec_decode_attention_workspace_bytes)])

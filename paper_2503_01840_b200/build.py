@@ -3,7 +3,7 @@
     python -m paper_2503_01840_b200.build [--force] [--verbose]
 
 nvcc cross-compiles without a GPU; the resulting .so is loaded by `binding` through ctypes.  g++ compiles _marshal.so, the part of the
-binding that takes torch tensors apart in C++.
+binding that takes torch tensors apart in C++ for the operators beside the step; each is built for itself where `binding` finds it missing or stale.
 """
 import concurrent.futures
 import os
@@ -22,18 +22,18 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std
          "--expt-relaxed-constexpr"]
 
 
-def _deps_mtime():
-    m = 0.0
-    for root in (CSRC, os.path.join(os.path.dirname(HERE), "include")):
-        for f in os.listdir(root):
-            if f.endswith((".cu", ".cuh", ".h", ".cpp")):
-                m = max(m, os.path.getmtime(os.path.join(root, f)))
-    return m
+def _stale(target, ends):
+    """Whether target is missing or older than the sources that end like this"""
+    if not os.path.exists(target):
+        return True
+    newest = max(os.path.getmtime(os.path.join(root, f)) for root in (CSRC, os.path.join(os.path.dirname(HERE), "include"))
+                 for f in os.listdir(root) if f.endswith(ends))
+    return os.path.getmtime(target) < newest
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    newest = _deps_mtime()
-    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= newest for f in (LIB, MARSHAL)):
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """libspec_b200.so, which SpecDecoder and the C ABI need: nvcc alone makes it."""
+    if not force and not _stale(LIB, (".cu", ".cuh", ".h")):
         return LIB
     os.makedirs(OBJ, exist_ok=True)
     extra = ["-Xptxas", "-v"] if verbose else []
@@ -43,36 +43,47 @@ def build(force: bool = False, verbose: bool = False) -> str:
         r = subprocess.run([NVCC, *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj], capture_output=True, text=True)
         return src, obj, r
 
-    def marshal():
-        import sysconfig
-
-        import torch
-        at = os.path.dirname(torch.__file__)
-        tmp = MARSHAL + ".%d.tmp" % os.getpid()
-        cuda = os.path.dirname(os.path.dirname(NVCC))
-        r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
-                            *["-I" + d for d in (at + "/include", at + "/include/torch/csrc/api/include", cuda + "/include", sysconfig.get_paths()["include"])],
-                            os.path.join(CSRC, "marshal.cpp"), "-o", tmp, "-L" + at + "/lib", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda",
-                            "-Wl,-rpath," + at + "/lib"], capture_output=True, text=True)
-        return tmp, r
-
     objs = []
     with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
-        tail = ex.submit(marshal)
         for src, obj, r in ex.map(cc, SOURCES):
             if verbose or r.returncode:
                 sys.stderr.write(f"--- {src}\n{r.stdout}{r.stderr}\n")
             if r.returncode:
                 raise RuntimeError(f"nvcc failed on {src}")
             objs.append(obj)
-        made, r = tail.result()
-        if r.returncode:
-            sys.stderr.write(f"--- marshal.cpp\n{r.stdout}{r.stderr}\n")
-            raise RuntimeError("g++ failed on marshal.cpp")
     tmp = LIB + ".%d.tmp" % os.getpid()
     subprocess.run([NVCC, "-shared", "-o", tmp, *objs, "-gencode", "arch=compute_100a,code=sm_100a"], check=True)
-    os.replace(made, MARSHAL)
     os.replace(tmp, LIB)
+    return LIB
+
+
+def build_marshal(force: bool = False) -> str:
+    """_marshal.so, which the operators beside the step need: with Python's and torch's headers and g++."""
+    if not force and not _stale(MARSHAL, ("marshal.cpp", ".h")):
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    at = os.path.dirname(torch.__file__)
+    tmp = MARSHAL + ".%d.tmp" % os.getpid()
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                        *["-I" + d for d in (at + "/include", at + "/include/torch/csrc/api/include", cuda + "/include", sysconfig.get_paths()["include"])],
+                        os.path.join(CSRC, "marshal.cpp"), "-o", tmp, "-L" + at + "/lib", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda",
+                        "-Wl,-rpath," + at + "/lib"], capture_output=True, text=True)
+    if r.returncode:
+        sys.stderr.write(f"--- marshal.cpp\n{r.stdout}{r.stderr}\n")
+        raise RuntimeError("the compiler failed on marshal.cpp")
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """Both; the library's path."""
+    with concurrent.futures.ThreadPoolExecutor(max_workers=1) as ex:
+        tail = ex.submit(build_marshal, force)
+        build_library(force, verbose)
+        tail.result()
     return LIB
 
 
