@@ -2,19 +2,21 @@
 
     python -m paper_2503_01840_b200.build [--force] [--verbose]
 
-nvcc cross-compiles without a GPU; the resulting .so is loaded by `binding` through ctypes.  g++ compiles _marshal.so, the part of the
+nvcc cross-compiles without a GPU; the resulting .so is loaded by `binding` through ctypes.  g++ compiles _marshal.*.so, the part of the
 binding that takes torch tensors apart in C++ for the operators beside the step; each is built for itself where `binding` finds it missing or stale.
 """
 import concurrent.futures
+import importlib.metadata
 import os
+import re
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libspec_b200.so")
-MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["api.cu", "elementwise.cu", "gemm_ref.cu", "tma_maps.cu", "gemm_fused.cu", "gemm_wide.cu", "attn_ref.cu", "attn_fast.cu",
            "attn_causal.cu", "tree.cu", "kv_cache.cu", "attn_decode.cu", "attn_decode_fma.cu", "attn_decode_mma.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
@@ -57,15 +59,20 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
-def build_marshal(force: bool = False) -> str:
-    """_marshal.so, which the operators beside the step need: with Python's and torch's headers and g++."""
-    if not force and not _stale(MARSHAL, ("marshal.cpp", ".h")):
-        return MARSHAL
-    import sysconfig
+def marshal_path() -> str:
+    """The module's file: made for one Python and one torch, whose names it carries, so that another one's is never loaded."""
+    torch_version = re.sub(r"[^A-Za-z0-9.]", "_", importlib.metadata.version("torch"))
+    return os.path.join(HERE, f"_marshal.torch-{torch_version}{sysconfig.get_config_var('EXT_SUFFIX')}")
 
+
+def build_marshal(force: bool = False) -> str:
+    """The module that the operators beside the step need: with Python's and torch's headers and g++."""
+    path = marshal_path()
+    if not force and not _stale(path, ("marshal.cpp", ".h")):
+        return path
     import torch
     at = os.path.dirname(torch.__file__)
-    tmp = MARSHAL + ".%d.tmp" % os.getpid()
+    tmp = path + ".%d.tmp" % os.getpid()
     cuda = os.path.dirname(os.path.dirname(NVCC))
     r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
                         *["-I" + d for d in (at + "/include", at + "/include/torch/csrc/api/include", cuda + "/include", sysconfig.get_paths()["include"])],
@@ -74,8 +81,8 @@ def build_marshal(force: bool = False) -> str:
     if r.returncode:
         sys.stderr.write(f"--- marshal.cpp\n{r.stdout}{r.stderr}\n")
         raise RuntimeError("the compiler failed on marshal.cpp")
-    os.replace(tmp, MARSHAL)
-    return MARSHAL
+    os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

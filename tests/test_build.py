@@ -25,7 +25,7 @@ def test_the_library_needs_no_headers_of_python_or_torch(monkeypatch, tmp_path):
     monkeypatch.setattr(build.subprocess, "run", run)
     monkeypatch.setattr(build, "LIB", str(tmp_path / "lib.so"))
     monkeypatch.setattr(build, "OBJ", str(tmp_path / "obj"))
-    monkeypatch.setattr(build, "MARSHAL", str(tmp_path / "_marshal.so"))
+    monkeypatch.setattr(build, "marshal_path", lambda: str(tmp_path / "_marshal.so"))
     monkeypatch.setenv("CXX", "false")
     assert build.build_library() == str(tmp_path / "lib.so") and all(c[0] == build.NVCC for c in ran)
     with pytest.raises(RuntimeError):
@@ -40,11 +40,11 @@ def test_the_library_needs_no_headers_of_python_or_torch(monkeypatch, tmp_path):
 
 def test_each_is_built_again_for_its_own_sources(monkeypatch, tmp_path):
     build.build_library()
-    monkeypatch.setattr(build, "MARSHAL", str(tmp_path / "_marshal.so"))
+    monkeypatch.setattr(build, "marshal_path", lambda: str(tmp_path / "_marshal.so"))
     monkeypatch.setattr(build, "LIB", str(tmp_path / "lib.so"))
     newest = {ends: max(os.path.getmtime(os.path.join(build.CSRC, f)) for f in os.listdir(build.CSRC) if f.endswith(ends)) for ends in ((".cu", ".cuh"), ("marshal.cpp",))}
     header = os.path.getmtime(os.path.join(os.path.dirname(build.HERE), "include", "spec_b200.h"))
-    for target, ends, check in ((build.LIB, (".cu", ".cuh"), (".cu", ".cuh", ".h")), (build.MARSHAL, ("marshal.cpp",), ("marshal.cpp", ".h"))):
+    for target, ends, check in ((build.LIB, (".cu", ".cuh"), (".cu", ".cuh", ".h")), (build.marshal_path(), ("marshal.cpp",), ("marshal.cpp", ".h"))):
         assert build._stale(target, check)
         open(target, "w").close()
         t = max(newest[ends], header)
@@ -52,3 +52,15 @@ def test_each_is_built_again_for_its_own_sources(monkeypatch, tmp_path):
         assert not build._stale(target, check)
         os.utime(target, (t - 1, t - 1))
         assert build._stale(target, check)
+
+
+def test_a_module_for_another_torch_or_python_is_not_loaded(monkeypatch):
+    here = build.marshal_path()
+    assert build.build_marshal() == here and os.path.exists(here)
+    with monkeypatch.context() as m:
+        m.setattr(build.importlib.metadata, "version", lambda name: "99.1+other")
+        other = build.marshal_path()
+        assert other != here and build._stale(other, ("marshal.cpp", ".h"))
+    with monkeypatch.context() as m:
+        m.setattr(build.sysconfig, "get_config_var", lambda name: ".cpython-399.so")
+        assert build.marshal_path() not in (here, other)
