@@ -511,15 +511,17 @@ def _need(ok: bool, what: str):
 
 
 def rope_frequencies(rot_dim: int, theta: float, scaling: Optional[str] = None, factor: float = 1.0, trained: int = 8192, low: float = 1.0,
-                     high: float = 4.0, device="cuda"):
+                     high: Optional[float] = None, device="cuda"):
     """(inv_freq float64 [rot_dim / 2] in radians a position, mscale) of rotary positions, theta^(-2 i / rot_dim) scaled for contexts
     `factor` times the `trained` one:
       None          as they are
       "linear"      all divided by the factor (positions interpolated)
       "ntk"         theta grown so that the slowest pair is divided by the factor and the fastest kept
       "wavelength"  pairs that turn more than `high` times in the trained context kept, less than `low` times divided, in between
-                    mixed in proportion to the turns
-      "rotations"   the same with the mixing in proportion to the pair's index (YaRN: low 1, high 32), and mscale 0.1 ln(factor) + 1"""
+                    mixed in proportion to the turns; high 4 unless given
+      "rotations"   the same with the mixing in proportion to the pair's index (YaRN), and mscale 0.1 ln(factor) + 1; high 32 unless given"""
+    if high is None:
+        high = 32.0 if scaling == "rotations" else 4.0
     _need(rot_dim > 0 and rot_dim % 2 == 0 and theta > 1 and factor >= 1 and trained > 0 and 0 < low < high,
           "rope_frequencies: rot_dim even and positive, theta > 1, factor >= 1, 0 < low < high")
     i = np.arange(0, rot_dim, 2, dtype=np.float64) / rot_dim

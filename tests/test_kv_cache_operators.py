@@ -132,6 +132,32 @@ def test_frequencies():
             sb.rope_frequencies(**{"rot_dim": 64, "theta": 1e4, "device": "cpu", **bad})
 
 
+@pytest.mark.parametrize("rot,theta,factor,trained", [(128, 5e5, 8.0, 8192), (64, 1e4, 4.0, 4096), (80, 1e6, 2.5, 32768)])
+def test_frequencies_between_their_ends(rot, theta, factor, trained):
+    """The by-parts scalings pair by pair, with the bounds that they have unless others are given."""
+    wav, one = sb.rope_frequencies(rot, theta, "wavelength", factor, trained, device="cpu")
+    rotations, m = sb.rope_frequencies(rot, theta, "rotations", factor, trained, device="cpu")
+    assert one == 1.0 and m == pytest.approx(0.1 * math.log(factor) + 1.0, rel=1e-15)
+    # the pairs (as real numbers) that turn 32 times and once in the trained context, brought to whole ones outwards
+    first, last = ((rot / 2) * math.log(trained / (2 * math.pi * turns), theta) for turns in (32.0, 1.0))
+    first, last = max(math.floor(first), 0), min(math.ceil(last), rot - 1)
+    for i in range(rot // 2):
+        f = theta ** (-2.0 * i / rot)
+        length = 2 * math.pi / f                                         # positions of a turn
+        if length < trained / 4:
+            want = f
+        elif length > trained:
+            want = f / factor
+        else:
+            part = (trained / length - 1.0) / 3.0
+            want = (1.0 - part) * f / factor + part * f
+        assert float(wav[i]) == pytest.approx(want, rel=1e-12)
+        part = min(max((i - first) / (last - first), 0.0), 1.0)
+        assert float(rotations[i]) == pytest.approx((1.0 - part) * f + part * f / factor, rel=1e-12)
+    assert torch.equal(rotations, sb.rope_frequencies(rot, theta, "rotations", factor, trained, 1.0, 32.0, device="cpu")[0])
+    assert torch.equal(wav, sb.rope_frequencies(rot, theta, "wavelength", factor, trained, 1.0, 4.0, device="cpu")[0])
+
+
 def make_cache(g, fmt, pages, G, ps, hd, seqs, pps):
     """Pools that hold junk, a table of distinct pages"""
     dev = {}
