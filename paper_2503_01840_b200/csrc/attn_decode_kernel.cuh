@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   // ---- units (tiles and beginnings) before each sequence, their sum, and the longest sequence's.  Up to 32 sequences: a lane each in every warp, and no barrier
   // on the way to the first load; more: a run of them per thread, a scan over the threads, and a table.
   const bool few = B <= 32;
-  auto units_of = [&](int len) { return len ? (len + TILE - 1) / TILE + DA_START : 0; };
+  auto units_of = [&](int len) { return len ? (len - 1) / TILE + 1 + DA_START : 0; };      // (len + TILE - 1 may be none of an int)
   int total, longest = 0, my_before = 0, my_tiles = 0;
   if (few) {
     my_tiles = lane < B ? units_of(da_length(p, lane)) : 0;

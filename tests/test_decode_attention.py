@@ -463,3 +463,23 @@ def test_scores_far_below_zero(dtype, fmt, hd):
                 # the score in its keys' rounding (bf16: 2^-8), sums of equal terms and the turn to powers of two and back
                 want = -size * (1.0 if best is None else 63 / 64)
                 assert ((lse[b].double() - want).abs() <= size * (2.0 ** -8 if fmt == "bf16" else 1e-5)).all(), (size, best, b)
+
+
+@pytest.mark.parametrize("dtype,fmt,hd", [("bf16", "e4m3", 64), ("fp32", "int8", 32)])
+def test_a_sequence_of_as_many_positions_as_an_int_counts(dtype, fmt, hd):
+    """2^31 - 2 of them, in pages that are all the same one: the output of that page alone, and its sum as many times.  (Tensor cores' tiles and plain FMAs'.)"""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ps, n = 42966, 49981
+    cache = pools(g, fmt, 1, 1, ps, hd)
+    table = torch.zeros(1, n, dtype=torch.int32, device="cuda")
+    q = torch.randn(1, 4, hd, generator=g, device="cuda").to(DT[dtype])
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    run = lambda m: sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, torch.tensor([m], dtype=torch.int32, device="cuda"), k_scale=cache["k_scale"],
+                                        v_scale=cache["v_scale"], want_lse=True, status=status)
+    one, lse1 = run(ps)
+    out, lse = run(ps * n)
+    assert not status.any() and ps * n == 2 ** 31 - 2
+    # a lane adds up to 2^18 terms one after the other, each sum rounded by 2^-24; bf16 outputs by 2^-8 twice; relative to sum p |v|, of which no value is above 6
+    assert ((lse - lse1) - math.log(n)).abs().max() <= 2.0 ** -6 + 1e-5
+    assert ((out.double() - one.double()).abs() <= 6 * 2.0 ** -5 + (2.0 ** -7 * one.double().abs() if dtype == "bf16" else 0)).all()
+    assert (out.double() - one.double()).norm() <= 0.05 * one.double().norm()
