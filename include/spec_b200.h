@@ -375,7 +375,8 @@ int spec_kv_read(const spec_kv_cache *cache, const int32_t *row_seq, const int32
  * g = h / (n_heads / n_kv_heads), over sequence b of the cache; lse (optional) float [batch][n_heads], the natural-log normaliser.
  * lengths int32 [batch]; a length of 0 gives zeros and -inf.  q: heads adjacent, tokens q_token_stride elements apart, 16-byte
  * aligned (stride too); out [batch][n_heads][head_dim].  scale 0: head_dim^-1/2.  batch <= 8192, batch <= n_seq,
- * n_heads <= 65536.
+ * n_heads <= 65536.  Work is counted in tiles of 16 positions or more on the device; the lengths are not known here, so SPEC_ERR_UNSUPPORTED goes by the page table's
+ * width: (pages_per_seq * page_size / 16 + 3) * batch * (chunks of at most 4 to 16 query heads of all KV heads) above 2^30 may be refused, below it is not.
  * workspace: spec_decode_attention_workspace_bytes() bytes, 256-byte aligned, zero before the first call; a call leaves it ready for
  * the next on the same stream, and calls that may overlap need one each. */
 size_t spec_decode_attention_workspace_bytes(void);

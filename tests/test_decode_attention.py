@@ -483,3 +483,16 @@ def test_a_sequence_of_as_many_positions_as_an_int_counts(dtype, fmt, hd):
     assert ((lse - lse1) - math.log(n)).abs().max() <= 2.0 ** -6 + 1e-5
     assert ((out.double() - one.double()).abs() <= 6 * 2.0 ** -5 + (2.0 ** -7 * one.double().abs() if dtype == "bf16" else 0)).all()
     assert (out.double() - one.double()).norm() <= 0.05 * one.double().norm()
+
+
+def test_large_calls_are_refused_by_the_tables_width():
+    """2^16 pages of 4096 positions for each of 128 sequences are more than 2^30 tiles, whatever the lengths say; for 32 sequences they are not."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    cache = pools(g, "e4m3", 2, 1, 4096, 128)
+    table = torch.zeros(1, 1 << 16, dtype=torch.int32, device="cuda").repeat(64, 1)
+    q = torch.randn(128, 1, 128, generator=g, device="cuda").to(torch.bfloat16)
+    run = lambda b, t: sb.decode_attention(q[:b], cache["k_pool"], cache["v_pool"], t, torch.full((b,), 5, dtype=torch.int32, device="cuda"), k_scale=cache["k_scale"], v_scale=cache["v_scale"])
+    with pytest.raises(sb.SpecError) as e:
+        run(128, table.repeat(2, 1))
+    assert e.value.code == -8
+    assert torch.equal(run(32, table[:32]), run(32, table[:32, :1].contiguous()))
