@@ -67,6 +67,7 @@ struct Heads {
 // [tokens][heads][head_dim] on the GPU with adjacent dimensions
 Heads heads(const at::Tensor &t, const char *what) {
   need(t.dim() == 3 && t.is_cuda() && (t.stride(2) == 1 || t.size(2) == 1), what);
+  for (int64_t n : t.sizes()) need(n <= INT32_MAX, "a tensor with more than 2^31 - 1 of something");
   return {address(t), t.stride(0), t.stride(1)};
 }
 
@@ -211,6 +212,7 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const spec_kv_cache c = cache_of(a);
     const at::Tensor &pool = THPVariable_Unpack(a[0]), &seq_t = tensor(a[5], "row_seq");
     const int64_t rows = seq_t.dim() == 1 ? seq_t.size(0) : -1;
+    need(rows <= INT32_MAX, "a tensor with more than 2^31 - 1 of something");
     const int32_t *seq = (const int32_t *)ints(a[5], rows, "kv_read: row_seq int32 [rows] on the GPU");
     const int32_t *pos = (const int32_t *)ints(a[6], rows, "kv_read: row_kvpos int32 [rows] on the GPU");
     const long dtype = PyLong_AsLong(a[7]);

@@ -509,3 +509,22 @@ def test_tensors_of_another_gpu_are_refused(monkeypatch):
                 f(**{**good, name: away(t)})
         f(**good)
     assert not status.any()
+
+
+@gpu
+def test_more_than_an_int_counts_is_refused():
+    """Tokens and heads are handed on in 32 bits.  (Expanded tensors: they have one element's memory, and no output is made for them.)"""
+    cache = make_cache(torch.Generator().manual_seed(1), "int8", 4, 2, 16, 64, 2, 2)
+    freq, _ = sb.rope_frequencies(64, 1e4)
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    x = torch.zeros(1, 1, 64, device="cuda")
+    many = (1 << 32) + 1
+    for wide in (x.expand(1, many, 64), x.expand(many, 1, 64)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            sb.rotary(wide, one, freq)
+        with pytest.raises(ValueError, match="2\\^31"):
+            sb.kv_append(x.expand(1, 2, 64), x.expand(1, 2, 64), cache["k_pool"], cache["v_pool"], cache["page_table"], one, one, cache["k_scale"], cache["v_scale"], q=wide)
+        with pytest.raises(ValueError, match="2\\^31"):
+            sb.decode_attention(wide, cache["k_pool"], cache["v_pool"], cache["page_table"], one, cache["k_scale"], cache["v_scale"])
+    with pytest.raises(ValueError, match="2\\^31"):
+        sb.kv_read(cache["k_pool"], cache["v_pool"], cache["page_table"], one.expand(many), one.expand(many), cache["k_scale"], cache["v_scale"])
