@@ -9,7 +9,9 @@
 // the probabilities: each head's products are multiplied by a power of two that puts its largest so far near 2^6 (f16 holds 2^-24 .. 2^16), and O is divided by it
 // in the end.  It follows the products, not the scales: a value's scale far above the others' costs those nothing where its probability is small.
 // The reference that probabilities are relative to follows the maximum only where a score passes it by more than 8 (in powers of two), and that power only where a product
-// passes 2^15; both change by whole powers of two, exactly.
+// passes 2^15; over 8-bit caches both change by whole powers of two, exactly.
+// Over a bf16 cache probabilities become bf16, as the MMA has both operands of one type and f16 would not hold the values: 2^-9 of each, which makes the output's error against 64 bits
+// 2.3e-3 where its own rounding to bf16 is 1.7e-3.  Two parts of each, as fp32 queries get, would take columns that groups of 5 and more heads use.
 //
 // Measured: 16 sequences of 4097 to 32768 positions, 64 / 8 heads of 128, in bf16 192 us (6.3 TB/s, 98 % of a copy's rate); 16 of 8192, 32 / 8 heads, in
 // bf16 91 us, in e4m3 55 (5.0 TB/s), in int8 57.  What is left there is the ten microseconds around the loop (launch, first loads, joins).
@@ -328,8 +330,10 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
             for (int u = 0; u < NG; u++) m = fmaxf(m, fmaxf(s[u][n][e], s[u][n][e + 2]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            m = ceilf(m);
-            float f = power_of_two(-(int)fminf(m - r[n][e], 127.0f));      // 2^-127: 0
+            // 8 bits: whole powers of two, so that both changes are exact (2^-127: 0).  bf16: the maximum itself, whose probability then is 1 and loses nothing
+            float f;
+            if constexpr (Q8) m = ceilf(m), f = power_of_two(-(int)fminf(m - r[n][e], 127.0f));
+            else f = da_ex2(r[n][e] - m);
             r[n][e] = m;
             l[n][e] *= f;
             if constexpr (Q8) {
