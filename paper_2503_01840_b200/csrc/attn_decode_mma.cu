@@ -10,8 +10,9 @@
 // in the end.  It follows the products, not the scales: a value's scale far above the others' costs those nothing where its probability is small.
 // The reference that probabilities are relative to follows the maximum only where a score passes it by more than 8 (in powers of two), and that power only where a product
 // passes 2^15; over 8-bit caches both change by whole powers of two, exactly.
-// Over a bf16 cache probabilities become bf16, as the MMA has both operands of one type and f16 would not hold the values: 2^-9 of each, which makes the output's error against 64 bits
-// 2.3e-3 where its own rounding to bf16 is 1.7e-3.  Two parts of each, as fp32 queries get, would take columns that groups of 5 and more heads use.
+// Over a bf16 cache the MMA has both operands in bf16 (f16 would not hold the values), so probabilities go in two parts of eight bits, one MMA each into the same O: in one part
+// they made the output's error against 64 bits 2.3e-3, where its own rounding to bf16 is 1.7e-3.  The tensor pipe has the room; us with one part /
+// two: 16 sequences of 4096, 32 / 8 heads of 128 51.3 / 51.3, 16 of 4097 to 32768, 64 / 8 195.8 / 196.2, 128 / 8 60.3 / 60.8, 7 of 16384, 64 / 4 heads of 64 39.4 / 39.7.
 //
 // Measured: 16 sequences of 4097 to 32768 positions, 64 / 8 heads of 128, in bf16 192 us (6.3 TB/s, 98 % of a copy's rate); 16 of 8192, 32 / 8 heads, in
 // bf16 91 us, in e4m3 55 (5.0 TB/s), in int8 57.  What is left there is the ten microseconds around the loop (launch, first loads, joins).
@@ -293,6 +294,7 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
             }
       }
       uint32_t b[NG][NB][2];                             // as the MMA takes them
+      uint32_t rest[Q8 ? 1 : NG][Q8 ? 1 : NB][2];        // bf16: what that leaves of them
       float sum[NB][2];
       // A second pass, after a reference or a power has changed, is rare past the first tiles.  (One copy of this code: with two, heads of 256 took 65 us
       // instead of 56, 16 sequences of 4096, 8 KV heads in e4m3.)
@@ -317,7 +319,12 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
                   over |= w[e] > 32768.0f;
                 }
               }
-              b[u][n][i] = Q8 ? part_of(w[0], w[1], SPLIT ? t >> 1 : 0) : pack_bf16(w[0], w[1]);
+              if constexpr (Q8) {
+                b[u][n][i] = part_of(w[0], w[1], SPLIT ? t >> 1 : 0);
+              } else {
+                b[u][n][i] = pack_bf16(w[0], w[1]);
+                rest[u][n][i] = pack_bf16(w[0] - __uint_as_float(b[u][n][i] << 16), w[1] - __uint_as_float(b[u][n][i] & 0xffff0000u));
+              }
             }
         }
         if (!__any_sync(0xffffffffu, over && pass == 0)) break;
@@ -357,7 +364,10 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
 #pragma unroll
         for (int u = 0; u < NG; u++)
 #pragma unroll
-          for (int i = 0; i < 2; i++) b[u][n][i] = da_transpose(b[u][n][i]);      // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
+          for (int i = 0; i < 2; i++) {
+            if constexpr (!Q8) rest[u][n][i] = da_transpose(rest[u][n][i]);
+            b[u][n][i] = da_transpose(b[u][n][i]);       // [positions g][heads 2t, 2t + 1] -> [head g][positions 2t, 2t + 1]
+          }
       }
       // ---- output
       if (live != FULL) {                                // a page that is none: zero times whatever stands in page 0 is to be zero
@@ -388,7 +398,10 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
           } else {
             const uint32_t a0 = __byte_perm(v0, v1, 0x5410), a1 = __byte_perm(v0, v1, 0x7632), a2 = __byte_perm(v2, v3, 0x5410), a3 = __byte_perm(v2, v3, 0x7632);
 #pragma unroll
-            for (int n = 0; n < NB; n++) da_mma<false>(o[n][j], a0, a1, a2, a3, b[u][n][0], b[u][n][1]);
+            for (int n = 0; n < NB; n++) {
+              da_mma<false>(o[n][j], a0, a1, a2, a3, b[u][n][0], b[u][n][1]);
+              da_mma<false>(o[n][j], a0, a1, a2, a3, rest[u][n][0], rest[u][n][1]);
+            }
           }
         }
       }

@@ -496,3 +496,25 @@ def test_large_calls_are_refused_by_the_tables_width():
         run(128, table.repeat(2, 1))
     assert e.value.code == -8
     assert torch.equal(run(32, table[:32]), run(32, table[:32, :1].contiguous()))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("H,G,hd", [(32, 8, 128), (16, 1, 128), (8, 4, 64), (8, 2, 256), (8, 2, 80)])
+def test_outputs_in_bf16_lose_little_but_their_own_rounding(fmt, H, G, hd):
+    """Keys of which some dimensions are larger than the others, so that few positions count: the error is that of rounding the definition to bf16, but for probabilities of sixteen bits or
+    (8-bit caches, times the value's scale) of eleven: 2^-12 of each at most, independent of one another, next to the output's 2^-9 in the mean; a 20th is more than that makes."""
+    g = torch.Generator(device="cuda").manual_seed(H + hd)
+    B, ps = 24, 16
+    lens = torch.randint(1, 1500, (B,), generator=g, device="cuda").tolist()
+    table, pages = table_for(g, lens, ps)
+    cache = pools(g, fmt, pages, G, ps, hd)
+    gain = torch.ones(hd, device="cuda")
+    gain[:: max(1, hd // 4)] = 6.0
+    if fmt in TOP:
+        cache["k_scale"] *= 2.5
+    else:
+        cache["k_pool"] = (cache["k_pool"].float() * gain).to(DT[fmt])
+    q = torch.randn(B, H, hd, generator=g, device="cuda").to(torch.bfloat16)
+    out = sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, torch.tensor(lens, dtype=torch.int32, device="cuda"), k_scale=cache["k_scale"], v_scale=cache["v_scale"])
+    want, _, _ = definition(q, cache, table, lens, ps, hd ** -0.5)
+    assert (out.double() - want).norm() <= 1.05 * (want.to(torch.bfloat16).double() - want).norm()
