@@ -22,7 +22,8 @@ constexpr int DECODE_MAX_BATCH = 8192;
 // How a call is taken apart: `heads` query heads a warp takes together, `chunks` of them a KV head; the body's columns (tensor cores, else room for as many heads),
 // groups of 16 positions a tile (0: plain FMAs) and warps
 struct DecodePlan { int chunks, heads, columns, groups, warps; };
-DecodePlan decode_attn_plan(int q_f32, int fmt, int batch, int H, int G, int hd, int ctas);
+// positions: that a sequence's row of the page table holds
+DecodePlan decode_attn_plan(int q_f32, int fmt, int batch, int H, int G, int hd, int ctas, long long positions = 1ll << 31);
 cudaError_t launch_decode_attn(const DecodeAttn &a, int dtype, int fmt, cudaStream_t s);
 
 }  // namespace spec

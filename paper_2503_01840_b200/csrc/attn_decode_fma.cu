@@ -8,6 +8,7 @@ namespace spec {
 // Eight lanes share a position's keys; then LPT lanes share a position's values, NV vectors of four dimensions each.
 template <int FMT_, int HP_, int DCLASS> struct FmaBody {
   static constexpr int FMT = FMT_, HP = HP_, TILE = 32, WARPS = da_fma_warps(DCLASS, HP);
+  static constexpr bool HALVES = false;
   static constexpr int LPT = DCLASS == 64 ? 16 : 32, NV = DCLASS == 256 ? 2 : 1, PER = 32 / LPT;
   typedef typename KvElem<FMT>::type E;
   static constexpr int VEC = 16 / sizeof(E), STEPS = DCLASS / VEC / 8 > 0 ? DCLASS / VEC / 8 : 1;      // rounds of eight 16-byte pieces over a row
@@ -23,12 +24,12 @@ template <int FMT_, int HP_, int DCLASS> struct FmaBody {
 
   __device__ __forceinline__ void init(const DaArgs &p, const DaSeg &sg, float *mem, int lane) {
     qs = mem;
-    const int hd = p.a.cache.hd, h0 = sg.kv * p.group + sg.chunk * p.heads, have = min(p.heads, p.group - sg.chunk * p.heads);
+    const int hd = p.a.cache.hd;
     __syncwarp();
     for (int i = lane; i < HP * hd; i += 32) {
       const int h = i / hd;
-      const size_t at = (size_t)sg.b * p.a.q_ts + (size_t)(h0 + h) * hd + (i - h * hd);
-      qs[i] = h < have ? (p.q_f32 ? ((const float *)p.a.q)[at] : to_f32(((const bf16 *)p.a.q)[at])) * (p.a.scale * 1.44269504088896341f) : 0.0f;
+      const size_t at = (size_t)sg.b * p.a.q_ts + (size_t)(sg.head + h) * hd + (i - h * hd);
+      qs[i] = h < sg.have ? (p.q_f32 ? ((const float *)p.a.q)[at] : to_f32(((const bf16 *)p.a.q)[at])) * (p.a.scale * 1.44269504088896341f) : 0.0f;
     }
     __syncwarp();
 #pragma unroll
@@ -177,9 +178,9 @@ template <int FMT, int HP> static cudaError_t fma_by_hd(const DaArgs &p, int cta
   return launch<FmaBody<FMT, HP, 256>>(p, ctas, s);
 }
 template <int FMT> static cudaError_t fma_by_heads(const DaArgs &p, int ctas, cudaStream_t s) {
-  if (p.heads <= 1) return fma_by_hd<FMT, 1>(p, ctas, s);
-  if (p.heads <= 2) return fma_by_hd<FMT, 2>(p, ctas, s);
-  if (p.heads <= 4) return fma_by_hd<FMT, 4>(p, ctas, s);
+  if (p.deal.heads <= 1) return fma_by_hd<FMT, 1>(p, ctas, s);
+  if (p.deal.heads <= 2) return fma_by_hd<FMT, 2>(p, ctas, s);
+  if (p.deal.heads <= 4) return fma_by_hd<FMT, 4>(p, ctas, s);
   return fma_by_hd<FMT, 8>(p, ctas, s);
 }
 

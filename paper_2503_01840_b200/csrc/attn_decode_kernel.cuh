@@ -15,17 +15,30 @@ namespace spec {
 // one sequence of 16384 18.6 / 17.5 / 17.4 / 17.7, 8 of 700 to 1500 14.0 / 12.6 / 12.7 / 13.3, 4 of 1000 to 8000 17.6 / 16.3 / 16.2 / 16.1, 64 of 256 to 2048
 // 42.1 / 41.8 / 41.4 / 40.9.
 constexpr int DA_START = 2;
+// Bodies of 16 columns take a KV head's heads by halves where there are fewer units than this a CTA, as the lengths on the device say: the join of 16 heads' states by 8 warps then costs more than
+// the second walk.  us whole / by halves, heads of 128 in e4m3, sequences x KV heads, tables of 65536 positions: 40 x 1 with 16 query heads of 100 to 400 (3 units) 19.5 / 10.8, of 1000 to 2000 (13)
+// 23.7 / 20.6, 60 x 1 (20) 25.2 / 22.6, 16 x 2 of 4096 (28) 27.2 / 26.2, 64 x 2 of 256 to 2048 (33) 30.7 / 35.1; bf16, 15 x 2 of 500 to 1500 (13) 21.6 / 17.2, 16 x 2 of 4096 (56) 29.5 / 33.0.
+constexpr int DA_HALVE_BELOW = 24;
 constexpr int DA_MAX_CTAS = 160;           // CTAs of a launch, at most
 constexpr int DA_PART_FLOATS = 8 * 256 + 16 * 2;      // a partial state: O of heads x hd <= 2048 elements, then (max, sum) of up to 16 heads
+
+// How the heads of a KV head go together
+struct DaDeal {
+  int heads, chunks;            // query heads a warp takes together, and how many such chunks share a KV head
+  int vheads, segs;             // KV heads x chunks; segments of the call
+  int whole;                    // segments that a CTA gets at most where they stay whole (0: they do not)
+};
 
 // workspace: partial states of each CTA's first and last segment, and a counter per CTA for the segment that starts in it
 struct DaArgs {
   DecodeAttn a;
   int page_shift;               // log2 of the page size, or -1
   int q_f32;                    // queries and output in fp32
-  int group, vheads, segs;      // query heads per KV head; KV heads x chunks; segments of the call
-  int whole, spare;             // segments that a CTA gets at most where they stay whole (0: they do not); tiles that one may have beyond its share then
-  int heads, chunks;            // query heads a warp takes together, and how many such chunks share a KV head
+  int group;                    // query heads per KV head
+  int spare;                    // tiles that a CTA may have beyond its share where segments stay whole
+  DaDeal deal;
+  DaDeal halves;                // bodies of 16 columns: where there are fewer units than halve_below (a KV head's heads as one chunk)
+  int halve_below;
   unsigned *count;              // [CTAs], zero between calls
   float *part;                  // [CTAs][2][part_floats], close together: another page of memory costs a walk of the page tables
 };
@@ -34,7 +47,8 @@ __host__ __device__ constexpr int da_part_floats(int heads, int hd) { return hea
 
 // A run of tiles of one (sequence, chunk of heads)
 struct DaSeg {
-  int b, kv, chunk;             // sequence, KV head, chunk of its query heads
+  int b, kv;                    // sequence, KV head
+  int head, have;               // its chunk's first query head, and how many there are
   int t0, t1, tiles;            // tiles t0 .. t1 - 1 of `tiles`
   int u0;                       // the first of them, in units over all segments
 };
@@ -150,12 +164,11 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   pdl_trigger();
   constexpr int W = Body::WARPS, THREADS = W * 32, TILE = Body::TILE;
   extern __shared__ __align__(16) char smem[];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.a.batch, hd = p.a.cache.hd, cta = blockIdx.x, VH = p.vheads;
-  const int heads = p.heads, part_floats = da_part_floats(heads, hd);     // O [heads][hd], then (max, sum) [heads]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.a.batch, hd = p.a.cache.hd, cta = blockIdx.x;
   int *before = (int *)smem;
   float *mem = (float *)(smem + ((size_t)(B + 1) * 4 + 15) / 16 * 16);
   float *warp_mem = mem + warp * Body::warp_smem_floats(hd);
-  float *states = mem + W * Body::warp_smem_floats(hd);                  // [2 W][part_floats]
+  float *const states = mem + W * Body::warp_smem_floats(hd);            // [2 W][part_floats]
   __shared__ int2 scan[W];
   __shared__ DaSeg seg[2 * W];                                           // of the partial states; b = -1: none
   __shared__ DaRun runs[2 * W];
@@ -207,6 +220,10 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     __syncthreads();
     total = before[B];
   }
+  bool halved = false;
+  if constexpr (Body::HALVES) halved = total * p.a.cache.G < p.halve_below;
+  const DaDeal &deal = halved ? p.halves : p.deal;
+  const int heads = deal.heads, chunks = deal.chunks, VH = deal.vheads, part_floats = da_part_floats(heads, hd);      // a state: O [heads][hd], then (max, sum) [heads]
   total *= VH;
   if (lane < 2) seg[2 * warp + lane].b = -1;
   // (units before sequence b, those of each of its segments); all lanes ask for the same one
@@ -224,15 +241,15 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   int c0 = cta < N ? begin_of(cta) : 0, c1 = cta < N ? begin_of(cta + 1) : 0;
   // Joining states of several CTAs takes six microseconds, in which a CTA reads `spare` tiles.  Where no CTA gets that many more than its
   // share when segments stay whole, they do.
-  if (p.whole && ((long long)p.whole * longest - p.spare) * (int)gridDim.x <= total) {
+  if (deal.whole && ((long long)deal.whole * longest - p.spare) * (int)gridDim.x <= total) {
     auto start_of = [&](int j) {
       const int b = da_quotient(j, VH);
       if (b >= B) return total;
       const int2 t = tiles_of(b);
       return t.x * VH + (j - b * VH) * t.y;
     };
-    c0 = start_of((int)((unsigned)p.segs * (unsigned)cta / gridDim.x));
-    c1 = start_of((int)((unsigned)p.segs * (unsigned)(cta + 1) / gridDim.x));
+    c0 = start_of((int)((unsigned)deal.segs * (unsigned)cta / gridDim.x));
+    c1 = start_of((int)((unsigned)deal.segs * (unsigned)(cta + 1) / gridDim.x));
   }
   const int w0 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)warp / W), w1 = c0 + (int)((unsigned)(c1 - c0) * (unsigned)(warp + 1) / W);
 
@@ -261,8 +278,10 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     }
     const int2 t = tiles_of(s.b);
     const int r = u - t.x * VH, v = da_quotient(r, t.y), x = r - v * t.y, end = min(t.y, x + (w1 - u));      // units x .. end - 1 of the segment's
-    s.kv = p.chunks == 1 ? v : da_quotient(v, p.chunks);
-    s.chunk = v - s.kv * p.chunks;
+    s.kv = chunks == 1 ? v : da_quotient(v, chunks);
+    const int before_it = (v - s.kv * chunks) * heads;                   // query heads of the chunks before this one
+    s.head = s.kv * p.group + before_it;
+    s.have = min(heads, p.group - before_it);
     s.tiles = t.y - DA_START;
     s.t0 = max(x - DA_START, 0);
     s.t1 = end - DA_START;
@@ -281,8 +300,8 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     });
     if (whole) {                                                         // the slot is free again until the run's last segment
       __syncwarp();
-      const size_t row = (size_t)s.b * p.a.H + s.kv * p.group + s.chunk * heads;
-      for (int h = 0; h < min(heads, p.group - s.chunk * heads); h++)
+      const size_t row = (size_t)s.b * p.a.H + s.head;
+      for (int h = 0; h < s.have; h++)
         da_join_head(st, part_floats, 0, 1u, heads * hd, h, hd, nullptr, (char *)p.a.out + (row + h) * hd * (p.q_f32 ? 4 : 2), p.q_f32, p.a.lse ? p.a.lse + row + h : nullptr);
     } else {
       if (lane == 0) seg[2 * warp + slot] = s;
@@ -298,13 +317,13 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
   constexpr int SHIFT = 5;                                               // states of a part
   static_assert(DA_MAX_CTAS / (1 << SHIFT) + 2 <= 2 * W, "room for the parts of level 1");
   auto make_run = [&](int at, const DaSeg &s, const float *from, int stride, int skew, uint32_t mask, float *to) {
-    runs[at] = DaRun{from, to, s.b * p.a.H + s.kv * p.group + s.chunk * heads, min(heads, p.group - s.chunk * heads), stride, skew, mask};
+    runs[at] = DaRun{from, to, s.b * p.a.H + s.head, s.have, stride, skew, mask};
   };
   int n_runs = 0, n_open = 0;
   DaSeg open_seg{};                                                      // lanes 0 and 1 of warp 0: what other CTAs have the rest of
   if (warp == 0) {
     // lane i looks at partial state i; a run of one segment's states begins where the one before it is another's
-    const DaSeg mine = lane < 2 * W ? seg[lane] : DaSeg{-1, 0, 0, 0, 0, 0, 0};
+    const DaSeg mine = lane < 2 * W ? seg[lane] : DaSeg{-1, 0, 0, 0, 0, 0, 0, 0};
     const uint32_t some = __ballot_sync(0xffffffffu, mine.b >= 0), below = (1u << lane) - 1;
     const int prev = (some & below) ? 31 - __clz(some & below) : lane;
     const int pu = __shfl_sync(0xffffffffu, mine.u0, prev);
@@ -319,8 +338,8 @@ __global__ void __launch_bounds__(Body::WARPS * 32, 1) decode_attn_kernel(const 
     const uint32_t opens = __ballot_sync(0xffffffffu, open);
     n_open = __popc(opens);
     const int from = lane == 0 ? __ffs(opens) - 1 : 31 - __clz(opens);
-    open_seg.b = __shfl_sync(0xffffffffu, mine.b, from & 31), open_seg.kv = __shfl_sync(0xffffffffu, mine.kv, from & 31);
-    open_seg.chunk = __shfl_sync(0xffffffffu, mine.chunk, from & 31), open_seg.tiles = __shfl_sync(0xffffffffu, mine.tiles, from & 31);
+    open_seg.b = __shfl_sync(0xffffffffu, mine.b, from & 31), open_seg.head = __shfl_sync(0xffffffffu, mine.head, from & 31);
+    open_seg.have = __shfl_sync(0xffffffffu, mine.have, from & 31), open_seg.tiles = __shfl_sync(0xffffffffu, mine.tiles, from & 31);
     open_seg.u0 = __shfl_sync(0xffffffffu, mine.u0, from & 31);
     if (lane == 0) to_do[0] = __popc(all), to_do[1] = n_open;
   }
@@ -395,11 +414,13 @@ inline size_t da_smem_bytes(int batch, int warps, int own_floats, int heads, int
 template <typename Body> static cudaError_t launch(DaArgs p, int ctas, cudaStream_t s) {
   static SmemLimit limit;
   const long long tiles = ((long long)p.a.cache.pages_per_seq * p.a.cache.page_size + Body::TILE - 1) / Body::TILE;
-  if ((tiles + DA_START) * p.a.batch * p.a.cache.G * p.chunks > (1 << 30)) return cudaErrorNotSupported;
+  const long long units = (tiles + DA_START) * p.a.batch * p.a.cache.G;
+  if (units * p.deal.chunks > (1 << 30)) return cudaErrorNotSupported;
   // (with fewer segments than half the CTAs the others stay without work: one user at 613 tokens 12.3 us dealt out evenly, 13.0 whole)
-  p.whole = p.segs * 2 >= ctas && p.segs < (1 << 24) ? (p.segs + ctas - 1) / ctas : 0;
+  for (DaDeal *d : {&p.deal, &p.halves}) d->whole = d->segs * 2 >= ctas && d->segs < (1 << 24) ? (d->segs + ctas - 1) / ctas : 0;
+  p.halve_below = Body::HALVES && units * p.halves.chunks <= (1 << 30) ? p.halve_below * ctas : 0;
   p.spare = DA_SPARE_BYTES / (Body::TILE * p.a.cache.hd * 2 * (int)sizeof(typename Body::E));
-  const size_t smem = da_smem_bytes(p.a.batch, Body::WARPS, Body::warp_smem_floats(p.a.cache.hd), p.heads, p.a.cache.hd);
+  const size_t smem = da_smem_bytes(p.a.batch, Body::WARPS, Body::warp_smem_floats(p.a.cache.hd), p.deal.heads, p.a.cache.hd);
   if (smem > DA_SMEM || !limit.ensure(decode_attn_kernel<Body>, (int)smem)) return cudaErrorInvalidValue;
   return launch_k(decode_attn_kernel<Body>, dim3(ctas), dim3(Body::WARPS * 32), smem, s, p);
 }

@@ -79,6 +79,7 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
   // values a tile ahead as well, where keys and values of a tile are not half a thread's registers
   static constexpr bool V_AHEAD = HD * EB < 512;
   static constexpr int WARPS = da_mma_warps(HD, EB, MR, NG);
+  static constexpr bool HALVES = MR == 16;
   static __host__ __device__ int warp_smem_floats(int) { return 0; }
 
   static constexpr float NONE = -3.40282346638528860e38f;      // the reference before any score: the lowest number, so that none is below it
@@ -90,12 +91,11 @@ template <int FMT_, int HD, int MR, bool SPLIT, int NG> struct MmaBody {
 
   // the dimensions of Q that this lane's piece of a key meets in contraction s, four at a time; heads past the last are zero
   __device__ __forceinline__ void load_queries(const DaArgs &p, const DaSeg &sg, int g, int t) {
-    const int h0 = sg.kv * p.group + sg.chunk * p.heads, have = min(p.heads, p.group - sg.chunk * p.heads);
 #pragma unroll
     for (int n = 0; n < NB; n++) {
       const int h = PER_BLOCK * n + g % PER_BLOCK;
-      const bool in = h < have;
-      const size_t x = (size_t)sg.b * p.a.q_ts + (size_t)(h0 + (in ? h : 0)) * HD;
+      const bool in = h < sg.have;
+      const size_t x = (size_t)sg.b * p.a.q_ts + (size_t)(sg.head + (in ? h : 0)) * HD;
 #pragma unroll
       for (int s = 0; s < STEPS; s++) {
         const int d = EB == 1 ? (s / 4) * 64 + t * 16 + (s % 4) * 4 : (s / 2) * 32 + t * 8 + (s % 2) * 4;

@@ -518,3 +518,19 @@ def test_outputs_in_bf16_lose_little_but_their_own_rounding(fmt, H, G, hd):
     out = sb.decode_attention(q, cache["k_pool"], cache["v_pool"], table, torch.tensor(lens, dtype=torch.int32, device="cuda"), k_scale=cache["k_scale"], v_scale=cache["v_scale"])
     want, _, _ = definition(q, cache, table, lens, ps, hd ** -0.5)
     assert (out.double() - want).norm() <= 1.05 * (want.to(torch.bfloat16).double() - want).norm()
+
+
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+@pytest.mark.parametrize("B,H,G,hd", [(24, 16, 1, 128), (12, 18, 2, 128), (8, 45, 3, 128), (3, 128, 8, 128), (23, 11, 1, 64), (11, 66, 2, 64), (80, 15, 1, 128)])
+@pytest.mark.parametrize("least,most", [(0, 100), (3000, 9000)])
+def test_many_heads_of_a_kv_head_in_a_wide_table(dtype, fmt, B, H, G, hd, least, most):
+    """Short sequences, whose heads go by halves although the table would hold long ones, and long ones, which go as one chunk (or the fewest): odd halves, three chunks, shared and whole segments."""
+    if B * G * most > 300000 and fmt == "fp32":
+        most = 4000                                      # plain FMAs know no halves
+    g = torch.Generator(device="cuda").manual_seed(B * H + most)
+    lens = torch.randint(least, most, (B,), generator=g, device="cuda").tolist()
+    table, pages = table_for(g, lens, 16)
+    table = torch.nn.functional.pad(table, (0, 3000 - table.shape[1]), value=-9)
+    cache = pools(g, fmt, pages, G, 16, hd)
+    spoil(cache, table, lens, 16)
+    check(torch.randn(B, H, hd, generator=g, device="cuda").to(DT[dtype]), cache, table, lens, 16)

@@ -11,8 +11,8 @@ ASK = r"""
 #include <cstdio>
 #include <cstdlib>
 #include "attn_decode.cuh"
-int main(int n, char **v) {                     // fp32 queries, format, batch, heads, KV heads, head size
-  const spec::DecodePlan p = spec::decode_attn_plan(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]), atoi(v[5]), atoi(v[6]), 148);
+int main(int n, char **v) {                     // fp32 queries, format, batch, heads, KV heads, head size, positions
+  const spec::DecodePlan p = spec::decode_attn_plan(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]), atoi(v[5]), atoi(v[6]), 148, atoll(v[7]));
   printf("%d %d %d %d %d", p.chunks, p.heads, p.columns, p.groups, p.warps);
 }
 """
@@ -29,8 +29,8 @@ def plan(tmp_path_factory):
     subprocess.run([build.NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, str(src), lib, "-o", str(exe),
                     "-Xlinker", "-rpath", "-Xlinker", os.path.dirname(lib)], check=True, capture_output=True)
 
-    def ask(dtype, fmt, batch, H, G, hd):
-        out = subprocess.run([str(exe), *map(str, (int(dtype == "fp32"), FORMATS[fmt], batch, H, G, hd))], check=True, capture_output=True).stdout
+    def ask(dtype, fmt, batch, H, G, hd, positions=1 << 31):
+        out = subprocess.run([str(exe), *map(str, (int(dtype == "fp32"), FORMATS[fmt], batch, H, G, hd, positions))], check=True, capture_output=True).stdout
         return dict(zip(("chunks", "heads", "columns", "groups", "warps"), map(int, out.split())))
     return ask
 
@@ -58,3 +58,11 @@ def test_plain_fmas_give_up_heads_only_for_a_table_that_leaves_no_room(plan, dty
     table = (4 * (batch + 1) + 15) // 16 * 16
     state = p["heads"] * hd + (2 * p["heads"] + 3) // 4 * 4
     assert table + 4 * p["warps"] * (p["columns"] * hd + 64 + 2 * state) <= 224 * 1024
+
+
+def test_a_narrow_table_of_few_sequences_is_walked_by_halves(plan):
+    """256 KB of keys and values a CTA, by what the table holds: 32 segments of 128-byte rows in 148 CTAs have that at 4736 positions, of 256-byte rows at 2368."""
+    for fmt, line in (("e4m3", 4736), ("bf16", 2368)):
+        assert plan("bf16", fmt, 16, 32, 2, 128, line)["chunks"] == 1 and plan("bf16", fmt, 16, 32, 2, 128, line - 1)["chunks"] == 2
+        assert plan("bf16", fmt, 16, 16, 2, 128, line - 1)["chunks"] == 1
+        assert plan("bf16", fmt, 37, 32, 2, 128, 16)["chunks"] == 1      # 74 segments may stay whole
