@@ -227,7 +227,7 @@ static bool whole_pieces(const void *p, long long ts, long long hs, size_t e) { 
 }
 
 // Few tokens: a round's heads a block (of several tokens where one has fewer heads than that and every SM has a block), so that no thread has a second round to wait
-// for; many: about six rounds a block.  One head goes as two of which the second is not there: ceil(2^32 / 1) is no 32-bit number.  us of 16384 tokens of one head of
+// for; many (more than 1184 rounds, eight for each SM): about six rounds a block.  One head goes as two of which the second is not there: ceil(2^32 / 1) is no 32-bit number.  us of 16384 tokens of one head of
 // 64 / 128 in bf16: a token a block 22.2 / 20.8, sixteen 4.3 / 6.1; of 64 tokens of two heads: sixteen a block 2.5, one 1.8.
 RopePlan rope_plan(int tokens, int heads, int step) {
   const long long rounds = ((long long)tokens * heads + step - 1) / step;
