@@ -325,9 +325,9 @@ int spec_ttt_attention(const void *q, const void *k_pool, const void *v_pool, co
  * The step above keeps its cache in the model's type and rotates whole heads by unscaled frequencies.  These four calls serve
  * loops of a program's own around other caches and other rotations; they share no state with a ctx, take caller-provided DEVICE
  * buffers, launch one kernel each on `stream`, allocate nothing and do not synchronise.  dtype: spec_dtype of queries,
- * keys, values and outputs.  status: optional int32 [4] device words, zero at the start: a sequence, position, length or page out
- * of range is left out and recorded there (code 2, site 60: sequence or position, 61 / 63: page, 62: length; two details).  Calls with no
- * token or row return SPEC_OK and launch nothing. */
+ * keys, values and outputs.  status: optional int32 [4] device words, zero at the start: a sequence, position or page out
+ * of range is left out, a length taken as 0 or all that the table holds, and recorded there (code 2, site 60: sequence or position, 61 / 63: page, 62: length;
+ * two details).  Calls with no token or row return SPEC_OK and launch nothing. */
 
 /* How pairs of a head's first rot_dim dimensions turn: at position p, pair i becomes mscale (a cos t - b sin t, b cos t + a sin t)
  * with t = p * inv_freq[i], formed in 64 bits.  layout 0: dimension i pairs with i + rot_dim / 2; 1: 2 i with 2 i + 1. */
@@ -378,7 +378,7 @@ int spec_kv_read(const spec_kv_cache *cache, const int32_t *row_seq, const int32
  * n_heads <= 65536.  Work is counted in tiles of 16 positions or more on the device; the lengths are not known here, so SPEC_ERR_UNSUPPORTED goes by the page table's
  * width: (pages_per_seq * page_size / 16 + 3) * batch * (chunks of at most 4 to 16 query heads of all KV heads) above 2^30 may be refused, below it is not.
  * workspace: spec_decode_attention_workspace_bytes() bytes, 256-byte aligned, zero before the first call; a call leaves it ready for
- * the next on the same stream, and calls that may overlap need one each. */
+ * the next on the same stream, and calls that may overlap, or replays of graphs that hold them, need one each. */
 size_t spec_decode_attention_workspace_bytes(void);
 int spec_decode_attention(int32_t dtype, const void *q, int64_t q_token_stride, const spec_kv_cache *cache, const int32_t *lengths,
                           int32_t batch, int32_t n_heads, float scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
