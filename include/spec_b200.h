@@ -384,6 +384,69 @@ int spec_decode_attention(int32_t dtype, const void *q, int64_t q_token_stride, 
                           int32_t batch, int32_t n_heads, float scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
                           int32_t *status, void *stream);
 
+/* ---- training and serving around the layers: embedding lookup, norms of a residual sum, distillation, with their gradients -----
+ * The draft head is trained on the target's own features and output distribution (Section 3.2); these are the pieces at its ends and between its
+ * layers, for loops of a program's own, in training and in serving.  As above: DEVICE buffers of the caller's, launches on `stream`, no allocation, no
+ * synchronisation.  Nothing is kept between calls; scratch (256-byte aligned, need not be zero) may be used again as soon as the stream has passed the call.  Sums and
+ * statistics are held in 32 bits, and added in an order that depends on the arguments alone: the same call gives the same bits. */
+
+/* Rows of elements: row r begins row_stride elements after row r - 1, its elements are adjacent; aligned to an element.  Outputs' rows do not
+ * overlap (row_stride >= the width); inputs may have any stride, 0 too.  type: SPEC_KV_F32 or SPEC_KV_BF16, of 8-bit outputs SPEC_KV_E4M3 or SPEC_KV_INT8. */
+typedef struct {
+  void *p;
+  int64_t row_stride;
+  int32_t type;
+} spec_rows;
+
+/* out[t] = scale * weight[ids[t]]; weight [vocab][dim], out [tokens][dim], each F32 or BF16; ids of id_bits 32 or 64 (int32_t, int64_t).  -1: a row of zeros; so is an id out
+ * of range, which `status` (as above) records: code 2, site 64, token and id.  dim <= 2^22, tokens <= 2^30. */
+int spec_embedding(const spec_rows *weight, int32_t vocab, int32_t dim, int32_t id_bits, const void *ids, int32_t tokens, float scale,
+                   const spec_rows *out, int32_t *status, void *stream);
+
+/* The gradient with respect to weight of one with respect to spec_embedding's output: out[v] = scale * sum of grad[t] over the t with ids[t] = v, zeros where there are none;
+ * with accumulate, that is added to out, and rows that no token names are not touched.  The tokens are sorted by id, and each run is summed in the tokens'
+ * order in pieces of a fixed length.  out [vocab][dim] must not overlap grad.  scratch: spec_embedding_backward_scratch_bytes(tokens, dim). */
+size_t spec_embedding_backward_scratch_bytes(int32_t tokens, int32_t dim);
+int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, const void *ids, int32_t tokens, int32_t vocab, int32_t dim, float scale,
+                            int32_t accumulate, const spec_rows *out, void *scratch, size_t scratch_bytes, int32_t *status, void *stream);
+
+/* s = x + residual (x where residual is NULL), y = s / sqrt(mean(s^2) + eps) * gain, the mean over a row's dim elements; both from the sum in 32 bits.
+ * sum (NULL without residual): s in the residual's type; its memory may be residual's or x's, with their stride and type.  y F32, BF16, or codes in 8 bits with scale float
+ * [rows][ceil(dim / group)]: value = code * scale, scale = max(largest magnitude of the group / top, 2^-120), top 448 (E4M3) or 127 (INT8), as in spec_kv_cache; a group with
+ * an infinity or a NaN reads back as NaN.  group: a multiple of 16, or 0 for the whole row; only 8-bit outputs look at it.  gain [dim] of gain_dtype.  dim <= 2^22. */
+int spec_rms_norm(const spec_rows *x, const spec_rows *residual, int32_t gain_dtype, const void *gain, float eps, const spec_rows *sum, const spec_rows *y,
+                  float *scale, int32_t group, int32_t rows, int32_t dim, void *stream);
+
+/* From the gradient g with respect to y, and s (spec_rms_norm's sum, or its x where it had no residual), with u = 1 / sqrt(mean(s^2) + eps) and h = s u:
+ *   dx = u (g gain - h mean(g gain h)) + grad_sum      the gradient with respect to x and to residual; grad_sum (may be NULL): the one with respect to sum
+ *   dgain = sum over rows of g h                       of gain_dtype
+ * dx may be any of the inputs, with its stride and type.  scratch: spec_rms_norm_backward_scratch_bytes(rows, dim). */
+size_t spec_rms_norm_backward_scratch_bytes(int32_t rows, int32_t dim);
+int spec_rms_norm_backward(const spec_rows *grad, const spec_rows *s, int32_t gain_dtype, const void *gain, float eps, const spec_rows *grad_sum,
+                           const spec_rows *dx, void *dgain, void *scratch, size_t scratch_bytes, int32_t rows, int32_t dim, void *stream);
+
+/* A teacher's top logits: for each row K ids (id_bits 32 or 64; -1: none) and their logits or log-probabilities (values_dtype), [rows][K].  id_map (may be NULL): int32
+ * [id_map_n], from the teacher's ids to the student's, -1 for those that the student lacks.  lse (may be NULL): float [rows], the log of the teacher's whole sum of exp(logit / temperature).
+ * An entry with id -1, or that the map sends there, or with a value of -inf, is none; ids and mapped ids out of range are none and recorded in `status` (code 2, sites 65 and 66,
+ * row and id).  The same id several times: its probabilities add up.  1 <= K <= 1024. */
+typedef struct {
+  const void *ids, *values;
+  const float *lse;
+  const int32_t *id_map;
+  int32_t id_bits, values_dtype, id_map_n, K;
+} spec_teacher;
+
+/* Row by row, with q = softmax(logits / temperature) over the student's vocab, and p over the teacher's entries that the student has, softmax(values / temperature)
+ * over them, or exp(values / temperature - lse):
+ *   loss[r] = sum p (ln p - ln q) (kl != 0) or - sum p ln q;     dlogits[r] = grad[r] / temperature * (q sum(p) - p)
+ * A row without an entry has loss 0 and gradient 0, whatever its logits.  A row of -inf alone has NaN, as have rows with a NaN or +inf.
+ * stats float [rows][2]: the row's largest logit, and its sum of exp((logit - largest) / temperature) (0 and 1 without an entry).
+ *   loss, no dlogits: the loss; stats are written where given      no loss, dlogits: the gradient, from the stats of a call for the loss
+ *   both: loss and gradient in one pass over the logits; stats are written where given
+ * grad float [rows], NULL for 1.  dlogits may be logits, with their stride and type.  1e-4 <= temperature <= 1e4. */
+int spec_distill(const spec_rows *logits, int32_t rows, int32_t vocab, const spec_teacher *teacher, float temperature, int32_t kl, const float *grad,
+                 float *loss, float *stats, const spec_rows *dlogits, int32_t *status, void *stream);
+
 /* Test hook for the calling thread's causal attention launches (prefill and training-time test): 0 = off, 1 = the warps that
  * wait for the last contraction of a tile come tens of microseconds late (results do not depend on it), 2 = one CTA never
  * receives its queries and its bounded waits run out: a prefill returns SPEC_ERR_DEVICE_STATUS, training-time test gives NaN

@@ -66,12 +66,22 @@ class _KvCache(C.Structure):
                [(n, C.c_int32) for n in ("n_seq", "pages_per_seq", "page_size", "num_pages", "n_kv_heads", "head_dim", "format")]
 
 
+class _Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("row_stride", C.c_int64), ("type", C.c_int32)]
+
+
+class _Teacher(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("ids", "values", "lse", "id_map")] + [(n, C.c_int32) for n in ("id_bits", "values_dtype", "id_map_n", "K")]
+
+
 EXPORTS = ("spec_workspace_bytes", "spec_init", "spec_prefill", "spec_step", "spec_step_async", "spec_step_sampled", "spec_plain_step",
            "spec_lengths", "spec_profile_step", "spec_tune", "spec_launches_per_step", "spec_step_bytes", "spec_free", "spec_last_error",
            "spec_debug_read", "spec_debug_read_kv", "spec_gemm", "spec_gemm_fused", "spec_gemm_swiglu", "spec_gemm_wide", "spec_gemm_topk_scratch_bytes", "spec_gemm_topk", "spec_ttt_attention_scratch_bytes", "spec_ttt_attention",
            "spec_debug_causal", "spec_debug_wide_gemm", "spec_topk_scratch_bytes", "spec_attn_scratch_bytes",
            "spec_attention", "spec_attention_static", "spec_attention_static_capacity", "spec_logsoftmax_topk", "spec_argmax",
-           "spec_rotary", "spec_kv_append", "spec_kv_read", "spec_decode_attention_workspace_bytes", "spec_decode_attention")
+           "spec_rotary", "spec_kv_append", "spec_kv_read", "spec_decode_attention_workspace_bytes", "spec_decode_attention",
+           "spec_embedding", "spec_embedding_backward_scratch_bytes", "spec_embedding_backward", "spec_rms_norm", "spec_rms_norm_backward_scratch_bytes",
+           "spec_rms_norm_backward", "spec_distill")
 
 
 def library_path() -> str:
@@ -135,6 +145,14 @@ def lib():
     L.spec_decode_attention_workspace_bytes.argtypes = []
     L.spec_decode_attention_workspace_bytes.restype = sz
     L.spec_decode_attention.argtypes = [i32, vp, i64, cache, vp, i32, i32, C.c_float, vp, vp, vp, sz, vp, vp]
+    rows = C.POINTER(_Rows)
+    L.spec_embedding.argtypes = [rows, i32, i32, i32, vp, i32, C.c_float, rows, vp, vp]
+    L.spec_embedding_backward_scratch_bytes.argtypes = L.spec_rms_norm_backward_scratch_bytes.argtypes = [i32, i32]
+    L.spec_embedding_backward_scratch_bytes.restype = L.spec_rms_norm_backward_scratch_bytes.restype = sz
+    L.spec_embedding_backward.argtypes = [rows, i32, vp, i32, i32, i32, C.c_float, i32, rows, vp, sz, vp, vp]
+    L.spec_rms_norm.argtypes = [rows, rows, i32, vp, C.c_float, rows, rows, vp, i32, i32, i32, vp]
+    L.spec_rms_norm_backward.argtypes = [rows, rows, i32, vp, C.c_float, rows, rows, vp, vp, sz, i32, i32, vp]
+    L.spec_distill.argtypes = [rows, i32, i32, C.POINTER(_Teacher), C.c_float, i32, vp, vp, vp, rows, vp, vp]
     _lib = L
     return L
 
@@ -500,7 +518,9 @@ def _marshal():
         spec = importlib.util.spec_from_file_location("_marshal", _build.build_marshal())
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)
-        m.use(*[C.cast(f, C.c_void_p).value for f in (L.spec_rotary, L.spec_kv_append, L.spec_kv_read, L.spec_decode_attention, L.spec_decode_attention_workspace_bytes)])
+        m.use(*[C.cast(f, C.c_void_p).value for f in (L.spec_rotary, L.spec_kv_append, L.spec_kv_read, L.spec_decode_attention, L.spec_decode_attention_workspace_bytes,
+                                                             L.spec_embedding, L.spec_embedding_backward_scratch_bytes, L.spec_embedding_backward, L.spec_rms_norm,
+                                                             L.spec_rms_norm_backward_scratch_bytes, L.spec_rms_norm_backward, L.spec_distill)])
         _marshal_module = m
     return _marshal_module
 
@@ -625,3 +645,143 @@ def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor
     if type(r) is int:
         raise SpecError(r, "spec_decode_attention")
     return r
+
+
+# ------------------------------------------------------------------ embedding lookup, norms of a residual sum, distillation, and their gradients
+def _done(r, what: str):
+    if type(r) is int:
+        raise SpecError(r, what)
+    return r
+
+
+def _adjacent(grad):
+    """A gradient whose columns are adjacent: of a sum, for one, it comes expanded."""
+    return grad if grad is None or grad.stride(-1) == 1 or grad.shape[-1] == 1 else grad.contiguous()
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, weight, ids, scale, dtype, status):
+        ctx.save_for_backward(ids)
+        ctx.how = weight.shape[0], weight.dtype, scale
+        return embedding(ids, weight, scale, dtype, None, status)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        vocab, dtype, scale = ctx.how
+        return embedding_backward(_adjacent(grad), ctx.saved_tensors[0], vocab, scale, dtype), None, None, None, None
+
+
+def embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+              status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale * weight[ids] as dtype (weight's, or out's, unless given): ids int32 or int64 [tokens], -1 for a row of zeros; weight [vocabulary][width] and out [tokens][width] may have
+    any row stride, so that out can be half of a wider input.  An id out of range gives zeros and is recorded in status (int32 [4], zero at the start).
+    Autograd takes weight's gradient through it (with out it refuses a weight that needs one)."""
+    r = (_marshal_module or _marshal()).embedding(ids, weight, scale, dtype, out, status)
+    if r is NotImplemented:
+        _need(out is None, "embedding: out goes with tensors that need no gradient")
+        return _Embedding.apply(weight, ids, scale, dtype, status)
+    return _done(r, "spec_embedding")
+
+
+def embedding_backward(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                       accumulate: bool = False, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient with respect to embedding's weight of one with respect to its output [tokens][width]: [vocab][width] of dtype (grad's, or out's, unless given), zeros where no token
+    is.  With accumulate it is added to out, and rows without a token are not touched.  Sums are held in 32 bits, and the same call gives the same bits."""
+    return _done((_marshal_module or _marshal()).embedding_backward(grad, ids, vocab, scale, dtype, out, accumulate, status), "spec_embedding_backward")
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, gain, eps, dtype):
+        ctx.set_materialize_grads(False)
+        got = rms_norm(x, gain, eps, residual, dtype)
+        ctx.save_for_backward(x if residual is None else got[1], gain)
+        ctx.how = eps, x.dtype, None if residual is None else residual.dtype
+        return got
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad, grad_sum=None):
+        s, gain = ctx.saved_tensors
+        eps, x_dtype, r_dtype = ctx.how
+        if grad is None:
+            dx, dgain = grad_sum, torch.zeros_like(gain)
+        else:
+            wide = torch.float32 if torch.float32 in (x_dtype, r_dtype) else torch.bfloat16      # rounded once for each of the two
+            dx, dgain = rms_norm_backward(_adjacent(grad), s, gain, eps, _adjacent(grad_sum), wide)
+        as_ = lambda dtype: None if dtype is None or dx is None else dx.to(dtype)
+        return as_(x_dtype), as_(r_dtype), dgain, None, None
+
+
+def rms_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-5, residual: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None, group: int = 0,
+             sum_out: Optional[torch.Tensor] = None):
+    """y = s / sqrt(mean(s^2) + eps) * gain by rows, s = x + residual, as dtype (x's unless given); x [rows][width] and residual (each fp32 or bf16, any row stride).
+      without residual   y
+      with               (y, sum): s in residual's dtype, in sum_out where given, which may be residual or x; y is taken of the sum before it is rounded
+    dtype float8_e4m3fn or int8: codes in the place of y, and behind them their scales, float32 [rows][groups], of `group` columns each (a multiple of 16; 0: the whole row); y = code * scale.
+    Autograd takes the gradients of x, residual and gain through it, of outputs that are not in 8 bits, without sum_out."""
+    r = (_marshal_module or _marshal()).rms_norm(x, gain, eps, residual, dtype, group, sum_out)
+    if r is NotImplemented:
+        _need(sum_out is None, "rms_norm: sum_out goes with tensors that need no gradient")
+        _need(dtype in (None, torch.float32, torch.bfloat16), "rms_norm: an output in 8 bits goes with tensors that need no gradient")
+        return _RmsNorm.apply(x, residual, gain, eps, dtype)
+    return _done(r, "spec_rms_norm")
+
+
+def rms_norm_backward(grad: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-5, grad_sum: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None):
+    """(dx, dgain) from the gradient with respect to rms_norm's y, by hand: x is what was normed, the sum where there was a residual; dx, of dtype (x's unless given), is the gradient of
+    both x and residual, with grad_sum, the one with respect to the sum, added.  Sums are held in 32 bits, and the same call gives the same bits."""
+    return _done((_marshal_module or _marshal()).rms_norm_backward(grad, x, gain, eps, grad_sum, dtype), "spec_rms_norm_backward")
+
+
+def _kl(kind: str) -> bool:
+    _need(kind in ("kl", "ce"), "distill_loss: kind is 'kl' or 'ce'")
+    return kind == "kl"
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, values, id_map, values_lse, temperature, kind, status):
+        loss, stats = distill_loss(logits, ids, values, id_map, values_lse, temperature, kind, True, status)
+        ctx.save_for_backward(logits, stats, ids, values, id_map, values_lse)
+        ctx.temperature = temperature
+        ctx.mark_non_differentiable(stats)
+        return loss, stats
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad, _):
+        logits, stats, ids, values, id_map, values_lse = ctx.saved_tensors
+        return (distill_loss_backward(grad.contiguous(), logits, stats, ids, values, id_map, values_lse, ctx.temperature),) + (None,) * 7
+
+
+def distill_loss(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, id_map: Optional[torch.Tensor] = None, values_lse: Optional[torch.Tensor] = None,
+                 temperature: float = 1.0, kind: str = "kl", want_stats: bool = False, status: Optional[torch.Tensor] = None):
+    """Loss of each row, float32 [rows], of a student's logits [rows][vocabulary] against a teacher's top K logits or log-probabilities: ids int32 or int64 and values fp32 or bf16, [rows][K],
+    id -1 for no entry; id_map int32 [teacher's vocabulary] gives the student's id, -1 for those that it lacks (of a draft's d2t: full -1, then id_map[d2t] = arange).
+    q = softmax(logits / temperature), p = softmax(values / temperature) over the entries that the student has, or exp(values / temperature - values_lse) with the teacher's
+    normaliser float32 [rows]; "kl": sum p (ln p - ln q), "ce": - sum p ln q (no factor temperature^2).  A row without an entry has loss 0 and gradient 0.
+    want_stats: (loss, stats float32 [rows][2]) for distill_loss_backward.  Autograd takes logits' gradient through it.  Ids out of range are no entries and recorded in status."""
+    kl = _kl(kind)
+    r = (_marshal_module or _marshal()).distill(logits, ids, values, id_map, values_lse, temperature, kl, None, None, 1 if want_stats else 0, None, None, status)
+    if r is NotImplemented:
+        loss, stats = _Distill.apply(logits, ids, values, id_map, values_lse, temperature, kind, status)
+        return (loss, stats) if want_stats else loss
+    return _done(r, "spec_distill")
+
+
+def distill_loss_backward(grad: Optional[torch.Tensor], logits: torch.Tensor, stats: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, id_map: Optional[torch.Tensor] = None,
+                          values_lse: Optional[torch.Tensor] = None, temperature: float = 1.0, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                          status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient with respect to logits, of dtype (logits', or out's, unless given), of one with respect to the loss (float32 [rows]; None: ones), from the stats that the loss left.
+    out may be logits."""
+    return _done((_marshal_module or _marshal()).distill(logits, ids, values, id_map, values_lse, temperature, False, grad, stats, 2, dtype, out, status), "spec_distill")
+
+
+def distill_loss_and_grad(grad: Optional[torch.Tensor], logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, id_map: Optional[torch.Tensor] = None,
+                          values_lse: Optional[torch.Tensor] = None, temperature: float = 1.0, kind: str = "kl", dtype: Optional[torch.dtype] = None,
+                          out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """(loss, gradient with respect to logits) at once, where the loss's own gradient (float32 [rows], 1 / rows for a mean; None: ones) is known before: the logits are read once."""
+    return _done((_marshal_module or _marshal()).distill(logits, ids, values, id_map, values_lse, temperature, _kl(kind), grad, None, 3, dtype, out, status), "spec_distill")

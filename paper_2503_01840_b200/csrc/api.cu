@@ -17,6 +17,8 @@
 #include "attn_fast.cuh"
 #include "attn_causal.cuh"
 #include "attn_decode.cuh"
+#include "distill.cuh"
+#include "rms_norm.cuh"
 #include "state.cuh"
 
 using namespace spec;
@@ -1845,4 +1847,146 @@ extern "C" int spec_decode_attention(int32_t dtype, const void *q, int64_t q_ts,
   a.scale = scale != 0.0f ? scale : 1.0f / sqrtf((float)cache->head_dim);
   EarlyLaunch early;
   return kv_status(launch_decode_attn(a, dtype, cache->format, (cudaStream_t)stream));
+}
+
+// ---------------------------------------------------------------- embedding, norms, distillation
+static bool is_float_type(int t) { return t == SPEC_KV_F32 || t == SPEC_KV_BF16; }
+static size_t size_of_type(int t) { return t == SPEC_KV_F32 ? 4 : t == SPEC_KV_BF16 ? 2 : 1; }
+// Rows that are read, or written: with an address, aligned to an element, and apart from one another
+static int rows_in(const spec_rows *r) {
+  if (!r || !r->p) return SPEC_ERR_NULL;
+  return is_float_type(r->type) && kv_aligned(r->p, size_of_type(r->type)) ? SPEC_OK : SPEC_ERR_INVALID_CFG;
+}
+static int rows_out(const spec_rows *r, int rows, int dim, bool eight = false) {
+  if (!r || !r->p) return SPEC_ERR_NULL;
+  if (!is_float_type(r->type) && !(eight && kv_is_8bit(r->type))) return SPEC_ERR_INVALID_CFG;
+  return kv_aligned(r->p, size_of_type(r->type)) && (rows < 2 || r->row_stride >= dim) ? SPEC_OK : SPEC_ERR_INVALID_CFG;
+}
+// rows that may share their memory row by row, or not at all
+static bool same_places(const spec_rows *a, const spec_rows *b) { return a->p != b->p || (a->row_stride == b->row_stride && a->type == b->type); }
+static int ids_of(const void *ids, int bits, Ids *out) {
+  if (bits != 32 && bits != 64) return SPEC_ERR_INVALID_CFG;
+  *out = Ids{ids, bits == 64};
+  return kv_aligned(ids, bits / 8) ? SPEC_OK : SPEC_ERR_INVALID_CFG;
+}
+constexpr int MOST_COLUMNS = 1 << 22, MOST_TOKENS = 1 << 30;
+
+extern "C" int spec_embedding(const spec_rows *weight, int32_t vocab, int32_t dim, int32_t id_bits, const void *ids, int32_t tokens, float scale,
+                              const spec_rows *out, int32_t *status, void *stream) {
+  Embed a{};
+  if (vocab < 1 || dim < 1 || tokens < 0 || !(fabsf(scale) < INFINITY)) return SPEC_ERR_INVALID_CFG;
+  if (dim > MOST_COLUMNS || tokens > MOST_TOKENS) return SPEC_ERR_UNSUPPORTED;
+  if (const int rc = ids_of(ids, id_bits, &a.ids)) return rc;
+  if (tokens == 0) return SPEC_OK;
+  if (const int rc = rows_in(weight)) return rc;
+  if (const int rc = rows_out(out, tokens, dim)) return rc;
+  if (!ids) return SPEC_ERR_NULL;
+  a.w = weight->p; a.w_rs = weight->row_stride; a.vocab = vocab; a.dim = dim; a.tokens = tokens; a.scale = scale;
+  a.out = out->p; a.o_rs = out->row_stride; a.status = status;
+  EarlyLaunch early;
+  return kv_status(launch_embed_rows(a, weight->type, out->type, (cudaStream_t)stream));
+}
+
+extern "C" size_t spec_embedding_backward_scratch_bytes(int32_t tokens, int32_t dim) {
+  return tokens < 0 || dim < 1 || dim > MOST_COLUMNS || tokens > MOST_TOKENS ? 0 : embed_grad_scratch_bytes(tokens, dim);
+}
+
+extern "C" int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, const void *ids, int32_t tokens, int32_t vocab, int32_t dim, float scale,
+                                       int32_t accumulate, const spec_rows *out, void *scratch, size_t scratch_bytes, int32_t *status, void *stream) {
+  EmbedGrad a{};
+  if (vocab < 1 || dim < 1 || tokens < 0 || !(fabsf(scale) < INFINITY)) return SPEC_ERR_INVALID_CFG;
+  if (dim > MOST_COLUMNS || tokens > MOST_TOKENS) return SPEC_ERR_UNSUPPORTED;
+  if (const int rc = ids_of(ids, id_bits, &a.ids)) return rc;
+  if (const int rc = rows_out(out, vocab, dim)) return rc;
+  if (tokens == 0 && accumulate) return SPEC_OK;
+  if (tokens) {
+    if (const int rc = rows_in(grad)) return rc;
+    if (!ids) return SPEC_ERR_NULL;
+    a.grad = grad->p; a.g_rs = grad->row_stride;
+  }
+  if (!scratch) return SPEC_ERR_NULL;
+  if (scratch_bytes < embed_grad_scratch_bytes(tokens, dim) || !kv_aligned(scratch, 256)) return SPEC_ERR_WORKSPACE;
+  a.vocab = vocab; a.dim = dim; a.tokens = tokens; a.scale = scale; a.out = out->p; a.o_rs = out->row_stride; a.accumulate = accumulate != 0;
+  a.scratch = scratch; a.status = status;
+  EarlyLaunch early;
+  return kv_status(launch_embed_grad(a, tokens ? grad->type : SPEC_KV_F32, out->type, (cudaStream_t)stream));
+}
+
+extern "C" int spec_rms_norm(const spec_rows *x, const spec_rows *residual, int32_t gain_dtype, const void *gain, float eps, const spec_rows *sum,
+                             const spec_rows *y, float *scale, int32_t group, int32_t rows, int32_t dim, void *stream) {
+  if (rows < 0 || dim < 1 || group < 0 || group % 16 || !(eps >= 0.0f && eps < INFINITY) || (gain_dtype != SPEC_F32 && gain_dtype != SPEC_BF16)) return SPEC_ERR_INVALID_CFG;
+  if (dim > MOST_COLUMNS) return SPEC_ERR_UNSUPPORTED;
+  if (rows == 0) return SPEC_OK;
+  RmsNorm a{};
+  if (const int rc = rows_in(x)) return rc;
+  if (const int rc = rows_out(y, rows, dim, true)) return rc;
+  if (!gain || (kv_is_8bit(y->type) && !scale)) return SPEC_ERR_NULL;
+  if (!kv_aligned(gain, gain_dtype == SPEC_F32 ? 4 : 2) || !kv_aligned(scale, 4)) return SPEC_ERR_INVALID_CFG;
+  if (residual) {
+    if (const int rc = rows_in(residual)) return rc;
+    if (const int rc = rows_out(sum, rows, dim)) return rc;
+    if (sum->type != residual->type || !same_places(sum, residual) || !same_places(sum, x)) return SPEC_ERR_INVALID_CFG;
+    a.res = residual->p; a.r_rs = residual->row_stride; a.r_type = residual->type; a.sum = sum->p; a.s_rs = sum->row_stride;
+  } else if (sum) {
+    return SPEC_ERR_INVALID_CFG;
+  }
+  a.x = x->p; a.x_rs = x->row_stride; a.x_type = x->type; a.gain = gain; a.g_type = gain_dtype; a.y = y->p; a.y_rs = y->row_stride; a.y_type = y->type;
+  a.scale = scale; a.rows = rows; a.dim = dim; a.group = group && group < dim ? group : dim; a.eps = eps;
+  EarlyLaunch early;
+  return kv_status(launch_rms_norm(a, (cudaStream_t)stream));
+}
+
+extern "C" size_t spec_rms_norm_backward_scratch_bytes(int32_t rows, int32_t dim) { return rows < 0 || dim < 1 || dim > MOST_COLUMNS ? 0 : rms_norm_grad_scratch_bytes(rows, dim); }
+
+extern "C" int spec_rms_norm_backward(const spec_rows *grad, const spec_rows *s, int32_t gain_dtype, const void *gain, float eps, const spec_rows *grad_sum,
+                                      const spec_rows *dx, void *dgain, void *scratch, size_t scratch_bytes, int32_t rows, int32_t dim, void *stream) {
+  if (rows < 0 || dim < 1 || !(eps >= 0.0f && eps < INFINITY) || (gain_dtype != SPEC_F32 && gain_dtype != SPEC_BF16)) return SPEC_ERR_INVALID_CFG;
+  if (dim > MOST_COLUMNS) return SPEC_ERR_UNSUPPORTED;
+  RmsNormGrad a{};
+  if (!gain || !dgain) return SPEC_ERR_NULL;
+  const size_t e = gain_dtype == SPEC_F32 ? 4 : 2;
+  if (!kv_aligned(gain, e) || !kv_aligned(dgain, e)) return SPEC_ERR_INVALID_CFG;
+  if (rows) {
+    if (const int rc = rows_in(grad)) return rc;
+    if (const int rc = rows_in(s)) return rc;
+    if (grad_sum)
+      if (const int rc = rows_in(grad_sum)) return rc;
+    if (const int rc = rows_out(dx, rows, dim)) return rc;
+    if (!same_places(dx, grad) || !same_places(dx, s) || (grad_sum && !same_places(dx, grad_sum))) return SPEC_ERR_INVALID_CFG;
+    if (!scratch) return SPEC_ERR_NULL;
+    if (scratch_bytes < rms_norm_grad_scratch_bytes(rows, dim) || !kv_aligned(scratch, 256)) return SPEC_ERR_WORKSPACE;
+    a.g = grad->p; a.g_rs = grad->row_stride; a.g_type = grad->type; a.x = s->p; a.x_rs = s->row_stride; a.x_type = s->type;
+    if (grad_sum) a.carried = grad_sum->p, a.c_rs = grad_sum->row_stride, a.c_type = grad_sum->type;
+    a.dx = dx->p; a.d_rs = dx->row_stride; a.d_type = dx->type;
+  }
+  a.gain = gain; a.w_type = gain_dtype; a.dgain = dgain; a.rows = rows; a.dim = dim; a.eps = eps; a.part = (float *)scratch;
+  EarlyLaunch early;
+  return kv_status(launch_rms_norm_grad(a, (cudaStream_t)stream));
+}
+
+extern "C" int spec_distill(const spec_rows *logits, int32_t rows, int32_t vocab, const spec_teacher *t, float temperature, int32_t kl, const float *grad,
+                            float *loss, float *stats, const spec_rows *dlogits, int32_t *status, void *stream) {
+  if (!t) return SPEC_ERR_NULL;
+  if (rows < 0 || vocab < 1 || t->K < 1 || !(temperature >= 1e-4f && temperature <= 1e4f) || (t->values_dtype != SPEC_F32 && t->values_dtype != SPEC_BF16) ||
+      (t->id_map && t->id_map_n < 1))
+    return SPEC_ERR_INVALID_CFG;
+  if (t->K > DISTILL_MAX_K) return SPEC_ERR_UNSUPPORTED;
+  Distill a{};
+  if (const int rc = ids_of(t->ids, t->id_bits, &a.ids)) return rc;
+  if (rows == 0) return SPEC_OK;
+  if (const int rc = rows_in(logits)) return rc;
+  if (!t->ids || !t->values || (!loss && (!dlogits || !stats))) return SPEC_ERR_NULL;
+  if (!kv_aligned(t->values, t->values_dtype == SPEC_F32 ? 4 : 2) || !kv_aligned(t->lse, 4) || !kv_aligned(t->id_map, 4) || !kv_aligned(grad, 4) || !kv_aligned(loss, 4) ||
+      !kv_aligned(stats, 8))
+    return SPEC_ERR_INVALID_CFG;
+  if (dlogits) {
+    if (const int rc = rows_out(dlogits, rows, vocab)) return rc;
+    if (!same_places(dlogits, logits)) return SPEC_ERR_INVALID_CFG;
+    a.dz = dlogits->p; a.d_rs = dlogits->row_stride; a.d_type = dlogits->type;
+  }
+  a.z = logits->p; a.z_rs = logits->row_stride; a.z_type = logits->type; a.values = t->values; a.v_type = t->values_dtype; a.lse = t->lse;
+  a.map = t->id_map; a.map_n = t->id_map_n; a.rows = rows; a.vocab = vocab; a.K = t->K; a.kl = kl != 0; a.temperature = temperature;
+  a.grad = grad; a.loss = loss; a.stats = (float2 *)stats; a.status = status;
+  EarlyLaunch early;
+  return kv_status(launch_distill(a, (cudaStream_t)stream));
 }

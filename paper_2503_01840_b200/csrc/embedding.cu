@@ -1,0 +1,204 @@
+// Embedding lookup, out[t] = scale w[ids[t]], and its gradient, dw[v] = scale * sum of grad[t] over the t with ids[t] = v, summed in 32 bits in an
+// order that depends on the ids alone.
+#include "embedding.cuh"
+
+#include <algorithm>
+
+#include "vec.cuh"
+
+namespace spec {
+
+using std::max;
+using std::min;
+
+// ---------------------------------------------------------------- lookup
+// any width, stride and alignment: a block per token and 1024 columns
+__global__ void __launch_bounds__(256) embed_any_kernel(Embed a, int w_dtype, int out_dtype) {
+  pdl_wait();
+  pdl_trigger();
+  const int t = blockIdx.x, id = id_at(a.ids, t);
+  const bool there = id >= 0 && id < a.vocab;
+  if (!there && id != -1 && threadIdx.x == 0) set_status(a.status, ST_BOUNDS, 64, t, id);
+  for (int c = blockIdx.y * 1024 + threadIdx.x; c < min(a.dim, (int)(blockIdx.y + 1) * 1024); c += 256)
+    store_from_f32(a.out, out_dtype, (long long)t * a.o_rs + c, there ? load_as_f32(a.w, w_dtype, (long long)id * a.w_rs + c) * a.scale : 0.0f);
+}
+
+cudaError_t launch_embed_rows(const Embed &a, int w_dtype, int out_dtype, cudaStream_t s) {
+  return launch_k(embed_any_kernel, dim3(a.tokens, (a.dim + 1023) / 1024), dim3(256), 0, s, a, w_dtype, out_dtype);
+}
+
+// ---------------------------------------------------------------- gradient: the tokens in the order of their ids
+// A block owns a range of the vocabulary.  It reads all ids, which are few and stay in L2: how many lie below its range is where its tokens begin in the sorted
+// order, so blocks need nothing from one another and one launch sorts.  Warps walk segments of the ids: counting first, then writing those of the range
+// one behind another, in the tokens' order, to `list`; one warp deals them to their rows' places, 32 at a time.  Rows of the range that no token has are zeroed here.
+constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_MAX_ROWS = 4096;
+
+struct EmbedSort {
+  int rows;              // of the vocabulary a block
+  int32_t *order, *id;   // tokens by id, and the ids
+  int2 *list;            // (token, row of the block's range) of the ranges, unsorted
+  int32_t *count;        // tokens with a row
+};
+
+__global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, EmbedSort so, int out_dtype) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ int have[SORT_MAX_ROWS], place[SORT_MAX_ROWS], below[SORT_WARPS], mine[SORT_WARPS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lo = blockIdx.x * so.rows, n_rows = min(so.rows, a.vocab - lo);
+  for (int i = threadIdx.x; i < n_rows; i += SORT_THREADS) have[i] = 0;
+  __syncthreads();
+  // a warp's segment, in steps of 32 ids
+  const long long steps = (a.tokens + 31LL) / 32, per = (steps + SORT_WARPS - 1) / SORT_WARPS, s0 = min((long long)warp * per, steps), s1 = min(s0 + per, steps);
+  int less = 0, in = 0;
+  for (long long s = s0; s < s1; s++) {
+    const long long t = s * 32 + lane;
+    if (t >= a.tokens) break;
+    const int id = id_at(a.ids, t);
+    if (id < 0 || id >= a.vocab) {
+      if (id != -1 && blockIdx.x == 0) set_status(a.status, ST_BOUNDS, 64, (int)t, id);
+      continue;
+    }
+    less += id < lo;
+    if (id >= lo && id - lo < n_rows) in++, atomicAdd(&have[id - lo], 1);
+  }
+  less = __reduce_add_sync(0xffffffffu, less);
+  in = __reduce_add_sync(0xffffffffu, in);
+  if (lane == 0) below[warp] = less, mine[warp] = in;
+  __syncthreads();
+  int base = 0, before_me = 0, total = 0;
+  for (int w = 0; w < SORT_WARPS; w++) {
+    base += below[w];
+    if (w < warp) before_me += mine[w];
+    total += mine[w];
+  }
+  if (threadIdx.x == 0 && lo + n_rows == a.vocab) *so.count = base + total;
+  if (total) {
+    if (in) {
+      int at = base + before_me;
+      for (long long s = s0; s < s1; s++) {
+        const long long t = s * 32 + lane;
+        const int id = t < a.tokens ? id_at(a.ids, t) : -1;
+        const bool hit = id >= lo && id - lo < n_rows;
+        const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+        if (hit) so.list[at + __popc(hits & ((1u << lane) - 1))] = make_int2((int)t, id - lo);
+        at += __popc(hits);
+      }
+    }
+    __syncthreads();
+    if (warp == 0) {
+      int run = base;                                    // where each row's tokens begin
+      for (int i = 0; i < n_rows; i += 32) {
+        const int h = i + lane < n_rows ? have[i + lane] : 0;
+        int sum = h;
+        for (int d = 1; d < 32; d <<= 1) {
+          const int o = __shfl_up_sync(0xffffffffu, sum, d);
+          if (lane >= d) sum += o;
+        }
+        if (i + lane < n_rows) place[i + lane] = run + sum - h;
+        run += __shfl_sync(0xffffffffu, sum, 31);
+      }
+      __syncwarp();
+      for (int i = 0; i < total; i += 32) {
+        const bool there = i + lane < total;
+        const int2 e = there ? so.list[base + i + lane] : make_int2(0, -1);
+        const uint32_t same = __match_any_sync(0xffffffffu, e.y);
+        const int rank = __popc(same & ((1u << lane) - 1));
+        int at = there ? place[e.y] : 0;
+        __syncwarp();
+        if (there && rank == 0) place[e.y] = at + __popc(same);
+        __syncwarp();
+        if (there) so.order[at + rank] = e.x, so.id[at + rank] = lo + e.y;
+      }
+    }
+  }
+  if (a.accumulate) return;
+  for (int r = warp; r < n_rows; r += SORT_WARPS) {
+    if (have[r]) continue;
+    for (int c = lane; c < a.dim; c += 32) store_from_f32(a.out, out_dtype, (lo + r) * a.o_rs + c, 0.0f);
+  }
+}
+
+// ---------------------------------------------------------------- gradient: sums of runs of equal ids
+// The sorted tokens are cut into chunks, whatever ids they have: no id, however frequent, makes a block longer than another.  A run inside a chunk is written where
+// it belongs; what a chunk has of a run that goes over its ends goes to `part` (slot 0: of a run that began before, 1: of one that begins here and goes on),
+// and the chunk in which a run begins adds those up, in order, in the next launch.
+struct EmbedRuns {
+  int per_chunk, chunks;
+  const int32_t *order, *id, *count;
+  float *part;           // [chunks][2][dim]
+};
+constexpr int CHUNK_MAX = 64;
+
+__device__ __forceinline__ void embed_grad_out(const EmbedGrad &a, int out_dtype, int id, int c, float sum) {
+  const long long at = id * a.o_rs + c;
+  const float v = sum * a.scale;
+  store_from_f32(a.out, out_dtype, at, a.accumulate ? load_as_f32(a.out, out_dtype, at) + v : v);
+}
+
+__global__ void __launch_bounds__(128) embed_runs_any_kernel(EmbedGrad a, EmbedRuns r, int g_dtype, int out_dtype) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ int token[CHUNK_MAX], id[CHUNK_MAX + 2];
+  const int n = *r.count, p0 = blockIdx.x * r.per_chunk, m = min(r.per_chunk, n - p0);
+  if (m <= 0) return;
+  for (int i = threadIdx.x; i < m; i += 128) token[i] = r.order[p0 + i];
+  for (int i = threadIdx.x; i < m + 2; i += 128) id[i] = p0 + i - 1 >= 0 && p0 + i - 1 < n ? r.id[p0 + i - 1] : -1;
+  __syncthreads();
+  const int c = blockIdx.y * 128 + threadIdx.x;
+  if (c >= a.dim) return;
+  float sum = 0.0f;
+  bool began = id[0] != id[1];                           // whether the run under way began in this chunk
+  for (int i = 0; i < m; i++) {
+    sum += load_as_f32(a.grad, g_dtype, token[i] * a.g_rs + c);
+    const int me = id[i + 1];
+    if (i + 1 < m && id[i + 2] == me) continue;
+    const bool ends = id[i + 2] != me;
+    if (began && ends) embed_grad_out(a, out_dtype, me, c, sum);
+    else r.part[(2LL * blockIdx.x + began) * a.dim + c] = sum;
+    sum = 0.0f;
+    began = true;
+  }
+}
+
+__global__ void __launch_bounds__(128) embed_join_kernel(EmbedGrad a, EmbedRuns r, int out_dtype) {
+  pdl_wait();
+  pdl_trigger();
+  const int n = *r.count, k = blockIdx.x, p1 = (k + 1) * r.per_chunk;
+  if (p1 >= n) return;
+  const int me = r.id[p1 - 1];
+  if (r.id[p1] != me || (k > 0 && r.id[k * r.per_chunk] == me && r.id[k * r.per_chunk - 1] == me)) return;      // no run goes on here, or it began before
+  const int c = blockIdx.y * 128 + threadIdx.x;
+  if (c >= a.dim) return;
+  float sum = r.part[(2LL * k + 1) * a.dim + c];
+  for (int j = k + 1; j < r.chunks && j * r.per_chunk < n && r.id[j * r.per_chunk] == me; j++) sum += r.part[2LL * j * a.dim + c];
+  embed_grad_out(a, out_dtype, me, c, sum);
+}
+
+static size_t up(size_t n) { return (n + 255) / 256 * 256; }
+static int chunk_of(int tokens) { return tokens >= 4096 ? 32 : 8; }
+
+size_t embed_grad_scratch_bytes(int tokens, int dim) {
+  const size_t T = tokens, chunks = (T + chunk_of(tokens) - 1) / chunk_of(tokens);
+  return up(4 * T) * 2 + up(8 * T) + 256 + chunks * 2 * dim * 4;
+}
+
+cudaError_t launch_embed_grad(const EmbedGrad &a, int g_dtype, int out_dtype, cudaStream_t s) {
+  char *p = (char *)a.scratch;
+  EmbedSort so;
+  so.count = (int32_t *)p, p += 256;
+  so.order = (int32_t *)p, p += up(4 * (size_t)a.tokens);
+  so.id = (int32_t *)p, p += up(4 * (size_t)a.tokens);
+  so.list = (int2 *)p, p += up(8 * (size_t)a.tokens);
+  so.rows = min(SORT_MAX_ROWS, (a.vocab + 295) / 296);
+  if (const cudaError_t e = launch_k(embed_sort_kernel, dim3((a.vocab + so.rows - 1) / so.rows), dim3(SORT_THREADS), 0, s, a, so, out_dtype)) return e;
+  if (a.tokens == 0) return cudaSuccess;
+  EmbedRuns r;
+  r.per_chunk = chunk_of(a.tokens);
+  r.chunks = (int)(((long long)a.tokens + r.per_chunk - 1) / r.per_chunk);
+  r.order = so.order, r.id = so.id, r.count = so.count, r.part = (float *)p;
+  const dim3 grid(r.chunks, (a.dim + 127) / 128);
+  if (const cudaError_t e = launch_k(embed_runs_any_kernel, grid, dim3(128), 0, s, a, r, g_dtype, out_dtype)) return e;
+  return launch_k(embed_join_kernel, grid, dim3(128), 0, s, a, r, out_dtype);
+}
+
+}  // namespace spec

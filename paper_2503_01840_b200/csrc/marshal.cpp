@@ -1,8 +1,9 @@
-// Marshalling of the operators that a decoding loop calls once a layer: checks of the tensors, allocation of the outputs, and the call of the
+// Marshalling of the operators that a decoding or training loop calls once a layer: checks of the tensors, allocation of the outputs, and the call of the
 // C entry point.  It does what binding.py's other functions do in Python, where the checks and the packing of some twenty arguments take longer
 // than most of these kernels run (one token's rotary: 9.8 us a call there, of which the launch is 3).
 //
 // Functions return their outputs, or the entry point's status as an int where it is not 0; binding.py raises it.
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -12,6 +13,8 @@
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <algorithm>
+#include <initializer_list>
 #include <map>
 #include <string>
 #include <utility>
@@ -25,6 +28,13 @@ decltype(&spec_kv_append) append_;
 decltype(&spec_kv_read) read_;
 decltype(&spec_decode_attention) attend_;
 decltype(&spec_decode_attention_workspace_bytes) workspace_bytes_;
+decltype(&spec_embedding) embedding_;
+decltype(&spec_embedding_backward_scratch_bytes) embedding_scratch_;
+decltype(&spec_embedding_backward) embedding_backward_;
+decltype(&spec_rms_norm) norm_;
+decltype(&spec_rms_norm_backward_scratch_bytes) norm_scratch_;
+decltype(&spec_rms_norm_backward) norm_backward_;
+decltype(&spec_distill) distill_;
 
 struct Refusal {
   PyObject *type;
@@ -272,11 +282,252 @@ PyObject *decode_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------- embedding, norms, distillation: rows of elements
+double number(PyObject *o, const char *what) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) {
+    PyErr_Clear();
+    throw Refusal{PyExc_TypeError, what};
+  }
+  return v;
+}
+at::ScalarType type_or(PyObject *o, at::ScalarType otherwise, const char *what) {
+  if (o == Py_None) return otherwise;
+  if (!THPDtype_Check(o)) throw Refusal{PyExc_TypeError, what};
+  return ((THPDtype *)o)->scalar_type;
+}
+int row_type(at::ScalarType t, bool eight = false) {
+  if (eight && t == at::kFloat8_e4m3fn) return SPEC_KV_E4M3;
+  if (eight && t == at::kChar) return SPEC_KV_INT8;
+  return dtype_of(t);                                    // the codes of fp32 and bf16 are the same
+}
+// [rows][columns] on the GPU with adjacent columns
+spec_rows rows_of(const at::Tensor &t, const char *what, bool eight = false) {
+  need(t.dim() == 2 && t.is_cuda() && (t.stride(1) == 1 || t.size(1) == 1), what);
+  for (int64_t n : t.sizes()) need(n <= INT32_MAX, "a tensor with more than 2^31 - 1 of something");
+  return {address(t), t.stride(0), row_type(t.scalar_type(), eight)};
+}
+struct IdList {
+  const void *p;
+  int bits;
+};
+IdList ids_of(const at::Tensor &t, const char *what) {
+  need((t.scalar_type() == at::kInt || t.scalar_type() == at::kLong) && t.is_cuda() && t.is_contiguous(), what);
+  for (int64_t n : t.sizes()) need(n <= INT32_MAX, "a tensor with more than 2^31 - 1 of something");
+  return {address(t), t.scalar_type() == at::kInt ? 32 : 64};
+}
+// float32 of n elements, one behind the other, on the GPU
+float *floats(PyObject *o, int64_t n, const char *what) {
+  const at::Tensor &t = tensor(o, what);
+  need(t.scalar_type() == at::kFloat && t.numel() == n && t.dim() >= 1 && t.size(0) == n / (t.dim() > 1 ? std::max<int64_t>(1, t.size(1)) : 1) && t.is_cuda() && t.is_contiguous(), what);
+  return (float *)address(t);
+}
+at::Tensor scratch_of(size_t bytes, const at::Tensor &like) { return at::empty({(int64_t)std::max<size_t>(bytes, 256)}, like.options().dtype(at::kByte)); }
+// whether autograd has to record a call on these
+template <typename... T> bool records(const T &...t) { return at::GradMode::is_enabled() && (... || (t.defined() && t.requires_grad())); }
+
+// ids, weight, scale, dtype, out, status.  NotImplemented where autograd has to record it: binding.py wraps it then (as those below).
+PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject * {
+    const char *const what = "embedding: weight [vocabulary][width] on the GPU with adjacent columns", *const ids_are = "embedding: ids int32 or int64 [tokens] on the GPU";
+    const at::Tensor &ids = tensor(a[0], ids_are), &w = tensor(a[1], what);
+    const spec_rows from = rows_of(w, what);
+    const double scale = number(a[2], "embedding: scale is a number");
+    need(ids.dim() == 1, ids_are);
+    const IdList id = ids_of(ids, ids_are);
+    const int64_t T = ids.size(0), k = w.size(1);
+    const at::ScalarType type = type_or(a[3], a[4] == Py_None ? w.scalar_type() : tensor(a[4], "out").scalar_type(), "embedding: dtype is a torch.dtype");
+    row_type(type);
+    const at::Tensor out = a[4] == Py_None ? at::empty({T, k}, w.options().dtype(type)) : tensor(a[4], "out");
+    need(out.dim() == 2 && out.size(0) == T && out.size(1) == k && out.scalar_type() == type, "embedding: out [tokens][width] of dtype");
+    if (records(w, out)) Py_RETURN_NOTIMPLEMENTED;
+    const spec_rows to = rows_of(out, "embedding: out [tokens][width] on the GPU with adjacent columns");
+    int32_t *const status = status_of(a[5]);
+    void *const s = stream_of_call();
+    const int rc = call([&] { return embedding_(&from, (int32_t)w.size(0), (int32_t)k, id.bits, id.p, (int32_t)T, (float)scale, &to, status, s); });
+    return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+  });
+}
+
+// grad, ids, vocab, scale, dtype, out, accumulate, status
+PyObject *embedding_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject * {
+    const char *const what = "embedding_backward: grad [tokens][width] on the GPU with adjacent columns", *const ids_are = "embedding_backward: ids int32 or int64 [tokens] on the GPU";
+    const at::Tensor &g = tensor(a[0], what), &ids = tensor(a[1], ids_are);
+    const spec_rows from = rows_of(g, what);
+    const int64_t T = g.size(0), k = g.size(1);
+    need(ids.dim() == 1 && ids.size(0) == T, ids_are);
+    const IdList id = ids_of(ids, ids_are);
+    const long long V = PyLong_AsLongLong(a[2]);
+    if (V == -1 && PyErr_Occurred()) throw python_error();
+    need(V >= 1 && V <= INT32_MAX, "embedding_backward: vocab is a number of rows");
+    const double scale = number(a[3], "embedding_backward: scale is a number");
+    const bool accumulate = PyObject_IsTrue(a[6]) == 1;
+    need(!accumulate || a[5] != Py_None, "embedding_backward: accumulate goes with out");
+    const at::ScalarType type = type_or(a[4], a[5] == Py_None ? g.scalar_type() : tensor(a[5], "out").scalar_type(), "embedding_backward: dtype is a torch.dtype");
+    row_type(type);
+    const at::Tensor out = a[5] == Py_None ? at::empty({V, k}, g.options().dtype(type)) : tensor(a[5], "out");
+    need(out.dim() == 2 && out.size(0) == V && out.size(1) == k && out.scalar_type() == type && !records(out), "embedding_backward: out [vocabulary][width] of dtype, without a gradient");
+    const spec_rows to = rows_of(out, "embedding_backward: out [vocabulary][width] on the GPU with adjacent columns");
+    int32_t *const status = status_of(a[7]);
+    void *const s = stream_of_call();
+    const size_t bytes = embedding_scratch_((int32_t)T, (int32_t)k);
+    const at::Tensor scratch = scratch_of(bytes, g);
+    const int rc = call([&] {
+      return embedding_backward_(&from, id.bits, id.p, (int32_t)T, (int32_t)V, (int32_t)k, (float)scale, accumulate, &to, scratch.data_ptr(), scratch.nbytes(), status, s);
+    });
+    return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+  });
+}
+
+PyObject *several(std::initializer_list<at::Tensor> t) {
+  PyObject *r = PyTuple_New((Py_ssize_t)t.size());
+  if (!r) return nullptr;
+  Py_ssize_t i = 0;
+  for (const at::Tensor &x : t) PyTuple_SET_ITEM(r, i++, THPVariable_Wrap(x));
+  return r;
+}
+const void *gain_of(const at::Tensor &w, int64_t k, const char *what) {
+  need(w.dim() == 1 && w.size(0) == k && w.is_cuda() && w.is_contiguous(), what);
+  return address(w);
+}
+
+// x, gain, eps, residual, dtype, group, sum_out
+PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject * {
+    const char *const what = "rms_norm: x [rows][width] on the GPU with adjacent columns", *const gain_is = "rms_norm: gain [width] on the GPU";
+    const at::Tensor &x = tensor(a[0], what), &w = tensor(a[1], gain_is);
+    const spec_rows from = rows_of(x, what);
+    const int64_t R = x.size(0), k = x.size(1);
+    const int gain_type = dtype_of(w.scalar_type());
+    const void *const gain = gain_of(w, k, gain_is);
+    const double eps = number(a[2], "rms_norm: eps is a number");
+    const at::ScalarType type = type_or(a[4], x.scalar_type(), "rms_norm: dtype is a torch.dtype");
+    const bool eight = row_type(type, true) >= SPEC_KV_E4M3;
+    const long group = PyLong_AsLong(a[5]);
+    if (group == -1 && PyErr_Occurred()) throw python_error();
+    need(group >= 0 && group % 16 == 0 && group <= INT32_MAX, "rms_norm: group is 0 or a multiple of 16");
+    at::Tensor res, sum, scale;
+    spec_rows add{}, total{};
+    if (a[3] != Py_None) {
+      const char *const res_is = "rms_norm: residual [rows][width] on the GPU with adjacent columns", *const sum_is = "rms_norm: sum_out [rows][width] of residual's dtype on the GPU with adjacent columns";
+      res = tensor(a[3], res_is);
+      need(res.sizes() == x.sizes(), res_is);
+      add = rows_of(res, res_is);
+      if (a[6] != Py_None) {
+        sum = tensor(a[6], sum_is);
+        need(sum.sizes() == x.sizes() && sum.scalar_type() == res.scalar_type(), sum_is);
+      } else {
+        sum = at::empty({R, k}, res.options());
+      }
+      total = rows_of(sum, sum_is);
+    } else {
+      need(a[6] == Py_None, "rms_norm: sum_out goes with residual");
+    }
+    if (records(x, w, res, sum)) Py_RETURN_NOTIMPLEMENTED;
+    const at::Tensor y = at::empty({R, k}, x.options().dtype(type));
+    const spec_rows to = rows_of(y, "y", true);
+    if (eight) scale = at::empty({R, k == 0 ? 0 : group ? (k + group - 1) / group : 1}, x.options().dtype(at::kFloat));
+    void *const s = stream_of_call();
+    const int rc = call([&] {
+      return norm_(&from, res.defined() ? &add : nullptr, gain_type, gain, (float)eps, res.defined() ? &total : nullptr, &to, eight ? (float *)scale.data_ptr() : nullptr,
+                   eight ? (int32_t)group : 0, (int32_t)R, (int32_t)k, s);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    if (eight) return res.defined() ? several({y, scale, sum}) : several({y, scale});
+    return res.defined() ? several({y, sum}) : THPVariable_Wrap(y);
+  });
+}
+
+// grad, s, gain, eps, grad_sum, dtype
+PyObject *rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject * {
+    const char *const grad_is = "rms_norm_backward: grad [rows][width] on the GPU with adjacent columns", *const x_is = "rms_norm_backward: x [rows][width] on the GPU with adjacent columns",
+                      *const gain_is = "rms_norm_backward: gain [width] on the GPU", *const sum_is = "rms_norm_backward: grad_sum [rows][width] on the GPU with adjacent columns";
+    const at::Tensor &g = tensor(a[0], grad_is), &x = tensor(a[1], x_is), &w = tensor(a[2], gain_is);
+    const spec_rows of_y = rows_of(g, grad_is), of_x = rows_of(x, x_is);
+    const int64_t R = x.size(0), k = x.size(1);
+    need(g.sizes() == x.sizes(), grad_is);
+    const int gain_type = dtype_of(w.scalar_type());
+    const void *const gain = gain_of(w, k, gain_is);
+    const double eps = number(a[3], "rms_norm_backward: eps is a number");
+    spec_rows carried{};
+    if (a[4] != Py_None) {
+      const at::Tensor &c = tensor(a[4], sum_is);
+      need(c.sizes() == x.sizes(), sum_is);
+      carried = rows_of(c, sum_is);
+    }
+    const at::ScalarType type = type_or(a[5], x.scalar_type(), "rms_norm_backward: dtype is a torch.dtype");
+    row_type(type);
+    const at::Tensor dx = at::empty({R, k}, x.options().dtype(type)), dw = at::empty({k}, w.options());
+    const spec_rows to = rows_of(dx, "dx");
+    void *const s = stream_of_call();
+    const at::Tensor scratch = scratch_of(norm_scratch_((int32_t)R, (int32_t)k), x);
+    const int rc = call([&] {
+      return norm_backward_(&of_y, &of_x, gain_type, gain, (float)eps, a[4] != Py_None ? &carried : nullptr, &to, dw.data_ptr(), scratch.data_ptr(), scratch.nbytes(), (int32_t)R,
+                            (int32_t)k, s);
+    });
+    return rc ? PyLong_FromLong(rc) : several({dx, dw});
+  });
+}
+
+// logits, ids, values, id_map, values_lse, temperature, kl, grad, stats, want: 0 the loss, 1 the loss and stats, 2 the gradient from stats, 3 loss and gradient; dtype, out, status
+PyObject *distill(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject * {
+    const char *const z_is = "distill_loss: logits [rows][vocabulary] on the GPU with adjacent columns", *const ids_are = "distill_loss: ids int32 or int64 [rows][K], contiguous on the GPU",
+                      *const values_are = "distill_loss: values [rows][K], contiguous on the GPU, without a gradient";
+    const at::Tensor &z = tensor(a[0], z_is), &ids = tensor(a[1], ids_are), &v = tensor(a[2], values_are);
+    const spec_rows from = rows_of(z, z_is);
+    const int64_t R = z.size(0), V = z.size(1);
+    need(ids.dim() == 2 && ids.size(0) == R, ids_are);
+    const IdList id = ids_of(ids, ids_are);
+    need(v.sizes() == ids.sizes() && v.is_cuda() && v.is_contiguous() && !records(v), values_are);
+    spec_teacher t{id.p, address(v), nullptr, nullptr, id.bits, dtype_of(v.scalar_type()), 0, (int32_t)ids.size(1)};
+    if (a[3] != Py_None) {
+      const at::Tensor &map = tensor(a[3], "distill_loss: id_map");
+      t.id_map_n = (int32_t)std::min<int64_t>(map.numel(), INT32_MAX);
+      t.id_map = (const int32_t *)ints(a[3], t.id_map_n, "distill_loss: id_map int32 [teacher's vocabulary] on the GPU");
+    }
+    if (a[4] != Py_None) {
+      need(!records(tensor(a[4], "distill_loss: values_lse")), "distill_loss: values_lse without a gradient");
+      t.lse = floats(a[4], R, "distill_loss: values_lse float32 [rows] on the GPU");
+    }
+    const double temperature = number(a[5], "distill_loss: temperature is a number");
+    const bool kl = PyObject_IsTrue(a[6]) == 1;
+    const long want = PyLong_AsLong(a[9]);
+    if (want < 2 && records(z)) Py_RETURN_NOTIMPLEMENTED;
+    const float *const grad = a[7] == Py_None ? nullptr : floats(a[7], R, "distill_loss: grad float32 [rows] on the GPU");
+    at::Tensor loss, stats, dz;
+    float *known = nullptr;
+    if (want != 2) loss = at::empty({R}, z.options().dtype(at::kFloat));
+    if (want == 1) stats = at::empty({R, 2}, z.options().dtype(at::kFloat)), known = (float *)stats.data_ptr();
+    if (want == 2) known = floats(a[8], 2 * R, "distill_loss: stats float32 [rows][2] on the GPU");
+    spec_rows to{};
+    if (want >= 2) {
+      const char *const out_is = "distill_loss: out [rows][vocabulary] of dtype on the GPU with adjacent columns, without a gradient";
+      const at::ScalarType type = type_or(a[10], a[11] == Py_None ? z.scalar_type() : tensor(a[11], out_is).scalar_type(), "distill_loss: dtype is a torch.dtype");
+      row_type(type);
+      dz = a[11] == Py_None ? at::empty({R, V}, z.options().dtype(type)) : tensor(a[11], out_is);
+      need(dz.sizes() == z.sizes() && dz.scalar_type() == type && (a[11] == Py_None || !records(dz)), out_is);
+      to = rows_of(dz, out_is);
+    }
+    int32_t *const status = status_of(a[12]);
+    void *const s = stream_of_call();
+    const int rc = call([&] {
+      return distill_(&from, (int32_t)R, (int32_t)V, &t, (float)temperature, kl, grad, loss.defined() ? (float *)loss.data_ptr() : nullptr, known, dz.defined() ? &to : nullptr, status, s);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    if (want == 1) return several({loss, stats});
+    if (want == 3) return several({loss, dz});
+    return THPVariable_Wrap(want == 2 ? dz : loss);
+  });
+}
+
 // addresses of the entry points, in the order of the declarations above
 PyObject *use(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return guarded(n, 5, [&]() -> PyObject * {
-    void *p[5];
-    for (int i = 0; i < 5; i++) {
+  return guarded(n, 12, [&]() -> PyObject * {
+    void *p[12];
+    for (int i = 0; i < 12; i++) {
       p[i] = PyLong_AsVoidPtr(a[i]);
       if (!p[i]) throw Refusal{PyExc_ValueError, "an entry point without an address"};
     }
@@ -285,6 +536,13 @@ PyObject *use(PyObject *, PyObject *const *a, Py_ssize_t n) {
     read_ = (decltype(read_))p[2];
     attend_ = (decltype(attend_))p[3];
     workspace_bytes_ = (decltype(workspace_bytes_))p[4];
+    embedding_ = (decltype(embedding_))p[5];
+    embedding_scratch_ = (decltype(embedding_scratch_))p[6];
+    embedding_backward_ = (decltype(embedding_backward_))p[7];
+    norm_ = (decltype(norm_))p[8];
+    norm_scratch_ = (decltype(norm_scratch_))p[9];
+    norm_backward_ = (decltype(norm_backward_))p[10];
+    distill_ = (decltype(distill_))p[11];
     Py_RETURN_NONE;
   });
 }
@@ -293,9 +551,14 @@ PyMethodDef methods[] = {{"rotary", (PyCFunction)(void *)rotary, METH_FASTCALL, 
                          {"kv_append", (PyCFunction)(void *)kv_append, METH_FASTCALL, nullptr},
                          {"kv_read", (PyCFunction)(void *)kv_read, METH_FASTCALL, nullptr},
                          {"decode_attention", (PyCFunction)(void *)decode_attention, METH_FASTCALL, nullptr},
+                         {"embedding", (PyCFunction)(void *)embedding, METH_FASTCALL, nullptr},
+                         {"embedding_backward", (PyCFunction)(void *)embedding_backward, METH_FASTCALL, nullptr},
+                         {"rms_norm", (PyCFunction)(void *)rms_norm, METH_FASTCALL, nullptr},
+                         {"rms_norm_backward", (PyCFunction)(void *)rms_norm_backward, METH_FASTCALL, nullptr},
+                         {"distill", (PyCFunction)(void *)distill, METH_FASTCALL, nullptr},
                          {"use", (PyCFunction)(void *)use, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Marshalling of the operators of serving loops", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Marshalling of the operators beside the step", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
