@@ -12,6 +12,30 @@ __device__ __forceinline__ void store_from_f32(void *p, int dtype, long long i, 
   else ((bf16 *)p)[i] = __float2bfloat16_rn(v);
 }
 
+// eight neighbours, 16-byte aligned
+__device__ __forceinline__ void unpack2(uint32_t u, float &a, float &b) { a = __uint_as_float(u << 16), b = __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *(const uint32_t *)&v;
+}
+__device__ __forceinline__ void load8(const float *p, float (&y)[8]) {
+  const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
+  y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w, y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16 *p, float (&y)[8]) {
+  const uint4 u = *(const uint4 *)p;
+  unpack2(u.x, y[0], y[1]), unpack2(u.y, y[2], y[3]), unpack2(u.z, y[4], y[5]), unpack2(u.w, y[6], y[7]);
+}
+__device__ __forceinline__ void store8(float *p, const float (&y)[8]) {
+  ((float4 *)p)[0] = make_float4(y[0], y[1], y[2], y[3]);
+  ((float4 *)p)[1] = make_float4(y[4], y[5], y[6], y[7]);
+}
+__device__ __forceinline__ void store8(bf16 *p, const float (&y)[8]) {
+  *(uint4 *)p = make_uint4(pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7]));
+}
+// rows whose pieces of 16 bytes are aligned, elements of e bytes
+inline bool pieces_aligned(const void *p, long long row_stride, size_t e) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(row_stride * (long long)e)) & 15) == 0; }
+
 // Sum and maximum over a block of whole warps, the same for every thread; `room`: 32 floats of shared memory, free again after the next barrier.
 __device__ __forceinline__ float block_sum(float v, float *room) {
 #pragma unroll
