@@ -61,7 +61,8 @@ __device__ __forceinline__ void join_lanes(float b, Running &r) {
 // ---------------------------------------------------------------- a row's entries
 struct Entries {
   int *id;               // the student's, -1: none
-  float *p, *ln_p, *z;   // z: the student's logit there
+  float *p, *ln_p;
+  float *write;          // for the gradient: p of all entries with this id at the first of them, -1 at the others
 };
 __host__ __device__ constexpr int fours(int K) { return (K + 3) / 4 * 4; }
 __host__ __device__ constexpr size_t entries_bytes(int K) { return (size_t)fours(K) * 16; }
@@ -73,7 +74,7 @@ __device__ __forceinline__ Entries entries_in(char *shared, int K) {
 __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e, long long row, bool *none) {
   const int lane = threadIdx.x & 31;
   const float inv_t = 1.0f / a.temperature;
-  const long long z0 = row * a.z_rs, at = row * a.K;
+  const long long at = row * a.K;
   float top = -INFINITY;
   bool some = false, nan = false;
   if (lane < fours(a.K) - a.K) e.id[a.K + lane] = -1;
@@ -94,7 +95,6 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
     if (v == -INFINITY) id = -1;
     e.id[k] = id;
     e.ln_p[k] = v;
-    e.z[k] = id >= 0 ? load_as_f32(a.z, a.z_type, z0 + id) : 0.0f;
     if (id < 0) continue;
     some = true;
     top = fmaxf(top, v);
@@ -126,34 +126,45 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
   for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
   return all;
 }
-// A warp's sum over its lanes' entries of p (ln p - ln q), ln q without the logarithm of q's normaliser
-__device__ __forceinline__ float entries_loss(const Distill &a, const Entries &e, float m) {
+// What the same warp does next for the gradient
+__device__ __forceinline__ void merge_entries(const Entries &e, int K) {
+  __syncwarp();
+  for (int k = threadIdx.x & 31; k < K; k += 32) {
+    const int id = e.id[k];
+    bool first = id >= 0;
+    float p = e.p[k];
+    for (int j = 0; first && j < K; j += 4) {
+      const int4 o = *(const int4 *)(e.id + j);
+      if (o.x != id && o.y != id && o.z != id && o.w != id) continue;
+      for (int x = j; x < j + 4; x++) {
+        if (e.id[x] != id) continue;
+        if (x < k) first = false;
+        if (x > k) p += e.p[x];
+      }
+    }
+    e.write[k] = first ? p : -1.0f;
+  }
+  __syncwarp();
+}
+// A warp's sum over its lanes' entries of p (ln p - ln q), ln q without the logarithm of q's normaliser; z(id): the student's logit
+template <typename F> __device__ __forceinline__ float entries_loss(const Distill &a, const Entries &e, float m, F z) {
   float loss = 0.0f;
   for (int k = threadIdx.x & 31; k < a.K; k += 32) {
-    const float p = e.p[k], ln_q = (e.z[k] - m) / a.temperature;
-    if (e.id[k] >= 0 && p != 0.0f) loss += p * (a.kl ? e.ln_p[k] - ln_q : -ln_q);
+    const float p = e.p[k];
+    if (e.id[k] < 0 || p == 0.0f) continue;
+    const float ln_q = (z(e.id[k]) - m) / a.temperature;
+    loss += p * (a.kl ? e.ln_p[k] - ln_q : -ln_q);
   }
 #pragma unroll
   for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
   return loss;
 }
-// The gradient at the entries' ids from c0 to c1: an id's first entry writes for all that name it.  d: of the row
-__device__ __forceinline__ void entries_gradient(const Distill &a, float b, const Entries &e, float m, float g, float of_q, int c0, int c1, long long d) {
-  for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+// A warp writes the gradient at the entries' ids from c0 to c1.  d: of the row
+template <typename F> __device__ __forceinline__ void entries_gradient(const Distill &a, float b, const Entries &e, float m, float g, float of_q, int c0, int c1, long long d, F z) {
+  for (int k = threadIdx.x & 31; k < a.K; k += 32) {
     const int id = e.id[k];
-    if (id < c0 || id >= c1) continue;
-    float p = e.p[k];
-    bool first = true;
-    for (int j = 0; j < a.K; j += 4) {
-      const int4 o = *(const int4 *)(e.id + j);
-      if (o.x != id && o.y != id && o.z != id && o.w != id) continue;
-      for (int x = j; x < j + 4; x++) {
-        if (e.id[x] != id) continue;
-        first &= x >= k;
-        if (x > k) p += e.p[x];
-      }
-    }
-    if (first) store_from_f32(a.dz, a.d_type, d + id, fmaf(of_q, exp_of(b, e.z[k] - m), -g * p));
+    const float p = e.write[k];
+    if (id >= c0 && id < c1 && !(p < 0.0f)) store_from_f32(a.dz, a.d_type, d + id, fmaf(of_q, exp_of(b, z(id) - m), -g * p));
   }
 }
 
@@ -165,12 +176,15 @@ __global__ void __launch_bounds__(512) distill_any_kernel(Distill a, float b) {
   __shared__ float of_s[16], of_m[16], mass;
   __shared__ int empty;
   const Entries e = entries_in(shared, a.K);
+  float *const kept = (float *)(shared + entries_bytes(a.K));     // the logits at the entries: the output may be the input
   const int tid = threadIdx.x;
   const long long row = blockIdx.x, z0 = row * a.z_rs, d0 = row * a.d_rs;
   if (tid < 32) {
     bool none;
     const float all = read_entries(a, e, row, &none);
     if (tid == 0) mass = all, empty = none;
+    for (int k = tid; k < a.K; k += 32) kept[k] = e.id[k] >= 0 ? load_as_f32(a.z, a.z_type, z0 + e.id[k]) : 0.0f;
+    if (a.dz) merge_entries(e, a.K);
   }
   __syncthreads();
   if (empty) {
@@ -196,21 +210,30 @@ __global__ void __launch_bounds__(512) distill_any_kernel(Distill a, float b) {
     r = (tid & 31) < 16 ? Running{of_m[tid & 31], of_s[tid & 31]} : Running{};
     join_lanes(b, r);
     if (r.m == -INFINITY) r.s = NAN;                     // no logit above -inf: there is no softmax
-    if (tid < 32) {
-      const float loss = entries_loss(a, e, r.m);
-      if (tid == 0) {
-        a.loss[row] = loss + all * logf(r.s);
-        if (a.stats) a.stats[row] = make_float2(r.m, r.s);
-      }
-    }
   } else {
     r.m = a.stats[row].x, r.s = a.stats[row].y;
+  }
+  // loss and gradient at the entries, whose list gives the place
+  if (tid < 32) {
+    float loss = 0.0f;
+    for (int k = tid; k < a.K; k += 32) {
+      if (e.id[k] < 0 || e.p[k] == 0.0f) continue;
+      const float ln_q = (kept[k] - r.m) / a.temperature;
+      loss += e.p[k] * (a.kl ? e.ln_p[k] - ln_q : -ln_q);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
+    if (a.loss && tid == 0) {
+      a.loss[row] = loss + all * logf(r.s);
+      if (a.stats) a.stats[row] = make_float2(r.m, r.s);
+    }
   }
   if (!a.dz) return;
   const float g = (a.grad ? a.grad[row] : 1.0f) / a.temperature, of_q = g * all / r.s;
   for (int c = tid; c < a.vocab; c += 512) store_from_f32(a.dz, a.d_type, d0 + c, of_q * exp_of(b, load_as_f32(a.z, a.z_type, z0 + c) - r.m));
   __syncthreads();
-  entries_gradient(a, b, e, r.m, g, of_q, 0, a.vocab, d0);
+  for (int k = tid; k < a.K; k += 512)
+    if (e.id[k] >= 0 && !(e.write[k] < 0.0f)) store_from_f32(a.dz, a.d_type, d0 + e.id[k], fmaf(of_q, exp_of(b, kept[k] - r.m), -g * e.write[k]));
 }
 
 // ---------------------------------------------------------------- rows held in shared memory
@@ -222,7 +245,6 @@ struct Slices {
   int n, per;            // slices of a row, elements of one: a multiple of 8
   int whole;             // units of the output are aligned pieces of 16 bytes
   int look_first;        // whether a row is not loaded before it is known that some id of it is not -1
-  int ahead;             // rows that are under way at a time: those after them have their entries fetched into L2
 };
 constexpr int SLICE = 66 << 10, SLICE_MOST = 200 << 10, CLUSTER_MOST = 8;
 
@@ -238,20 +260,67 @@ __device__ __forceinline__ float2 of_cta(const float2 *p, int rank) {
   return v;
 }
 
-// the largest of eight; of NaN and a number the number
-__device__ __forceinline__ float largest(const float *p) {
-  float y[8];
-  load8(p, y);
-  return fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-}
-__device__ __forceinline__ float largest(const bf16 *p) {
-  const uint4 u = *(const uint4 *)p;
-  const __nv_bfloat162 a = *(const __nv_bfloat162 *)&u.x, b = *(const __nv_bfloat162 *)&u.y, c = *(const __nv_bfloat162 *)&u.z, d = *(const __nv_bfloat162 *)&u.w;
-  const __nv_bfloat162 m = __hmax2(__hmax2(a, b), __hmax2(c, d));
-  return fmaxf(__low2float(m), __high2float(m));
-}
+// Eight neighbours as they lie in memory; the largest of them (of NaN and a number the number).
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void take(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
+  __device__ __forceinline__ void floats(float (&y)[8]) const { y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w, y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w; }
+  __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)), fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w))); }
+};
+template <> struct Eight<bf16> {
+  uint4 u;
+  __device__ __forceinline__ void take(const bf16 *p) { u = *(const uint4 *)p; }
+  __device__ __forceinline__ void floats(float (&y)[8]) const { unpack2(u.x, y[0], y[1]), unpack2(u.y, y[2], y[3]), unpack2(u.z, y[4], y[5]), unpack2(u.w, y[6], y[7]); }
+  __device__ __forceinline__ float largest() const {
+    const __nv_bfloat162 a = *(const __nv_bfloat162 *)&u.x, b = *(const __nv_bfloat162 *)&u.y, c = *(const __nv_bfloat162 *)&u.z, d = *(const __nv_bfloat162 *)&u.w;
+    const __nv_bfloat162 m = __hmax2(__hmax2(a, b), __hmax2(c, d));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+};
 
 constexpr int WALKERS = 256;      // threads that copy and walk; another warp looks the entries up and takes the loss
+
+// A unit's part of a thread's maximum and sum
+template <typename T> __device__ __forceinline__ Running walk(const T *at, float b, Running r) {
+  Eight<T> x;
+  x.take(at);
+  const float top = x.largest();
+  if (top > r.m) r.s *= exp_of(b, r.m == -INFINITY ? 0.0f : r.m - top), r.m = top;
+  float y[8], even, odd;
+  Pair p[4];
+  x.floats(y);
+  exp_of(b, relative_to(r.m), y, p);
+  unpair(add(add(p[0], p[1]), add(p[2], p[3])), even, odd);
+  r.s += even + odd;
+  return r;
+}
+
+// an element of another CTA's shared memory, at the place that p has in this one's
+__device__ __forceinline__ float of_cta(const float *p, int rank) {
+  uint32_t at;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_of(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float of_cta(const bf16 *p, int rank) {
+  uint32_t at;
+  uint16_t v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_of(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+  return __uint_as_float((uint32_t)v << 16);
+}
+// named barriers, for all threads
+enum { ROW_SEEN = 1, ROW_WRITTEN = 2 };
+template <int ID> __device__ __forceinline__ void arrive() {
+  __syncwarp();
+  asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(WALKERS + 32) : "memory");
+}
+template <int ID> __device__ __forceinline__ void wait() {
+  __syncwarp();
+  asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(WALKERS + 32) : "memory");
+}
 
 template <typename T, typename O, int MODE>
 __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __grid_constant__ Distill a, float b, const __grid_constant__ Slices sl) {
@@ -269,24 +338,18 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
   const int shift = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T)), units = (shift + n + 7) / 8;
   const Entries e = entries_in(shared, a.K);
   T *const buf = (T *)(shared + entries_bytes(a.K));     // element c of the slice at buf[shift + c]
-  if (sl.ahead && !walks && row + sl.ahead < a.rows) {
-    const long long at = (row + sl.ahead) * a.K;
-    for (int k = lane * 32; k < a.K * (a.ids.wide ? 2 : 1); k += 1024) asm volatile("prefetch.global.L2 [%0];" ::"l"((const char *)a.ids.p + at * (a.ids.wide ? 8 : 4) + k * 4));
-    for (int k = lane * 32; k < a.K; k += 1024) asm volatile("prefetch.global.L2 [%0];" ::"l"((const char *)a.values + (at + k) * (a.v_type == 0 ? 4 : 2)));
-  }
   bool there = true;
   if (sl.look_first) {
     there = false;
     for (int k = 0; k < a.K && !there; k += 32) there = __any_sync(0xffffffffu, k + lane < a.K && id_at(a.ids, row * a.K + k + lane) != -1);
   }
-  // steps of a unit a thread; in `inner` ones every unit is whole and in the slice
-  const int steps = (units + WALKERS - 1) / WALKERS, inner0 = shift ? 1 : 0, inner1 = max(inner0, (shift + n) / 8 / WALKERS), quarter = (steps + 3) / 4;
+  const int steps = (units + WALKERS - 1) / WALKERS, quarter = (steps + 3) / 4;      // a unit of each thread a step
   if (there && walks) {
 #pragma unroll
     for (int q = 0; q < 4; q++) {
       for (int i = q * quarter; i < min(steps, (q + 1) * quarter); i++) {
         const int u = i * WALKERS + tid, c = u * 8 - shift;
-        if ((i >= inner0 && i < inner1) || (u < units && c >= 0 && c + 8 <= n)) {
+        if (c >= 0 && c + 8 <= n) {
           copy16(buf + u * 8, z + c);
           if (sizeof(T) == 4) copy16(buf + u * 8 + 4, z + c + 4);
         } else if (u < units) {
@@ -296,93 +359,104 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
-  } else if (there) {
-    bool none;
-    const float all = read_entries(a, e, row, &none);
-    if (lane == 0) mass = all, empty = none;
-  } else if (tid == 0) {
-    empty = 1;
+  }
+  // the row's maximum and sum from the walkers' warps, or from the cluster's CTAs; given, where the gradient alone is wanted
+  auto seen = [&]() {
+    Running r;
+    if (there && lane < WALKERS / 32) r = Running{of_warp[lane].x, of_warp[lane].y};
+    join_lanes(b, r);
+    return r;
+  };
+  auto agreed = [&]() {
+    Running r;
+    if (lane < sl.n) {
+      const float2 v = of_cta(&mine, lane);
+      r = Running{v.x, v.y};
+    }
+    join_lanes(b, r);
+    return r;
+  };
+  auto factors = [&](bool none, float s, float &g, float &of_q) {
+    g = none ? 0.0f : (a.grad ? a.grad[row] : 1.0f) / a.temperature;
+    of_q = none ? 0.0f : g * mass / s;
+  };
+  const bool joint = MODE != GRADIENT && sl.n > 1;
+  if (!walks) {
+    bool none = true;
+    if (there) {
+      const float all = read_entries(a, e, row, &none);
+      if (lane == 0) mass = all;
+    }
+    if (lane == 0) empty = none;
+    arrive<ROW_SEEN>();
+    if (joint) cluster_arrive();
+    if (MODE != LOSS && !none) merge_entries(e, a.K);
+    if (joint) cluster_wait();
+    wait<ROW_WRITTEN>();
+    Running r;
+    if (MODE == GRADIENT) {
+      if (!none) r = Running{a.stats[row].x, a.stats[row].y};
+    } else {
+      r = joint ? agreed() : seen();
+      if (r.m == -INFINITY) r.s = NAN;
+      if (rank == 0) {
+        auto logit = [&](int id) {
+          if (!joint) return to_f32(buf[shift + id]);
+          const int k = id / sl.per;
+          return of_cta(buf + shift + (id - k * sl.per), k);
+        };
+        const float loss = none ? 0.0f : entries_loss(a, e, r.m, logit) + mass * logf(r.s);
+        if (lane == 0) {
+          a.loss[row] = loss;
+          if (a.stats) a.stats[row] = none ? make_float2(0.0f, 1.0f) : make_float2(r.m, r.s);
+        }
+      }
+    }
+    if (MODE != LOSS && !none) {
+      float g, of_q;
+      factors(none, r.s, g, of_q);
+      entries_gradient(a, b, e, r.m, g, of_q, c0, c0 + n, row * a.d_rs, [&](int id) { return to_f32(buf[shift + id - c0]); });
+    }
+    __syncwarp();
+    if (joint) cluster_arrive(), cluster_wait();         // nobody leaves while its numbers may be read
+    return;
   }
   Running r;
-  if (MODE != GRADIENT && there && walks) {
-    auto seen = [&](int u) {
-      float y[8];
-      load8(buf + u * 8, y);
-      const float top = largest(buf + u * 8);
-      if (top > r.m) r.s *= exp_of(b, r.m == -INFINITY ? 0.0f : r.m - top), r.m = top;
-      Pair p[4];
-      exp_of(b, relative_to(r.m), y, p);
-      float even, odd;
-      unpair(add(add(p[0], p[1]), add(p[2], p[3])), even, odd);
-      r.s += even + odd;
-    };
+  if (MODE != GRADIENT && there) {
 #pragma unroll
     for (int q = 0; q < 4; q++) {
       if (q == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
       if (q == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
       if (q == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
       if (q == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
-      int i = q * quarter;
-      const int end = min(steps, (q + 1) * quarter);
-      for (; i + 2 <= end && (i + 1 < inner1 || (i + 1) * WALKERS + WALKERS <= units); i += 2) {     // two units at a time
-        float y[8], w[8];
-        const T *const at = buf + (i * WALKERS + tid) * 8;
-        load8(at, y);
-        load8(at + WALKERS * 8, w);
-        const float top = fmaxf(largest(at), largest(at + WALKERS * 8));
-        if (top > r.m) r.s *= exp_of(b, r.m == -INFINITY ? 0.0f : r.m - top), r.m = top;
-        const float m = relative_to(r.m);
-        Pair p[4], o[4];
-        exp_of(b, m, y, p);
-        exp_of(b, m, w, o);
-        float even, odd;
-        unpair(add(add(add(p[0], p[1]), add(p[2], p[3])), add(add(o[0], o[1]), add(o[2], o[3]))), even, odd);
-        r.s += even + odd;
-      }
-      for (; i < end; i++)
-        if (i * WALKERS + tid < units) seen(i * WALKERS + tid);
+      for (int i = q * quarter; i < min(steps, (q + 1) * quarter); i++)
+        if (i * WALKERS + tid < units) r = walk(buf + (i * WALKERS + tid) * 8, b, r);
     }
     join_lanes(b, r);
     if (lane == 0) of_warp[warp] = make_float2(r.m, r.s);
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();
-  if (MODE != GRADIENT) {
-    r = Running{};
-    if (there && lane < WALKERS / 32) r = Running{of_warp[lane].x, of_warp[lane].y};
-    join_lanes(b, r);
-    if (sl.n > 1) {                                      // the others have read their row's entries by the end of the wait: the output may be the input
+  wait<ROW_SEEN>();
+  const bool none = empty;
+  if (MODE == GRADIENT) {
+    if (!none) r = Running{a.stats[row].x, a.stats[row].y};
+  } else {
+    r = seen();
+    if (joint) {
       if (tid == 0) mine = make_float2(r.m, r.s);
       __syncwarp();
       cluster_arrive();
       cluster_wait();
-      r = Running{};
-      if (lane < sl.n) {
-        const float2 v = of_cta(&mine, lane);
-        r = Running{v.x, v.y};
-      }
-      __syncwarp();
+      r = agreed();
       cluster_arrive();
-      join_lanes(b, r);
     }
     if (r.m == -INFINITY) r.s = NAN;                     // no logit above -inf: there is no softmax
-    if (rank == 0 && !walks) {
-      const float loss = empty ? 0.0f : entries_loss(a, e, r.m) + mass * logf(r.s);
-      if (lane == 0) {
-        a.loss[row] = loss;
-        if (a.stats) a.stats[row] = empty ? make_float2(0.0f, 1.0f) : make_float2(r.m, r.s);
-      }
-    }
-  } else if (!empty) {
-    r.m = a.stats[row].x, r.s = a.stats[row].y;
   }
   if (MODE != LOSS) {
-    const bool none = empty;
-    const float g = none ? 0.0f : (a.grad ? a.grad[row] : 1.0f) / a.temperature, of_q = none ? 0.0f : g * mass / r.s;
-    const long long d0 = row * a.d_rs;
-    O *const d = (O *)a.dz + d0 + c0;
-    if (!walks) {
-    } else if (none) {
+    float g, of_q;
+    factors(none, r.s, g, of_q);
+    O *const d = (O *)a.dz + row * a.d_rs + c0;
+    if (none) {
       if (sl.whole) {
         const float y[8] = {};
         for (int u = tid; u < n / 8; u += WALKERS) store8(d + u * 8, y);
@@ -405,13 +479,10 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
     } else {
       for (int c = tid; c < n; c += WALKERS) d[c] = from_f32<O>(of_q * exp_of(b, to_f32(buf[shift + c]) - r.m));
     }
-    if (!none) {
-      __syncthreads();
-      entries_gradient(a, b, e, r.m, g, of_q, c0, c0 + n, d0);
-    }
   }
+  arrive<ROW_WRITTEN>();                                 // the other warp writes over what they have written
   __syncwarp();
-  if (MODE != GRADIENT && sl.n > 1) cluster_wait();      // nobody leaves while its numbers may be read
+  if (joint) cluster_wait();
 }
 
 // Slices of about SLICE bytes, so that three CTAs are on an SM; smaller ones where rows alone do not fill the SMs twice, down to 2 KB.
@@ -424,7 +495,6 @@ static bool slices_of(const Distill &a, Slices *sl) {
   sl->per = (int)(((a.vocab + n - 1LL) / n + 7) / 8 * 8);
   sl->whole = a.dz && pieces_aligned(a.dz, a.rows > 1 ? a.d_rs : 0, a.d_type == 0 ? 4 : 2);
   sl->look_first = (long long)a.rows * n > 4 * 148;
-  sl->ahead = sl->look_first ? 3 * 148 / n : 0;
   return (size_t)sl->per * e <= SLICE_MOST && (long long)a.rows * n <= INT32_MAX;
 }
 
@@ -452,7 +522,7 @@ template <typename T, typename O> static cudaError_t rows_in_shared(const Distil
 cudaError_t launch_distill(const Distill &a, cudaStream_t s) {
   const float b = (float)(1.4426950408889634 / a.temperature);
   Slices sl;
-  if (!slices_of(a, &sl)) return launch_k(distill_any_kernel, dim3(a.rows), dim3(512), entries_bytes(a.K), s, a, b);
+  if (!slices_of(a, &sl)) return launch_k(distill_any_kernel, dim3(a.rows), dim3(512), entries_bytes(a.K) + (size_t)a.K * 4, s, a, b);
   if (a.z_type == 0) {
     if (!a.dz) return rows_in_shared<float, float, LOSS>(a, b, sl, s);
     return a.d_type == 0 ? rows_in_shared<float, float>(a, b, sl, s) : rows_in_shared<float, bf16>(a, b, sl, s);
