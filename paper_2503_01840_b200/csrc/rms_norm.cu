@@ -58,67 +58,32 @@ __global__ void __launch_bounds__(256) rms_norm_any_kernel(RmsNorm a) {
   }
 }
 
-// ---------------------------------------------------------------- rows held in registers
-// Widths of whole eights up to 16384, aligned to 16 bytes: every thread has N times eight neighbours, of which the row has its threads or, up to 1024 columns, a warp.  Each
-// input is read once and all of it is asked for before the first sum.  In 8 bits a scale's group is part of a warp's 256 columns, or the row.
+// ---------------------------------------------------------------- rows of whole eights
+// Widths of whole eights up to 16384, aligned to 16 bytes.  A thread has N times eight neighbours in every row that its block takes in turn; rows come through a ring of STAGES in shared
+// memory, in which a thread's part is its own, so that the next rows are under way while one is summed, without a register for them and with one barrier a row.
+// Up to 256 columns a warp has a row, and nothing to wait for.  In 8 bits a scale's group is part of a warp's 256 columns, or the row.
+constexpr int STAGES = 3;
+
 template <int FMT> __device__ __forceinline__ uint2 codes_of(const float (&y)[8], float inv) {
   return make_uint2(kv_encode4<FMT>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), kv_encode4<FMT>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
 }
+// of a warp's lanes, and of a block's warps through `room`
+__device__ __forceinline__ float sum_of(float v, float *room, bool block) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  if (!block) return v;
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) room[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = lane < (blockDim.x >> 5) ? room[lane & 15] : 0.0f;
+#pragma unroll
+  for (int d = 8; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return __shfl_sync(0xffffffffu, v, 0);
+}
 
-template <typename TX, typename TR, int N, bool WARP>
-__global__ void __launch_bounds__(512) rms_norm_kernel(const __grid_constant__ RmsNorm a) {
-  pdl_wait();
-  pdl_trigger();
-  __shared__ float room[2][16];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, of_row = WARP ? 32 : blockDim.x, t = WARP ? lane : threadIdx.x;
-  const long long row = WARP ? (long long)blockIdx.x * (blockDim.x >> 5) + warp : blockIdx.x;
-  if (WARP && row >= a.rows) return;
-  const TX *const x = (const TX *)a.x + row * a.x_rs;
-  float v[N][8], w[N][8];
-#pragma unroll
-  for (int i = 0; i < N; i++) {
-    const int c = (i * of_row + t) * 8;
-    if (c < a.dim) {
-      load8(x + c, v[i]);
-      if (a.g_type == KV_F32) load8((const float *)a.gain + c, w[i]);
-      else load8((const bf16 *)a.gain + c, w[i]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; k++) v[i][k] = w[i][k] = 0.0f;
-    }
-  }
-  if (a.res) {
-    float r[N][8];
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-      const int c = (i * of_row + t) * 8;
-      if (c < a.dim) load8((const TR *)a.res + row * a.r_rs + c, r[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-      const int c = (i * of_row + t) * 8;
-      if (c >= a.dim) continue;
-#pragma unroll
-      for (int k = 0; k < 8; k++) v[i][k] += r[i][k];
-      store8((TR *)a.sum + row * a.s_rs + c, v[i]);
-    }
-  }
-  float ss = 0.0f;
-#pragma unroll
-  for (int i = 0; i < N; i++)
-#pragma unroll
-    for (int k = 0; k < 8; k++) ss = fmaf(v[i][k], v[i][k], ss);
-#pragma unroll
-  for (int d = 16; d; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-  if (!WARP) {
-    if (lane == 0) room[0][warp] = ss;
-    __syncthreads();
-    ss = lane < (blockDim.x >> 5) ? room[0][lane & 15] : 0.0f;
-#pragma unroll
-    for (int d = 8; d; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-    ss = __shfl_sync(0xffffffffu, ss, 0);
-  }
-  const float u = rsqrtf(ss / a.dim + a.eps);
+// What follows the sum: v is the residual sum, w the gain; thread t of `of_row` threads of the row
+template <int N> __device__ __forceinline__ void norm_out(const RmsNorm &a, long long row, int t, int of_row, float (&v)[N][8], const float (&w)[N][8], float u, float *room, bool block) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int i = 0; i < N; i++)
 #pragma unroll
@@ -134,7 +99,7 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const __grid_constant__ R
     return;
   }
   const bool whole = a.group >= a.dim;
-  const int groups = whole ? 1 : (a.dim + a.group - 1) / a.group, lanes = a.group >> 3;      // lanes: of a group, 4 to 32
+  const int shift = whole ? 0 : 31 - __clz(a.group), groups = whole ? 1 : (a.dim + a.group - 1) >> shift, lanes = a.group >> 3;      // lanes of a group: 4 to 32
   uint32_t top[N];                                       // bits of the largest magnitude: NaN counts as the largest of all
 #pragma unroll
   for (int i = 0; i < N; i++) {
@@ -146,10 +111,10 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const __grid_constant__ R
 #pragma unroll
     for (int i = 1; i < N; i++) top[0] = max(top[0], top[i]);
     top[0] = __reduce_max_sync(0xffffffffu, top[0]);
-    if (!WARP) {
-      if (lane == 0) room[1][warp] = __uint_as_float(top[0]);
+    if (block) {
+      if (lane == 0) room[16 + (threadIdx.x >> 5)] = __uint_as_float(top[0]);
       __syncthreads();
-      top[0] = __reduce_max_sync(0xffffffffu, lane < (blockDim.x >> 5) ? __float_as_uint(room[1][lane & 15]) : 0u);
+      top[0] = __reduce_max_sync(0xffffffffu, lane < (blockDim.x >> 5) ? __float_as_uint(room[16 + (lane & 15)]) : 0u);
     }
 #pragma unroll
     for (int i = 1; i < N; i++) top[i] = top[0];
@@ -164,7 +129,101 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const __grid_constant__ R
     if (c >= a.dim) continue;
     const float scale = a.y_type == KV_E4M3 ? kv_scale<KV_E4M3>(top[i]) : kv_scale<KV_INT8>(top[i]), inv = 1.0f / scale;
     *(uint2 *)((uint8_t *)a.y + row * a.y_rs + c) = a.y_type == KV_E4M3 ? codes_of<KV_E4M3>(v[i], inv) : codes_of<KV_INT8>(v[i], inv);
-    if (whole ? i == 0 && t == 0 : (t & (lanes - 1)) == 0) a.scale[row * groups + (whole ? 0 : c / a.group)] = scale;
+    if (whole ? i == 0 && t == 0 : (t & (lanes - 1)) == 0) a.scale[row * groups + (whole ? 0 : c >> shift)] = scale;
+  }
+}
+template <int N> __device__ __forceinline__ void gain_of(const RmsNorm &a, int t, int of_row, float (&w)[N][8]) {
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    const int c = (i * of_row + t) * 8;
+#pragma unroll
+    for (int k = 0; k < 8; k++) w[i][k] = 0.0f;
+    if (c >= a.dim) continue;
+    if (a.g_type == KV_F32) load8((const float *)a.gain + c, w[i]);
+    else load8((const bf16 *)a.gain + c, w[i]);
+  }
+}
+template <int N> __device__ __forceinline__ float square_of(const float (&v)[N][8]) {
+  float ss = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; i++)
+#pragma unroll
+    for (int k = 0; k < 8; k++) ss = fmaf(v[i][k], v[i][k], ss);
+  return ss;
+}
+
+template <typename TX, typename TR>
+__global__ void __launch_bounds__(128) rms_norm_warp_kernel(const __grid_constant__ RmsNorm a) {
+  pdl_wait();
+  pdl_trigger();
+  const int t = threadIdx.x & 31, c = t * 8;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= a.rows) return;
+  float v[1][8] = {}, w[1][8];
+  if (c < a.dim) {
+    Raw8<TX> x;
+    Raw8<TR> r;
+    x.take((const TX *)a.x + row * a.x_rs + c);
+    if (a.res) r.take((const TR *)a.res + row * a.r_rs + c);
+    x.floats(v[0]);
+    if (a.res) {
+      float y[8];
+      r.floats(y);
+#pragma unroll
+      for (int k = 0; k < 8; k++) v[0][k] += y[k];
+      store8((TR *)a.sum + row * a.s_rs + c, v[0]);
+    }
+  }
+  gain_of<1>(a, t, 32, w);
+  norm_out<1>(a, row, t, 32, v, w, rsqrtf(sum_of(square_of<1>(v), nullptr, false) / a.dim + a.eps), nullptr, false);
+}
+
+template <typename TX, typename TR, int N>
+__global__ void __launch_bounds__(512) rms_norm_kernel(const __grid_constant__ RmsNorm a) {
+  pdl_wait();
+  pdl_trigger();
+  extern __shared__ __align__(16) char ring[];
+  __shared__ float room[2][32];
+  const int t = threadIdx.x, of_row = blockDim.x;
+  TX *const xs = (TX *)ring;                             // [stages][dim]
+  TR *const rs = (TR *)(ring + (size_t)STAGES * a.dim * sizeof(TX));
+  auto ask = [&](long long row, int stage) {
+    if (row < a.rows)
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int c = (i * of_row + t) * 8;
+        if (c >= a.dim) continue;
+        copy8(xs + stage * a.dim + c, (const TX *)a.x + row * a.x_rs + c);
+        if (a.res) copy8(rs + stage * a.dim + c, (const TR *)a.res + row * a.r_rs + c);
+      }
+    copies_commit();
+  };
+  long long row = blockIdx.x;
+#pragma unroll
+  for (int k = 0; k < STAGES; k++) ask(row + (long long)k * gridDim.x, k);
+  float w[N][8];
+  gain_of<N>(a, t, of_row, w);
+  for (int stage = 0, turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
+    copies_but<STAGES - 1>();
+    float v[N][8];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int c = (i * of_row + t) * 8;
+#pragma unroll
+      for (int k = 0; k < 8; k++) v[i][k] = 0.0f;
+      if (c >= a.dim) continue;
+      load8(xs + stage * a.dim + c, v[i]);
+      if (!a.res) continue;
+      float y[8];
+      load8(rs + stage * a.dim + c, y);
+#pragma unroll
+      for (int k = 0; k < 8; k++) v[i][k] += y[k];
+      store8((TR *)a.sum + row * a.s_rs + c, v[i]);
+    }
+    const float u = rsqrtf(sum_of(square_of<N>(v), room[turn], true) / a.dim + a.eps);
+    ask(row + (long long)STAGES * gridDim.x, stage);
+    norm_out<N>(a, row, t, of_row, v, w, u, room[turn], true);
+    stage = stage == STAGES - 1 ? 0 : stage + 1;
   }
 }
 
@@ -173,44 +232,45 @@ static bool rows_aligned(const void *p, long long row_stride, int type, int rows
   return ((reinterpret_cast<uintptr_t>(p) | (rows > 1 ? (uintptr_t)(row_stride * (long long)bytes_of(type)) : 0)) & (to - 1)) == 0;
 }
 
-template <typename TX, typename TR> static cudaError_t rms_norm_in_registers(const RmsNorm &a, cudaStream_t s) {
-  if (a.dim <= 1024) {
-    // a warp a row, of four in a block
-    const dim3 grid((a.rows + 3) / 4), block(128);
-    if (a.dim <= 256) return launch_k(rms_norm_kernel<TX, TR, 1, true>, grid, block, 0, s, a);
-    if (a.dim <= 512) return launch_k(rms_norm_kernel<TX, TR, 2, true>, grid, block, 0, s, a);
-    return launch_k(rms_norm_kernel<TX, TR, 4, true>, grid, block, 0, s, a);
-  }
-  const int n = a.dim <= 4096 ? 1 : a.dim <= 8192 ? 2 : 4;
-  const dim3 block((a.dim / 8 + 32 * n - 1) / (32 * n) * 32);
-  if (n == 1) return launch_k(rms_norm_kernel<TX, TR, 1, false>, dim3(a.rows), block, 0, s, a);
-  if (n == 2) return launch_k(rms_norm_kernel<TX, TR, 2, false>, dim3(a.rows), block, 0, s, a);
-  return launch_k(rms_norm_kernel<TX, TR, 4, false>, dim3(a.rows), block, 0, s, a);
+template <typename TX, typename TR, int N> static cudaError_t rms_norm_by_ring(const RmsNorm &a, cudaStream_t s) {
+  static SmemLimit limit;
+  const int threads = (a.dim + 256 * N - 1) / (256 * N) * 32;
+  const size_t smem = (size_t)STAGES * a.dim * (sizeof(TX) + (a.res ? sizeof(TR) : 0));
+  if (smem > 46 << 10 && !limit.ensure(rms_norm_kernel<TX, TR, N>, (int)smem)) return cudaErrorInvalidValue;
+  const int per_sm = max(1, min(min((int)((227 << 10) / (smem + 1280)), 16), (N == 1 ? 1536 : N == 2 ? 1024 : 512) / threads));      // as many threads as registers allow
+  return launch_k(rms_norm_kernel<TX, TR, N>, dim3(min(a.rows, 148 * per_sm)), dim3(threads), smem, s, a);
+}
+template <typename TX, typename TR> static cudaError_t rms_norm_in_eights(const RmsNorm &a, cudaStream_t s) {
+  if (a.dim <= 256) return launch_k(rms_norm_warp_kernel<TX, TR>, dim3((a.rows + 3) / 4), dim3(128), 0, s, a);
+  if (a.dim <= 1024) return rms_norm_by_ring<TX, TR, 1>(a, s);
+  if (a.dim <= 8192) return rms_norm_by_ring<TX, TR, 2>(a, s);
+  return rms_norm_by_ring<TX, TR, 4>(a, s);
 }
 
 cudaError_t launch_rms_norm(const RmsNorm &a, cudaStream_t s) {
   const bool eight = kv_is_8bit(a.y_type);
-  const bool pieces = a.dim % 8 == 0 && a.dim <= 16384 && rows_aligned(a.x, a.x_rs, a.x_type, a.rows) && rows_aligned(a.gain, 0, a.g_type, 1) &&
+  const size_t stage = (size_t)a.dim * (bytes_of(a.x_type) + (a.res ? bytes_of(a.r_type) : 0));
+  const bool pieces = a.dim % 8 == 0 && a.dim <= 16384 && STAGES * stage <= 220 << 10 && rows_aligned(a.x, a.x_rs, a.x_type, a.rows) && rows_aligned(a.gain, 0, a.g_type, 1) &&
                       (!a.res || (rows_aligned(a.res, a.r_rs, a.r_type, a.rows) && rows_aligned(a.sum, a.s_rs, a.r_type, a.rows))) &&
                       rows_aligned(a.y, a.y_rs, a.y_type, a.rows, eight ? 8 : 16) &&
                       (!eight || a.group >= a.dim || a.group == 32 || a.group == 64 || a.group == 128 || a.group == 256);
   if (!pieces) return launch_k(rms_norm_any_kernel, dim3(a.rows), dim3(256), 0, s, a);
   const bool r = a.res && a.r_type == KV_BF16;
-  if (a.x_type == KV_F32) return r ? rms_norm_in_registers<float, bf16>(a, s) : rms_norm_in_registers<float, float>(a, s);
-  return r || !a.res ? rms_norm_in_registers<bf16, bf16>(a, s) : rms_norm_in_registers<bf16, float>(a, s);
+  if (a.x_type == KV_F32) return r ? rms_norm_in_eights<float, bf16>(a, s) : rms_norm_in_eights<float, float>(a, s);
+  return r || !a.res ? rms_norm_in_eights<bf16, bf16>(a, s) : rms_norm_in_eights<bf16, float>(a, s);
 }
 
 // ---------------------------------------------------------------- gradient
 // Blocks take rows in turn and keep their own sums for the gain's gradient, which the next launch adds up in the blocks' order.
 struct GradPlan {
-  int threads, n, blocks;      // threads of a block, eights of a thread
+  int n, threads, stages, blocks;      // eights of a thread, threads of a block, rows of the ring
 };
-// A thread has its columns in every row: eight up to 4096 of them, sixteen up to 8192.  Two blocks an SM of the widest, up to eight of narrow ones.
-static GradPlan grad_plan(int rows, int dim) {
-  const int n = dim <= 4096 ? 1 : 2, threads = min(512, (dim + 256 * n - 1) / (256 * n) * 32);
-  return {threads, n, min(rows, 148 * max(2, min(8, 1024 / threads)))};
+// row: bytes of a row of all inputs, of which as many are under way as there is shared memory for (2 to 4 in a block)
+static GradPlan grad_plan(int rows, int dim, size_t row) {
+  const int n = dim <= 1024 ? 1 : 2, threads = min(512, (dim + 256 * n - 1) / (256 * n) * 32);
+  const int per_sm = (int)max<size_t>(1, min<size_t>(max(1, min(8, (n == 1 ? 1024 : 512) / threads)), (220 << 10) / (2 * row + 1280)));
+  return {n, threads, (int)max<size_t>(2, min<size_t>(4, ((220 << 10) / per_sm - 1280) / row)), min(rows, 148 * per_sm)};
 }
-
 __global__ void __launch_bounds__(256) rms_norm_grad_any_kernel(RmsNormGrad a) {
   pdl_wait();
   pdl_trigger();
@@ -233,68 +293,60 @@ __global__ void __launch_bounds__(256) rms_norm_grad_any_kernel(RmsNormGrad a) {
   }
 }
 
-// Rows of whole eights up to 8192, aligned to 16 bytes, as they lie in memory: the next row is asked for before this one's sums.
-template <typename T> struct Raw8;
-template <> struct Raw8<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
-  __device__ __forceinline__ void floats(float (&y)[8]) const { y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w, y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w; }
-};
-template <> struct Raw8<bf16> {
-  uint4 u;
-  __device__ __forceinline__ void load(const bf16 *p) { u = *(const uint4 *)p; }
-  __device__ __forceinline__ void floats(float (&y)[8]) const { unpack2(u.x, y[0], y[1]), unpack2(u.y, y[2], y[3]), unpack2(u.z, y[4], y[5]), unpack2(u.w, y[6], y[7]); }
-};
-
+// The gradient's rows come through a ring as the norm's do
 template <typename TG, typename TX, typename TD, int N>
-__global__ void __launch_bounds__(512, 3 - N) rms_norm_grad_kernel(const __grid_constant__ RmsNormGrad a) {
+__global__ void __launch_bounds__(512) rms_norm_grad_kernel(const __grid_constant__ RmsNormGrad a, int stages) {
   pdl_wait();
   pdl_trigger();
+  extern __shared__ __align__(16) char ring[];
   __shared__ float2 room[2][16];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  Raw8<TG> g[N];
-  Raw8<TX> x[N];
-  Raw8<TD> c[N];
-  float w[N][8], sum[N][8] = {};
-  int at[N];
-  bool mine[N];
+  const int t = threadIdx.x, of_row = blockDim.x, lane = t & 31, warp = t >> 5, warps = of_row >> 5;
+  TG *const gs = (TG *)ring;                             // [stages][dim]
+  TX *const xs = (TX *)(ring + (size_t)stages * a.dim * sizeof(TG));
+  TD *const cs = (TD *)(ring + (size_t)stages * a.dim * (sizeof(TG) + sizeof(TX)));
+  auto ask = [&](long long row, int stage) {
+    if (row < a.rows)
 #pragma unroll
-  for (int i = 0; i < N; i++) {
-    at[i] = (i * blockDim.x + threadIdx.x) * 8;
-    mine[i] = at[i] < a.dim;
-#pragma unroll
-    for (int k = 0; k < 8; k++) w[i][k] = 0.0f;
-    if (!mine[i]) continue;
-    if (a.w_type == KV_F32) load8((const float *)a.gain + at[i], w[i]);
-    else load8((const bf16 *)a.gain + at[i], w[i]);
-  }
-  auto load = [&](long long row) {
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-      if (!mine[i]) continue;
-      g[i].load((const TG *)a.g + row * a.g_rs + at[i]);
-      x[i].load((const TX *)a.x + row * a.x_rs + at[i]);
-      if (a.carried) c[i].load((const TD *)a.carried + row * a.c_rs + at[i]);
-    }
+      for (int i = 0; i < N; i++) {
+        const int c = (i * of_row + t) * 8;
+        if (c >= a.dim) continue;
+        copy8(gs + stage * a.dim + c, (const TG *)a.g + row * a.g_rs + c);
+        copy8(xs + stage * a.dim + c, (const TX *)a.x + row * a.x_rs + c);
+        if (a.carried) copy8(cs + stage * a.dim + c, (const TD *)a.carried + row * a.c_rs + c);
+      }
+    copies_commit();
   };
   long long row = blockIdx.x;
-  load(row);
-  for (int turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
-    float gr[N][8], xr[N][8], cr[N][8], ss = 0.0f, dot = 0.0f;
+  for (int k = 0; k < stages; k++) ask(row + (long long)k * gridDim.x, k);
+  float w[N][8], sum[N][8] = {};
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    const int c = (i * of_row + t) * 8;
+#pragma unroll
+    for (int k = 0; k < 8; k++) w[i][k] = 0.0f;
+    if (c >= a.dim) continue;
+    if (a.w_type == KV_F32) load8((const float *)a.gain + c, w[i]);
+    else load8((const bf16 *)a.gain + c, w[i]);
+  }
+  for (int stage = 0, turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
+    if (stages == 2) copies_but<1>();
+    else if (stages == 3) copies_but<2>();
+    else copies_but<3>();
+    Raw8<TG> g[N];
+    Raw8<TX> x[N];
+    float ss = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; i++) {
+      const int c = (i * of_row + t) * 8;
+      if (c >= a.dim) continue;
+      g[i].take(gs + stage * a.dim + c);
+      x[i].take(xs + stage * a.dim + c);
+      float gr[8], xr[8];
+      g[i].floats(gr);
+      x[i].floats(xr);
 #pragma unroll
-      for (int k = 0; k < 8; k++) gr[i][k] = xr[i][k] = cr[i][k] = 0.0f;
-      if (!mine[i]) continue;
-      g[i].floats(gr[i]);
-      x[i].floats(xr[i]);
-      if (a.carried) c[i].floats(cr[i]);
+      for (int k = 0; k < 8; k++) ss = fmaf(xr[k], xr[k], ss), dot = fmaf(gr[k] * w[i][k], xr[k], dot);
     }
-    if (row + gridDim.x < a.rows) load(row + gridDim.x);
-#pragma unroll
-    for (int i = 0; i < N; i++)
-#pragma unroll
-      for (int k = 0; k < 8; k++) ss = fmaf(xr[i][k], xr[i][k], ss), dot = fmaf(gr[i][k] * w[i][k], xr[i][k], dot);
 #pragma unroll
     for (int d = 16; d; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d), dot += __shfl_xor_sync(0xffffffffu, dot, d);
     if (lane == 0) room[turn][warp] = make_float2(ss, dot);
@@ -307,18 +359,27 @@ __global__ void __launch_bounds__(512, 3 - N) rms_norm_grad_kernel(const __grid_
     const float u = rsqrtf(ss / a.dim + a.eps), along = dot / a.dim * u * u;
 #pragma unroll
     for (int i = 0; i < N; i++) {
-      if (!mine[i]) continue;
+      const int c = (i * of_row + t) * 8;
+      if (c >= a.dim) continue;
+      float gr[8], xr[8], d[8] = {};
+      g[i].floats(gr);
+      x[i].floats(xr);
+      if (a.carried) load8(cs + stage * a.dim + c, d);
 #pragma unroll
       for (int k = 0; k < 8; k++) {
-        sum[i][k] = fmaf(gr[i][k], xr[i][k] * u, sum[i][k]);
-        cr[i][k] = fmaf(u, fmaf(-xr[i][k], along, gr[i][k] * w[i][k]), cr[i][k]);
+        sum[i][k] = fmaf(gr[k], xr[k] * u, sum[i][k]);
+        d[k] = fmaf(u, fmaf(-xr[k], along, gr[k] * w[i][k]), d[k]);
       }
-      store8((TD *)a.dx + row * a.d_rs + at[i], cr[i]);
+      store8((TD *)a.dx + row * a.d_rs + c, d);
     }
+    ask(row + (long long)stages * gridDim.x, stage);
+    stage = stage == stages - 1 ? 0 : stage + 1;
   }
 #pragma unroll
-  for (int i = 0; i < N; i++)
-    if (mine[i]) store8(a.part + (long long)blockIdx.x * a.dim + at[i], sum[i]);
+  for (int i = 0; i < N; i++) {
+    const int c = (i * of_row + t) * 8;
+    if (c < a.dim) store8(a.part + (long long)blockIdx.x * a.dim + c, sum[i]);
+  }
 }
 
 // 32 columns a block, blocks' sums in eight runs that are then added in order
@@ -338,26 +399,31 @@ __global__ void __launch_bounds__(256) rms_norm_gain_kernel(RmsNormGrad a, int b
   store_from_f32(a.dgain, a.w_type, c, sum);
 }
 
-size_t rms_norm_grad_scratch_bytes(int rows, int dim) { return (size_t)grad_plan(rows, dim).blocks * dim * sizeof(float); }
+size_t rms_norm_grad_scratch_bytes(int rows, int dim) { return (size_t)grad_plan(rows, dim, 4 * (size_t)dim).blocks * dim * sizeof(float); }      // with one input of 32 bits: as many blocks as any has
 
-template <typename TG, typename TX, typename TD> static cudaError_t rms_norm_grad_in_registers(const RmsNormGrad &a, const GradPlan &p, cudaStream_t s) {
-  return p.n == 1 ? launch_k(rms_norm_grad_kernel<TG, TX, TD, 1>, dim3(p.blocks), dim3(p.threads), 0, s, a) : launch_k(rms_norm_grad_kernel<TG, TX, TD, 2>, dim3(p.blocks), dim3(p.threads), 0, s, a);
+template <typename TG, typename TX, typename TD, int N> static cudaError_t rms_norm_grad_by_ring(const RmsNormGrad &a, const GradPlan &p, size_t row, cudaStream_t s) {
+  static SmemLimit limit;
+  const size_t smem = p.stages * row;
+  if (smem > 46 << 10 && !limit.ensure(rms_norm_grad_kernel<TG, TX, TD, N>, (int)smem)) return cudaErrorInvalidValue;
+  return launch_k(rms_norm_grad_kernel<TG, TX, TD, N>, dim3(p.blocks), dim3(p.threads), smem, s, a, p.stages);
 }
-template <typename TG, typename TX> static cudaError_t rms_norm_grad_in_registers(const RmsNormGrad &a, const GradPlan &p, cudaStream_t s) {
-  return a.d_type == KV_F32 ? rms_norm_grad_in_registers<TG, TX, float>(a, p, s) : rms_norm_grad_in_registers<TG, TX, bf16>(a, p, s);
+template <typename TG, typename TX> static cudaError_t rms_norm_grad_in_eights(const RmsNormGrad &a, const GradPlan &p, size_t row, cudaStream_t s) {
+  if (a.d_type == KV_F32) return p.n == 1 ? rms_norm_grad_by_ring<TG, TX, float, 1>(a, p, row, s) : rms_norm_grad_by_ring<TG, TX, float, 2>(a, p, row, s);
+  return p.n == 1 ? rms_norm_grad_by_ring<TG, TX, bf16, 1>(a, p, row, s) : rms_norm_grad_by_ring<TG, TX, bf16, 2>(a, p, row, s);
 }
 
 cudaError_t launch_rms_norm_grad(const RmsNormGrad &a, cudaStream_t s) {
-  const GradPlan p = grad_plan(a.rows, a.dim);
+  const size_t row = (size_t)a.dim * (bytes_of(a.g_type) + bytes_of(a.x_type) + (a.carried ? bytes_of(a.d_type) : 0));
+  GradPlan p = grad_plan(a.rows, a.dim, row);
   if (a.rows) {
     // what is carried has the output's type, as it has where both are of the residual stream
-    const bool pieces = a.dim % 8 == 0 && a.dim <= 8192 && rows_aligned(a.g, a.g_rs, a.g_type, a.rows) && rows_aligned(a.x, a.x_rs, a.x_type, a.rows) &&
+    const bool pieces = a.dim % 8 == 0 && a.dim <= 8192 && 2 * row <= 220 << 10 && rows_aligned(a.g, a.g_rs, a.g_type, a.rows) && rows_aligned(a.x, a.x_rs, a.x_type, a.rows) &&
                         rows_aligned(a.gain, 0, a.w_type, 1) && rows_aligned(a.dx, a.d_rs, a.d_type, a.rows) &&
                         (!a.carried || (a.c_type == a.d_type && rows_aligned(a.carried, a.c_rs, a.c_type, a.rows)));
     cudaError_t e;
     if (!pieces) e = launch_k(rms_norm_grad_any_kernel, dim3(p.blocks), dim3(256), 0, s, a);
-    else if (a.g_type == KV_F32) e = a.x_type == KV_F32 ? rms_norm_grad_in_registers<float, float>(a, p, s) : rms_norm_grad_in_registers<float, bf16>(a, p, s);
-    else e = a.x_type == KV_F32 ? rms_norm_grad_in_registers<bf16, float>(a, p, s) : rms_norm_grad_in_registers<bf16, bf16>(a, p, s);
+    else if (a.g_type == KV_F32) e = a.x_type == KV_F32 ? rms_norm_grad_in_eights<float, float>(a, p, row, s) : rms_norm_grad_in_eights<float, bf16>(a, p, row, s);
+    else e = a.x_type == KV_F32 ? rms_norm_grad_in_eights<bf16, float>(a, p, row, s) : rms_norm_grad_in_eights<bf16, bf16>(a, p, row, s);
     if (e) return e;
   }
   return launch_k(rms_norm_gain_kernel, dim3((a.dim + 31) / 32), dim3(256), 0, s, a, a.rows ? p.blocks : 0);

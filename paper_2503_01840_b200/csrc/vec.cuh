@@ -33,6 +33,28 @@ __device__ __forceinline__ void store8(float *p, const float (&y)[8]) {
 __device__ __forceinline__ void store8(bf16 *p, const float (&y)[8]) {
   *(uint4 *)p = make_uint4(pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7]));
 }
+// Eight neighbours as they lie in memory
+template <typename T> struct Raw8;
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void take(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
+  __device__ __forceinline__ void floats(float (&y)[8]) const { y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w, y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w; }
+};
+template <> struct Raw8<bf16> {
+  uint4 u;
+  __device__ __forceinline__ void take(const bf16 *p) { u = *(const uint4 *)p; }
+  __device__ __forceinline__ void floats(float (&y)[8]) const { unpack2(u.x, y[0], y[1]), unpack2(u.y, y[2], y[3]), unpack2(u.z, y[4], y[5]), unpack2(u.w, y[6], y[7]); }
+};
+// Copies to shared memory that run on while the thread does; those of a thread complete by groups, in order.
+__device__ __forceinline__ uint32_t smem_of(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(void *to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_of(to)), "l"(from) : "memory"); }
+template <typename T> __device__ __forceinline__ void copy8(T *to, const T *from) {      // eight elements
+  copy16(to, from);
+  if (sizeof(T) == 4) copy16(to + 4, from + 4);
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }      // all groups but the last N are there
+
 // rows whose pieces of 16 bytes are aligned, elements of e bytes
 inline bool pieces_aligned(const void *p, long long row_stride, size_t e) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(row_stride * (long long)e)) & 15) == 0; }
 
