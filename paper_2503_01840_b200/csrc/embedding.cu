@@ -23,8 +23,60 @@ __global__ void __launch_bounds__(256) embed_any_kernel(Embed a, int w_dtype, in
     store_from_f32(a.out, out_dtype, (long long)t * a.o_rs + c, there ? load_as_f32(a.w, w_dtype, (long long)id * a.w_rs + c) * a.scale : 0.0f);
 }
 
+// Widths of whole eights, aligned to 16 bytes: a thread has up to four units of eight under way.  A block has 1024 units of a token, or as many tokens as make 1024.
+constexpr int LOOK_UNITS = 1024;
+struct EmbedGrid {
+  int units, tokens;     // of a token; of a block
+  uint32_t by_units;     // ceil(2^32 / units), where a block has several tokens
+};
+template <typename TW, typename TO>
+__global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ Embed a, const __grid_constant__ EmbedGrid gr) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr int U = LOOK_UNITS / 256;
+  const int t0 = blockIdx.x * gr.tokens, u0 = blockIdx.y * LOOK_UNITS, n = gr.tokens == 1 ? min(LOOK_UNITS + 0, gr.units - u0) : min(gr.tokens, a.tokens - t0) * gr.units;
+  int token[U], unit[U], id[U];
+#pragma unroll
+  for (int k = 0; k < U; k++) {
+    const int i = threadIdx.x + k * 256;
+    token[k] = -1;
+    if (i >= n) continue;
+    const int q = gr.tokens == 1 ? 0 : (int)__umulhi((uint32_t)i, gr.by_units);
+    token[k] = t0 + q, unit[k] = u0 + i - q * gr.units;
+    id[k] = id_at(a.ids, token[k]);
+    if (id[k] >= 0 && id[k] < a.vocab) continue;
+    if (id[k] != -1 && unit[k] == 0) set_status(a.status, ST_BOUNDS, 64, token[k], id[k]);
+    id[k] = -1;
+  }
+  Raw8<TW> x[U];
+#pragma unroll
+  for (int k = 0; k < U; k++)
+    if (token[k] >= 0 && id[k] >= 0) x[k].take((const TW *)a.w + (long long)id[k] * a.w_rs + unit[k] * 8);
+#pragma unroll
+  for (int k = 0; k < U; k++) {
+    if (token[k] < 0) continue;
+    float y[8] = {};
+    if (id[k] >= 0) {
+      x[k].floats(y);
+#pragma unroll
+      for (int c = 0; c < 8; c++) y[c] *= a.scale;
+    }
+    store8((TO *)a.out + (long long)token[k] * a.o_rs + unit[k] * 8, y);
+  }
+}
+
+static size_t bytes_of(int dtype) { return dtype == 0 ? 4 : 2; }
+
 cudaError_t launch_embed_rows(const Embed &a, int w_dtype, int out_dtype, cudaStream_t s) {
-  return launch_k(embed_any_kernel, dim3(a.tokens, (a.dim + 1023) / 1024), dim3(256), 0, s, a, w_dtype, out_dtype);
+  if (a.dim % 8 || a.dim < 16 || !pieces_aligned(a.w, a.vocab > 1 ? a.w_rs : 0, bytes_of(w_dtype)) || !pieces_aligned(a.out, a.tokens > 1 ? a.o_rs : 0, bytes_of(out_dtype)))
+    return launch_k(embed_any_kernel, dim3(a.tokens, (a.dim + 1023) / 1024), dim3(256), 0, s, a, w_dtype, out_dtype);
+  EmbedGrid gr;
+  gr.units = a.dim / 8;
+  gr.tokens = max(1, min(LOOK_UNITS / gr.units, a.tokens / 296));      // every SM has two blocks before one has two tokens
+  gr.by_units = (uint32_t)((0x100000000ull + gr.units - 1) / gr.units);
+  const dim3 grid((a.tokens + gr.tokens - 1) / gr.tokens, gr.tokens == 1 ? (gr.units + LOOK_UNITS - 1) / LOOK_UNITS : 1);
+  if (w_dtype == 0) return out_dtype == 0 ? launch_k(embed_kernel<float, float>, grid, dim3(256), 0, s, a, gr) : launch_k(embed_kernel<float, bf16>, grid, dim3(256), 0, s, a, gr);
+  return out_dtype == 0 ? launch_k(embed_kernel<bf16, float>, grid, dim3(256), 0, s, a, gr) : launch_k(embed_kernel<bf16, bf16>, grid, dim3(256), 0, s, a, gr);
 }
 
 // ---------------------------------------------------------------- gradient: the tokens in the order of their ids
@@ -38,6 +90,7 @@ struct EmbedSort {
   int32_t *order, *id;   // tokens by id, and the ids
   int2 *list;            // (token, row of the block's range) of the ranges, unsorted
   int32_t *count;        // tokens with a row
+  int wide;              // whether rows are aligned pieces of 16 bytes
 };
 
 __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, EmbedSort so, int out_dtype) {
@@ -50,16 +103,23 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
   // a warp's segment, in steps of 32 ids
   const long long steps = (a.tokens + 31LL) / 32, per = (steps + SORT_WARPS - 1) / SORT_WARPS, s0 = min((long long)warp * per, steps), s1 = min(s0 + per, steps);
   int less = 0, in = 0;
-  for (long long s = s0; s < s1; s++) {
-    const long long t = s * 32 + lane;
-    if (t >= a.tokens) break;
-    const int id = id_at(a.ids, t);
-    if (id < 0 || id >= a.vocab) {
-      if (id != -1 && blockIdx.x == 0) set_status(a.status, ST_BOUNDS, 64, (int)t, id);
-      continue;
+  constexpr int U = 8;                                   // steps under way
+  for (long long s = s0; s < s1; s += U) {
+    int id[U];
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      const long long t = (s + k) * 32 + lane;
+      id[k] = s + k < s1 && t < a.tokens ? id_at(a.ids, t) : -1;
     }
-    less += id < lo;
-    if (id >= lo && id - lo < n_rows) in++, atomicAdd(&have[id - lo], 1);
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      if (id[k] < 0 || id[k] >= a.vocab) {
+        if (id[k] != -1 && blockIdx.x == 0) set_status(a.status, ST_BOUNDS, 64, (int)((s + k) * 32 + lane), id[k]);
+        continue;
+      }
+      less += id[k] < lo;
+      if (id[k] >= lo && id[k] - lo < n_rows) in++, atomicAdd(&have[id[k] - lo], 1);
+    }
   }
   less = __reduce_add_sync(0xffffffffu, less);
   in = __reduce_add_sync(0xffffffffu, in);
@@ -75,13 +135,20 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
   if (total) {
     if (in) {
       int at = base + before_me;
-      for (long long s = s0; s < s1; s++) {
-        const long long t = s * 32 + lane;
-        const int id = t < a.tokens ? id_at(a.ids, t) : -1;
-        const bool hit = id >= lo && id - lo < n_rows;
-        const uint32_t hits = __ballot_sync(0xffffffffu, hit);
-        if (hit) so.list[at + __popc(hits & ((1u << lane) - 1))] = make_int2((int)t, id - lo);
-        at += __popc(hits);
+      for (long long s = s0; s < s1; s += U) {
+        int id[U];
+#pragma unroll
+        for (int k = 0; k < U; k++) {
+          const long long t = (s + k) * 32 + lane;
+          id[k] = s + k < s1 && t < a.tokens ? id_at(a.ids, t) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < U; k++) {
+          const bool hit = id[k] >= lo && id[k] - lo < n_rows;
+          const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+          if (hit) so.list[at + __popc(hits & ((1u << lane) - 1))] = make_int2((int)((s + k) * 32 + lane), id[k] - lo);
+          at += __popc(hits);
+        }
       }
     }
     __syncthreads();
@@ -114,7 +181,12 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
   if (a.accumulate) return;
   for (int r = warp; r < n_rows; r += SORT_WARPS) {
     if (have[r]) continue;
-    for (int c = lane; c < a.dim; c += 32) store_from_f32(a.out, out_dtype, (lo + r) * a.o_rs + c, 0.0f);
+    if (so.wide) {
+      uint4 *const p = (uint4 *)((char *)a.out + (lo + r) * a.o_rs * (out_dtype == 0 ? 4 : 2));
+      for (int c = lane; c < a.dim * (out_dtype == 0 ? 4 : 2) / 16; c += 32) p[c] = make_uint4(0, 0, 0, 0);
+    } else {
+      for (int c = lane; c < a.dim; c += 32) store_from_f32(a.out, out_dtype, (lo + r) * a.o_rs + c, 0.0f);
+    }
   }
 }
 
@@ -131,8 +203,16 @@ constexpr int CHUNK_MAX = 64;
 
 __device__ __forceinline__ void embed_grad_out(const EmbedGrad &a, int out_dtype, int id, int c, float sum) {
   const long long at = id * a.o_rs + c;
-  const float v = sum * a.scale;
-  store_from_f32(a.out, out_dtype, at, a.accumulate ? load_as_f32(a.out, out_dtype, at) + v : v);
+  store_from_f32(a.out, out_dtype, at, a.accumulate ? fmaf(sum, a.scale, load_as_f32(a.out, out_dtype, at)) : sum * a.scale);
+}
+
+template <typename TO> __device__ __forceinline__ void embed_grad_out8(const EmbedGrad &a, int id, int c, const float (&sum)[8]) {
+  TO *const at = (TO *)a.out + id * a.o_rs + c;
+  float y[8] = {};
+  if (a.accumulate) load8(at, y);
+#pragma unroll
+  for (int e = 0; e < 8; e++) y[e] = a.accumulate ? fmaf(sum[e], a.scale, y[e]) : sum[e] * a.scale;
+  store8(at, y);
 }
 
 __global__ void __launch_bounds__(128) embed_runs_any_kernel(EmbedGrad a, EmbedRuns r, int g_dtype, int out_dtype) {
@@ -158,6 +238,76 @@ __global__ void __launch_bounds__(128) embed_runs_any_kernel(EmbedGrad a, EmbedR
     sum = 0.0f;
     began = true;
   }
+}
+
+// Widths of whole eights, aligned to 16 bytes: eight columns a thread, eight tokens of them under way
+template <typename TG, typename TO>
+__global__ void __launch_bounds__(128) embed_runs_kernel(const __grid_constant__ EmbedGrad a, const __grid_constant__ EmbedRuns r) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ int token[CHUNK_MAX], id[CHUNK_MAX + 2];
+  const int n = *r.count, p0 = blockIdx.x * r.per_chunk, m = min(r.per_chunk, n - p0);
+  if (m <= 0) return;
+  for (int i = threadIdx.x; i < m; i += 128) token[i] = r.order[p0 + i];
+  for (int i = threadIdx.x; i < m + 2; i += 128) id[i] = p0 + i - 1 >= 0 && p0 + i - 1 < n ? r.id[p0 + i - 1] : -1;
+  __syncthreads();
+  const int c = (blockIdx.y * 128 + threadIdx.x) * 8;
+  if (c >= a.dim) return;
+  constexpr int U = 8;
+  float sum[8] = {};
+  bool began = id[0] != id[1];
+  for (int i0 = 0; i0 < m; i0 += U) {
+    Raw8<TG> x[U];
+#pragma unroll
+    for (int k = 0; k < U; k++)
+      if (i0 + k < m) x[k].take((const TG *)a.grad + token[i0 + k] * a.g_rs + c);
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      const int i = i0 + k;
+      if (i >= m) continue;
+      float y[8];
+      x[k].floats(y);
+#pragma unroll
+      for (int e = 0; e < 8; e++) sum[e] += y[e];
+      const int me = id[i + 1];
+      const bool ends = id[i + 2] != me;
+      if (i + 1 < m && !ends) continue;
+      if (began && ends) embed_grad_out8<TO>(a, me, c, sum);
+      else store8(r.part + (2LL * blockIdx.x + began) * a.dim + c, sum);
+#pragma unroll
+      for (int e = 0; e < 8; e++) sum[e] = 0.0f;
+      began = true;
+    }
+  }
+}
+
+template <typename TO>
+__global__ void __launch_bounds__(128) embed_join_eights_kernel(const __grid_constant__ EmbedGrad a, const __grid_constant__ EmbedRuns r) {
+  pdl_wait();
+  pdl_trigger();
+  const int n = *r.count, k = blockIdx.x, p1 = (k + 1) * r.per_chunk;
+  if (p1 >= n) return;
+  const int me = r.id[p1 - 1];
+  if (r.id[p1] != me || (k > 0 && r.id[k * r.per_chunk] == me && r.id[k * r.per_chunk - 1] == me)) return;
+  const int c = (blockIdx.y * 128 + threadIdx.x) * 8;
+  if (c >= a.dim) return;
+  // the run's last chunk: ids are sorted
+  int lo = k + 1, hi = min(r.chunks, (n + r.per_chunk - 1) / r.per_chunk);
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (r.id[mid * r.per_chunk] == me) lo = mid;
+    else hi = mid;
+  }
+  float sum[8];
+  load8(r.part + (2LL * k + 1) * a.dim + c, sum);
+#pragma unroll 4
+  for (int j = k + 1; j <= lo; j++) {
+    float y[8];
+    load8(r.part + 2LL * j * a.dim + c, y);
+#pragma unroll
+    for (int e = 0; e < 8; e++) sum[e] += y[e];
+  }
+  embed_grad_out8<TO>(a, me, c, sum);
 }
 
 __global__ void __launch_bounds__(128) embed_join_kernel(EmbedGrad a, EmbedRuns r, int out_dtype) {
@@ -190,15 +340,24 @@ cudaError_t launch_embed_grad(const EmbedGrad &a, int g_dtype, int out_dtype, cu
   so.id = (int32_t *)p, p += up(4 * (size_t)a.tokens);
   so.list = (int2 *)p, p += up(8 * (size_t)a.tokens);
   so.rows = min(SORT_MAX_ROWS, (a.vocab + 295) / 296);
+  const bool out_wide = a.dim * bytes_of(out_dtype) % 16 == 0 && pieces_aligned(a.out, a.vocab > 1 ? a.o_rs : 0, bytes_of(out_dtype));
+  so.wide = out_wide;
   if (const cudaError_t e = launch_k(embed_sort_kernel, dim3((a.vocab + so.rows - 1) / so.rows), dim3(SORT_THREADS), 0, s, a, so, out_dtype)) return e;
   if (a.tokens == 0) return cudaSuccess;
   EmbedRuns r;
   r.per_chunk = chunk_of(a.tokens);
   r.chunks = (int)(((long long)a.tokens + r.per_chunk - 1) / r.per_chunk);
   r.order = so.order, r.id = so.id, r.count = so.count, r.part = (float *)p;
-  const dim3 grid(r.chunks, (a.dim + 127) / 128);
-  if (const cudaError_t e = launch_k(embed_runs_any_kernel, grid, dim3(128), 0, s, a, r, g_dtype, out_dtype)) return e;
-  return launch_k(embed_join_kernel, grid, dim3(128), 0, s, a, r, out_dtype);
+  if (a.dim % 8 || !out_wide || !pieces_aligned(a.grad, a.tokens > 1 ? a.g_rs : 0, bytes_of(g_dtype))) {
+    const dim3 grid(r.chunks, (a.dim + 127) / 128);
+    if (const cudaError_t e = launch_k(embed_runs_any_kernel, grid, dim3(128), 0, s, a, r, g_dtype, out_dtype)) return e;
+    return launch_k(embed_join_kernel, grid, dim3(128), 0, s, a, r, out_dtype);
+  }
+  const dim3 grid(r.chunks, (a.dim + 1023) / 1024);
+  const cudaError_t e = g_dtype == 0 ? (out_dtype == 0 ? launch_k(embed_runs_kernel<float, float>, grid, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<float, bf16>, grid, dim3(128), 0, s, a, r))
+                                     : (out_dtype == 0 ? launch_k(embed_runs_kernel<bf16, float>, grid, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<bf16, bf16>, grid, dim3(128), 0, s, a, r));
+  if (e) return e;
+  return out_dtype == 0 ? launch_k(embed_join_eights_kernel<float>, grid, dim3(128), 0, s, a, r) : launch_k(embed_join_eights_kernel<bf16>, grid, dim3(128), 0, s, a, r);
 }
 
 }  // namespace spec
