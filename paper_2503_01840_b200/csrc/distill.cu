@@ -10,24 +10,7 @@ namespace spec {
 using std::max;
 using std::min;
 
-// exp(d / T) = 2^(d c), c = log2(e) / T.  c's own rounding is 2^-25 of the exponent at most, as much as the product's is.  Pairs of 32-bit numbers take one instruction.
-typedef unsigned long long Pair;
-__device__ __forceinline__ Pair pair(float a, float b) {
-  Pair p;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
-  return p;
-}
-__device__ __forceinline__ void unpair(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
-__device__ __forceinline__ Pair add(Pair a, Pair b) {
-  Pair p;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(p) : "l"(a), "l"(b));
-  return p;
-}
-__device__ __forceinline__ Pair mul(Pair a, Pair b) {
-  Pair p;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p) : "l"(a), "l"(b));
-  return p;
-}
+// exp(d / T) = 2^(d c), c = log2(e) / T.  c's own rounding is 2^-25 of the exponent at most, as much as the product's is.
 __device__ __forceinline__ float power_of_two(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

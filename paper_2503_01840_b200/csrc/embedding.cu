@@ -289,19 +289,19 @@ __global__ void __launch_bounds__(128) embed_join_eights_kernel(const __grid_con
   if (p1 >= n) return;
   const int me = r.id[p1 - 1];
   if (r.id[p1] != me || (k > 0 && r.id[k * r.per_chunk] == me && r.id[k * r.per_chunk - 1] == me)) return;
+  int last = k + 1;                                      // the run's last chunk: ids are sorted
+  for (bool more = true; more;) {
+    const int j = last + 1 + (threadIdx.x & 31);
+    const uint32_t on = __ballot_sync(0xffffffffu, j < r.chunks && (long long)j * r.per_chunk < n && r.id[j * r.per_chunk] == me);
+    more = on == 0xffffffffu;
+    last += more ? 32 : __ffs(~on) - 1;
+  }
   const int c = (blockIdx.y * 128 + threadIdx.x) * 8;
   if (c >= a.dim) return;
-  // the run's last chunk: ids are sorted
-  int lo = k + 1, hi = min(r.chunks, (n + r.per_chunk - 1) / r.per_chunk);
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (r.id[mid * r.per_chunk] == me) lo = mid;
-    else hi = mid;
-  }
   float sum[8];
   load8(r.part + (2LL * k + 1) * a.dim + c, sum);
-#pragma unroll 4
-  for (int j = k + 1; j <= lo; j++) {
+#pragma unroll 8
+  for (int j = k + 1; j <= last; j++) {
     float y[8];
     load8(r.part + 2LL * j * a.dim + c, y);
 #pragma unroll
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(128) embed_join_kernel(EmbedGrad a, EmbedRuns 
 }
 
 static size_t up(size_t n) { return (n + 255) / 256 * 256; }
-static int chunk_of(int tokens) { return tokens >= 4096 ? 32 : 8; }
+static int chunk_of(int tokens) { return tokens >= 4096 ? 32 : 16; }
 
 size_t embed_grad_scratch_bytes(int tokens, int dim) {
   const size_t T = tokens, chunks = (T + chunk_of(tokens) - 1) / chunk_of(tokens);

@@ -64,8 +64,10 @@ __global__ void __launch_bounds__(256) rms_norm_any_kernel(RmsNorm a) {
 // Up to 256 columns a warp has a row, and nothing to wait for.  In 8 bits a scale's group is part of a warp's 256 columns, or the row.
 constexpr int STAGES = 3;
 
-template <int FMT> __device__ __forceinline__ uint2 codes_of(const float (&y)[8], float inv) {
-  return make_uint2(kv_encode4<FMT>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), kv_encode4<FMT>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+template <int FMT> __device__ __forceinline__ uint2 codes_of(float (&y)[8], float inv) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) unpair(mul(pair(y[k], y[k + 1]), pair(inv, inv)), y[k], y[k + 1]);
+  return make_uint2(kv_encode4<FMT>(y[0], y[1], y[2], y[3]), kv_encode4<FMT>(y[4], y[5], y[6], y[7]));
 }
 // of a warp's lanes, and of a block's warps through `room`
 __device__ __forceinline__ float sum_of(float v, float *room, bool block) {
@@ -87,7 +89,7 @@ template <int N> __device__ __forceinline__ void norm_out(const RmsNorm &a, long
 #pragma unroll
   for (int i = 0; i < N; i++)
 #pragma unroll
-    for (int k = 0; k < 8; k++) v[i][k] = v[i][k] * u * w[i][k];
+    for (int k = 0; k < 8; k += 2) unpair(mul(mul(pair(v[i][k], v[i][k + 1]), pair(u, u)), pair(w[i][k], w[i][k + 1])), v[i][k], v[i][k + 1]);
   if (a.y_type == KV_F32 || a.y_type == KV_BF16) {
 #pragma unroll
     for (int i = 0; i < N; i++) {
@@ -103,9 +105,10 @@ template <int N> __device__ __forceinline__ void norm_out(const RmsNorm &a, long
   uint32_t top[N];                                       // bits of the largest magnitude: NaN counts as the largest of all
 #pragma unroll
   for (int i = 0; i < N; i++) {
-    top[i] = 0;
+    float m = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 8; k++) top[i] = max(top[i], __float_as_uint(v[i][k]) & 0x7fffffffu);
+    for (int k = 0; k < 8; k++) asm("max.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(m) : "f"(v[i][k]));      // up to a sign
+    top[i] = __float_as_uint(m) & 0x7fffffffu;
   }
   if (whole) {
 #pragma unroll
@@ -144,12 +147,17 @@ template <int N> __device__ __forceinline__ void gain_of(const RmsNorm &a, int t
   }
 }
 template <int N> __device__ __forceinline__ float square_of(const float (&v)[N][8]) {
-  float ss = 0.0f;
+  Pair ss = pair(0.0f, 0.0f);
 #pragma unroll
   for (int i = 0; i < N; i++)
 #pragma unroll
-    for (int k = 0; k < 8; k++) ss = fmaf(v[i][k], v[i][k], ss);
-  return ss;
+    for (int k = 0; k < 8; k += 2) {
+      const Pair p = pair(v[i][k], v[i][k + 1]);
+      ss = fma(p, p, ss);
+    }
+  float even, odd;
+  unpair(ss, even, odd);
+  return even + odd;
 }
 
 template <typename TX, typename TR>
@@ -268,7 +276,7 @@ struct GradPlan {
 // row: bytes of a row of all inputs, of which as many are under way as there is shared memory for (2 to 4 in a block)
 static GradPlan grad_plan(int rows, int dim, size_t row) {
   const int n = dim <= 1024 ? 1 : 2, threads = min(512, (dim + 256 * n - 1) / (256 * n) * 32);
-  const int per_sm = (int)max<size_t>(1, min<size_t>(max(1, min(8, (n == 1 ? 1024 : 512) / threads)), (220 << 10) / (2 * row + 1280)));
+  const int per_sm = (int)max<size_t>(1, min<size_t>(max(1, min(16, (n == 1 ? 1024 : 512) / threads)), (220 << 10) / (2 * row + 1280)));
   return {n, threads, (int)max<size_t>(2, min<size_t>(4, ((220 << 10) / per_sm - 1280) / row)), min(rows, 148 * per_sm)};
 }
 __global__ void __launch_bounds__(256) rms_norm_grad_any_kernel(RmsNormGrad a) {
@@ -382,21 +390,22 @@ __global__ void __launch_bounds__(512) rms_norm_grad_kernel(const __grid_constan
   }
 }
 
-// 32 columns a block, blocks' sums in eight runs that are then added in order
-__global__ void __launch_bounds__(256) rms_norm_gain_kernel(RmsNormGrad a, int blocks) {
+// 32 columns a block; its warps add up runs of the blocks' sums, and each of them then one column's 32
+__global__ void __launch_bounds__(1024) rms_norm_gain_kernel(RmsNormGrad a, int blocks) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float some[8][32];
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, per = (blocks + 7) / 8;
+  __shared__ float some[32][33];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, per = (blocks + 31) / 32;
   float sum = 0.0f;
   if (c < a.dim)
 #pragma unroll 8
     for (int b = w * per; b < min(blocks, (w + 1) * per); b++) sum += a.part[(long long)b * a.dim + c];
   some[w][lane] = sum;
   __syncthreads();
-  if (w || c >= a.dim) return;
-  for (int i = 1; i < 8; i++) sum += some[i][lane];
-  store_from_f32(a.dgain, a.w_type, c, sum);
+  sum = some[lane][w];
+#pragma unroll
+  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0 && blockIdx.x * 32 + w < a.dim) store_from_f32(a.dgain, a.w_type, blockIdx.x * 32 + w, sum);
 }
 
 size_t rms_norm_grad_scratch_bytes(int rows, int dim) { return (size_t)grad_plan(rows, dim, 4 * (size_t)dim).blocks * dim * sizeof(float); }      // with one input of 32 bits: as many blocks as any has
@@ -426,7 +435,7 @@ cudaError_t launch_rms_norm_grad(const RmsNormGrad &a, cudaStream_t s) {
     else e = a.x_type == KV_F32 ? rms_norm_grad_in_eights<bf16, float>(a, p, row, s) : rms_norm_grad_in_eights<bf16, bf16>(a, p, row, s);
     if (e) return e;
   }
-  return launch_k(rms_norm_gain_kernel, dim3((a.dim + 31) / 32), dim3(256), 0, s, a, a.rows ? p.blocks : 0);
+  return launch_k(rms_norm_gain_kernel, dim3((a.dim + 31) / 32), dim3(1024), 0, s, a, a.rows ? p.blocks : 0);
 }
 
 }  // namespace spec
