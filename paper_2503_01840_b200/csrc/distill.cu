@@ -109,23 +109,27 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
   for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
   return all;
 }
-// What the same warp does next for the gradient
+// What the same warp does next for the gradient: entries with one id become one.  Ids of a warp's 32 are compared at once, with those of the others by fours.
 __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
   __syncwarp();
-  for (int k = threadIdx.x & 31; k < K; k += 32) {
-    const int id = e.id[k];
-    bool first = id >= 0;
-    float p = e.p[k];
-    for (int j = 0; first && j < K; j += 4) {
+  const int lane = threadIdx.x & 31;
+  for (int k0 = 0; k0 < K; k0 += 32) {
+    const int k = k0 + lane, id = k < K ? e.id[k] : -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, id);
+    bool first = id >= 0 && __ffs(same) - 1 == lane;
+    float p = id >= 0 ? e.p[k] : 0.0f;
+    if (first)
+      for (uint32_t rest = same & (same - 1); rest; rest &= rest - 1) p += e.p[k0 + __ffs(rest) - 1];
+    for (int j = 0; j < fours(K); j += 4) {
+      if (j >= k0 && j < k0 + 32) continue;
       const int4 o = *(const int4 *)(e.id + j);
-      if (o.x != id && o.y != id && o.z != id && o.w != id) continue;
-      for (int x = j; x < j + 4; x++) {
-        if (e.id[x] != id) continue;
-        if (x < k) first = false;
-        if (x > k) p += e.p[x];
-      }
+      if (!first || (o.x != id && o.y != id && o.z != id && o.w != id)) continue;
+      if (j < k0) first = false;
+      else
+        for (int x = j; x < j + 4; x++)
+          if (e.id[x] == id) p += e.p[x];
     }
-    e.write[k] = first ? p : -1.0f;
+    if (k < K) e.write[k] = first ? p : -1.0f;
   }
   __syncwarp();
 }
@@ -141,14 +145,6 @@ template <typename F> __device__ __forceinline__ float entries_loss(const Distil
 #pragma unroll
   for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
   return loss;
-}
-// A warp writes the gradient at the entries' ids from c0 to c1.  d: of the row
-template <typename F> __device__ __forceinline__ void entries_gradient(const Distill &a, float b, const Entries &e, float m, float g, float of_q, int c0, int c1, long long d, F z) {
-  for (int k = threadIdx.x & 31; k < a.K; k += 32) {
-    const int id = e.id[k];
-    const float p = e.write[k];
-    if (id >= c0 && id < c1 && !(p < 0.0f)) store_from_f32(a.dz, a.d_type, d + id, fmaf(of_q, exp_of(b, z(id) - m), -g * p));
-  }
 }
 
 // ---------------------------------------------------------------- any vocabulary: a block a row, read once for each step
@@ -228,6 +224,7 @@ struct Slices {
   int n, per;            // slices of a row, elements of one: a multiple of 8
   int whole;             // units of the output are aligned pieces of 16 bytes
   int look_first;        // whether a row is not loaded before it is known that some id of it is not -1
+  int ahead;             // rows that are under way at a time, if there are more
 };
 constexpr int SLICE = 66 << 10, SLICE_MOST = 200 << 10, CLUSTER_MOST = 8;
 
@@ -292,15 +289,14 @@ __device__ __forceinline__ float of_cta(const bf16 *p, int rank) {
   asm volatile("ld.shared::cluster.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
   return __uint_as_float((uint32_t)v << 16);
 }
-// named barriers, for all threads
-enum { ROW_SEEN = 1, ROW_WRITTEN = 2 };
-template <int ID> __device__ __forceinline__ void arrive() {
+// the walkers have written the row's gradient: they go on, the other warp waits for them
+__device__ __forceinline__ void written_arrive() {
   __syncwarp();
-  asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(WALKERS + 32) : "memory");
+  asm volatile("bar.arrive 1, %0;" ::"n"(WALKERS + 32) : "memory");
 }
-template <int ID> __device__ __forceinline__ void wait() {
+__device__ __forceinline__ void written_wait() {
   __syncwarp();
-  asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(WALKERS + 32) : "memory");
+  asm volatile("bar.sync 1, %0;" ::"n"(WALKERS + 32) : "memory");
 }
 
 template <typename T, typename O, int MODE>
@@ -319,6 +315,17 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
   const int shift = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T)), units = (shift + n + 7) / 8;
   const Entries e = entries_in(shared, a.K);
   T *const buf = (T *)(shared + entries_bytes(a.K));     // element c of the slice at buf[shift + c]
+  // what is needed later is asked for now, and the entries of the row that comes to this place next go to L2
+  const float grad = MODE != LOSS && a.grad ? a.grad[row] : 1.0f;
+  const float2 stats = MODE == GRADIENT ? a.stats[row] : make_float2(0.0f, 1.0f);
+  if (!walks && sl.ahead && row + sl.ahead < a.rows) {
+    const long long at = (row + sl.ahead) * a.K;
+    const int ids = a.ids.wide ? 8 : 4, values = a.v_type == 0 ? 4 : 2;
+    for (int k = lane * 32; k < a.K; k += 1024) {
+      for (int x = 0; x < ids / 4 && k + 16 * x < a.K; x++) asm volatile("prefetch.global.L2 [%0];" ::"l"((const char *)a.ids.p + (at + k) * ids + x * 128));
+      asm volatile("prefetch.global.L2 [%0];" ::"l"((const char *)a.values + (at + k) * values));
+    }
+  }
   bool there = true;
   if (sl.look_first) {
     there = false;
@@ -341,69 +348,17 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
   }
-  // the row's maximum and sum from the walkers' warps, or from the cluster's CTAs; given, where the gradient alone is wanted
-  auto seen = [&]() {
-    Running r;
-    if (there && lane < WALKERS / 32) r = Running{of_warp[lane].x, of_warp[lane].y};
-    join_lanes(b, r);
-    return r;
-  };
-  auto agreed = [&]() {
-    Running r;
-    if (lane < sl.n) {
-      const float2 v = of_cta(&mine, lane);
-      r = Running{v.x, v.y};
-    }
-    join_lanes(b, r);
-    return r;
-  };
-  auto factors = [&](bool none, float s, float &g, float &of_q) {
-    g = none ? 0.0f : (a.grad ? a.grad[row] : 1.0f) / a.temperature;
-    of_q = none ? 0.0f : g * mass / s;
-  };
-  const bool joint = MODE != GRADIENT && sl.n > 1;
-  if (!walks) {
+  else if (!walks) {
     bool none = true;
     if (there) {
       const float all = read_entries(a, e, row, &none);
       if (lane == 0) mass = all;
+      if (MODE != LOSS && !none) merge_entries(e, a.K);
     }
     if (lane == 0) empty = none;
-    arrive<ROW_SEEN>();
-    if (joint) cluster_arrive();
-    if (MODE != LOSS && !none) merge_entries(e, a.K);
-    if (joint) cluster_wait();
-    wait<ROW_WRITTEN>();
-    Running r;
-    if (MODE == GRADIENT) {
-      if (!none) r = Running{a.stats[row].x, a.stats[row].y};
-    } else {
-      r = joint ? agreed() : seen();
-      if (r.m == -INFINITY) r.s = NAN;
-      if (rank == 0) {
-        auto logit = [&](int id) {
-          if (!joint) return to_f32(buf[shift + id]);
-          const int k = id / sl.per;
-          return of_cta(buf + shift + (id - k * sl.per), k);
-        };
-        const float loss = none ? 0.0f : entries_loss(a, e, r.m, logit) + mass * logf(r.s);
-        if (lane == 0) {
-          a.loss[row] = loss;
-          if (a.stats) a.stats[row] = none ? make_float2(0.0f, 1.0f) : make_float2(r.m, r.s);
-        }
-      }
-    }
-    if (MODE != LOSS && !none) {
-      float g, of_q;
-      factors(none, r.s, g, of_q);
-      entries_gradient(a, b, e, r.m, g, of_q, c0, c0 + n, row * a.d_rs, [&](int id) { return to_f32(buf[shift + id - c0]); });
-    }
-    __syncwarp();
-    if (joint) cluster_arrive(), cluster_wait();         // nobody leaves while its numbers may be read
-    return;
   }
   Running r;
-  if (MODE != GRADIENT && there) {
+  if (MODE != GRADIENT && there && walks) {
 #pragma unroll
     for (int q = 0; q < 4; q++) {
       if (q == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
@@ -417,25 +372,61 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
     if (lane == 0) of_warp[warp] = make_float2(r.m, r.s);
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  wait<ROW_SEEN>();
-  const bool none = empty;
+  __syncthreads();
+  const bool none = empty, joint = MODE != GRADIENT && sl.n > 1;
   if (MODE == GRADIENT) {
-    if (!none) r = Running{a.stats[row].x, a.stats[row].y};
+    r = Running{stats.x, stats.y};
   } else {
-    r = seen();
+    r = Running{};
+    if (there && lane < WALKERS / 32) r = Running{of_warp[lane].x, of_warp[lane].y};
+    join_lanes(b, r);
     if (joint) {
       if (tid == 0) mine = make_float2(r.m, r.s);
       __syncwarp();
       cluster_arrive();
       cluster_wait();
-      r = agreed();
-      cluster_arrive();
+      r = Running{};
+      if (lane < sl.n) {
+        const float2 v = of_cta(&mine, lane);
+        r = Running{v.x, v.y};
+      }
+      join_lanes(b, r);
+      if (walks) cluster_arrive();
     }
     if (r.m == -INFINITY) r.s = NAN;                     // no logit above -inf: there is no softmax
   }
+  const float g = none ? 0.0f : grad / a.temperature, of_q = none ? 0.0f : g * mass / r.s;
+  if (!walks) {                                          // while the others write
+    if (MODE != GRADIENT && rank == 0) {
+      auto logit = [&](int id) {
+        if (!joint) return to_f32(buf[shift + id]);
+        const int k = id / sl.per;
+        return of_cta(buf + shift + (id - k * sl.per), k);
+      };
+      const float loss = none ? 0.0f : entries_loss(a, e, r.m, logit) + mass * logf(r.s);
+      if (lane == 0) {
+        a.loss[row] = loss;
+        if (a.stats) a.stats[row] = none ? make_float2(0.0f, 1.0f) : make_float2(r.m, r.s);
+      }
+    }
+    if (MODE != LOSS) {
+      if (!none)
+        for (int k = lane; k < a.K; k += 32) {           // what is written over theirs
+          const int id = e.id[k];
+          const float p = e.write[k];
+          if (id >= c0 && id < c0 + n && !(p < 0.0f)) e.write[k] = fmaf(of_q, exp_of(b, to_f32(buf[shift + id - c0]) - r.m), -g * p);
+          else e.id[k] = -1;
+        }
+      written_wait();
+      if (!none)
+        for (int k = lane; k < a.K; k += 32)
+          if (e.id[k] >= 0) store_from_f32(a.dz, a.d_type, row * a.d_rs + e.id[k], e.write[k]);
+    }
+    __syncwarp();
+    if (joint) cluster_arrive(), cluster_wait();         // nobody leaves while its numbers may be read
+    return;
+  }
   if (MODE != LOSS) {
-    float g, of_q;
-    factors(none, r.s, g, of_q);
     O *const d = (O *)a.dz + row * a.d_rs + c0;
     if (none) {
       if (sl.whole) {
@@ -461,7 +452,7 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
       for (int c = tid; c < n; c += WALKERS) d[c] = from_f32<O>(of_q * exp_of(b, to_f32(buf[shift + c]) - r.m));
     }
   }
-  arrive<ROW_WRITTEN>();                                 // the other warp writes over what they have written
+  if (MODE != LOSS) written_arrive();
   __syncwarp();
   if (joint) cluster_wait();
 }
@@ -476,6 +467,7 @@ static bool slices_of(const Distill &a, Slices *sl) {
   sl->per = (int)(((a.vocab + n - 1LL) / n + 7) / 8 * 8);
   sl->whole = a.dz && pieces_aligned(a.dz, a.rows > 1 ? a.d_rs : 0, a.d_type == 0 ? 4 : 2);
   sl->look_first = (long long)a.rows * n > 4 * 148;
+  sl->ahead = sl->look_first ? 3 * 148 / n : 0;
   return (size_t)sl->per * e <= SLICE_MOST && (long long)a.rows * n <= INT32_MAX;
 }
 
