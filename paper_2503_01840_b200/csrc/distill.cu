@@ -120,14 +120,18 @@ __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
     float p = id >= 0 ? e.p[k] : 0.0f;
     if (first)
       for (uint32_t rest = same & (same - 1); rest; rest &= rest - 1) p += e.p[k0 + __ffs(rest) - 1];
-    for (int j = 0; j < fours(K); j += 4) {
-      if (j >= k0 && j < k0 + 32) continue;
-      const int4 o = *(const int4 *)(e.id + j);
-      if (!first || (o.x != id && o.y != id && o.z != id && o.w != id)) continue;
-      if (j < k0) first = false;
-      else
-        for (int x = j; x < j + 4; x++)
-          if (e.id[x] == id) p += e.p[x];
+    for (int j0 = 0; j0 < K; j0 += 32) {                 // the other 32s
+      if (j0 == k0) continue;
+      bool some = false;
+#pragma unroll
+      for (int j = 0; j < 32; j += 4) {
+        const int4 o = j0 + j < K ? *(const int4 *)(e.id + j0 + j) : make_int4(-1, -1, -1, -1);
+        some |= o.x == id || o.y == id || o.z == id || o.w == id;
+      }
+      if (!some || !first) continue;
+      first = j0 > k0;
+      for (int x = j0; first && x < min(K, j0 + 32); x++)
+        if (e.id[x] == id) p += e.p[x];
     }
     if (k < K) e.write[k] = first ? p : -1.0f;
   }
@@ -238,32 +242,21 @@ __device__ __forceinline__ float2 of_cta(const float2 *p, int rank) {
   return v;
 }
 
-// Eight neighbours as they lie in memory; the largest of them (of NaN and a number the number).
-template <typename T> struct Eight;
-template <> struct Eight<float> {
-  float4 a, b;
-  __device__ __forceinline__ void take(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
-  __device__ __forceinline__ void floats(float (&y)[8]) const { y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w, y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w; }
-  __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)), fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w))); }
-};
-template <> struct Eight<bf16> {
-  uint4 u;
-  __device__ __forceinline__ void take(const bf16 *p) { u = *(const uint4 *)p; }
-  __device__ __forceinline__ void floats(float (&y)[8]) const { unpack2(u.x, y[0], y[1]), unpack2(u.y, y[2], y[3]), unpack2(u.z, y[4], y[5]), unpack2(u.w, y[6], y[7]); }
-  __device__ __forceinline__ float largest() const {
-    const __nv_bfloat162 a = *(const __nv_bfloat162 *)&u.x, b = *(const __nv_bfloat162 *)&u.y, c = *(const __nv_bfloat162 *)&u.z, d = *(const __nv_bfloat162 *)&u.w;
-    const __nv_bfloat162 m = __hmax2(__hmax2(a, b), __hmax2(c, d));
-    return fmaxf(__low2float(m), __high2float(m));
-  }
-};
+// the largest of eight (of NaN and a number the number)
+__device__ __forceinline__ float largest(const Raw8<float> &x) { return fmaxf(fmaxf(fmaxf(x.a.x, x.a.y), fmaxf(x.a.z, x.a.w)), fmaxf(fmaxf(x.b.x, x.b.y), fmaxf(x.b.z, x.b.w))); }
+__device__ __forceinline__ float largest(const Raw8<bf16> &x) {
+  const __nv_bfloat162 a = *(const __nv_bfloat162 *)&x.u.x, b = *(const __nv_bfloat162 *)&x.u.y, c = *(const __nv_bfloat162 *)&x.u.z, d = *(const __nv_bfloat162 *)&x.u.w;
+  const __nv_bfloat162 m = __hmax2(__hmax2(a, b), __hmax2(c, d));
+  return fmaxf(__low2float(m), __high2float(m));
+}
 
 constexpr int WALKERS = 256;      // threads that copy and walk; another warp looks the entries up and takes the loss
 
 // A unit's part of a thread's maximum and sum
 template <typename T> __device__ __forceinline__ Running walk(const T *at, float b, Running r) {
-  Eight<T> x;
+  Raw8<T> x;
   x.take(at);
-  const float top = x.largest();
+  const float top = largest(x);
   if (top > r.m) r.s *= exp_of(b, r.m == -INFINITY ? 0.0f : r.m - top), r.m = top;
   float y[8], even, odd;
   Pair p[4];
@@ -338,17 +331,15 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
       for (int i = q * quarter; i < min(steps, (q + 1) * quarter); i++) {
         const int u = i * WALKERS + tid, c = u * 8 - shift;
         if (c >= 0 && c + 8 <= n) {
-          copy16(buf + u * 8, z + c);
-          if (sizeof(T) == 4) copy16(buf + u * 8 + 4, z + c + 4);
+          copy8(buf + u * 8, z + c);
         } else if (u < units) {
 #pragma unroll
           for (int x = 0; x < 8; x++) buf[u * 8 + x] = c + x >= 0 && c + x < n ? z[c + x] : from_f32<T>(-INFINITY);
         }
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      copies_commit();
     }
-  }
-  else if (!walks) {
+  } else if (!walks) {
     bool none = true;
     if (there) {
       const float all = read_entries(a, e, row, &none);
@@ -361,17 +352,17 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
   if (MODE != GRADIENT && there && walks) {
 #pragma unroll
     for (int q = 0; q < 4; q++) {
-      if (q == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
-      if (q == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
-      if (q == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-      if (q == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      if (q == 0) copies_but<3>();
+      if (q == 1) copies_but<2>();
+      if (q == 2) copies_but<1>();
+      if (q == 3) copies_but<0>();
       for (int i = q * quarter; i < min(steps, (q + 1) * quarter); i++)
         if (i * WALKERS + tid < units) r = walk(buf + (i * WALKERS + tid) * 8, b, r);
     }
     join_lanes(b, r);
     if (lane == 0) of_warp[warp] = make_float2(r.m, r.s);
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  copies_but<0>();
   __syncthreads();
   const bool none = empty, joint = MODE != GRADIENT && sl.n > 1;
   if (MODE == GRADIENT) {
@@ -460,9 +451,9 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
 // Slices of about SLICE bytes, so that three CTAs are on an SM; smaller ones where rows alone do not fill the SMs twice, down to 2 KB.
 static bool slices_of(const Distill &a, Slices *sl) {
   const size_t e = a.z_type == 0 ? 4 : 2, row = (size_t)a.vocab * e;
-  const int most = a.loss ? CLUSTER_MOST : 64;
-  int n = (int)min<size_t>((row + SLICE - 1) / SLICE, most);
-  while (n < most && n < 8 && (long long)a.rows * n < 2 * 148 && row / (n + 1) >= 2048) n++;
+  const size_t most = a.loss ? CLUSTER_MOST : INT32_MAX;
+  int n = (int)min((row + SLICE - 1) / SLICE, most);
+  while (n < CLUSTER_MOST && (long long)a.rows * n < 2 * 148 && row / (n + 1) >= 2048) n++;
   sl->n = n;
   sl->per = (int)(((a.vocab + n - 1LL) / n + 7) / 8 * 8);
   sl->whole = a.dz && pieces_aligned(a.dz, a.rows > 1 ? a.d_rs : 0, a.d_type == 0 ? 4 : 2);
