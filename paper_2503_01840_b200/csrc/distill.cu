@@ -220,15 +220,20 @@ __global__ void __launch_bounds__(512) distill_any_kernel(Distill a, float b) {
 }
 
 // ---------------------------------------------------------------- rows held in shared memory
-// A cluster of up to eight CTAs has a row, a slice of up to SLICE bytes each, read from memory once: copied to shared memory while a warp looks the entries up, walked for the maximum and the sum, which
-// the CTAs exchange, and walked again for the gradient.  Elements keep their place modulo 16 bytes, so any alignment will do; a thread copies and walks the same units of eight.
-// Where the statistics are given the CTAs have nothing to exchange and are no cluster.
+// A cluster of up to eight CTAs has a row, a slice of up to SLICE bytes each, read from memory once: copied to shared memory, walked for the maximum and the sum, which the CTAs
+// exchange, and walked again for the gradient.  Where the statistics are given the CTAs have nothing to exchange and are no cluster.  Elements keep their place modulo 16 bytes, so any
+// alignment will do; a thread copies and walks the same units of eight and waits for its own copies alone.  Meanwhile another warp looks the entries up (some four microseconds, most of
+// them waiting), takes the loss, and writes over what the walkers wrote at the entries' ids.
+// The gradient from statistics is bound by bytes: 2048 rows of 128256 fp32 to bf16 242 us, 6.5 TB/s, a copy's rate.  Loss and gradient at once wait, load, walk and write in turn, three
+// CTAs an SM side by side: 8192 rows of 32000 bf16, a tenth of them without entries, 195 us, 5.1 TB/s, 78 % of a copy's; two exponentials an element are 116 us of its unit's time.
+// Slices of 44 KB and four CTAs 292 / 259 us (clusters wait for one another), of 100 KB 196 / 247; 384 walkers 206 / 269.  CTAs that stay, with the next row's entries and copies under way,
+// 244 / 299: their one look-up warp is what they wait for.  Rows that have no id are not read: 233 us without that, and 210 without the next entries' way into L2.
 enum { LOSS = 0, GRADIENT = 1, BOTH = 2 };
 struct Slices {
   int n, per;            // slices of a row, elements of one: a multiple of 8
   int whole;             // units of the output are aligned pieces of 16 bytes
   int look_first;        // whether a row is not loaded before it is known that some id of it is not -1
-  int ahead;             // rows that are under way at a time, if there are more
+  int ahead;             // rows that are under way at a time, if there are more: the entries of the row that far on go to L2
 };
 constexpr int SLICE = 66 << 10, SLICE_MOST = 200 << 10, CLUSTER_MOST = 8;
 
@@ -308,7 +313,7 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
   const int shift = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T)), units = (shift + n + 7) / 8;
   const Entries e = entries_in(shared, a.K);
   T *const buf = (T *)(shared + entries_bytes(a.K));     // element c of the slice at buf[shift + c]
-  // what is needed later is asked for now, and the entries of the row that comes to this place next go to L2
+  // what is needed later is asked for now, for this row and for the one that comes to this place on the SM next
   const float grad = MODE != LOSS && a.grad ? a.grad[row] : 1.0f;
   const float2 stats = MODE == GRADIENT ? a.stats[row] : make_float2(0.0f, 1.0f);
   if (!walks && sl.ahead && row + sl.ahead < a.rows) {

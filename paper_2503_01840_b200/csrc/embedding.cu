@@ -24,6 +24,7 @@ __global__ void __launch_bounds__(256) embed_any_kernel(Embed a, int w_dtype, in
 }
 
 // Widths of whole eights, aligned to 16 bytes: a thread has up to four units of eight under way.  A block has 1024 units of a token, or as many tokens as make 1024.
+// Bytes bound it: 16384 tokens of 8192 in bf16 66 us, 8.1 TB/s as counted: rows that several tokens ask for come from L2.  512 units 70 us, 2048 78.
 constexpr int LOOK_UNITS = 1024;
 struct EmbedGrid {
   int units, tokens;     // of a token; of a block
@@ -81,8 +82,9 @@ cudaError_t launch_embed_rows(const Embed &a, int w_dtype, int out_dtype, cudaSt
 
 // ---------------------------------------------------------------- gradient: the tokens in the order of their ids
 // A block owns a range of the vocabulary.  It reads all ids, which are few and stay in L2: how many lie below its range is where its tokens begin in the sorted
-// order, so blocks need nothing from one another and one launch sorts.  Warps walk segments of the ids: counting first, then writing those of the range
-// one behind another, in the tokens' order, to `list`; one warp deals them to their rows' places, 32 at a time.  Rows of the range that no token has are zeroed here.
+// order, so blocks need nothing from one another and one launch sorts (8192 ids 5 us, under the zeros).  Warps walk segments of the ids: counting first, then writing those of the range
+// one behind another, in the tokens' order, to `list`; one warp deals them to their rows' places, 32 at a time.  Rows of the range that no token has are zeroed here, which is most
+// of the gradient's time: of 128256 rows of 4096 bf16 for 8192 tokens 168 of 199 us (1111 MB in all at 5.6 TB/s, 85 % of a copy's rate).
 constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_MAX_ROWS = 4096;
 
 struct EmbedSort {
@@ -193,7 +195,8 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
 // ---------------------------------------------------------------- gradient: sums of runs of equal ids
 // The sorted tokens are cut into chunks, whatever ids they have: no id, however frequent, makes a block longer than another.  A run inside a chunk is written where
 // it belongs; what a chunk has of a run that goes over its ends goes to `part` (slot 0: of a run that began before, 1: of one that begins here and goes on),
-// and the chunk in which a run begins adds those up, in order, in the next launch.
+// and the chunk in which a run begins adds those up, in order, in the next launch.  Chunks of 32 tokens: 199 us as above, and 173 for 16384 tokens of 32000 x 5120 to fp32; of 16 201 / 181, of 64 203 / 172.
+// Few tokens go by 16s: 2003 of 4096 x 256 fp32 16.4 us (three launches one behind the other), by 32s 18.5.
 struct EmbedRuns {
   int per_chunk, chunks;
   const int32_t *order, *id, *count;

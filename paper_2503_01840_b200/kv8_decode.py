@@ -3,7 +3,7 @@
     python -m paper_2503_01840_b200.kv8_decode [--shape C2] [--layers 4] [--batch 2] [--prompt 700] [--steps 16] [--cache e4m3,int8,bf16]
 
 SpecDecoder keeps its cache in bf16 or fp32.  This is a loop of a program's own around the single operators: projections by
-gemm_fused / gemm_wide, gate/up by gemm_swiglu, and for the cache
+gemm_fused / gemm_wide, gate/up by gemm_swiglu, tokens' rows by embedding, the residual stream's sums and norms by rms_norm, and for the cache
   kv_append         rotates queries and keys, quantises keys and values, writes them to the pages
   kv_read           reads a prompt's keys and values back for its own attention (ttt_attention without simulated steps: plain causal)
   decode_attention  attends from every sequence's new token
@@ -42,29 +42,36 @@ class CachedDecoder:
         return sum(t.nbytes // (t.shape[0] * t.shape[2]) for l in self.layers for n, t in l.items() if t is not None and n != "page_table")
 
     # -- pieces of a layer
-    def _norm(self, x, gain):
-        return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + self.m.rms_eps) * gain.float()).bfloat16()
+    def _norm(self, x, y, gain):
+        """(the norm of the residual stream x with y added in bf16, the stream): y is what the part before has left to add, if any"""
+        if y is None:
+            return sb.rms_norm(x, gain, self.m.rms_eps, dtype=torch.bfloat16), x
+        return sb.rms_norm(y, gain, self.m.rms_eps, residual=x, dtype=torch.bfloat16, sum_out=x)
 
     def _linear(self, x, w):
         return sb.gemm_fused(x, w) if x.shape[0] <= 128 else sb.gemm_wide(x, w)[0]
 
-    def _mlp(self, x, l):
-        h = self._norm(x, l["mlp_norm"])
+    def _mlp(self, x, y, l):
+        h, x = self._norm(x, y, l["mlp_norm"])
         act = sb.gemm_swiglu(h, l["w_gate"], l["w_up"]) if h.shape[0] <= 128 else sb.gemm_wide(h, l["w_gate"], l["w_up"])[0]
-        return x + self._linear(act, l["w_down"])
+        return x, self._linear(act, l["w_down"])
 
-    def _layer(self, i, x, seq, pos, attend):
-        """attend(queries, layer's cache) -> [rows][heads * head_dim]"""
+    def _layer(self, i, x, y, seq, pos, attend):
+        """attend(queries, layer's cache) -> [rows][heads * head_dim]; (x, y) as of _norm"""
         m, l = self.m, self.w["layers"][i]
-        qkv = self._linear(self._norm(x, l["attn_norm"]), self.wqkv[i]).bfloat16().view(-1, m.n_heads + 2 * m.n_kv_heads, m.head_dim)
+        h, x = self._norm(x, y, l["attn_norm"])
+        qkv = self._linear(h, self.wqkv[i]).bfloat16().view(-1, m.n_heads + 2 * m.n_kv_heads, m.head_dim)
         H, G = m.n_heads, m.n_kv_heads
         q = sb.kv_append(qkv[:, H: H + G], qkv[:, H + G:], row_seq=seq, row_pos=pos, q=qkv[:, :H], inv_freq=self.freq, mscale=self.mscale, **self.layers[i])
-        return self._mlp(x + self._linear(attend(q, self.layers[i]).reshape(x.shape[0], -1), l["wo"]), l)
+        return self._mlp(x, self._linear(attend(q, self.layers[i]).reshape(x.shape[0], -1), l["wo"]), l)
 
-    def _tokens(self, x):
+    def _tokens(self, x, y):
         """(greedy tokens int32, final hidden states)"""
-        h = self._norm(x, self.w["final_norm"])
+        h, _ = self._norm(x, y, self.w["final_norm"])
         return sb.argmax(self._linear(h, self.w["lm_head"])), h
+
+    def _embed(self, tokens):
+        return sb.embedding(tokens, self.w["embed"], dtype=torch.float32)
 
     # -- the loop
     def prefill(self, prompts):
@@ -85,10 +92,13 @@ class CachedDecoder:
                     pool.append(rows.view(pages, ps, m.n_kv_heads, m.head_dim).transpose(1, 2).contiguous())
                 return sb.ttt_attention(q, *pool, order, None, None)
 
-            x = self.w["embed"][torch.as_tensor(prompt, device="cuda").long()].float()
+            ids = torch.as_tensor(prompt)
+            if not bool(((ids >= 0) & (ids < m.vocab)).all()):
+                raise ValueError(f"prefill: token ids from 0 to {m.vocab - 1}")
+            x, y = self._embed(ids.to("cuda", torch.int64)), None
             for i in range(m.n_layers):
-                x = self._layer(i, x, seq, pos, attend)
-            first.append(self._tokens(x[-1:].contiguous())[0])
+                x, y = self._layer(i, x, y, seq, pos, attend)
+            first.append(self._tokens(x[-1:], y[-1:])[0])
         self.tokens = torch.cat(first)
         self.lengths = torch.tensor([len(p) for p in prompts], dtype=torch.int32, device="cuda")
         self.longest = max(len(p) for p in prompts)                      # known here without asking the GPU
@@ -101,11 +111,11 @@ class CachedDecoder:
             raise ValueError(f"step: a sequence has the cache's {self.max_ctx} positions")
         self.longest += 1
         pos, seen = self.lengths, self.lengths + 1
-        x = self.w["embed"][self.tokens.long()].float()
+        x, y = self._embed(self.tokens), None
         for i in range(self.m.n_layers):
-            x = self._layer(i, x, self.seqs, pos, lambda q, cache: sb.decode_attention(q, lengths=seen, workspace=self.workspace, **cache))
+            x, y = self._layer(i, x, y, self.seqs, pos, lambda q, cache: sb.decode_attention(q, lengths=seen, workspace=self.workspace, **cache))
         self.lengths = seen
-        self.tokens, hidden = self._tokens(x)
+        self.tokens, hidden = self._tokens(x, y)
         return self.tokens, hidden
 
 

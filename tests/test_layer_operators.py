@@ -656,6 +656,18 @@ def test_on_another_stream_and_in_a_graph():
             assert torch.equal(a, b)
 
 
+@gpu
+def test_the_decoding_loop_refuses_ids_that_the_table_lacks():
+    from paper_2503_01840_b200 import synth
+    from paper_2503_01840_b200.kv8_decode import CachedDecoder
+    cfg = synth.ModelCfg("K", "bf16", 1, 512, 4, 2, 128, 1408, 2048, 1024, (0, 0, 0), 1e4, batch=1, tree_depth=2, tree_topk=2, tree_nodes=4, seed=3)
+    dec = CachedDecoder(cfg, synth.make_target_weights(cfg, "cuda"), 1, 24, "bf16")
+    for bad in ([1, 2048], [-1, 5]):
+        with pytest.raises(ValueError):
+            dec.prefill([torch.tensor(bad)])
+    dec.prefill([torch.tensor([0, 2047])])
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 def rows_struct(p=4096, stride=64, kind=0):
     return sb._Rows(p, stride, kind)
