@@ -405,8 +405,8 @@ int spec_embedding(const spec_rows *weight, int32_t vocab, int32_t dim, int32_t 
 
 /* The gradient with respect to weight of one with respect to spec_embedding's output: out[v] = scale * sum of grad[t] over the t with ids[t] = v, zeros where there are none;
  * with accumulate, that is added to out, and rows that no token names are not touched.  The tokens are sorted by id, and each run is summed in the tokens'
- * order in pieces of a fixed length.  out [vocab][dim] must not overlap grad.  scratch: spec_embedding_backward_scratch_bytes(tokens, dim). */
-size_t spec_embedding_backward_scratch_bytes(int32_t tokens, int32_t dim);
+ * order in pieces of a fixed length.  out [vocab][dim] must not overlap grad.  scratch: spec_embedding_backward_scratch_bytes(tokens, vocab, dim). */
+size_t spec_embedding_backward_scratch_bytes(int32_t tokens, int32_t vocab, int32_t dim);
 int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, const void *ids, int32_t tokens, int32_t vocab, int32_t dim, float scale,
                             int32_t accumulate, const spec_rows *out, void *scratch, size_t scratch_bytes, int32_t *status, void *stream);
 

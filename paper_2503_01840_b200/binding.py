@@ -147,7 +147,8 @@ def lib():
     L.spec_decode_attention.argtypes = [i32, vp, i64, cache, vp, i32, i32, C.c_float, vp, vp, vp, sz, vp, vp]
     rows = C.POINTER(_Rows)
     L.spec_embedding.argtypes = [rows, i32, i32, i32, vp, i32, C.c_float, rows, vp, vp]
-    L.spec_embedding_backward_scratch_bytes.argtypes = L.spec_rms_norm_backward_scratch_bytes.argtypes = [i32, i32]
+    L.spec_embedding_backward_scratch_bytes.argtypes = [i32, i32, i32]
+    L.spec_rms_norm_backward_scratch_bytes.argtypes = [i32, i32]
     L.spec_embedding_backward_scratch_bytes.restype = L.spec_rms_norm_backward_scratch_bytes.restype = sz
     L.spec_embedding_backward.argtypes = [rows, i32, vp, i32, i32, i32, C.c_float, i32, rows, vp, sz, vp, vp]
     L.spec_rms_norm.argtypes = [rows, rows, i32, vp, C.c_float, rows, rows, vp, i32, i32, i32, vp]

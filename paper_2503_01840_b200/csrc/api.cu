@@ -1887,8 +1887,8 @@ extern "C" int spec_embedding(const spec_rows *weight, int32_t vocab, int32_t di
   return kv_status(launch_embed_rows(a, weight->type, out->type, (cudaStream_t)stream));
 }
 
-extern "C" size_t spec_embedding_backward_scratch_bytes(int32_t tokens, int32_t dim) {
-  return tokens < 0 || dim < 1 || dim > MOST_COLUMNS || tokens > MOST_TOKENS ? 0 : embed_grad_scratch_bytes(tokens, dim);
+extern "C" size_t spec_embedding_backward_scratch_bytes(int32_t tokens, int32_t vocab, int32_t dim) {
+  return tokens < 0 || vocab < 1 || dim < 1 || dim > MOST_COLUMNS || tokens > MOST_TOKENS ? 0 : embed_grad_scratch_bytes(tokens, vocab, dim);
 }
 
 extern "C" int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, const void *ids, int32_t tokens, int32_t vocab, int32_t dim, float scale,
@@ -1905,7 +1905,7 @@ extern "C" int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, c
     a.grad = grad->p; a.g_rs = grad->row_stride;
   }
   if (!scratch) return SPEC_ERR_NULL;
-  if (scratch_bytes < embed_grad_scratch_bytes(tokens, dim) || !kv_aligned(scratch, 256)) return SPEC_ERR_WORKSPACE;
+  if (scratch_bytes < embed_grad_scratch_bytes(tokens, vocab, dim) || !kv_aligned(scratch, 256)) return SPEC_ERR_WORKSPACE;
   a.vocab = vocab; a.dim = dim; a.tokens = tokens; a.scale = scale; a.out = out->p; a.o_rs = out->row_stride; a.accumulate = accumulate != 0;
   a.scratch = scratch; a.status = status;
   EarlyLaunch early;

@@ -82,23 +82,23 @@ cudaError_t launch_embed_rows(const Embed &a, int w_dtype, int out_dtype, cudaSt
 
 // ---------------------------------------------------------------- gradient: the tokens in the order of their ids
 // A block owns a range of the vocabulary.  It reads all ids, which are few and stay in L2: how many lie below its range is where its tokens begin in the sorted
-// order, so blocks need nothing from one another and one launch sorts (8192 ids 5 us, under the zeros).  Warps walk segments of the ids: counting first, then writing those of the range
-// one behind another, in the tokens' order, to `list`; one warp deals them to their rows' places, 32 at a time.  Rows of the range that no token has are zeroed here, which is most
-// of the gradient's time: of 128256 rows of 4096 bf16 for 8192 tokens 168 of 199 us (1111 MB in all at 5.6 TB/s, 85 % of a copy's rate).
-constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_MAX_ROWS = 4096;
+// order, so blocks need nothing from one another and one launch sorts.  Warps walk segments of the ids: counting first, then writing those of the range
+// one behind another, in the tokens' order, to `list`; one warp deals them to their rows' places, 32 at a time (16384 tokens of one id: some 13 us).
+constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_MAX_ROWS = 4096, SORT_NEAR = 1024;
 
 struct EmbedSort {
   int rows;              // of the vocabulary a block
   int32_t *order, *id;   // tokens by id, and the ids
   int2 *list;            // (token, row of the block's range) of the ranges, unsorted
   int32_t *count;        // tokens with a row
-  int wide;              // whether rows are aligned pieces of 16 bytes
+  uint32_t *present;     // a bit for each row of the vocabulary that a token has; null: rows without are zeroed here
 };
 
 __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, EmbedSort so, int out_dtype) {
   pdl_wait();
   pdl_trigger();
-  __shared__ int have[SORT_MAX_ROWS], place[SORT_MAX_ROWS], below[SORT_WARPS], mine[SORT_WARPS];
+  __shared__ int have[SORT_MAX_ROWS], place[SORT_MAX_ROWS], below[SORT_WARPS], mine[SORT_WARPS], upto[SORT_WARPS];
+  __shared__ int2 near_by[SORT_NEAR];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lo = blockIdx.x * so.rows, n_rows = min(so.rows, a.vocab - lo);
   for (int i = threadIdx.x; i < n_rows; i += SORT_THREADS) have[i] = 0;
   __syncthreads();
@@ -135,8 +135,9 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
   }
   if (threadIdx.x == 0 && lo + n_rows == a.vocab) *so.count = base + total;
   if (total) {
+    int2 *const list = total <= SORT_NEAR ? near_by : so.list + base;      // long ones in memory
     if (in) {
-      int at = base + before_me;
+      int at = before_me;
       for (long long s = s0; s < s1; s += U) {
         int id[U];
 #pragma unroll
@@ -148,28 +149,37 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
         for (int k = 0; k < U; k++) {
           const bool hit = id[k] >= lo && id[k] - lo < n_rows;
           const uint32_t hits = __ballot_sync(0xffffffffu, hit);
-          if (hit) so.list[at + __popc(hits & ((1u << lane) - 1))] = make_int2((int)((s + k) * 32 + lane), id[k] - lo);
+          if (hit) list[at + __popc(hits & ((1u << lane) - 1))] = make_int2((int)((s + k) * 32 + lane), id[k] - lo);
           at += __popc(hits);
         }
       }
     }
+    // where each row's tokens begin
+    constexpr int EACH = SORT_MAX_ROWS / SORT_THREADS;
+    const int each = (n_rows + SORT_THREADS - 1) / SORT_THREADS, r0 = threadIdx.x * each;
+    int first[EACH], sum = 0;
+#pragma unroll
+    for (int k = 0; k < EACH; k++) {
+      first[k] = sum;
+      if (k < each && r0 + k < n_rows) sum += have[r0 + k];
+    }
+    int run = sum;
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, run, d);
+      if (lane >= d) run += o;
+    }
+    if (lane == 31) upto[warp] = run;
     __syncthreads();
-    if (warp == 0) {
-      int run = base;                                    // where each row's tokens begin
-      for (int i = 0; i < n_rows; i += 32) {
-        const int h = i + lane < n_rows ? have[i + lane] : 0;
-        int sum = h;
-        for (int d = 1; d < 32; d <<= 1) {
-          const int o = __shfl_up_sync(0xffffffffu, sum, d);
-          if (lane >= d) sum += o;
-        }
-        if (i + lane < n_rows) place[i + lane] = run + sum - h;
-        run += __shfl_sync(0xffffffffu, sum, 31);
-      }
-      __syncwarp();
+    run += base - sum;
+    for (int w = 0; w < warp; w++) run += upto[w];
+#pragma unroll
+    for (int k = 0; k < EACH; k++)
+      if (k < each && r0 + k < n_rows) place[r0 + k] = run + first[k];
+    __syncthreads();
+    if (warp == 0)
       for (int i = 0; i < total; i += 32) {
         const bool there = i + lane < total;
-        const int2 e = there ? so.list[base + i + lane] : make_int2(0, -1);
+        const int2 e = there ? list[i + lane] : make_int2(0, -1);
         const uint32_t same = __match_any_sync(0xffffffffu, e.y);
         const int rank = __popc(same & ((1u << lane) - 1));
         int at = there ? place[e.y] : 0;
@@ -178,15 +188,15 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
         __syncwarp();
         if (there) so.order[at + rank] = e.x, so.id[at + rank] = lo + e.y;
       }
-    }
   }
-  if (a.accumulate) return;
-  for (int r = warp; r < n_rows; r += SORT_WARPS) {
-    if (have[r]) continue;
-    if (so.wide) {
-      uint4 *const p = (uint4 *)((char *)a.out + (lo + r) * a.o_rs * (out_dtype == 0 ? 4 : 2));
-      for (int c = lane; c < a.dim * (out_dtype == 0 ? 4 : 2) / 16; c += 32) p[c] = make_uint4(0, 0, 0, 0);
-    } else {
+  if (so.present) {                                      // a block's range is whole words
+    for (int i = threadIdx.x; i < (n_rows + 31) / 32 * 32; i += SORT_THREADS) {
+      const uint32_t bits = __ballot_sync(0xffffffffu, i < n_rows && have[i]);
+      if (lane == 0) so.present[(lo + i) / 32] = bits;
+    }
+  } else if (!a.accumulate) {
+    for (int r = warp; r < n_rows; r += SORT_WARPS) {
+      if (have[r]) continue;
       for (int c = lane; c < a.dim; c += 32) store_from_f32(a.out, out_dtype, (lo + r) * a.o_rs + c, 0.0f);
     }
   }
@@ -195,12 +205,15 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(EmbedGrad a, E
 // ---------------------------------------------------------------- gradient: sums of runs of equal ids
 // The sorted tokens are cut into chunks, whatever ids they have: no id, however frequent, makes a block longer than another.  A run inside a chunk is written where
 // it belongs; what a chunk has of a run that goes over its ends goes to `part` (slot 0: of a run that began before, 1: of one that begins here and goes on),
-// and the chunk in which a run begins adds those up, in order, in the next launch.  Chunks of 32 tokens: 199 us as above, and 173 for 16384 tokens of 32000 x 5120 to fp32; of 16 201 / 181, of 64 203 / 172.
+// and the chunk in which a run begins adds those up, in order, in the next launch.  Blocks behind the chunks' write the zeros of rows without tokens, which are most of the bytes:
+// 8192 tokens of 128256 x 4096 bf16 176 us (1111 MB, 6.3 TB/s, 96 % of a copy's rate); by the sorting blocks before them 199.  Chunks of 16 tokens 2 us more, of 64 4 more.
 // Few tokens go by 16s: 2003 of 4096 x 256 fp32 16.4 us (three launches one behind the other), by 32s 18.5.
 struct EmbedRuns {
   int per_chunk, chunks;
   const int32_t *order, *id, *count;
   float *part;           // [chunks][2][dim]
+  const uint32_t *present;
+  int zeroing;           // blocks that write zeros to rows without tokens, behind the others
 };
 constexpr int CHUNK_MAX = 64;
 
@@ -248,13 +261,23 @@ template <typename TG, typename TO>
 __global__ void __launch_bounds__(128) embed_runs_kernel(const __grid_constant__ EmbedGrad a, const __grid_constant__ EmbedRuns r) {
   pdl_wait();
   pdl_trigger();
+  const int slabs = (a.dim + 1023) / 1024, chunk = blockIdx.x / slabs;
+  if (chunk >= r.chunks) {
+    const int words = a.dim * (int)sizeof(TO) / 16;
+    for (int v = blockIdx.x - slabs * r.chunks; v < a.vocab; v += r.zeroing) {
+      if (r.present[v >> 5] >> (v & 31) & 1) continue;
+      uint4 *const p = (uint4 *)((TO *)a.out + v * a.o_rs);
+      for (int i = threadIdx.x; i < words; i += 128) p[i] = make_uint4(0, 0, 0, 0);
+    }
+    return;
+  }
   __shared__ int token[CHUNK_MAX], id[CHUNK_MAX + 2];
-  const int n = *r.count, p0 = blockIdx.x * r.per_chunk, m = min(r.per_chunk, n - p0);
+  const int n = *r.count, p0 = chunk * r.per_chunk, m = min(r.per_chunk, n - p0);
   if (m <= 0) return;
   for (int i = threadIdx.x; i < m; i += 128) token[i] = r.order[p0 + i];
   for (int i = threadIdx.x; i < m + 2; i += 128) id[i] = p0 + i - 1 >= 0 && p0 + i - 1 < n ? r.id[p0 + i - 1] : -1;
   __syncthreads();
-  const int c = (blockIdx.y * 128 + threadIdx.x) * 8;
+  const int c = ((blockIdx.x - chunk * slabs) * 128 + threadIdx.x) * 8;
   if (c >= a.dim) return;
   constexpr int U = 8;
   float sum[8] = {};
@@ -276,7 +299,7 @@ __global__ void __launch_bounds__(128) embed_runs_kernel(const __grid_constant__
       const bool ends = id[i + 2] != me;
       if (i + 1 < m && !ends) continue;
       if (began && ends) embed_grad_out8<TO>(a, me, c, sum);
-      else store8(r.part + (2LL * blockIdx.x + began) * a.dim + c, sum);
+      else store8(r.part + (2LL * chunk + began) * a.dim + c, sum);
 #pragma unroll
       for (int e = 0; e < 8; e++) sum[e] = 0.0f;
       began = true;
@@ -330,37 +353,40 @@ __global__ void __launch_bounds__(128) embed_join_kernel(EmbedGrad a, EmbedRuns 
 static size_t up(size_t n) { return (n + 255) / 256 * 256; }
 static int chunk_of(int tokens) { return tokens >= 4096 ? 32 : 16; }
 
-size_t embed_grad_scratch_bytes(int tokens, int dim) {
+size_t embed_grad_scratch_bytes(int tokens, int vocab, int dim) {
   const size_t T = tokens, chunks = (T + chunk_of(tokens) - 1) / chunk_of(tokens);
-  return up(4 * T) * 2 + up(8 * T) + 256 + chunks * 2 * dim * 4;
+  return up(4 * T) * 2 + up(8 * T) + 256 + up(((size_t)vocab + 31) / 32 * 4) + chunks * 2 * dim * 4;
 }
 
 cudaError_t launch_embed_grad(const EmbedGrad &a, int g_dtype, int out_dtype, cudaStream_t s) {
+  const bool eights = a.tokens && a.dim % 8 == 0 && pieces_aligned(a.out, a.vocab > 1 ? a.o_rs : 0, bytes_of(out_dtype)) && pieces_aligned(a.grad, a.tokens > 1 ? a.g_rs : 0, bytes_of(g_dtype));
   char *p = (char *)a.scratch;
   EmbedSort so;
   so.count = (int32_t *)p, p += 256;
   so.order = (int32_t *)p, p += up(4 * (size_t)a.tokens);
   so.id = (int32_t *)p, p += up(4 * (size_t)a.tokens);
   so.list = (int2 *)p, p += up(8 * (size_t)a.tokens);
-  so.rows = min(SORT_MAX_ROWS, (a.vocab + 295) / 296);
-  const bool out_wide = a.dim * bytes_of(out_dtype) % 16 == 0 && pieces_aligned(a.out, a.vocab > 1 ? a.o_rs : 0, bytes_of(out_dtype));
-  so.wide = out_wide;
+  so.present = eights && !a.accumulate ? (uint32_t *)p : nullptr, p += up(((size_t)a.vocab + 31) / 32 * 4);
+  so.rows = min(SORT_MAX_ROWS, (a.vocab / 296 + 32) / 32 * 32);      // two blocks an SM
   if (const cudaError_t e = launch_k(embed_sort_kernel, dim3((a.vocab + so.rows - 1) / so.rows), dim3(SORT_THREADS), 0, s, a, so, out_dtype)) return e;
   if (a.tokens == 0) return cudaSuccess;
   EmbedRuns r;
   r.per_chunk = chunk_of(a.tokens);
   r.chunks = (int)(((long long)a.tokens + r.per_chunk - 1) / r.per_chunk);
-  r.order = so.order, r.id = so.id, r.count = so.count, r.part = (float *)p;
-  if (a.dim % 8 || !out_wide || !pieces_aligned(a.grad, a.tokens > 1 ? a.g_rs : 0, bytes_of(g_dtype))) {
-    const dim3 grid(r.chunks, (a.dim + 127) / 128);
+  r.order = so.order, r.id = so.id, r.count = so.count, r.part = (float *)p, r.present = so.present;
+  // about 48 KB of zeros a block, and blocks for every SM: 128256 x 4096 bf16 for 8192 tokens 176 us so, 198 with 2368 blocks that stay, 184 with one for each of two rows
+  r.zeroing = so.present ? (int)min<long long>(a.vocab, max(592LL, (long long)a.vocab * a.dim * (long long)bytes_of(out_dtype) / (48 << 10))) : 0;
+  const dim3 grid(r.chunks, (a.dim + 127) / 128);
+  if (!eights) {
     if (const cudaError_t e = launch_k(embed_runs_any_kernel, grid, dim3(128), 0, s, a, r, g_dtype, out_dtype)) return e;
     return launch_k(embed_join_kernel, grid, dim3(128), 0, s, a, r, out_dtype);
   }
-  const dim3 grid(r.chunks, (a.dim + 1023) / 1024);
-  const cudaError_t e = g_dtype == 0 ? (out_dtype == 0 ? launch_k(embed_runs_kernel<float, float>, grid, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<float, bf16>, grid, dim3(128), 0, s, a, r))
-                                     : (out_dtype == 0 ? launch_k(embed_runs_kernel<bf16, float>, grid, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<bf16, bf16>, grid, dim3(128), 0, s, a, r));
+  const int slabs = (a.dim + 1023) / 1024;
+  const dim3 runs(r.chunks * slabs + r.zeroing), join(r.chunks, slabs);
+  const cudaError_t e = g_dtype == 0 ? (out_dtype == 0 ? launch_k(embed_runs_kernel<float, float>, runs, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<float, bf16>, runs, dim3(128), 0, s, a, r))
+                                     : (out_dtype == 0 ? launch_k(embed_runs_kernel<bf16, float>, runs, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<bf16, bf16>, runs, dim3(128), 0, s, a, r));
   if (e) return e;
-  return out_dtype == 0 ? launch_k(embed_join_eights_kernel<float>, grid, dim3(128), 0, s, a, r) : launch_k(embed_join_eights_kernel<bf16>, grid, dim3(128), 0, s, a, r);
+  return out_dtype == 0 ? launch_k(embed_join_eights_kernel<float>, join, dim3(128), 0, s, a, r) : launch_k(embed_join_eights_kernel<bf16>, join, dim3(128), 0, s, a, r);
 }
 
 }  // namespace spec

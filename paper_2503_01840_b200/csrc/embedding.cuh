@@ -44,7 +44,7 @@ struct EmbedGrad {
   void *scratch;
   int32_t *status;
 };
-size_t embed_grad_scratch_bytes(int tokens, int dim);
+size_t embed_grad_scratch_bytes(int tokens, int vocab, int dim);
 cudaError_t launch_embed_grad(const EmbedGrad &a, int g_dtype, int out_dtype, cudaStream_t s);
 
 }  // namespace spec

@@ -371,7 +371,7 @@ PyObject *embedding_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const spec_rows to = rows_of(out, "embedding_backward: out [vocabulary][width] on the GPU with adjacent columns");
     int32_t *const status = status_of(a[7]);
     void *const s = stream_of_call();
-    const size_t bytes = embedding_scratch_((int32_t)T, (int32_t)k);
+    const size_t bytes = embedding_scratch_((int32_t)T, (int32_t)V, (int32_t)k);
     const at::Tensor scratch = scratch_of(bytes, g);
     const int rc = call([&] {
       return embedding_backward_(&from, id.bits, id.p, (int32_t)T, (int32_t)V, (int32_t)k, (float)scale, accumulate, &to, scratch.data_ptr(), scratch.nbytes(), status, s);

@@ -690,11 +690,11 @@ def test_entry_points_refuse_what_they_cannot_do():
     def backward(**kw):
         a = {**back, **kw}
         return L.spec_embedding_backward(a["g"] and ref(a["g"]), a["bits"], a["ids"], a["tokens"], a["vocab"], a["dim"], a["scale"], a["acc"], a["out"] and ref(a["out"]), a["scratch"], a["n"], None, None)
-    need = L.spec_embedding_backward_scratch_bytes(3, 64)
+    need = L.spec_embedding_backward_scratch_bytes(3, 10, 64)
     for kw, rc in ((dict(g=None), -2), (dict(out=None), -2), (dict(scratch=None), -2), (dict(ids=None), -2), (dict(n=need - 1), -3), (dict(scratch=p + 16), -3), (dict(out=r(stride=63)), bad),
                    (dict(g=r(kind=3)), bad), (dict(vocab=0), bad), (dict(scale=math.nan), bad), (dict(tokens=0, acc=1, g=None, scratch=None), 0)):
         assert backward(**kw) == rc, kw
-    assert L.spec_embedding_backward_scratch_bytes(-1, 64) == 0 and need > 0
+    assert L.spec_embedding_backward_scratch_bytes(-1, 10, 64) == 0 and need > 0
     norm = dict(x=r(), res=None, gt=0, gain=p, eps=1e-5, sum=None, y=r(), scale=None, group=0, rows=3, dim=64)
     def rms(**kw):
         a = {**norm, **kw}
