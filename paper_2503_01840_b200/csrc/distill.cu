@@ -46,12 +46,14 @@ struct Entries {
   int *id;               // the student's, -1: none
   float *p, *ln_p;
   float *write;          // for the gradient: p of all entries with this id at the first of them, -1 at the others
+  int *table;            // of the ids
 };
 __host__ __device__ constexpr int fours(int K) { return (K + 3) / 4 * 4; }
-__host__ __device__ constexpr size_t entries_bytes(int K) { return (size_t)fours(K) * 16; }
+__host__ __device__ constexpr int table_bits(int K) { return K <= 16 ? 6 : K <= 64 ? 8 : K <= 256 ? 10 : 12; }      // four places an entry, or more
+__host__ __device__ constexpr size_t entries_bytes(int K) { return (size_t)fours(K) * 16 + ((size_t)4 << table_bits(K)); }
 __device__ __forceinline__ Entries entries_in(char *shared, int K) {
   float *const f = (float *)shared;
-  return {(int *)f, f + fours(K), f + 2 * fours(K), f + 3 * fours(K)};
+  return {(int *)f, f + fours(K), f + 2 * fours(K), f + 3 * fours(K), (int *)f + 4 * fours(K)};
 }
 // One warp fills them in and returns sum p; *none: whether the row has no entry (sum p may be 0 otherwise too, where every p is too small).
 __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e, long long row, bool *none) {
@@ -109,31 +111,36 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
   for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
   return all;
 }
-// What the same warp does next for the gradient: entries with one id become one.  Ids of a warp's 32 are compared at once, with those of the others by fours.
+// What the same warp does next for the gradient: entries with one id become one, its first.  A table of the ids tells whether there is anything to do.
 __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
+  const int lane = threadIdx.x & 31, bits = table_bits(K), mask = (1 << bits) - 1;
+  for (int k = lane; k <= mask >> 2; k += 32) ((int4 *)e.table)[k] = make_int4(-1, -1, -1, -1);
   __syncwarp();
-  const int lane = threadIdx.x & 31;
-  for (int k0 = 0; k0 < K; k0 += 32) {
-    const int k = k0 + lane, id = k < K ? e.id[k] : -1;
-    const uint32_t same = __match_any_sync(0xffffffffu, id);
-    bool first = id >= 0 && __ffs(same) - 1 == lane;
-    float p = id >= 0 ? e.p[k] : 0.0f;
-    if (first)
-      for (uint32_t rest = same & (same - 1); rest; rest &= rest - 1) p += e.p[k0 + __ffs(rest) - 1];
-    for (int j0 = 0; j0 < K; j0 += 32) {                 // the other 32s
-      if (j0 == k0) continue;
-      bool some = false;
-#pragma unroll
-      for (int j = 0; j < 32; j += 4) {
-        const int4 o = j0 + j < K ? *(const int4 *)(e.id + j0 + j) : make_int4(-1, -1, -1, -1);
-        some |= o.x == id || o.y == id || o.z == id || o.w == id;
-      }
-      if (!some || !first) continue;
-      first = j0 > k0;
-      for (int x = j0; first && x < min(K, j0 + 32); x++)
-        if (e.id[x] == id) p += e.p[x];
+  bool twice = false;
+  for (int k = lane; k < K; k += 32) {
+    const int id = e.id[k];
+    e.write[k] = id < 0 ? -1.0f : e.p[k];
+    if (id < 0) continue;
+    int at = (int)((uint32_t)id * 2654435769u >> (32 - bits));      // 2^32 over the golden ratio spreads neighbours
+    for (;;) {                                           // ends: a table is at most a quarter full
+      const int was = atomicCAS(e.table + at, -1, id);
+      twice |= was == id;
+      if (was < 0 || was == id) break;
+      at = (at + 1) & mask;
     }
-    if (k < K) e.write[k] = first ? p : -1.0f;
+  }
+  __syncwarp();
+  if (!__any_sync(0xffffffffu, twice)) return;
+  for (int k = lane; k < K; k += 32) {
+    const int id = e.id[k];
+    bool first = id >= 0;
+    float p = e.p[k];
+    for (int j = 0; first && j < K; j++) {
+      if (j == k || e.id[j] != id) continue;
+      if (j < k) first = false;
+      else p += e.p[j];
+    }
+    e.write[k] = first ? p : -1.0f;
   }
   __syncwarp();
 }
@@ -235,7 +242,7 @@ struct Slices {
   int look_first;        // whether a row is not loaded before it is known that some id of it is not -1
   int ahead;             // rows that are under way at a time, if there are more: the entries of the row that far on go to L2
 };
-constexpr int SLICE = 66 << 10, SLICE_MOST = 200 << 10, CLUSTER_MOST = 8;
+constexpr int SLICE = 66 << 10, SHARED_MOST = 224 << 10, CLUSTER_MOST = 8;
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -258,9 +265,7 @@ __device__ __forceinline__ float largest(const Raw8<bf16> &x) {
 constexpr int WALKERS = 256;      // threads that copy and walk; another warp looks the entries up and takes the loss
 
 // A unit's part of a thread's maximum and sum
-template <typename T> __device__ __forceinline__ Running walk(const T *at, float b, Running r) {
-  Raw8<T> x;
-  x.take(at);
+template <typename T> __device__ __forceinline__ Running walk(const Raw8<T> &x, float b, Running r) {
   const float top = largest(x);
   if (top > r.m) r.s *= exp_of(b, r.m == -INFINITY ? 0.0f : r.m - top), r.m = top;
   float y[8], even, odd;
@@ -362,7 +367,11 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
       if (q == 2) copies_but<1>();
       if (q == 3) copies_but<0>();
       for (int i = q * quarter; i < min(steps, (q + 1) * quarter); i++)
-        if (i * WALKERS + tid < units) r = walk(buf + (i * WALKERS + tid) * 8, b, r);
+        if (i * WALKERS + tid < units) {
+          Raw8<T> x;
+          x.take(buf + (i * WALKERS + tid) * 8);
+          r = walk(x, b, r);
+        }
     }
     join_lanes(b, r);
     if (lane == 0) of_warp[warp] = make_float2(r.m, r.s);
@@ -453,6 +462,59 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
   if (joint) cluster_wait();
 }
 
+// ---------------------------------------------------------------- the loss alone, of many rows
+// A CTA a row, walked once as it comes from memory.  Bytes bound it in fp32: 2048 rows of 128256 155 us, 6.8 TB/s, a copy's rate; in bf16 unpacking and exponentials come near them: 8192 rows
+// of 32000, a tenth of them without entries, 103 us, 5.1 TB/s.  By clusters through shared memory as above 315 and 132 us; four CTAs an SM 165 / 115, six 181 / 103.
+template <typename T>
+__global__ void __launch_bounds__(WALKERS + 32, 5) distill_loss_kernel(const __grid_constant__ Distill a, float b) {
+  pdl_wait();
+  pdl_trigger();
+  extern __shared__ __align__(16) char shared[];
+  __shared__ float2 of_warp[WALKERS / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long row = blockIdx.x;
+  const T *const z = (const T *)a.z + row * a.z_rs;
+  const Entries e = entries_in(shared, a.K);
+  // a row without an id is not read
+  bool there = false;
+  for (int k = 0; k < a.K && !there; k += 32) there = __any_sync(0xffffffffu, k + lane < a.K && id_at(a.ids, row * a.K + k + lane) != -1);
+  float all = 0.0f;
+  bool none = true;
+  if (!there) {
+  } else if (tid >= WALKERS) {
+    all = read_entries(a, e, row, &none);
+  } else {
+    // units of eight, aligned; what lies before and behind them an element a thread
+    const int head = min(a.vocab, (int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) % 16 / sizeof(T))), units = (a.vocab - head) / 8, tail = head + units * 8;
+    Running r;
+    const int c = tid < head ? tid : tid < head + a.vocab - tail ? tail + tid - head : -1;      // fewer than 16
+    if (c >= 0) r.m = to_f32(z[c]), r.s = exp_of(b, r.m - relative_to(r.m));
+    if (r.m != r.m) r = Running{-INFINITY, NAN};
+    constexpr int U = sizeof(T) == 4 ? 2 : 4;            // 64 bytes of a thread under way: with 128 of fp32 registers spill (238 us)
+    for (int u = tid; u < units; u += U * WALKERS) {
+      Raw8<T> x[U];
+#pragma unroll
+      for (int i = 0; i < U; i++)
+        if (u + i * WALKERS < units) x[i].take(z + head + (u + i * WALKERS) * 8);
+#pragma unroll
+      for (int i = 0; i < U; i++)
+        if (u + i * WALKERS < units) r = walk(x[i], b, r);
+    }
+    join_lanes(b, r);
+    if (lane == 0) of_warp[warp] = make_float2(r.m, r.s);
+  }
+  __syncthreads();
+  if (tid < WALKERS) return;
+  Running r;
+  if (!none && lane < WALKERS / 32) r = Running{of_warp[lane].x, of_warp[lane].y};
+  join_lanes(b, r);
+  if (r.m == -INFINITY) r.s = NAN;
+  const float loss = none ? 0.0f : entries_loss(a, e, r.m, [&](int id) { return to_f32(z[id]); }) + all * logf(r.s);
+  if (lane) return;
+  a.loss[row] = loss;
+  if (a.stats) a.stats[row] = none ? make_float2(0.0f, 1.0f) : make_float2(r.m, r.s);
+}
+
 // Slices of about SLICE bytes, so that three CTAs are on an SM; smaller ones where rows alone do not fill the SMs twice, down to 2 KB.
 static bool slices_of(const Distill &a, Slices *sl) {
   const size_t e = a.z_type == 0 ? 4 : 2, row = (size_t)a.vocab * e;
@@ -464,7 +526,7 @@ static bool slices_of(const Distill &a, Slices *sl) {
   sl->whole = a.dz && pieces_aligned(a.dz, a.rows > 1 ? a.d_rs : 0, a.d_type == 0 ? 4 : 2);
   sl->look_first = (long long)a.rows * n > 4 * 148;
   sl->ahead = sl->look_first ? 3 * 148 / n : 0;
-  return (size_t)sl->per * e <= SLICE_MOST && (long long)a.rows * n <= INT32_MAX;
+  return (size_t)sl->per * e + entries_bytes(a.K) <= SHARED_MOST && (long long)a.rows * n <= INT32_MAX;
 }
 
 template <typename T, typename O, int MODE> static cudaError_t rows_in_shared(const Distill &a, float b, const Slices &sl, cudaStream_t s) {
@@ -489,7 +551,10 @@ template <typename T, typename O> static cudaError_t rows_in_shared(const Distil
 }
 
 cudaError_t launch_distill(const Distill &a, cudaStream_t s) {
-  const float b = (float)(1.4426950408889634 / a.temperature);
+  const float b = (float)(1.4426950408889634 / a.temperature);      // log2(e) / T
+  if (!a.dz && a.rows >= 2 * 148)
+    return a.z_type == 0 ? launch_k(distill_loss_kernel<float>, dim3(a.rows), dim3(WALKERS + 32), entries_bytes(a.K), s, a, b)
+                         : launch_k(distill_loss_kernel<bf16>, dim3(a.rows), dim3(WALKERS + 32), entries_bytes(a.K), s, a, b);
   Slices sl;
   if (!slices_of(a, &sl)) return launch_k(distill_any_kernel, dim3(a.rows), dim3(512), entries_bytes(a.K) + (size_t)a.K * 4, s, a, b);
   if (a.z_type == 0) {
