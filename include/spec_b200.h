@@ -399,7 +399,7 @@ typedef struct {
 } spec_rows;
 
 /* out[t] = scale * weight[ids[t]]; weight [vocab][dim], out [tokens][dim], each F32 or BF16; ids of id_bits 32 or 64 (int32_t, int64_t).  -1: a row of zeros; so is an id out
- * of range, which `status` (as above) records: code 2, site 64, token and id.  dim <= 2^22, tokens <= 2^30. */
+ * of range, which `status` (as above) records: code 2, site 64, token and id.  dim <= 2^22, tokens and vocab <= 2^30. */
 int spec_embedding(const spec_rows *weight, int32_t vocab, int32_t dim, int32_t id_bits, const void *ids, int32_t tokens, float scale,
                    const spec_rows *out, int32_t *status, void *stream);
 
@@ -413,7 +413,7 @@ int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, const void *
 /* s = x + residual (x where residual is NULL), y = s / sqrt(mean(s^2) + eps) * gain, the mean over a row's dim elements; both from the sum in 32 bits.
  * sum (NULL without residual): s in the residual's type; its memory may be residual's or x's, with their stride and type.  y F32, BF16, or codes in 8 bits with scale float
  * [rows][ceil(dim / group)]: value = code * scale, scale = max(largest magnitude of the group / top, 2^-120), top 448 (E4M3) or 127 (INT8), as in spec_kv_cache; a group with
- * an infinity or a NaN reads back as NaN.  group: a multiple of 16, or 0 for the whole row; only 8-bit outputs look at it.  gain [dim] of gain_dtype.  dim <= 2^22. */
+ * an infinity or a NaN reads back as NaN.  group: a multiple of 16, or 0 for the whole row; only 8-bit outputs look at it.  gain [dim] of gain_dtype.  dim <= 2^22, rows <= 2^30. */
 int spec_rms_norm(const spec_rows *x, const spec_rows *residual, int32_t gain_dtype, const void *gain, float eps, const spec_rows *sum, const spec_rows *y,
                   float *scale, int32_t group, int32_t rows, int32_t dim, void *stream);
 
@@ -428,7 +428,7 @@ int spec_rms_norm_backward(const spec_rows *grad, const spec_rows *s, int32_t ga
 /* A teacher's top logits: for each row K ids (id_bits 32 or 64; -1: none) and their logits or log-probabilities (values_dtype), [rows][K].  id_map (may be NULL): int32
  * [id_map_n], from the teacher's ids to the student's, -1 for those that the student lacks.  lse (may be NULL): float [rows], the log of the teacher's whole sum of exp(logit / temperature).
  * An entry with id -1, or that the map sends there, or with a value of -inf, is none; ids and mapped ids out of range are none and recorded in `status` (code 2, sites 65 and 66,
- * row and id).  The same id several times: its probabilities add up.  1 <= K <= 1024. */
+ * row and id).  The same id several times: its probabilities add up.  1 <= K <= 1024; rows and vocab <= 2^30. */
 typedef struct {
   const void *ids, *values;
   const float *lse;

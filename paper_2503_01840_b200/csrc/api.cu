@@ -1869,13 +1869,13 @@ static int ids_of(const void *ids, int bits, Ids *out) {
   *out = Ids{ids, bits == 64};
   return kv_aligned(ids, bits / 8) ? SPEC_OK : SPEC_ERR_INVALID_CFG;
 }
-constexpr int MOST_COLUMNS = 1 << 22, MOST_TOKENS = 1 << 30;
+constexpr int MOST_COLUMNS = 1 << 22, MOST_ROWS = 1 << 30;      // indices and the next multiples of blocks' shares stay below 2^31
 
 extern "C" int spec_embedding(const spec_rows *weight, int32_t vocab, int32_t dim, int32_t id_bits, const void *ids, int32_t tokens, float scale,
                               const spec_rows *out, int32_t *status, void *stream) {
   Embed a{};
   if (vocab < 1 || dim < 1 || tokens < 0 || !(fabsf(scale) < INFINITY)) return SPEC_ERR_INVALID_CFG;
-  if (dim > MOST_COLUMNS || tokens > MOST_TOKENS) return SPEC_ERR_UNSUPPORTED;
+  if (dim > MOST_COLUMNS || tokens > MOST_ROWS || vocab > MOST_ROWS) return SPEC_ERR_UNSUPPORTED;
   if (const int rc = ids_of(ids, id_bits, &a.ids)) return rc;
   if (tokens == 0) return SPEC_OK;
   if (const int rc = rows_in(weight)) return rc;
@@ -1888,14 +1888,14 @@ extern "C" int spec_embedding(const spec_rows *weight, int32_t vocab, int32_t di
 }
 
 extern "C" size_t spec_embedding_backward_scratch_bytes(int32_t tokens, int32_t vocab, int32_t dim) {
-  return tokens < 0 || vocab < 1 || dim < 1 || dim > MOST_COLUMNS || tokens > MOST_TOKENS ? 0 : embed_grad_scratch_bytes(tokens, vocab, dim);
+  return tokens < 0 || vocab < 1 || dim < 1 || dim > MOST_COLUMNS || tokens > MOST_ROWS || vocab > MOST_ROWS ? 0 : embed_grad_scratch_bytes(tokens, vocab, dim);
 }
 
 extern "C" int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, const void *ids, int32_t tokens, int32_t vocab, int32_t dim, float scale,
                                        int32_t accumulate, const spec_rows *out, void *scratch, size_t scratch_bytes, int32_t *status, void *stream) {
   EmbedGrad a{};
   if (vocab < 1 || dim < 1 || tokens < 0 || !(fabsf(scale) < INFINITY)) return SPEC_ERR_INVALID_CFG;
-  if (dim > MOST_COLUMNS || tokens > MOST_TOKENS) return SPEC_ERR_UNSUPPORTED;
+  if (dim > MOST_COLUMNS || tokens > MOST_ROWS || vocab > MOST_ROWS) return SPEC_ERR_UNSUPPORTED;
   if (const int rc = ids_of(ids, id_bits, &a.ids)) return rc;
   if (const int rc = rows_out(out, vocab, dim)) return rc;
   if (tokens == 0 && accumulate) return SPEC_OK;
@@ -1915,7 +1915,7 @@ extern "C" int spec_embedding_backward(const spec_rows *grad, int32_t id_bits, c
 extern "C" int spec_rms_norm(const spec_rows *x, const spec_rows *residual, int32_t gain_dtype, const void *gain, float eps, const spec_rows *sum,
                              const spec_rows *y, float *scale, int32_t group, int32_t rows, int32_t dim, void *stream) {
   if (rows < 0 || dim < 1 || group < 0 || group % 16 || !(eps >= 0.0f && eps < INFINITY) || (gain_dtype != SPEC_F32 && gain_dtype != SPEC_BF16)) return SPEC_ERR_INVALID_CFG;
-  if (dim > MOST_COLUMNS) return SPEC_ERR_UNSUPPORTED;
+  if (dim > MOST_COLUMNS || rows > MOST_ROWS) return SPEC_ERR_UNSUPPORTED;
   if (rows == 0) return SPEC_OK;
   RmsNorm a{};
   if (const int rc = rows_in(x)) return rc;
@@ -1936,12 +1936,12 @@ extern "C" int spec_rms_norm(const spec_rows *x, const spec_rows *residual, int3
   return kv_status(launch_rms_norm(a, (cudaStream_t)stream));
 }
 
-extern "C" size_t spec_rms_norm_backward_scratch_bytes(int32_t rows, int32_t dim) { return rows < 0 || dim < 1 || dim > MOST_COLUMNS ? 0 : rms_norm_grad_scratch_bytes(rows, dim); }
+extern "C" size_t spec_rms_norm_backward_scratch_bytes(int32_t rows, int32_t dim) { return rows < 0 || dim < 1 || dim > MOST_COLUMNS || rows > MOST_ROWS ? 0 : rms_norm_grad_scratch_bytes(rows, dim); }
 
 extern "C" int spec_rms_norm_backward(const spec_rows *grad, const spec_rows *s, int32_t gain_dtype, const void *gain, float eps, const spec_rows *grad_sum,
                                       const spec_rows *dx, void *dgain, void *scratch, size_t scratch_bytes, int32_t rows, int32_t dim, void *stream) {
   if (rows < 0 || dim < 1 || !(eps >= 0.0f && eps < INFINITY) || (gain_dtype != SPEC_F32 && gain_dtype != SPEC_BF16)) return SPEC_ERR_INVALID_CFG;
-  if (dim > MOST_COLUMNS) return SPEC_ERR_UNSUPPORTED;
+  if (dim > MOST_COLUMNS || rows > MOST_ROWS) return SPEC_ERR_UNSUPPORTED;
   RmsNormGrad a{};
   if (!gain || !dgain) return SPEC_ERR_NULL;
   const size_t e = gain_dtype == SPEC_F32 ? 4 : 2;
@@ -1970,7 +1970,7 @@ extern "C" int spec_distill(const spec_rows *logits, int32_t rows, int32_t vocab
   if (rows < 0 || vocab < 1 || t->K < 1 || !(temperature >= 1e-4f && temperature <= 1e4f) || (t->values_dtype != SPEC_F32 && t->values_dtype != SPEC_BF16) ||
       (t->id_map && t->id_map_n < 1))
     return SPEC_ERR_INVALID_CFG;
-  if (t->K > DISTILL_MAX_K) return SPEC_ERR_UNSUPPORTED;
+  if (t->K > DISTILL_MAX_K || rows > MOST_ROWS || vocab > MOST_ROWS) return SPEC_ERR_UNSUPPORTED;
   Distill a{};
   if (const int rc = ids_of(t->ids, t->id_bits, &a.ids)) return rc;
   if (rows == 0) return SPEC_OK;

@@ -382,6 +382,7 @@ cudaError_t launch_embed_grad(const EmbedGrad &a, int g_dtype, int out_dtype, cu
     return launch_k(embed_join_kernel, grid, dim3(128), 0, s, a, r, out_dtype);
   }
   const int slabs = (a.dim + 1023) / 1024;
+  if ((long long)r.chunks * slabs + r.zeroing > INT32_MAX) return cudaErrorNotSupported;
   const dim3 runs(r.chunks * slabs + r.zeroing), join(r.chunks, slabs);
   const cudaError_t e = g_dtype == 0 ? (out_dtype == 0 ? launch_k(embed_runs_kernel<float, float>, runs, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<float, bf16>, runs, dim3(128), 0, s, a, r))
                                      : (out_dtype == 0 ? launch_k(embed_runs_kernel<bf16, float>, runs, dim3(128), 0, s, a, r) : launch_k(embed_runs_kernel<bf16, bf16>, runs, dim3(128), 0, s, a, r));

@@ -323,13 +323,15 @@ float *floats(PyObject *o, int64_t n, const char *what) {
   return (float *)address(t);
 }
 at::Tensor scratch_of(size_t bytes, const at::Tensor &like) { return at::empty({(int64_t)std::max<size_t>(bytes, 256)}, like.options().dtype(at::kByte)); }
+// A caller's tensor is about to be written: autograd refuses to go back through what saved it before.
+void written(const at::Tensor &t) { t.unsafeGetTensorImpl()->bump_version(); }
 // whether autograd has to record a call on these
 template <typename... T> bool records(const T &...t) { return at::GradMode::is_enabled() && (... || (t.defined() && t.requires_grad())); }
 
 // ids, weight, scale, dtype, out, status.  NotImplemented where autograd has to record it: binding.py wraps it then (as those below).
 PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 6, [&]() -> PyObject * {
-    const char *const what = "embedding: weight [vocabulary][width] on the GPU with adjacent columns", *const ids_are = "embedding: ids int32 or int64 [tokens] on the GPU";
+    const char *const what = "embedding: weight [vocabulary][width] on the GPU with adjacent columns", *const ids_are = "embedding: ids int32 or int64 [tokens], contiguous on the GPU";
     const at::Tensor &ids = tensor(a[0], ids_are), &w = tensor(a[1], what);
     const spec_rows from = rows_of(w, what);
     const double scale = number(a[2], "embedding: scale is a number");
@@ -344,6 +346,7 @@ PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const spec_rows to = rows_of(out, "embedding: out [tokens][width] on the GPU with adjacent columns");
     int32_t *const status = status_of(a[5]);
     void *const s = stream_of_call();
+    if (a[4] != Py_None) written(out);
     const int rc = call([&] { return embedding_(&from, (int32_t)w.size(0), (int32_t)k, id.bits, id.p, (int32_t)T, (float)scale, &to, status, s); });
     return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
   });
@@ -352,7 +355,7 @@ PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // grad, ids, vocab, scale, dtype, out, accumulate, status
 PyObject *embedding_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 8, [&]() -> PyObject * {
-    const char *const what = "embedding_backward: grad [tokens][width] on the GPU with adjacent columns", *const ids_are = "embedding_backward: ids int32 or int64 [tokens] on the GPU";
+    const char *const what = "embedding_backward: grad [tokens][width] on the GPU with adjacent columns", *const ids_are = "embedding_backward: ids int32 or int64 [tokens], contiguous on the GPU";
     const at::Tensor &g = tensor(a[0], what), &ids = tensor(a[1], ids_are);
     const spec_rows from = rows_of(g, what);
     const int64_t T = g.size(0), k = g.size(1);
@@ -373,6 +376,7 @@ PyObject *embedding_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *const s = stream_of_call();
     const size_t bytes = embedding_scratch_((int32_t)T, (int32_t)V, (int32_t)k);
     const at::Tensor scratch = scratch_of(bytes, g);
+    if (a[5] != Py_None) written(out);
     const int rc = call([&] {
       return embedding_backward_(&from, id.bits, id.p, (int32_t)T, (int32_t)V, (int32_t)k, (float)scale, accumulate, &to, scratch.data_ptr(), scratch.nbytes(), status, s);
     });
@@ -427,6 +431,7 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (records(x, w, res, sum)) Py_RETURN_NOTIMPLEMENTED;
     const at::Tensor y = at::empty({R, k}, x.options().dtype(type));
     const spec_rows to = rows_of(y, "y", true);
+    if (a[6] != Py_None) written(sum);
     if (eight) scale = at::empty({R, k == 0 ? 0 : group ? (k + group - 1) / group : 1}, x.options().dtype(at::kFloat));
     void *const s = stream_of_call();
     const int rc = call([&] {
@@ -510,6 +515,7 @@ PyObject *distill(PyObject *, PyObject *const *a, Py_ssize_t n) {
       dz = a[11] == Py_None ? at::empty({R, V}, z.options().dtype(type)) : tensor(a[11], out_is);
       need(dz.sizes() == z.sizes() && dz.scalar_type() == type && (a[11] == Py_None || !records(dz)), out_is);
       to = rows_of(dz, out_is);
+      if (a[11] != Py_None) written(dz);
     }
     int32_t *const status = status_of(a[12]);
     void *const s = stream_of_call();

@@ -668,6 +668,50 @@ def test_the_decoding_loop_refuses_ids_that_the_table_lacks():
     dec.prefill([torch.tensor([0, 2047])])
 
 
+@gpu
+def test_what_is_written_in_place_is_known_to_autograd():
+    """A graph that saved a tensor does not go back through it once a call has written over it."""
+    x = torch.randn(4, 32, device="cuda").requires_grad_()
+    w, z = torch.ones(32, device="cuda"), torch.randn(4, 32, device="cuda")
+    ids, v = torch.zeros(4, 1, dtype=torch.int32, device="cuda"), torch.zeros(4, 1, device="cuda")
+    for over in (lambda t: sb.rms_norm(z, w, residual=t, sum_out=t), lambda t: sb.distill_loss_and_grad(None, t, ids, v, out=t), lambda t: sb.embedding(ids[:, 0], z, out=t),
+                 lambda t: sb.embedding_backward(z, ids[:, 0], 4, out=t, accumulate=True)):
+        y = x * 2
+        total = (y * y).sum()
+        with torch.no_grad():
+            over(y.detach())
+        with pytest.raises(RuntimeError):
+            total.backward()
+
+
+@gpu
+def test_a_first_call_may_be_captured():
+    """In a process of its own: nothing has been launched before, and the larger kernels' shared memory has to be asked for."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2503_01840_b200 import binding as sb
+g = torch.Generator(device="cuda").manual_seed(1)
+z = torch.randn(600, 40000, generator=g, device="cuda")
+x, w = torch.randn(300, 8192, generator=g, device="cuda"), torch.ones(8192, device="cuda")
+ids, v = torch.randint(0, 40000, (600, 5), generator=g, device="cuda"), torch.randn(600, 5, generator=g, device="cuda")
+few = ids[:300, 0].contiguous() % 100
+sb._marshal()
+def run():
+    y, s = sb.rms_norm(x, w, residual=x)
+    loss, dz = sb.distill_loss_and_grad(None, z, ids, v)
+    plain, stats = sb.distill_loss(z, ids, v, want_stats=True)
+    return [y, s, loss, dz, plain, stats, *sb.rms_norm_backward(y, s, w, grad_sum=x), sb.embedding_backward(x, few, 100), sb.distill_loss_backward(None, z, stats, ids, v)]
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    kept = run()
+graph.replay()
+assert all(torch.equal(a, b) for a, b in zip(kept, run()))
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, timeout=300)
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 def rows_struct(p=4096, stride=64, kind=0):
     return sb._Rows(p, stride, kind)
