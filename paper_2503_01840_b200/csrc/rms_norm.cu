@@ -62,8 +62,9 @@ __global__ void __launch_bounds__(256) rms_norm_any_kernel(RmsNorm a) {
 // Widths of whole eights up to 16384, aligned to 16 bytes.  A thread has N times eight neighbours in every row that its block takes in turn; rows come through a ring of STAGES in shared
 // memory, in which a thread's part is its own, so that the next rows are under way while one is summed, without a register for them and with one barrier a row.
 // Up to 256 columns a warp has a row, and nothing to wait for.  In 8 bits a scale's group is part of a warp's 256 columns, or the row.
-// Bytes bound it: 16384 rows of 4096 in bf16 with the residual 98 us (5.5 TB/s, 84 % of a copy's rate), to e4m3 87 us (5.4 TB/s); 8192 rows of 8192 without 47 us (5.7 TB/s).  A block a row with the
-// row in registers 106 / 125 / 82 us; half as many blocks an SM 98 / 107 / 61; two or four stages 98 / 87 / 47 and 98 / 90 / 49; eight neighbours a thread at 4096 columns 101 / 87.
+// Bytes bound it: 16384 rows of 4096 in bf16 with the residual 97 us (5.5 TB/s, 85 % of a copy's rate), 8192 rows of 8192 without 46 us (5.8 TB/s); to e4m3 84 us (5.6 TB/s) with the scales'
+// and codes' instructions close to them.  A block a row with the row in registers 106 / 82 / 125 us; half as many blocks an SM 98 / 61 / 107; two or four stages 98 / 47 / 87 and 98 / 49 / 90; at 4096 columns
+// eight neighbours a thread 101 / - / 87, 32 of them 95 / 46 / 88.
 constexpr int STAGES = 3;
 
 template <int FMT> __device__ __forceinline__ uint2 codes_of(float (&y)[8], float inv) {
@@ -79,10 +80,10 @@ __device__ __forceinline__ float sum_of(float v, float *room, bool block) {
   const int lane = threadIdx.x & 31;
   if (lane == 0) room[threadIdx.x >> 5] = v;
   __syncthreads();
-  v = lane < (blockDim.x >> 5) ? room[lane & 15] : 0.0f;
+  v = (lane & 15) < (blockDim.x >> 5) ? room[lane & 15] : 0.0f;      // both halves of the warp alike
 #pragma unroll
   for (int d = 8; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-  return __shfl_sync(0xffffffffu, v, 0);
+  return v;
 }
 
 // What follows the sum: v is the residual sum, w the gain; thread t of `of_row` threads of the row
@@ -213,6 +214,7 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const __grid_constant__ R
   for (int k = 0; k < STAGES; k++) ask(row + (long long)k * gridDim.x, k);
   float w[N][8];
   gain_of<N>(a, t, of_row, w);
+  const float over_dim = 1.0f / a.dim;
   for (int stage = 0, turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
     copies_but<STAGES - 1>();
     float v[N][8];
@@ -230,7 +232,7 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const __grid_constant__ R
       for (int k = 0; k < 8; k++) v[i][k] += y[k];
       store8((TR *)a.sum + row * a.s_rs + c, v[i]);
     }
-    const float u = rsqrtf(sum_of(square_of<N>(v), room[turn], true) / a.dim + a.eps);
+    const float u = rsqrtf(fmaf(sum_of(square_of<N>(v), room[turn], true), over_dim, a.eps));
     ask(row + (long long)STAGES * gridDim.x, stage);
     norm_out<N>(a, row, t, of_row, v, w, u, room[turn], true);
     stage = stage == STAGES - 1 ? 0 : stage + 1;
@@ -330,6 +332,7 @@ __global__ void __launch_bounds__(512) rms_norm_grad_kernel(const __grid_constan
   long long row = blockIdx.x;
   for (int k = 0; k < stages; k++) ask(row + (long long)k * gridDim.x, k);
   float w[N][8], sum[N][8] = {};
+  const float over_dim = 1.0f / a.dim;
 #pragma unroll
   for (int i = 0; i < N; i++) {
     const int c = (i * of_row + t) * 8;
@@ -362,12 +365,11 @@ __global__ void __launch_bounds__(512) rms_norm_grad_kernel(const __grid_constan
     for (int d = 16; d; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d), dot += __shfl_xor_sync(0xffffffffu, dot, d);
     if (lane == 0) room[turn][warp] = make_float2(ss, dot);
     __syncthreads();
-    const float2 some = lane < warps ? room[turn][lane & 15] : make_float2(0.0f, 0.0f);
+    const float2 some = (lane & 15) < warps ? room[turn][lane & 15] : make_float2(0.0f, 0.0f);      // both halves of the warp alike
     ss = some.x, dot = some.y;
 #pragma unroll
     for (int d = 8; d; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d), dot += __shfl_xor_sync(0xffffffffu, dot, d);
-    ss = __shfl_sync(0xffffffffu, ss, 0), dot = __shfl_sync(0xffffffffu, dot, 0);
-    const float u = rsqrtf(ss / a.dim + a.eps), along = dot / a.dim * u * u;
+    const float u = rsqrtf(fmaf(ss, over_dim, a.eps)), along = dot * over_dim * u * u;
 #pragma unroll
     for (int i = 0; i < N; i++) {
       const int c = (i * of_row + t) * 8;
