@@ -669,6 +669,105 @@ def test_the_decoding_loop_refuses_ids_that_the_table_lacks():
 
 
 @gpu
+def test_two_streams_at_once():
+    """Calls that overlap on the GPU share nothing."""
+    g = gen(9)
+    z, ids, v = randn(g, 3000, 32000).cuda(), torch.randint(0, 32000, (3000, 20), generator=g).cuda(), randn(g, 3000, 20).cuda()
+    x, w, tok = randn(g, 6000, 4096).bfloat16().cuda(), torch.ones(4096, device="cuda"), torch.randint(0, 30000, (6000,), generator=g).cuda()
+    a = lambda: [*sb.distill_loss_and_grad(None, z, ids, v), sb.embedding_backward(x, tok, 30000)]
+    b = lambda: [*sb.rms_norm_backward(x, x, w), sb.embedding_backward(x, tok.flip(0), 30000), *sb.rms_norm(x, w, residual=x, dtype=torch.int8)]
+    want = a(), b()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for s, f in zip(streams, (a, b)):
+        with torch.cuda.stream(s):
+            got.append(f())
+    torch.cuda.synchronize()
+    for one, other in zip(want, got):
+        assert all(torch.equal(p, q) for p, q in zip(one, other))
+
+
+@gpu
+def test_a_training_step_in_a_graph():
+    """Forward, backward through autograd and the leaves' gradients, captured after a warm-up whose graph is gone; replayed on other inputs as the same step without."""
+    g = gen(14)
+    T, V, k, Vd, K = 90, 400, 256, 500, 6
+    leaves = [randn(g, V, k).cuda().requires_grad_(), torch.ones(k, device="cuda").requires_grad_(), (randn(g, Vd, k) / 16).cuda().requires_grad_()]
+    ids, tid, values = torch.randint(0, V, (T,), generator=g).cuda(), torch.randint(0, Vd, (T, K), generator=g).cuda(), randn(g, T, K).cuda()
+
+    def step():
+        x = sb.embedding(ids, leaves[0])
+        y, _ = sb.rms_norm(x, leaves[1], residual=x * 0.5)
+        loss = sb.distill_loss(y @ leaves[2].T, tid, values).mean()
+        loss.backward()
+        return loss.detach()
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step()
+            for t in leaves:
+                t.grad = None
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss = step()
+    kept = [t.grad for t in leaves]
+    for seed in (3, 4):
+        h = gen(seed)
+        ids.copy_(torch.randint(0, V, (T,), generator=h))
+        tid.copy_(torch.randint(0, Vd, (T, K), generator=h))
+        values.copy_(randn(h, T, K))
+        graph.replay()
+        replayed = [loss.clone()] + [t.clone() for t in kept]
+        for t in leaves:
+            t.grad = None
+        plain = [step()] + [t.grad for t in leaves]
+        assert all(torch.allclose(p, q, rtol=1e-5, atol=1e-7) for p, q in zip(replayed, plain))      # the products are another library's, which may choose by the stream
+
+
+@gpu
+def test_offsets_that_pass_32_bits():
+    """The last rows of tensors of more than 2^31 elements: the same bits as by themselves."""
+    g = gen(6)
+    n, k = 530000, 4096
+    big = torch.zeros(n, k, dtype=torch.bfloat16, device="cuda")
+    last = randn(g, 40, k).bfloat16().cuda()
+    big[-40:] = last
+    assert big.numel() > 1 << 31
+    ids = torch.arange(n - 40, n, device="cuda")
+    assert torch.equal(sb.embedding(ids, big), last)
+    w = torch.ones(k, device="cuda")
+    y, s = sb.rms_norm(big, w, 1e-5, residual=big)
+    y1, s1 = sb.rms_norm(last, w, 1e-5, residual=last)
+    assert torch.equal(y[-40:], y1) and torch.equal(s[-40:], s1)
+    del s
+    dx = sb.rms_norm_backward(big, y, w, 1e-5)[0]
+    assert torch.equal(dx[-40:], sb.rms_norm_backward(last, y1, w, 1e-5)[0])
+    del y, dx
+    out = sb.embedding_backward(last, ids, n)
+    assert torch.equal(out[-40:], last) and not out[: n - 40].any()
+    tokens = torch.full((n,), -1, device="cuda")
+    tokens[-40:] = torch.arange(40, device="cuda")
+    assert torch.equal(sb.embedding_backward(big, tokens, 40), last)
+    del out, tokens
+    z = big.view(-1)[: 67000 * 32400].view(67000, 32400)
+    assert z.numel() > 1 << 31
+    z[-5:] = randn(g, 5, 32400).bfloat16().cuda()
+    tid, values = torch.full((67000, 3), -1, dtype=torch.int32, device="cuda"), torch.zeros(67000, 3, device="cuda")
+    tid[-5:] = torch.randint(0, 32400, (5, 3), generator=g).int().cuda()
+    loss, stats = sb.distill_loss(z, tid, values, want_stats=True)
+    one, dz = sb.distill_loss_and_grad(None, z, tid, values)
+    few, dfew = sb.distill_loss_and_grad(None, z[-5:].clone(), tid[-5:].clone(), values[-5:].clone())
+    # the few rows go by more and smaller slices, so their sums are added in another order
+    assert torch.allclose(one[-5:], few, rtol=1e-5) and torch.allclose(loss[-5:], few, rtol=1e-5) and not loss[:-5].any() and not one[:-5].any()
+    assert torch.allclose(dz[-5:].float(), dfew.float(), rtol=2.0 ** -7, atol=0) and not dz[:-5].any()
+    assert torch.allclose(sb.distill_loss_backward(None, z, stats, tid, values)[-5:].float(), dfew.float(), rtol=2.0 ** -7, atol=0)
+
+
+@gpu
 def test_what_is_written_in_place_is_known_to_autograd():
     """A graph that saved a tensor does not go back through it once a call has written over it."""
     x = torch.randn(4, 32, device="cuda").requires_grad_()
