@@ -63,7 +63,7 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
   float top = -INFINITY;
   bool some = false, nan = false;
   if (lane < fours(a.K) - a.K) e.id[a.K + lane] = -1;
-#pragma unroll 2
+#pragma unroll 1
   for (int k = lane; k < a.K; k += 32) {
     int id = id_at(a.ids, at + k);
     const float v = load_as_f32(a.values, a.v_type, at + k);
@@ -94,6 +94,7 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
   } else {
     top = key_value(__reduce_max_sync(0xffffffffu, nan ? 0xffffffffu : ordered_key(top)));
     float sum = 0.0f;
+#pragma unroll 1
     for (int k = lane; k < a.K; k += 32)
       if (e.id[k] >= 0) sum += expf((e.ln_p[k] - top) * inv_t);
 #pragma unroll
@@ -101,6 +102,7 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
     ln_sum = logf(sum);
   }
   float all = 0.0f;
+#pragma unroll 1
   for (int k = lane; k < a.K; k += 32) {
     const float ln_p = (e.ln_p[k] - top) * inv_t - (a.lse ? lse : ln_sum), p = e.id[k] >= 0 ? expf(ln_p) : 0.0f;
     e.ln_p[k] = ln_p;
@@ -117,6 +119,7 @@ __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
   for (int k = lane; k <= mask >> 2; k += 32) ((int4 *)e.table)[k] = make_int4(-1, -1, -1, -1);
   __syncwarp();
   bool twice = false;
+#pragma unroll 1
   for (int k = lane; k < K; k += 32) {
     const int id = e.id[k];
     e.write[k] = id < 0 ? -1.0f : e.p[k];
@@ -131,10 +134,12 @@ __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
   }
   __syncwarp();
   if (!__any_sync(0xffffffffu, twice)) return;
+#pragma unroll 1
   for (int k = lane; k < K; k += 32) {
     const int id = e.id[k];
     bool first = id >= 0;
     float p = e.p[k];
+#pragma unroll 1
     for (int j = 0; first && j < K; j++) {
       if (j == k || e.id[j] != id) continue;
       if (j < k) first = false;
@@ -147,6 +152,7 @@ __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
 // A warp's sum over its lanes' entries of p (ln p - ln q), ln q without the logarithm of q's normaliser; z(id): the student's logit
 template <typename F> __device__ __forceinline__ float entries_loss(const Distill &a, const Entries &e, float m, F z) {
   float loss = 0.0f;
+#pragma unroll 1
   for (int k = threadIdx.x & 31; k < a.K; k += 32) {
     const float p = e.p[k];
     if (e.id[k] < 0 || p == 0.0f) continue;
@@ -231,10 +237,11 @@ __global__ void __launch_bounds__(512) distill_any_kernel(Distill a, float b) {
 // exchange, and walked again for the gradient.  Where the statistics are given the CTAs have nothing to exchange and are no cluster.  Elements keep their place modulo 16 bytes, so any
 // alignment will do; a thread copies and walks the same units of eight and waits for its own copies alone.  Meanwhile another warp looks the entries up (some four microseconds, most of
 // them waiting), takes the loss, and writes over what the walkers wrote at the entries' ids.
-// The gradient from statistics is bound by bytes: 2048 rows of 128256 fp32 to bf16 242 us, 6.5 TB/s, a copy's rate.  Loss and gradient at once wait, load, walk and write in turn, three
-// CTAs an SM side by side: 8192 rows of 32000 bf16, a tenth of them without entries, 195 us, 5.1 TB/s, 78 % of a copy's; two exponentials an element are 116 us of its unit's time.
+// The gradient from statistics is bound by bytes: 2048 rows of 128256 fp32 to bf16 241 us, 6.5 TB/s, a copy's rate.  Loss and gradient at once wait, load, walk and write in turn, three
+// CTAs an SM side by side: 8192 rows of 32000 bf16, a tenth of them without entries, 187 us, 5.4 TB/s, 82 % of a copy's; two exponentials an element are 116 us of its unit's time.
 // Slices of 44 KB and four CTAs 292 / 259 us (clusters wait for one another), of 100 KB 196 / 247; 384 walkers 206 / 269.  CTAs that stay, with the next row's entries and copies under way,
-// 244 / 299: their one look-up warp is what they wait for.  Rows that have no id are not read: 233 us without that, and 210 without the next entries' way into L2.
+// 244 / 299: their one look-up warp is what they wait for.  Rows that have no id are not read: 233 us without that, and 210 without the next entries' way into L2.  Loops stay rolled: two warps'
+// paths have to stay in the instruction cache together, and the same loops unrolled, with fewer checks, take 205 to 218 us.  One unit a thread at a time 193 us, four 188.
 enum { LOSS = 0, GRADIENT = 1, BOTH = 2 };
 struct Slices {
   int n, per;            // slices of a row, elements of one: a multiple of 8
@@ -263,16 +270,27 @@ __device__ __forceinline__ float largest(const Raw8<bf16> &x) {
 }
 
 constexpr int WALKERS = 256;      // threads that copy and walk; another warp looks the entries up and takes the loss
+constexpr int UNITS = 2;          // that a thread walks at a time
 
-// A unit's part of a thread's maximum and sum
-template <typename T> __device__ __forceinline__ Running walk(const Raw8<T> &x, float b, Running r) {
-  const float top = largest(x);
+// The part of N units in a thread's maximum and sum
+template <int N, typename T> __device__ __forceinline__ Running walk(const Raw8<T> (&x)[N], float b, Running r) {
+  float top = largest(x[0]);
+#pragma unroll
+  for (int i = 1; i < N; i++) top = fmaxf(top, largest(x[i]));
   if (top > r.m) r.s *= exp_of(b, r.m == -INFINITY ? 0.0f : r.m - top), r.m = top;
-  float y[8], even, odd;
-  Pair p[4];
-  x.floats(y);
-  exp_of(b, relative_to(r.m), y, p);
-  unpair(add(add(p[0], p[1]), add(p[2], p[3])), even, odd);
+  const float m = relative_to(r.m);
+  Pair s[4];
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    float y[8];
+    Pair p[4];
+    x[i].floats(y);
+    exp_of(b, m, y, p);
+#pragma unroll
+    for (int k = 0; k < 4; k++) s[k] = i ? add(s[k], p[k]) : p[k];
+  }
+  float even, odd;
+  unpair(add(add(s[0], s[1]), add(s[2], s[3])), even, odd);
   r.s += even + odd;
   return r;
 }
@@ -329,26 +347,31 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
       asm volatile("prefetch.global.L2 [%0];" ::"l"((const char *)a.values + (at + k) * values));
     }
   }
-  bool there = true;
-  if (sl.look_first) {
-    there = false;
-    for (int k = 0; k < a.K && !there; k += 32) there = __any_sync(0xffffffffu, k + lane < a.K && id_at(a.ids, row * a.K + k + lane) != -1);
-  }
   const int steps = (units + WALKERS - 1) / WALKERS, quarter = (steps + 3) / 4;      // a unit of each thread a step
-  if (there && walks) {
-#pragma unroll
-    for (int q = 0; q < 4; q++) {
+  auto copy_quarters = [&](int q0, int q1) {
+#pragma unroll 1
+    for (int q = q0; q < q1; q++) {
+#pragma unroll 1
       for (int i = q * quarter; i < min(steps, (q + 1) * quarter); i++) {
         const int u = i * WALKERS + tid, c = u * 8 - shift;
         if (c >= 0 && c + 8 <= n) {
           copy8(buf + u * 8, z + c);
         } else if (u < units) {
-#pragma unroll
+#pragma unroll 1
           for (int x = 0; x < 8; x++) buf[u * 8 + x] = c + x >= 0 && c + x < n ? z[c + x] : from_f32<T>(-INFINITY);
         }
       }
       copies_commit();
     }
+  };
+  bool there = true;
+  if (sl.look_first) {
+    there = false;
+#pragma unroll 1
+    for (int k = 0; k < a.K && !there; k += 32) there = __any_sync(0xffffffffu, k + lane < a.K && id_at(a.ids, row * a.K + k + lane) != -1);
+  }
+  if (there && walks) {
+    copy_quarters(0, 4);
   } else if (!walks) {
     bool none = true;
     if (there) {
@@ -360,17 +383,27 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
   }
   Running r;
   if (MODE != GRADIENT && there && walks) {
-#pragma unroll
+#pragma unroll 1
     for (int q = 0; q < 4; q++) {
       if (q == 0) copies_but<3>();
       if (q == 1) copies_but<2>();
       if (q == 2) copies_but<1>();
       if (q == 3) copies_but<0>();
-      for (int i = q * quarter; i < min(steps, (q + 1) * quarter); i++)
+      int i = q * quarter;
+      const int end = min(steps, (q + 1) * quarter);
+#pragma unroll 1
+      for (; i + UNITS <= end && (i + UNITS) * WALKERS <= units; i += UNITS) {
+        Raw8<T> x[UNITS];
+#pragma unroll
+        for (int k = 0; k < UNITS; k++) x[k].take(buf + ((i + k) * WALKERS + tid) * 8);
+        r = walk<UNITS>(x, b, r);
+      }
+#pragma unroll 1
+      for (; i < end; i++)
         if (i * WALKERS + tid < units) {
-          Raw8<T> x;
-          x.take(buf + (i * WALKERS + tid) * 8);
-          r = walk(x, b, r);
+          Raw8<T> x[1];
+          x[0].take(buf + (i * WALKERS + tid) * 8);
+          r = walk<1>(x, b, r);
         }
     }
     join_lanes(b, r);
@@ -416,6 +449,7 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
     }
     if (MODE != LOSS) {
       if (!none)
+#pragma unroll 1
         for (int k = lane; k < a.K; k += 32) {           // what is written over theirs
           const int id = e.id[k];
           const float p = e.write[k];
@@ -424,6 +458,7 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
         }
       written_wait();
       if (!none)
+#pragma unroll 1
         for (int k = lane; k < a.K; k += 32)
           if (e.id[k] >= 0) store_from_f32(a.dz, a.d_type, row * a.d_rs + e.id[k], e.write[k]);
     }
@@ -436,10 +471,12 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
     if (none) {
       if (sl.whole) {
         const float y[8] = {};
+#pragma unroll 1
         for (int u = tid; u < n / 8; u += WALKERS) store8(d + u * 8, y);
         for (int c = n / 8 * 8 + tid; c < n; c += WALKERS) d[c] = from_f32<O>(0.0f);
       } else {
-        for (int c = tid; c < n; c += WALKERS) d[c] = from_f32<O>(0.0f);
+  #pragma unroll 1
+      for (int c = tid; c < n; c += WALKERS) d[c] = from_f32<O>(0.0f);
       }
     } else if (sl.whole && shift == 0) {
 #pragma unroll 2
@@ -452,8 +489,10 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
         for (int x = 0; x < 4; x++) unpair(mul(p[x], pair(of_q, of_q)), y[2 * x], y[2 * x + 1]);
         store8(d + u * 8, y);
       }
+#pragma unroll 1
       for (int c = n / 8 * 8 + tid; c < n; c += WALKERS) d[c] = from_f32<O>(of_q * exp_of(b, to_f32(buf[c]) - r.m));
     } else {
+#pragma unroll 2
       for (int c = tid; c < n; c += WALKERS) d[c] = from_f32<O>(of_q * exp_of(b, to_f32(buf[shift + c]) - r.m));
     }
   }
@@ -492,13 +531,13 @@ __global__ void __launch_bounds__(WALKERS + 32, 5) distill_loss_kernel(const __g
     if (r.m != r.m) r = Running{-INFINITY, NAN};
     constexpr int U = sizeof(T) == 4 ? 2 : 4;            // 64 bytes of a thread under way: with 128 of fp32 registers spill (238 us)
     for (int u = tid; u < units; u += U * WALKERS) {
-      Raw8<T> x[U];
+      Raw8<T> x[U][1];
 #pragma unroll
       for (int i = 0; i < U; i++)
-        if (u + i * WALKERS < units) x[i].take(z + head + (u + i * WALKERS) * 8);
+        if (u + i * WALKERS < units) x[i][0].take(z + head + (u + i * WALKERS) * 8);
 #pragma unroll
       for (int i = 0; i < U; i++)
-        if (u + i * WALKERS < units) r = walk(x[i], b, r);
+        if (u + i * WALKERS < units) r = walk<1>(x[i], b, r);
     }
     join_lanes(b, r);
     if (lane == 0) of_warp[warp] = make_float2(r.m, r.s);
