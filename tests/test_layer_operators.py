@@ -415,7 +415,8 @@ def entries(g, rows, V, K, Vt, share=0.0):
 
 
 DISTILL = [(1, 1, 1, 0, 1.0), (3, 5, 9, 0, 1.0), (61, 1024, 16, 4096, 1.0), (7, 1000, 7, 0, 2.0), (5, 32000, 64, 128256, 1.0), (4, 10007, 33, 20000, 0.7), (2, 128256, 16, 0, 3.0), (300, 250, 5, 0, 1.0),
-           (9, 50257, 200, 0, 1.0), (2, 4097, 1024, 5000, 1.0), (40, 32001, 3, 0, 0.25), (200, 8192, 4, 9000, 10.0)]
+           (9, 50257, 200, 0, 1.0), (2, 4097, 1024, 5000, 1.0), (40, 32001, 3, 0, 0.25), (200, 8192, 4, 9000, 10.0),
+           (3, 600001, 9, 0, 1.0), (320, 4100, 1024, 0, 1.0)]
 
 
 @gpu
@@ -521,6 +522,33 @@ def test_distillation_of_masked_and_odd_logits(V, mode):
         assert loss[r] == 0 and not dz[r].any()
     assert loss[12] == math.inf and dz[12].isfinite().all() and dz[12, 3] < 0
     within(dz[12: 13], dwant[12: 13], dtol[12: 13].nan_to_num(0.0) + 1e-7)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1000, 1001])
+def test_masked_and_odd_logits_in_many_rows(V, dtype):
+    """As above, where rows are many: each kind of row is what it is by itself."""
+    g = gen(V, 2)
+    z = randn(g, 8, V)
+    z[0, V // 2:] = -math.inf
+    z[1, 10:] = torch.finfo(torch.bfloat16).min
+    z[2] = -math.inf
+    z[3, V - 1] = math.inf
+    z[4, V - 2] = math.nan
+    z[5, : V - 1] = -math.inf
+    z[6] = math.nan
+    ids, values = torch.arange(5).repeat(8, 1), randn(g, 8, 5)
+    ids[5], ids[6] = V - 1, -1
+    z = z.to(DT[dtype])
+    for off in (0, 1):
+        few = sb.distill_loss(strided(z, off), ids.cuda(), values.cuda(), want_stats=True)
+        many = sb.distill_loss(strided(z.repeat(50, 1), off), ids.repeat(50, 1).cuda(), values.repeat(50, 1).cuda(), want_stats=True)
+        for a, b in zip(few, many):
+            assert torch.allclose(a.repeat(50, *[1] * (a.dim() - 1)), b, rtol=1e-5, atol=1e-6, equal_nan=True)
+    want, tol, _, _ = distilled(z, ids, values, None, None, 1.0, "kl", None)
+    within(few[0][[0, 1, 5, 7]], want[[0, 1, 5, 7]], tol[[0, 1, 5, 7]] + 1e-6)
+    assert few[0][[2, 3, 4]].isnan().all() and few[0][6] == 0
 
 
 @gpu
