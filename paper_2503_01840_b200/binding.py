@@ -649,6 +649,7 @@ def decode_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor
 
 
 # ------------------------------------------------------------------ embedding lookup, norms of a residual sum, distillation, and their gradients
+# Autograd records embedding, rms_norm and distill_loss (rotary too) backwards, once; a tensor with a forward-mode tangent is refused.
 def _done(r, what: str):
     if type(r) is int:
         raise SpecError(r, what)

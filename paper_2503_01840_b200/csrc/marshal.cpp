@@ -9,6 +9,7 @@
 
 #include <ATen/Functions.h>
 #include <ATen/core/grad_mode.h>
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
@@ -148,6 +149,12 @@ template <typename F> int call(F f) {
   return rc;
 }
 
+// Whether autograd has to record a call on these: backwards, or forwards, where one carries a tangent (which no_grad does not turn off).
+template <typename... T> bool records(const T &...t) {
+  return (at::GradMode::is_enabled() && (... || (t.defined() && t.requires_grad()))) ||
+         (c10::AutogradState::get_tls_state().get_fw_grad_mode() && (... || (t.defined() && t._fw_grad(0).defined())));
+}
+
 // x, positions, inv_freq, layout, mscale, out, transpose.  NotImplemented where autograd has to record it: binding.py wraps it then.
 PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> PyObject * {
@@ -157,7 +164,7 @@ PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int dtype = dtype_of(x.scalar_type());
     const at::Tensor out = a[5] == Py_None ? at::empty(x.sizes(), x.options(), at::MemoryFormat::Contiguous) : tensor(a[5], "out");
     need(out.sizes() == x.sizes() && out.scalar_type() == x.scalar_type(), "rotary: out has x's shape and dtype");
-    if (at::GradMode::is_enabled() && (x.requires_grad() || out.requires_grad())) Py_RETURN_NOTIMPLEMENTED;
+    if (records(x, out)) Py_RETURN_NOTIMPLEMENTED;
     const Heads to = heads(out, "rotary: out [tokens][heads][head_dim] on the GPU with adjacent dimensions");
     need(rope_of(a[2], a[3], a[4], &r), "rotary: inv_freq");
     const int32_t *pos = (const int32_t *)ints(a[1], x.size(0), "rotary: positions int32 [tokens] on the GPU");
@@ -325,8 +332,6 @@ float *floats(PyObject *o, int64_t n, const char *what) {
 at::Tensor scratch_of(size_t bytes, const at::Tensor &like) { return at::empty({(int64_t)std::max<size_t>(bytes, 256)}, like.options().dtype(at::kByte)); }
 // A caller's tensor is about to be written: autograd refuses to go back through what saved it before.
 void written(const at::Tensor &t) { t.unsafeGetTensorImpl()->bump_version(); }
-// whether autograd has to record a call on these
-template <typename... T> bool records(const T &...t) { return at::GradMode::is_enabled() && (... || (t.defined() && t.requires_grad())); }
 
 // ids, weight, scale, dtype, out, status.  NotImplemented where autograd has to record it: binding.py wraps it then (as those below).
 PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n) {
