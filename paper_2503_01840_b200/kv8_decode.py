@@ -73,7 +73,8 @@ class CachedDecoder:
     def _embed(self, tokens):
         return sb.embedding(tokens, self.w["embed"], dtype=torch.float32)
 
-    # -- the loop
+    # -- the loop; weights may be parameters of a module: nothing is recorded for their gradients
+    @torch.no_grad()
     def prefill(self, prompts):
         """Prompts (id sequences) one after the other; the first token of each."""
         if len(prompts) != self.batch or not all(1 <= len(p) <= self.max_ctx for p in prompts):
@@ -105,6 +106,7 @@ class CachedDecoder:
         self.seqs = torch.arange(self.batch, dtype=torch.int32, device="cuda")
         return self.tokens
 
+    @torch.no_grad()
     def step(self):
         """(the next token of every sequence int32 [batch] on the GPU, hidden states); nothing waits for the GPU."""
         if self.longest >= self.max_ctx:

@@ -1,0 +1,31 @@
+"""The decoding loop over an 8-bit cache: weights, prompts and tokens as programs have them."""
+import pytest
+import torch
+
+from paper_2503_01840_b200 import synth
+
+pytestmark = pytest.mark.gpu
+
+
+def model(batch):
+    cfg = synth.ModelCfg("K", "bf16", 1, 512, 4, 2, 128, 1408, 2048, 1024, (0, 0, 0), 1e4, batch=batch, tree_depth=2, tree_topk=2, tree_nodes=4, seed=3)
+    return cfg, synth.make_target_weights(cfg, "cuda")
+
+
+def prompts(*lengths):
+    g = torch.Generator().manual_seed(7)
+    return [torch.randint(0, 2048, (n,), generator=g) for n in lengths]
+
+
+def test_weights_that_need_gradients():
+    """A module's parameters, with gradients on: the same tokens and hidden states as without."""
+    from paper_2503_01840_b200.kv8_decode import CachedDecoder
+    cfg, w = model(2)
+    plain = CachedDecoder(cfg, w, 2, 64, "bf16")
+    want = [plain.prefill(prompts(9, 20)), *plain.step(), *plain.step()]
+    leaf = lambda t: {n: leaf(x) for n, x in t.items()} if isinstance(t, dict) else [leaf(x) for x in t] if isinstance(t, list) else torch.nn.Parameter(t)
+    trained = CachedDecoder(cfg, leaf(w), 2, 64, "bf16")
+    got = [trained.prefill(prompts(9, 20)), *trained.step(), *trained.step()]
+    assert torch.is_grad_enabled()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b) and not a.requires_grad
