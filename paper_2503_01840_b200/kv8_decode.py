@@ -79,6 +79,9 @@ class CachedDecoder:
         """Prompts (id sequences) one after the other; the first token of each."""
         if len(prompts) != self.batch or not all(1 <= len(p) <= self.max_ctx for p in prompts):
             raise ValueError(f"prefill: {self.batch} prompts of 1 to {self.max_ctx} tokens")
+        prompts = [torch.as_tensor(p) for p in prompts]
+        if not all(bool(((p >= 0) & (p < self.m.vocab)).all()) for p in prompts):      # before anything is written
+            raise ValueError(f"prefill: token ids from 0 to {self.m.vocab - 1}")
         first, m, ps = [], self.m, 16
         for b, prompt in enumerate(prompts):
             T = len(prompt)
@@ -93,10 +96,7 @@ class CachedDecoder:
                     pool.append(rows.view(pages, ps, m.n_kv_heads, m.head_dim).transpose(1, 2).contiguous())
                 return sb.ttt_attention(q, *pool, order, None, None)
 
-            ids = torch.as_tensor(prompt)
-            if not bool(((ids >= 0) & (ids < m.vocab)).all()):
-                raise ValueError(f"prefill: token ids from 0 to {m.vocab - 1}")
-            x, y = self._embed(ids.to("cuda", torch.int64)), None
+            x, y = self._embed(prompt.to("cuda", torch.int64)), None
             for i in range(m.n_layers):
                 x, y = self._layer(i, x, y, seq, pos, attend)
             first.append(self._tokens(x[-1:], y[-1:])[0])

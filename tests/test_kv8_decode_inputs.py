@@ -29,3 +29,18 @@ def test_weights_that_need_gradients():
     assert torch.is_grad_enabled()
     for a, b in zip(got, want):
         assert torch.equal(a, b) and not a.requires_grad
+
+
+def test_a_refused_prompt_leaves_the_sequences_as_they_were():
+    """Ids that the table lacks in the second prompt: nothing of the first has been written, and the sequences go on."""
+    from paper_2503_01840_b200.kv8_decode import CachedDecoder
+    cfg, w = model(2)
+    kept, other = CachedDecoder(cfg, w, 2, 64, "bf16"), CachedDecoder(cfg, w, 2, 64, "bf16")
+    for dec in (kept, other):
+        dec.prefill(prompts(30, 20))
+    for bad in (2048, -1):
+        with pytest.raises(ValueError):
+            kept.prefill([prompts(25, 25)[1], torch.tensor([5, bad, 6])])
+    for _ in range(2):
+        for a, b in zip(kept.step(), other.step()):
+            assert torch.equal(a, b)
