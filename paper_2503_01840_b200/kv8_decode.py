@@ -71,7 +71,10 @@ class CachedDecoder:
         return sb.argmax(self._linear(h, self.w["lm_head"])), h
 
     def _embed(self, tokens):
-        return sb.embedding(tokens, self.w["embed"], dtype=torch.float32)
+        """tokens: integers of any type and stride, on the GPU or not"""
+        if tokens.dtype not in (torch.int32, torch.int64):
+            tokens = tokens.long()
+        return sb.embedding(tokens.cuda().contiguous(), self.w["embed"], dtype=torch.float32)
 
     # -- the loop; weights may be parameters of a module: nothing is recorded for their gradients
     @torch.no_grad()
@@ -79,7 +82,7 @@ class CachedDecoder:
         """Prompts (id sequences) one after the other; the first token of each."""
         if len(prompts) != self.batch or not all(1 <= len(p) <= self.max_ctx for p in prompts):
             raise ValueError(f"prefill: {self.batch} prompts of 1 to {self.max_ctx} tokens")
-        prompts = [torch.as_tensor(p) for p in prompts]
+        prompts = [torch.as_tensor(p).long() for p in prompts]
         if not all(bool(((p >= 0) & (p < self.m.vocab)).all()) for p in prompts):      # before anything is written
             raise ValueError(f"prefill: token ids from 0 to {self.m.vocab - 1}")
         first, m, ps = [], self.m, 16
@@ -96,7 +99,7 @@ class CachedDecoder:
                     pool.append(rows.view(pages, ps, m.n_kv_heads, m.head_dim).transpose(1, 2).contiguous())
                 return sb.ttt_attention(q, *pool, order, None, None)
 
-            x, y = self._embed(prompt.to("cuda", torch.int64)), None
+            x, y = self._embed(prompt), None
             for i in range(m.n_layers):
                 x, y = self._layer(i, x, y, seq, pos, attend)
             first.append(self._tokens(x[-1:], y[-1:])[0])

@@ -44,3 +44,17 @@ def test_a_refused_prompt_leaves_the_sequences_as_they_were():
     for _ in range(2):
         for a, b in zip(kept.step(), other.step()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("of", [lambda t: t.long(), lambda t: t.to(torch.int16), lambda t: torch.stack([t, t.flip(0)], 1)[:, 0], lambda t: t.cpu()])
+def test_tokens_that_a_program_puts_in_the_place_of_the_greedy_ones(of):
+    """Of any integer type, a column of a table of them, on the host; prompts too."""
+    from paper_2503_01840_b200.kv8_decode import CachedDecoder
+    cfg, w = model(2)
+    plain, forced = CachedDecoder(cfg, w, 2, 64, "bf16"), CachedDecoder(cfg, w, 2, 64, "bf16")
+    tokens = torch.tensor([2047, 3], dtype=torch.int32, device="cuda")
+    given = [p.cuda() for p in prompts(9, 20)]
+    assert torch.equal(plain.prefill(given), forced.prefill([of(p) for p in given]))
+    plain.tokens, forced.tokens = tokens, of(tokens)
+    for a, b in zip(plain.step(), forced.step()):
+        assert torch.equal(a, b)
