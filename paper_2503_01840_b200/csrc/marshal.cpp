@@ -495,6 +495,7 @@ PyObject *distill(PyObject *, PyObject *const *a, Py_ssize_t n) {
     spec_teacher t{id.p, address(v), nullptr, nullptr, id.bits, dtype_of(v.scalar_type()), 0, (int32_t)ids.size(1)};
     if (a[3] != Py_None) {
       const at::Tensor &map = tensor(a[3], "distill_loss: id_map");
+      need(map.numel() > 0, "distill_loss: id_map without an entry");      // and so without an address, which would stand for no map
       t.id_map_n = (int32_t)std::min<int64_t>(map.numel(), INT32_MAX);
       t.id_map = (const int32_t *)ints(a[3], t.id_map_n, "distill_loss: id_map int32 [teacher's vocabulary] on the GPU");
     }

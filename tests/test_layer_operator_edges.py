@@ -25,3 +25,19 @@ def test_forward_mode_tangents_are_refused_not_dropped(grads):
                 call()
         for call in (lambda: sb.embedding(pos, x), lambda: sb.rms_norm(x, w), lambda: sb.distill_loss(x, ids, v), lambda: sb.rotary(h, pos, freq)):
             assert fwd.unpack_dual(call()).tangent is None      # no tensor has one: the calls go on as outside
+
+
+def teacher():
+    return torch.randn(4, 32, device="cuda"), torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, device="cuda")
+
+
+@gpu
+def test_an_id_map_without_entries_is_refused():
+    """It is no map of ids, and not the absence of one either: ids would be taken for the student's own."""
+    z, ids, v = teacher()
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    _, stats = sb.distill_loss(z, ids, v, want_stats=True)
+    for call in (lambda: sb.distill_loss(z, ids, v, id_map=none), lambda: sb.distill_loss_and_grad(None, z, ids, v, id_map=none),
+                 lambda: sb.distill_loss_backward(None, z, stats, ids, v, id_map=none)):
+        with pytest.raises(ValueError):
+            call()
