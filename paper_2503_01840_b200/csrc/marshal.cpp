@@ -323,10 +323,21 @@ IdList ids_of(const at::Tensor &t, const char *what) {
   for (int64_t n : t.sizes()) need(n <= INT32_MAX, "a tensor with more than 2^31 - 1 of something");
   return {address(t), t.scalar_type() == at::kInt ? 32 : 64};
 }
-// float32 of n elements, one behind the other, on the GPU
-float *floats(PyObject *o, int64_t n, const char *what) {
+// float32 of this shape up to dimensions of 1, or flat, contiguous on the GPU
+float *floats(PyObject *o, std::initializer_list<int64_t> shape, const char *what) {
   const at::Tensor &t = tensor(o, what);
-  need(t.scalar_type() == at::kFloat && t.numel() == n && t.dim() >= 1 && t.size(0) == n / (t.dim() > 1 ? std::max<int64_t>(1, t.size(1)) : 1) && t.is_cuda() && t.is_contiguous(), what);
+  int64_t n = 1;
+  for (int64_t k : shape) n *= k;
+  bool fits = t.dim() >= 1 && t.numel() == n;
+  if (fits && t.dim() > 1) {
+    auto at = shape.begin();
+    for (int64_t k : t.sizes()) {
+      if (k == 1) continue;
+      while (at != shape.end() && *at == 1) at++;
+      fits = fits && at != shape.end() && *at++ == k;
+    }
+  }
+  need(t.scalar_type() == at::kFloat && fits && t.is_cuda() && t.is_contiguous(), what);
   return (float *)address(t);
 }
 at::Tensor scratch_of(size_t bytes, const at::Tensor &like) { return at::empty({(int64_t)std::max<size_t>(bytes, 256)}, like.options().dtype(at::kByte)); }
@@ -501,18 +512,18 @@ PyObject *distill(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
     if (a[4] != Py_None) {
       need(!records(tensor(a[4], "distill_loss: values_lse")), "distill_loss: values_lse without a gradient");
-      t.lse = floats(a[4], R, "distill_loss: values_lse float32 [rows] on the GPU");
+      t.lse = floats(a[4], {R}, "distill_loss: values_lse float32 [rows] on the GPU");
     }
     const double temperature = number(a[5], "distill_loss: temperature is a number");
     const bool kl = PyObject_IsTrue(a[6]) == 1;
     const long want = PyLong_AsLong(a[9]);
     if (want < 2 && records(z)) Py_RETURN_NOTIMPLEMENTED;
-    const float *const grad = a[7] == Py_None ? nullptr : floats(a[7], R, "distill_loss: grad float32 [rows] on the GPU");
+    const float *const grad = a[7] == Py_None ? nullptr : floats(a[7], {R}, "distill_loss: grad float32 [rows] on the GPU");
     at::Tensor loss, stats, dz;
     float *known = nullptr;
     if (want != 2) loss = at::empty({R}, z.options().dtype(at::kFloat));
     if (want == 1) stats = at::empty({R, 2}, z.options().dtype(at::kFloat)), known = (float *)stats.data_ptr();
-    if (want == 2) known = floats(a[8], 2 * R, "distill_loss: stats float32 [rows][2] on the GPU");
+    if (want == 2) known = floats(a[8], {R, 2}, "distill_loss: stats float32 [rows][2] on the GPU");
     spec_rows to{};
     if (want >= 2) {
       const char *const out_is = "distill_loss: out [rows][vocabulary] of dtype on the GPU with adjacent columns, without a gradient";

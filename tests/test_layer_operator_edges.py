@@ -41,3 +41,24 @@ def test_an_id_map_without_entries_is_refused():
                  lambda: sb.distill_loss_backward(None, z, stats, ids, v, id_map=none)):
         with pytest.raises(ValueError):
             call()
+
+
+@gpu
+def test_row_values_of_another_shape_are_refused():
+    """Two rows of two are not four rows; a dimension of 1 more, or none, is no other shape."""
+    z, ids, v = teacher()
+    loss, stats = sb.distill_loss(z, ids, v, want_stats=True)
+    lse, g = torch.rand(4, device="cuda"), torch.rand(4, device="cuda")
+    calls = [lambda x=x: sb.distill_loss(z, ids, v, values_lse=x) for x in (lse.view(2, 2), lse.view(2, 1, 2), lse[:2])]
+    calls += [lambda x=x: sb.distill_loss_backward(x, z, stats, ids, v) for x in (g.view(2, 2), g[:3])]
+    calls += [lambda x=x: sb.distill_loss_and_grad(x, z, ids, v) for x in (g.view(2, 2), g[:3])]
+    calls += [lambda x=x: sb.distill_loss_backward(None, z, x, ids, v) for x in (stats.view(2, 4), stats.view(2, 2, 2), stats.T.contiguous(), stats[:3])]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    for x in (lse[:, None], lse[None], lse[None, :, None]):
+        assert torch.equal(sb.distill_loss(z, ids, v, values_lse=x), sb.distill_loss(z, ids, v, values_lse=lse))
+    for x, y in ((g[:, None], stats.flatten()), (g[None], stats[None]), (g, stats[:, :, None])):
+        assert torch.equal(sb.distill_loss_backward(x, z, y, ids, v), sb.distill_loss_backward(g, z, stats, ids, v))
+    row = lambda t: t[:1]
+    assert torch.equal(sb.distill_loss_backward(row(g)[None], row(z), row(stats)[0], row(ids), row(v)), sb.distill_loss_backward(g, z, stats, ids, v)[:1])
