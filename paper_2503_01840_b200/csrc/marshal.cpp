@@ -54,6 +54,11 @@ int dtype_of(at::ScalarType t) {
   if (t == at::kBFloat16) return SPEC_BF16;
   throw Refusal{PyExc_TypeError, std::string("unsupported dtype ") + c10::toString(t)};
 }
+bool truth(PyObject *o) {
+  const int t = PyObject_IsTrue(o);
+  if (t < 0) throw python_error();
+  return t;
+}
 // The current device, asked for once a call (each of the binding's functions sets it to -1): a launch goes there, so every tensor has to be there.
 thread_local int device_of_call = -1;
 void *address(const at::Tensor &t) {
@@ -169,7 +174,7 @@ PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
     need(rope_of(a[2], a[3], a[4], &r), "rotary: inv_freq");
     const int32_t *pos = (const int32_t *)ints(a[1], x.size(0), "rotary: positions int32 [tokens] on the GPU");
     void *const s = stream_of_call();
-    const bool transpose = PyObject_IsTrue(a[6]) == 1;
+    const bool transpose = truth(a[6]);
     const int32_t T = (int32_t)x.size(0), H = (int32_t)x.size(1), hd = (int32_t)x.size(2);
     const int rc = call([&] { return rotary_(dtype, from.p, from.ts, from.hs, to.p, to.ts, to.hs, pos, T, H, hd, &r, transpose, s); });
     return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
@@ -271,7 +276,7 @@ PyObject *decode_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor out = a[9] == Py_None ? at::empty(q.sizes(), q.options(), at::MemoryFormat::Contiguous) : tensor(a[9], "out");
     need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type() && out.is_contiguous() && out.is_cuda(), "decode_attention: out contiguous, of q's shape and dtype");
     void *const to = address(out);
-    const bool want_lse = PyObject_IsTrue(a[8]) == 1;
+    const bool want_lse = truth(a[8]);
     at::Tensor lse;
     if (want_lse) lse = at::empty({B, H}, q.options().dtype(at::kFloat));
     const int32_t *length = (const int32_t *)ints(a[6], B, "decode_attention: lengths int32 [batch] on the GPU");
@@ -381,7 +386,7 @@ PyObject *embedding_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (V == -1 && PyErr_Occurred()) throw python_error();
     need(V >= 1 && V <= INT32_MAX, "embedding_backward: vocab is a number of rows");
     const double scale = number(a[3], "embedding_backward: scale is a number");
-    const bool accumulate = PyObject_IsTrue(a[6]) == 1;
+    const bool accumulate = truth(a[6]);
     need(!accumulate || a[5] != Py_None, "embedding_backward: accumulate goes with out");
     const at::ScalarType type = type_or(a[4], a[5] == Py_None ? g.scalar_type() : tensor(a[5], "out").scalar_type(), "embedding_backward: dtype is a torch.dtype");
     row_type(type);
@@ -515,7 +520,7 @@ PyObject *distill(PyObject *, PyObject *const *a, Py_ssize_t n) {
       t.lse = floats(a[4], {R}, "distill_loss: values_lse float32 [rows] on the GPU");
     }
     const double temperature = number(a[5], "distill_loss: temperature is a number");
-    const bool kl = PyObject_IsTrue(a[6]) == 1;
+    const bool kl = truth(a[6]);
     const long want = PyLong_AsLong(a[9]);
     if (want < 2 && records(z)) Py_RETURN_NOTIMPLEMENTED;
     const float *const grad = a[7] == Py_None ? nullptr : floats(a[7], {R}, "distill_loss: grad float32 [rows] on the GPU");

@@ -62,3 +62,15 @@ def test_row_values_of_another_shape_are_refused():
         assert torch.equal(sb.distill_loss_backward(x, z, y, ids, v), sb.distill_loss_backward(g, z, stats, ids, v))
     row = lambda t: t[:1]
     assert torch.equal(sb.distill_loss_backward(row(g)[None], row(z), row(stats)[0], row(ids), row(v)), sb.distill_loss_backward(g, z, stats, ids, v)[:1])
+
+
+@gpu
+def test_a_flag_that_is_neither_true_nor_false_is_refused():
+    """Before anything is written: accumulating is not overwriting."""
+    z, ids, _ = teacher()
+    out = torch.full((4, 32), 3.0, device="cuda")
+    with pytest.raises(RuntimeError):
+        sb.embedding_backward(z, ids[:, 0].contiguous(), 4, out=out, accumulate=torch.ones(2))
+    assert (out == 3).all()
+    again = sb.embedding_backward(z, ids[:, 0].contiguous(), 4, out=out.clone(), accumulate=torch.ones(1))
+    assert torch.equal(again, sb.embedding_backward(z, ids[:, 0].contiguous(), 4, out=out, accumulate=True))
