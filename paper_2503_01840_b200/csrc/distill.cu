@@ -114,6 +114,8 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
   return all;
 }
 // What the same warp does next for the gradient: entries with one id become one, its first.  A table of the ids tells whether there is anything to do.
+// Loss and gradient of 8192 x 32000 bf16 with 64, 200, 1024 entries a row 195 / 275 / 1053 us; the last of them repeating the first 197 / 324 / 1401, each one's id twice 213 / 391 / 2017.
+// (Comparing every entry with every other 324 / 2015 / 60234, and 320 / 1700 / 39449.)
 __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
   const int lane = threadIdx.x & 31, bits = table_bits(K), mask = (1 << bits) - 1;
   for (int k = lane; k <= mask >> 2; k += 32) ((int4 *)e.table)[k] = make_int4(-1, -1, -1, -1);
@@ -134,20 +136,40 @@ __device__ __forceinline__ void merge_entries(const Entries &e, int K) {
   }
   __syncwarp();
   if (!__any_sync(0xffffffffu, twice)) return;
-#pragma unroll 1
-  for (int k = lane; k < K; k += 32) {
-    const int id = e.id[k];
-    bool first = id >= 0;
-    float p = e.p[k];
-#pragma unroll 1
-    for (int j = 0; first && j < K; j++) {
-      if (j == k || e.id[j] != id) continue;
-      if (j < k) first = false;
-      else p += e.p[j];
-    }
-    e.write[k] = first ? p : -1.0f;
-  }
+  // Again with the entries' places in the table, 32 entries at a time: the lowest lane of an id looks for the id's first entry, or is it, and adds its lanes' probabilities in turn.
+  for (int k = lane; k <= mask >> 2; k += 32) ((int4 *)e.table)[k] = make_int4(-1, -1, -1, -1);
   __syncwarp();
+#pragma unroll 1
+  for (int k0 = 0; k0 < K; k0 += 32) {
+    const int k = k0 + lane, id = k < K ? e.id[k] : -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, id);
+    const bool leads = id >= 0 && (same & ((1u << lane) - 1)) == 0;
+    const float p = id >= 0 ? e.p[k] : 0.0f;
+    int first = k;
+    if (leads) {
+      int at = (int)((uint32_t)id * 2654435769u >> (32 - bits));
+      for (;;) {                                         // ends as above; other lanes put other ids in
+        const int was = atomicCAS(e.table + at, -1, k);
+        if (was < 0) break;
+        if (e.id[was] == id) {
+          first = was;
+          break;
+        }
+        at = (at + 1) & mask;
+      }
+    }
+    __syncwarp();
+    float sum = first == k ? p : e.write[first];
+#pragma unroll 1
+    for (uint32_t rest = __reduce_or_sync(0xffffffffu, leads ? first == k ? same & (same - 1) : same : 0u); rest; rest &= rest - 1) {
+      const int j = __ffs(rest) - 1;
+      const float other = __shfl_sync(0xffffffffu, p, j);
+      if ((same >> j & 1) && (j != lane || first != k)) sum += other;
+    }
+    if (leads) e.write[first] = sum;
+    if (id >= 0 && (!leads || first != k)) e.write[k] = -1.0f;
+    __syncwarp();
+  }
 }
 // A warp's sum over its lanes' entries of p (ln p - ln q), ln q without the logarithm of q's normaliser; z(id): the student's logit
 template <typename F> __device__ __forceinline__ float entries_loss(const Distill &a, const Entries &e, float m, F z) {

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import test_layer_operators as layers
 from paper_2503_01840_b200 import binding as sb
 
 gpu = pytest.mark.gpu
@@ -74,3 +75,57 @@ def test_a_flag_that_is_neither_true_nor_false_is_refused():
     assert (out == 3).all()
     again = sb.embedding_backward(z, ids[:, 0].contiguous(), 4, out=out.clone(), accumulate=torch.ones(1))
     assert torch.equal(again, sb.embedding_backward(z, ids[:, 0].contiguous(), 4, out=out, accumulate=True))
+
+
+def repeated(how, rows, K, V, g):
+    """ids that differ in a row but for: the last as the first; the second half as the first; every fifth; all alike; each as the one before it; with holes"""
+    ids = (torch.randint(0, V, (rows, 1), generator=g) + 7919 * torch.arange(K)) % V
+    at = torch.arange(K)
+    place = {"none": at, "one": at.where(at < K - 1, torch.zeros_like(at)), "halves": at % max(1, K // 2), "fifths": at.where(at % 5 > 0, torch.zeros_like(at)), "all": at * 0,
+             "pairs": at // 2 * 2, "holes": at % max(1, K // 3)}[how]
+    ids = ids[:, place]
+    if how == "holes":
+        ids[torch.rand(rows, K, generator=g) < 0.3] = -1
+    return ids
+
+
+@gpu
+@pytest.mark.parametrize("K", [2, 31, 32, 33, 64, 200, 1024])
+@pytest.mark.parametrize("how", ["one", "halves", "fifths", "all", "pairs", "holes"])
+def test_repeated_ids_in_the_gradient(how, K):
+    """In clusters, slices and the kernel for any vocabulary: against 64 bits, and the same bits where the entries come from a map of many ids to one."""
+    g = torch.Generator().manual_seed(K)
+    for rows, V in ((7, 8009), (400, 8009), (2, 450001)):
+        z, ids, values = 2 * torch.randn(rows, V, generator=g), repeated(how, rows, K, V, g), 2 * torch.randn(rows, K, generator=g)
+        loss, tol, want, dtol = layers.distilled(z, ids, values, None, None, 1.0, "kl", None)
+        got, dz = sb.distill_loss_and_grad(None, z.cuda(), ids.cuda(), values.cuda())
+        layers.within(got, loss, tol)
+        layers.within(dz, want, dtol + want.abs() * layers.E)
+        # the same through a map: twice as many ids, one behind the other to the same
+        twin = torch.where(ids >= 0, ids * 2 + torch.randint(0, 2, ids.shape, generator=g), ids)
+        many = torch.arange(V, dtype=torch.int32).repeat_interleave(2).cuda()
+        again, dagain = sb.distill_loss_and_grad(None, z.cuda(), twin.cuda(), values.cuda(), id_map=many)
+        assert torch.equal(again, got) and torch.equal(dagain, dz)
+
+
+@gpu
+def test_a_repeated_id_does_not_cost_the_square_of_the_entries():
+    """Rows of a thousand entries, one of which repeats another's id, all of them, or none: an entry more or less to add up is no reason for many times the time."""
+    g = torch.Generator().manual_seed(1)
+    rows, V, K = 2000, 32000, 1024
+    z, values = torch.randn(rows, V, generator=g).bfloat16().cuda(), torch.randn(rows, K, generator=g).cuda()
+
+    def time_of(how):
+        ids = repeated(how, rows, K, V, g).int().cuda()
+        best = float("inf")
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            sb.distill_loss_and_grad(None, z, ids, values)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+    plain = time_of("none")
+    for how in ("one", "halves", "all"):
+        assert time_of(how) < 4 * plain, how
