@@ -46,14 +46,13 @@ struct Entries {
   int *id;               // the student's, -1: none
   float *p, *ln_p;
   float *write;          // for the gradient: p of all entries with this id at the first of them, -1 at the others
-  int *table;            // of the ids
+  int *table;            // of the ids, or of the places of their first entries
 };
-__host__ __device__ constexpr int fours(int K) { return (K + 3) / 4 * 4; }
 __host__ __device__ constexpr int table_bits(int K) { return K <= 16 ? 6 : K <= 64 ? 8 : K <= 256 ? 10 : 12; }      // four places an entry, or more
-__host__ __device__ constexpr size_t entries_bytes(int K) { return (size_t)fours(K) * 16 + ((size_t)4 << table_bits(K)); }
+__host__ __device__ constexpr size_t entries_bytes(int K) { return (size_t)K * 16 + ((size_t)4 << table_bits(K)); }      // the table, and what lies behind it, aligned to 16
 __device__ __forceinline__ Entries entries_in(char *shared, int K) {
   float *const f = (float *)shared;
-  return {(int *)f, f + fours(K), f + 2 * fours(K), f + 3 * fours(K), (int *)f + 4 * fours(K)};
+  return {(int *)f, f + K, f + 2 * K, f + 3 * K, (int *)f + 4 * K};
 }
 // One warp fills them in and returns sum p; *none: whether the row has no entry (sum p may be 0 otherwise too, where every p is too small).
 __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e, long long row, bool *none) {
@@ -62,7 +61,6 @@ __device__ __forceinline__ float read_entries(const Distill &a, const Entries &e
   const long long at = row * a.K;
   float top = -INFINITY;
   bool some = false, nan = false;
-  if (lane < fours(a.K) - a.K) e.id[a.K + lane] = -1;
 #pragma unroll 1
   for (int k = lane; k < a.K; k += 32) {
     int id = id_at(a.ids, at + k);
