@@ -428,7 +428,7 @@ int spec_rms_norm_backward(const spec_rows *grad, const spec_rows *s, int32_t ga
 /* A teacher's top logits: for each row K ids (id_bits 32 or 64; -1: none) and their logits or log-probabilities (values_dtype), [rows][K].  id_map (may be NULL): int32
  * [id_map_n], from the teacher's ids to the student's, -1 for those that the student lacks.  lse (may be NULL): float [rows], the log of the teacher's whole sum of exp(logit / temperature).
  * An entry with id -1, or that the map sends there, or with a value of -inf, is none; ids and mapped ids out of range are none and recorded in `status` (code 2, sites 65 and 66,
- * row and id).  The same id several times: its probabilities add up.  1 <= K <= 1024; rows and vocab <= 2^30. */
+ * row and id).  1 <= K <= 1024; rows and vocab <= 2^30. */
 typedef struct {
   const void *ids, *values;
   const float *lse;
@@ -439,6 +439,8 @@ typedef struct {
 /* Row by row, with q = softmax(logits / temperature) over the student's vocab, and p over the teacher's entries that the student has, softmax(values / temperature)
  * over them, or exp(values / temperature - lse):
  *   loss[r] = sum p (ln p - ln q) (kl != 0) or - sum p ln q;     dlogits[r] = grad[r] / temperature * (q sum(p) - p)
+ * An id several times, given so or by the map: the sums go over the entries as they stand, in dlogits p is the sum of an id's.  kl is then not the divergence of the added-up p from q, but
+ * lies below it by sum p ln(P / p), P what an entry's id has in all: a number of the teacher's alone, without a part in the gradient, that can take kl below 0.
  * A row without an entry has loss 0 and gradient 0, whatever its logits.  A row of -inf alone has NaN, as have rows with a NaN or +inf.
  * stats float [rows][2]: the row's largest logit, and its sum of exp((logit - largest) / temperature) (0 and 1 without an entry).
  *   loss, no dlogits: the loss; stats are written where given      no loss, dlogits: the gradient, from the stats of a call for the loss

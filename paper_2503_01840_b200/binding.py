@@ -765,6 +765,8 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, 
     id -1 for no entry; id_map int32 [teacher's vocabulary] gives the student's id, -1 for those that it lacks (of a draft's d2t: full -1, then id_map[d2t] = arange).
     q = softmax(logits / temperature), p = softmax(values / temperature) over the entries that the student has, or exp(values / temperature - values_lse) with the teacher's
     normaliser float32 [rows]; "kl": sum p (ln p - ln q), "ce": - sum p ln q (no factor temperature^2).  A row without an entry has loss 0 and gradient 0.
+    An id several times in a row, or entries that the map sends to one: the sum goes over the entries as they stand.  The gradient is that of their added-up probabilities, but "kl" lies below
+    their divergence from q by sum p ln(P / p), P what an entry's id has in all, which does not depend on the logits, and may be below 0; K different ids have no such part.
     want_stats: (loss, stats float32 [rows][2]) for distill_loss_backward.  Autograd takes logits' gradient through it.  Ids out of range are no entries and recorded in status."""
     kl = _kl(kind)
     r = (_marshal_module or _marshal()).distill(logits, ids, values, id_map, values_lse, temperature, kl, None, None, 1 if want_stats else 0, None, None, status)

@@ -8,6 +8,7 @@ constexpr int DISTILL_MAX_K = 1024;
 
 // Row r: q = softmax(z[r] / T); p over the K entries that the student has (id through the map, where there is one): softmax(values / T) over them, or
 // exp(values / T - lse[r]).  loss = sum p (ln p - ln q), or - sum p ln q; dz = grad[r] / T (q sum p - p).  stats: largest logit, sum of exp((z - largest) / T).
+// An id several times: the loss is the sum over the entries as they stand, the gradient has the sum of their p.
 struct Distill {
   const void *z;
   long long z_rs;

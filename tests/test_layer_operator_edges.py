@@ -129,3 +129,31 @@ def test_a_repeated_id_does_not_cost_the_square_of_the_entries():
     plain = time_of("none")
     for how in ("one", "halves", "all"):
         assert time_of(how) < 4 * plain, how
+
+
+@gpu
+@pytest.mark.parametrize("how", ["none", "halves", "all", "holes"])
+@pytest.mark.parametrize("rows", [9, 400])
+def test_what_kl_is_where_ids_repeat(how, rows):
+    """The sum over the entries as they stand: the divergence of the added-up probabilities from the student's less sum p ln(P / p); "ce" and the gradient are those of the added-up ones."""
+    g = torch.Generator().manual_seed(rows)
+    V, K = 3001, 24
+    z, ids, values = torch.randn(rows, V, generator=g), repeated(how, rows, K, V, g), torch.randn(rows, K, generator=g)
+    z[0] = -100.0
+    z[0, ids[0].clamp_min(0)] = 100.0                    # a student that is sure of the teacher's entries
+    has, p, ln_p = layers.target(ids, values, None, None, 1.0, V)
+    dense = torch.zeros(rows, V, dtype=torch.float64).scatter_add_(1, has.clamp_min(0), p)
+    ln_q = torch.log_softmax(z.double(), 1)
+    merged = torch.where(dense > 0, dense * (dense.clamp_min(1e-300).log() - ln_q), torch.zeros_like(dense)).sum(1)
+    less = torch.where(p > 0, p * (dense.gather(1, has.clamp_min(0)).clamp_min(1e-300).log() - ln_p), torch.zeros_like(p)).sum(1)
+    assert (merged > -1e-12).all() and (less > -1e-12).all() and (how != "none" or less.abs().max() < 1e-12)
+    loss, tol, _, _ = layers.distilled(z, ids, values, None, None, 1.0, "kl", None)
+    got, dz = sb.distill_loss_and_grad(None, z.cuda(), ids.cuda(), values.cuda())
+    layers.within(got, merged - less, tol)
+    layers.within(sb.distill_loss(z.cuda(), ids.cuda(), values.cuda()), merged - less, tol)
+    _, tol, _, dtol = layers.distilled(z, ids, values, None, None, 1.0, "ce", None)
+    layers.within(sb.distill_loss(z.cuda(), ids.cuda(), values.cuda(), kind="ce"), -(dense * ln_q).sum(1), tol)
+    want = ln_q.exp() * dense.sum(1, keepdim=True) - dense
+    layers.within(dz, want, dtol + want.abs() * layers.E)
+    if how == "all":
+        assert got[0] < -1.0                             # below 0: the merged divergence is 0 there
