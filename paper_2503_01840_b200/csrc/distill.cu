@@ -522,8 +522,9 @@ __global__ void __launch_bounds__(WALKERS + 32, 3) distill_rows_kernel(const __g
 }
 
 // ---------------------------------------------------------------- the loss alone, of many rows
-// A CTA a row, walked once as it comes from memory.  Bytes bound it in fp32: 2048 rows of 128256 155 us, 6.8 TB/s, a copy's rate; in bf16 unpacking and exponentials come near them: 8192 rows
-// of 32000, a tenth of them without entries, 103 us, 5.1 TB/s.  By clusters through shared memory as above 315 and 132 us; four CTAs an SM 165 / 115, six 181 / 103.
+// A CTA a row, walked once as it comes from memory.  Bytes bound it in fp32: 2048 rows of 128256 154 us, 6.8 TB/s, a copy's rate; in bf16 unpacking and exponentials come near them: 8192 rows
+// of 32000 109 us, 4.8 TB/s; 96 us, 4.9 TB/s of what is read, where a tenth of the rows have no entry and are not.  Where the first and the last of these took 155 / 103, by clusters through
+// shared memory as above 315 / 132, four CTAs an SM 165 / 115, six 181 / 103.
 template <typename T>
 __global__ void __launch_bounds__(WALKERS + 32, 5) distill_loss_kernel(const __grid_constant__ Distill a, float b) {
   pdl_wait();
